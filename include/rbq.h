@@ -58,6 +58,9 @@ typedef enum rbq_status {
 
 typedef enum rbq_dtype { RBQ_F32 = 0, RBQ_BF16 = 1 } rbq_dtype;
 
+/* formats of the 8-bit cache (arguments named kv8_dtype; no other call takes them) */
+typedef enum rbq_kv8_dtype { RBQ_E4M3 = 16, RBQ_I8 = 17 } rbq_kv8_dtype;
+
 /* flags of rbq_encode_keys */
 #define RBQ_ENCODE_SET_CENTROID 1u
 
@@ -67,6 +70,7 @@ typedef enum rbq_dtype { RBQ_F32 = 0, RBQ_BF16 = 1 } rbq_dtype;
 #define RBQ_OP_SPARSE_DECODE 3
 #define RBQ_OP_DENSE_DECODE 4
 #define RBQ_OP_DECODE_STEP 5
+#define RBQ_OP_DECODE_KV8 6       /* rbq_sparse_decode_kv8 and rbq_dense_decode_kv8 */
 
 #define RBQ_QSCAL_STRIDE 8   /* floats per query head in qscal */
 #define RBQ_MAX_WINDOW 4096  /* largest local window accepted by the decode calls */
@@ -376,6 +380,82 @@ rbq_status rbq_decode_step_noalloc(int32_t batch, int32_t heads_q, int32_t heads
                                    float sm_scale, uint32_t* qplanes, float* qscal, float* scores,
                                    int32_t* sel_idx, int32_t* sel_count, float* out, float* lse,
                                    hipStream_t stream);
+
+/*
+ * The 8-bit cache -- K and V rows as one byte per value with one scale per
+ * (sequence, KV head, block of `block` tokens) and tensor: half the bytes of a
+ * bf16 cache for the rows that the decode attention reads. (The estimate, the
+ * selection and the index do not read the cache and are unchanged.) The newest
+ * rows stay in full precision in the local window (Section 3.4) and enter the
+ * 8-bit cache when the window is flushed.
+ *   K8, V8   [B][Hkv][cap][D] bytes, in format kv8_dtype: RBQ_E4M3 (OCP e4m3,
+ *            no infinities) or RBQ_I8 (two's complement)
+ *   k_scale, v_scale [B][Hkv][ceil(cap / block)] float: a value is code * scale
+ *   block    tokens per scale: 16, 32, 64, 128 or 256 (another power of two:
+ *            RBQ_EUNSUPPORTED; anything else: RBQ_EINVAL); block i holds rows
+ *            [i * block, (i + 1) * block)
+ *
+ * rbq_quantize_kv writes n_new rows per (b, kv-head), K_new / V_new
+ * [B][Hkv][ld][D] rows [0, n_new) in dtype RBQ_F32 or RBQ_BF16, as cache rows
+ * [offset, offset + n_new). For each token block they touch, amax is the largest
+ * finite magnitude of the new rows in it, and
+ *   RBQ_E4M3: s = 2^e with the smallest e >= -126 such that amax <= 448 * 2^e;
+ *             codes are x / s rounded to nearest even
+ *   RBQ_I8:   s = max(amax / 127, 2^-126), codes are x * (1 / s) rounded to the
+ *             nearest whole number (even on ties) and clamped to +-127, with s
+ *             and 1 / s as correctly rounded floats
+ * (s = 0 where amax = 0). NaN is stored as 0 and an infinity as the largest code
+ * of its sign (0 where s = 0), so the cache holds neither.
+ * A block that starts before `offset` holds rows already (its scale and rows must
+ * be valid): they are kept, under s' = max(s, the block's scale); where that is
+ * larger than the block's scale, their codes are re-encoded as code * (scale / s'),
+ * rounded like new ones. Rows behind the new ones in the last block are no longer
+ * valid (their scale may have changed) and may be appended later.
+ *   seq_off, seq_new: NULL, or [B] int32 (device): sequence b's own offset and
+ *     count, clamped to [0, offset] and [0, n_new].
+ *   RBQ_EINVAL also where (offset + n_new) * D >= 2^31.
+ */
+rbq_status rbq_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim,
+                           const void* K_new, const void* V_new, int32_t dtype, int64_t ld,
+                           int32_t n_new, int32_t offset, int32_t cap, int32_t block, int32_t kv8_dtype,
+                           void* K8, void* V8, float* k_scale, float* v_scale,
+                           const int32_t* seq_off, const int32_t* seq_new, hipStream_t stream);
+
+/* rbq_dequantize_kv -- cache rows [offset, offset + n_rows) back as rows
+ * [0, n_rows) of K / V [B][Hkv][ld][D] in dtype RBQ_F32 or RBQ_BF16 (code * scale as
+ * a float, and that rounded to bf16): for attention of a prompt's chunk over rows already cached, or to
+ * index them. seq_off, seq_rows: as seq_off, seq_new of rbq_quantize_kv; rows
+ * behind a sequence's own are left as they were. */
+rbq_status rbq_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K8, const void* V8,
+                             int32_t kv8_dtype, int32_t block, const float* k_scale, const float* v_scale,
+                             int32_t cap, int32_t n_rows, int32_t offset, void* K, void* V, int32_t dtype,
+                             int64_t ld, const int32_t* seq_off, const int32_t* seq_rows, hipStream_t stream);
+
+/*
+ * rbq_dense_decode_kv8 / rbq_sparse_decode_kv8 -- rbq_dense_decode and
+ * rbq_sparse_decode over the 8-bit cache: exact attention (fp32 accumulation)
+ * over the values that its rows [0, n), or the selected ones, stand for, plus w
+ * window rows K_loc / V_loc [B][Hkv][loc_ld][D] in loc_dtype (RBQ_F32 or
+ * RBQ_BF16; NULL allowed when w == 0). Everything else as in those calls.
+ *   seq_n, seq_w: NULL, or [B] int32 (device): ragged batches, sequence b's
+ *     cached rows and window rows, clamped to [0, n] and [0, w] (its window
+ *     starts at row 0 of its block of K_loc / V_loc). A selection holds rows
+ *     below seq_n[b] only.
+ *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w) bytes.
+ */
+rbq_status rbq_dense_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                const void* K8, const void* V8, int32_t kv8_dtype, int32_t block,
+                                const float* k_scale, const float* v_scale, int32_t cap, int32_t n,
+                                const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                                float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                                const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream);
+rbq_status rbq_sparse_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                 const void* K8, const void* V8, int32_t kv8_dtype, int32_t block,
+                                 const float* k_scale, const float* v_scale, int32_t cap, int32_t n,
+                                 const int32_t* sel_idx, const int32_t* sel_count,
+                                 const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                                 float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                                 const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream);
 
 /*
  * rbq_mapped_device_pointer -- the device address of pinned host memory

@@ -15,7 +15,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "librbq.so")
 
-HIP_SOURCES = ["api.hip", "score.hip", "quantize.hip", "encode.hip", "topp.hip", "decode.hip"]
+HIP_SOURCES = ["api.hip", "score.hip", "quantize.hip", "encode.hip", "topp.hip", "decode.hip", "kv8.hip",
+               "decode_kv8.hip"]
 CXX_SOURCES = ["validate.cpp"]          # plain C++ (no HIP): host-side argument checks
 
 ARCH = "gfx950"
@@ -34,10 +35,10 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
-# per-source additions: the decode kernels keep their MFMA accumulators in
+# per-source additions: the decode kernels (of both caches) keep their MFMA accumulators in
 # ordinary VGPRs (the softmax rescales them with vector ALU ops; accumulation
 # registers would cost copies and a wave per SIMD)
-EXTRA_FLAGS = {"decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("decode.hip", "decode_kv8.hip")}
 
 
 def _run(cmd, verbose):

@@ -429,3 +429,60 @@ rbq_status rbq_decode_step_varlen_f16(int32_t batch, int32_t heads_q, int32_t he
 }
 
 }  // extern "C"
+
+extern "C" {
+
+rbq_status rbq_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K_new, const void* V_new,
+                           int32_t dtype, int64_t ld, int32_t n_new, int32_t offset, int32_t cap, int32_t block,
+                           int32_t kv8_dtype, void* K8, void* V8, float* k_scale, float* v_scale,
+                           const int32_t* seq_off, const int32_t* seq_new, hipStream_t stream) {
+  const rbq_status s = check_quantize_kv(batch, heads_kv, head_dim, K_new, V_new, dtype, ld, n_new, offset, cap, block,
+                                         kv8_dtype, K8, V8, k_scale, v_scale, seq_off, seq_new);
+  if (s != RBQ_OK) return s;
+  return launch_quantize_kv(batch, heads_kv, head_dim, K_new, V_new, dtype, ld, n_new, offset, cap, block, kv8_dtype,
+                            K8, V8, k_scale, v_scale, seq_off, seq_new, stream);
+}
+
+rbq_status rbq_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K8, const void* V8,
+                             int32_t kv8_dtype, int32_t block, const float* k_scale, const float* v_scale,
+                             int32_t cap, int32_t n_rows, int32_t offset, void* K, void* V, int32_t dtype,
+                             int64_t ld, const int32_t* seq_off, const int32_t* seq_rows, hipStream_t stream) {
+  const rbq_status s = check_quantize_kv(batch, heads_kv, head_dim, K, V, dtype, ld, n_rows, offset, cap, block,
+                                         kv8_dtype, K8, V8, k_scale, v_scale, seq_off, seq_rows);
+  if (s != RBQ_OK) return s;
+  return launch_dequantize_kv(batch, heads_kv, head_dim, K8, V8, kv8_dtype, block, k_scale, v_scale, cap, n_rows,
+                              offset, K, V, dtype, ld, seq_off, seq_rows, stream);
+}
+
+rbq_status rbq_dense_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                const void* K8, const void* V8, int32_t kv8_dtype, int32_t block,
+                                const float* k_scale, const float* v_scale, int32_t cap, int32_t n,
+                                const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                                float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                                const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream) {
+  const Kv8Cache c{K8, V8, k_scale, v_scale, kv8_dtype, block, cap};
+  const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
+  const rbq_status s = check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, false, nullptr, nullptr, win,
+                                        sm_scale, out, ws, ws_bytes, seq_n, seq_w);
+  if (s != RBQ_OK) return s;
+  return launch_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, nullptr, nullptr, win, sm_scale, out, lse, ws,
+                           false, stream, nullptr, 0, seq_n, seq_w);
+}
+
+rbq_status rbq_sparse_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                 const void* K8, const void* V8, int32_t kv8_dtype, int32_t block,
+                                 const float* k_scale, const float* v_scale, int32_t cap, int32_t n,
+                                 const int32_t* sel_idx, const int32_t* sel_count, const void* K_loc,
+                                 const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w, float sm_scale,
+                                 float* out, float* lse, void* ws, size_t ws_bytes, const int32_t* seq_n,
+                                 const int32_t* seq_w, hipStream_t stream) {
+  const Kv8Cache c{K8, V8, k_scale, v_scale, kv8_dtype, block, cap};
+  const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
+  const rbq_status s = check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win,
+                                        sm_scale, out, ws, ws_bytes, seq_n, seq_w);
+  if (s != RBQ_OK) return s;
+  return launch_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, sel_idx, sel_count, win, sm_scale, out, lse,
+                           ws, true, stream, nullptr, 0, seq_n, seq_w);
+}
+
+}  // extern "C"

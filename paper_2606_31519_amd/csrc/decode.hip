@@ -829,4 +829,13 @@ rbq_status launch_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, const
   return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
 }
 
+rbq_status launch_decode_combine(int32_t rows, int32_t head_dim, int32_t splits, const float* part, float* out, float* lse,
+                                 hipStream_t stream) {
+  if (head_dim == 64)
+    decode_combine_kernel<64><<<dim3(rows, kCombSlices), kCombThreads, 0, stream>>>(part, splits, out, lse);
+  else
+    decode_combine_kernel<kHeadDim><<<dim3(rows, kCombSlices), kCombThreads, 0, stream>>>(part, splits, out, lse);
+  return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
+}
+
 }  // namespace rbq

@@ -33,6 +33,29 @@ rbq_status check_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_
                         int64_t loc_ld, int32_t w, float sm_scale, const float* out, const void* ws,
                         size_t ws_bytes);
 
+rbq_status check_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
+                             int32_t dtype, int64_t ld, int32_t rows, int32_t offset, int32_t cap, int32_t block,
+                             int32_t kv8_dtype, const void* K8, const void* V8, const float* k_scale,
+                             const float* v_scale, const int32_t* seq_off, const int32_t* seq_rows);
+
+// The 8-bit cache and the window of the calls that read it.
+constexpr int kMinKv8Block = 16, kMaxKv8Block = 256;   // tokens per scale, a power of two
+struct Kv8Cache {
+  const void *K8, *V8;
+  const float *k_scale, *v_scale;   // [B][Hkv][ceil(cap / block)]
+  int32_t dtype, block, cap;
+};
+struct Kv8Window {
+  const void *K, *V;   // [B][Hkv][ld][D]
+  int32_t dtype;
+  int64_t ld;
+  int32_t w;
+};
+rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                            const Kv8Cache& c, int32_t n, bool sparse, const int32_t* sel_idx,
+                            const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
+                            const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w);
+
 // ---------------------------------------------------------------- workspace layouts
 // Top-p: a row of scores of at most kSelRowMax keys is selected by one block; a
 // longer one is cut into parts of spb sub-chunks of kSelSub keys, one block of
@@ -215,5 +238,22 @@ rbq_status launch_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, const
                          int32_t head_dim = kHeadDim);
 // (ragged: seq_n / seq_w [B] indexed and window rows per sequence, the window
 // being the sequence's cache tail; K_loc, V_loc and loc_ld are then ignored)
+
+// joins the splits of each of `rows` query heads: part [rows][splits][D + 2] {m (log2 domain), l, acc}
+rbq_status launch_decode_combine(int32_t rows, int32_t head_dim, int32_t splits, const float* part, float* out,
+                                 float* lse, hipStream_t stream);
+rbq_status launch_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
+                              int32_t dtype, int64_t ld, int32_t n_new, int32_t offset, int32_t cap, int32_t block,
+                              int32_t kv8_dtype, void* K8, void* V8, float* k_scale, float* v_scale,
+                              const int32_t* seq_off, const int32_t* seq_new, hipStream_t stream);
+rbq_status launch_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K8, const void* V8,
+                                int32_t kv8_dtype, int32_t block, const float* k_scale, const float* v_scale,
+                                int32_t cap, int32_t n_rows, int32_t offset, void* K, void* V, int32_t dtype,
+                                int64_t ld, const int32_t* seq_off, const int32_t* seq_rows, hipStream_t stream);
+rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                             const Kv8Cache& cache, int32_t n, const int32_t* sel_idx, const int32_t* sel_count,
+                             const Kv8Window& win, float sm_scale, float* out, float* lse, void* ws, bool sparse,
+                             hipStream_t stream, const unsigned long long* sel_mask = nullptr, int32_t mask_words = 0,
+                             const int32_t* seq_n = nullptr, const int32_t* seq_w = nullptr);
 
 }  // namespace rbq

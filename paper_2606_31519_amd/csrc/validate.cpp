@@ -172,6 +172,55 @@ rbq_status check_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_
   return RBQ_OK;
 }
 
+namespace {
+bool bad_seq(const int32_t* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+rbq_status check_kv8_form(int32_t block, int32_t kv8_dtype) {
+  if (kv8_dtype != RBQ_E4M3 && kv8_dtype != RBQ_I8) return RBQ_EUNSUPPORTED;
+  if (block < 1 || (block & (block - 1)) != 0) return RBQ_EINVAL;
+  if (block < kMinKv8Block || block > kMaxKv8Block) return RBQ_EUNSUPPORTED;
+  return RBQ_OK;
+}
+}  // namespace
+
+rbq_status check_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
+                             int32_t dtype, int64_t ld, int32_t rows, int32_t offset, int32_t cap, int32_t block,
+                             int32_t kv8_dtype, const void* K8, const void* V8, const float* k_scale,
+                             const float* v_scale, const int32_t* seq_off, const int32_t* seq_rows) {
+  rbq_status s = check_heads(batch, heads_kv, heads_kv, head_dim);
+  if (s != RBQ_OK) return s;
+  if (dtype != RBQ_F32 && dtype != RBQ_BF16) return RBQ_EUNSUPPORTED;
+  if ((s = check_kv8_form(block, kv8_dtype)) != RBQ_OK) return s;
+  if (rows < 0 || offset < 0 || cap < 0 || ld < rows || ld >= kMaxRows) return RBQ_EINVAL;
+  if (int64_t(offset) + rows > cap) return RBQ_EINVAL;
+  if ((int64_t(offset) + rows) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;   // as the calls that read them
+  if (bad_seq(seq_off) || bad_seq(seq_rows)) return RBQ_EINVAL;
+  if (rows > 0 && (bad_ptr(K) || bad_ptr(V) || bad_ptr(K8) || bad_ptr(V8) || bad_ptr(k_scale) || bad_ptr(v_scale)))
+    return RBQ_EINVAL;
+  return RBQ_OK;
+}
+
+rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                            const Kv8Cache& c, int32_t n, bool sparse, const int32_t* sel_idx,
+                            const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
+                            const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w) {
+  rbq_status s = check_heads(batch, heads_q, heads_kv, head_dim);
+  if (s != RBQ_OK) return s;
+  if ((s = check_kv8_form(c.block, c.dtype)) != RBQ_OK) return s;
+  if (win.w != 0 && win.dtype != RBQ_F32 && win.dtype != RBQ_BF16) return RBQ_EUNSUPPORTED;
+  const int32_t G = heads_q / heads_kv;
+  if (G & (G - 1)) return RBQ_EUNSUPPORTED;   // the decode kernels are built for G in {1, 2, 4, 8, 16}
+  if (n < 0 || c.cap < 0 || n > c.cap || win.w < 0 || win.w > RBQ_MAX_WINDOW) return RBQ_EINVAL;
+  if (!std::isfinite(sm_scale) || !(sm_scale > 0.0f)) return RBQ_EINVAL;
+  if (bad_ptr(q) || bad_ptr(out) || bad_seq(seq_n) || bad_seq(seq_w)) return RBQ_EINVAL;
+  if (n > 0 && (bad_ptr(c.K8) || bad_ptr(c.V8) || bad_ptr(c.k_scale) || bad_ptr(c.v_scale))) return RBQ_EINVAL;
+  if (sparse && (bad_ptr(sel_count) || (n > 0 && bad_ptr(sel_idx)))) return RBQ_EINVAL;
+  if (win.w > 0 && (bad_ptr(win.K) || bad_ptr(win.V) || win.ld < win.w || win.ld >= kMaxRows)) return RBQ_EINVAL;
+  // rows of one (sequence, KV head) are addressed with 32-bit byte offsets
+  if (int64_t(n) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;
+  if (bad_ptr(ws) || ws_bytes < decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, win.w)) return RBQ_EINVAL;
+  return RBQ_OK;
+}
+
 // Keys per lane of the score kernel: enough blocks to cover the 256 CUs
 // several times over, as many keys in flight per lane as that allows.
 int score_keys_per_lane(int32_t batch, int32_t heads_kv, int32_t n) {
@@ -215,6 +264,7 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
       return rbq::topp_workspace(nullptr, int64_t(batch) * heads_q, n).bytes;
     case RBQ_OP_SPARSE_DECODE:
     case RBQ_OP_DENSE_DECODE:
+    case RBQ_OP_DECODE_KV8:
       return rbq::decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_DECODE_STEP:
       if (heads_q % heads_kv != 0) return 0;

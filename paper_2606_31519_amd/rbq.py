@@ -17,8 +17,10 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librbq.so")
 
 RBQ_OK, RBQ_EINVAL, RBQ_EUNSUPPORTED, RBQ_EDEVICE = 0, 1, 2, 3
 RBQ_F32, RBQ_BF16 = 0, 1
+RBQ_E4M3, RBQ_I8 = 16, 17   # formats of the 8-bit cache
 RBQ_ENCODE_SET_CENTROID = 1
 RBQ_OP_ENCODE, RBQ_OP_TOPP, RBQ_OP_SPARSE_DECODE, RBQ_OP_DENSE_DECODE, RBQ_OP_DECODE_STEP = 1, 2, 3, 4, 5
+RBQ_OP_DECODE_KV8 = 6
 QSCAL_STRIDE = 8
 RBQ_MAX_WINDOW = 4096   # largest local window accepted by the decode calls
 RBQ_NOALLOC_SCRATCH_BYTES = 16 << 20   # the static scratch of rbq_decode_step_noalloc
@@ -32,6 +34,7 @@ EXPORTED = [
     "rbq_score_q8", "rbq_score_ints_q8", "rbq_mapped_device_pointer",
     "rbq_encode_keys_f16", "rbq_score_f16", "rbq_decode_step_f16", "rbq_score_varlen_f16", "rbq_decode_step_varlen_f16",
     "rbq_decode_step_noalloc",
+    "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8",
 ]
 
 
@@ -84,6 +87,13 @@ def _load():
         "rbq_score_varlen_f16": [i32, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp],
         "rbq_decode_step_varlen_f16": [i32, i32, i32, i32, vp, vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp,
                                        i32, vp, f32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        # the 8-bit cache
+        "rbq_quantize_kv": [i32, i32, i32, vp, vp, i32, i64, i32, i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, vp],
+        "rbq_dequantize_kv": [i32, i32, i32, vp, vp, i32, i32, vp, vp, i32, i32, i32, vp, vp, i32, i64, vp, vp, vp],
+        "rbq_dense_decode_kv8": [i32, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, i64, i32,
+                                 f32, vp, vp, vp, sz, vp, vp, vp],
+        "rbq_sparse_decode_kv8": [i32, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32,
+                                  i64, i32, f32, vp, vp, vp, sz, vp, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -175,6 +185,14 @@ def kv_dtype_code(t: torch.Tensor) -> int:
     if t.dtype == torch.float32:
         return RBQ_F32
     raise ValueError(f"unsupported key/value dtype {t.dtype}")
+
+
+def kv8_dtype_code(t: torch.Tensor) -> int:
+    if t.dtype == torch.float8_e4m3fn:
+        return RBQ_E4M3
+    if t.dtype == torch.int8:
+        return RBQ_I8
+    raise ValueError(f"unsupported 8-bit cache dtype {t.dtype}")
 
 
 def rbq_workspace_bytes(op, batch, heads_q, heads_kv, head_dim, n, w=0) -> int:
@@ -411,3 +429,83 @@ def rbq_decode_step_varlen_f16(batch, heads_q, heads_kv, head_dim, q, P, c_k, K,
         w, _ptr(seq_n), _ptr(seq_w), _ptr(codes), _ptr(kfac16), int(bool(flush)), _ptr(seq_p), sm_scale,
         _ptr(qplanes), _ptr(qscal), _ptr(scores), _ptr(sel_idx), _ptr(sel_count), _ptr(out), _ptr(lse), _ptr(ws),
         ws_bytes, _stream(stream)))
+
+
+# ---- the 8-bit cache: K8, V8 [B][Hkv][cap][D] torch.float8_e4m3fn or torch.int8, k_scale, v_scale
+# [B][Hkv][ceil(cap / block)] float32; seq_*: per-sequence counts of ragged batches (int32 device tensors) or None
+
+
+def _need_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale):
+    if K8.dtype != V8.dtype:
+        raise ValueError(f"{name}: K8 is {K8.dtype}, V8 {V8.dtype}")
+    blocks = batch * heads_kv * ((cap + block - 1) // block) if block > 0 else 0
+    _need(name, K8=(K8, batch * heads_kv * cap * head_dim), V8=(V8, batch * heads_kv * cap * head_dim),
+          k_scale=(k_scale, blocks), v_scale=(v_scale, blocks))
+
+
+def rbq_quantize_kv(batch, heads_kv, head_dim, K, V, ld, n_new, offset, cap, block, K8, V8, k_scale, v_scale,
+                    seq_off=None, seq_new=None, stream=None):
+    """Append rows [0, n_new) of K / V [B][Hkv][ld][D] to the 8-bit cache as rows [offset, offset + n_new)."""
+    _need_kv8("rbq_quantize_kv", batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    if K.dtype != V.dtype:
+        raise ValueError(f"rbq_quantize_kv: K is {K.dtype}, V {V.dtype}")
+    rows = ((batch * heads_kv - 1) * ld + n_new) * head_dim if n_new > 0 else 0
+    _need("rbq_quantize_kv", K=(K, rows), V=(V, rows), seq_off=(seq_off, batch), seq_new=(seq_new, batch))
+    _check("rbq_quantize_kv", lib.rbq_quantize_kv(
+        batch, heads_kv, head_dim, _ptr(K), _ptr(V), kv_dtype_code(K), ld, n_new, offset, cap, block,
+        kv8_dtype_code(K8), _ptr(K8), _ptr(V8), _ptr(k_scale), _ptr(v_scale), _ptr(seq_off), _ptr(seq_new),
+        _stream(stream)))
+
+
+def rbq_dequantize_kv(batch, heads_kv, head_dim, K8, V8, block, k_scale, v_scale, cap, n_rows, offset, K, V, ld,
+                      seq_off=None, seq_rows=None, stream=None):
+    """Cache rows [offset, offset + n_rows) as rows [0, n_rows) of K / V [B][Hkv][ld][D] (bf16 or fp32)."""
+    _need_kv8("rbq_dequantize_kv", batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    if K.dtype != V.dtype:
+        raise ValueError(f"rbq_dequantize_kv: K is {K.dtype}, V {V.dtype}")
+    rows = ((batch * heads_kv - 1) * ld + n_rows) * head_dim if n_rows > 0 else 0
+    _need("rbq_dequantize_kv", K=(K, rows), V=(V, rows), seq_off=(seq_off, batch), seq_rows=(seq_rows, batch))
+    _check("rbq_dequantize_kv", lib.rbq_dequantize_kv(
+        batch, heads_kv, head_dim, _ptr(K8), _ptr(V8), kv8_dtype_code(K8), block, _ptr(k_scale), _ptr(v_scale), cap,
+        n_rows, offset, _ptr(K), _ptr(V), kv_dtype_code(K), ld, _ptr(seq_off), _ptr(seq_rows), _stream(stream)))
+
+
+def _kv8_window(name, K_loc, V_loc):
+    if K_loc is None or V_loc is None:
+        return RBQ_BF16
+    if K_loc.dtype != V_loc.dtype:
+        raise ValueError(f"{name}: K_loc is {K_loc.dtype}, V_loc {V_loc.dtype}")
+    return kv_dtype_code(K_loc)
+
+
+def rbq_dense_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, n, K_loc, V_loc,
+                         loc_ld, w, sm_scale, out, lse, ws, seq_n=None, seq_w=None, stream=None):
+    """rbq_dense_decode over an 8-bit cache and a window [B][Hkv][loc_ld][D] in bf16 or fp32."""
+    name = "rbq_dense_decode_kv8"
+    _need_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    rows = ((batch * heads_kv - 1) * loc_ld + w) * head_dim if w > 0 else 0
+    _need(name, q=(q, batch * heads_q * head_dim), K_loc=(K_loc, rows), V_loc=(V_loc, rows),
+          out=(out, batch * heads_q * head_dim), lse=(lse, batch * heads_q), seq_n=(seq_n, batch), seq_w=(seq_w, batch))
+    ws_bytes = ws.numel() * ws.element_size()
+    _check(name, lib.rbq_dense_decode_kv8(
+        batch, heads_q, heads_kv, head_dim, _ptr(q), _ptr(K8), _ptr(V8), kv8_dtype_code(K8), block, _ptr(k_scale),
+        _ptr(v_scale), cap, n, _ptr(K_loc), _ptr(V_loc), _kv8_window(name, K_loc, V_loc), loc_ld, w, sm_scale,
+        _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _ptr(seq_n), _ptr(seq_w), _stream(stream)))
+
+
+def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, n, sel_idx,
+                          sel_count, K_loc, V_loc, loc_ld, w, sm_scale, out, lse, ws, seq_n=None, seq_w=None,
+                          stream=None):
+    """rbq_sparse_decode over an 8-bit cache and a window [B][Hkv][loc_ld][D] in bf16 or fp32."""
+    name = "rbq_sparse_decode_kv8"
+    _need_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    rows = ((batch * heads_kv - 1) * loc_ld + w) * head_dim if w > 0 else 0
+    _need(name, q=(q, batch * heads_q * head_dim), K_loc=(K_loc, rows), V_loc=(V_loc, rows),
+          sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q),
+          out=(out, batch * heads_q * head_dim), lse=(lse, batch * heads_q), seq_n=(seq_n, batch), seq_w=(seq_w, batch))
+    ws_bytes = ws.numel() * ws.element_size()
+    _check(name, lib.rbq_sparse_decode_kv8(
+        batch, heads_q, heads_kv, head_dim, _ptr(q), _ptr(K8), _ptr(V8), kv8_dtype_code(K8), block, _ptr(k_scale),
+        _ptr(v_scale), cap, n, _ptr(sel_idx), _ptr(sel_count), _ptr(K_loc), _ptr(V_loc),
+        _kv8_window(name, K_loc, V_loc), loc_ld, w, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _ptr(seq_n),
+        _ptr(seq_w), _stream(stream)))

@@ -1,0 +1,303 @@
+"""The 8-bit cache on the GPU: rows written and appended (codes and scales exactly
+those of the definition), read back, and attended to, densely and sparsely, against
+64 bits on the values that the cache holds."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import kv8_util as ku
+
+pytestmark = pytest.mark.gpu
+
+CODE = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def R():
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    from paper_2606_31519_amd import rbq
+    return rbq
+
+
+def dev(a, dtype=None):
+    t = torch.from_numpy(np.ascontiguousarray(a))
+    return (t if dtype is None else t.to(dtype)).cuda()
+
+
+def cache_of(codes, fmt):
+    """uint8 codes as a device tensor of the format."""
+    return dev(codes.view(np.int8)).view(CODE[fmt])
+
+
+def codes_np(t):
+    return t.view(torch.int8).cpu().numpy().view(np.uint8)
+
+
+def rows_like(rng, shape, dt):
+    """Rows of all sizes: outlier channels, large and tiny tokens, rounded to the type; as float64."""
+    x = rng.standard_normal(shape) * np.exp(rng.uniform(-3, 3, shape[:-1] + (1,)))
+    x[..., rng.integers(0, shape[-1], 3)] *= 9.0
+    return torch.from_numpy(x).to(DT[dt]).double().numpy()
+
+
+# B, Hkv, D, block, cap, [(offset per sequence, rows per sequence), ...]: the writes one after another
+WRITES = [
+    (1, 2, 128, 64, 300, [([0], [300])]),
+    (1, 1, 64, 16, 50, [([0], [1]), ([1], [1]), ([2], [15]), ([17], [33])]),                 # token by token over block ends
+    (3, 2, 128, 32, 200, [([0, 5, 64], [70, 0, 33]), ([70, 0, 97], [1, 3, 100])]),
+    (2, 1, 64, 256, 920, [([0, 0], [255, 257]), ([255, 257], [2, 256]), ([257, 513], [400, 187])]),
+    (2, 2, 128, 128, 513, [([0, 0], [513, 1]), ([100, 1], [20, 130])]),                      # over rows already written
+    (1, 3, 128, 16, 16, [([0], [3]), ([3], [13])]),
+    (5, 1, 128, 256, 257, [([0, 1, 0, 0, 0], [256, 0, 17, 1, 100])]),
+]
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("case", WRITES, ids=[f"D{c[2]}-block{c[3]}-cap{c[4]}" for c in WRITES])
+def test_rows_written_are_those_of_the_definition(R, case, dt, fmt):
+    B, H, D, block, cap, writes = case
+    print("write", case, dt, fmt, flush=True)
+    rng = np.random.default_rng(cap + D)
+    nblk = (cap + block - 1) // block
+    ref = {k: (rng.integers(0, 120, (B, H, cap, D)).astype(np.uint8), np.full((B, H, nblk), 0.5)) for k in "KV"}
+    d = {k: (cache_of(c, fmt), dev(s, torch.float32)) for k, (c, s) in ref.items()}
+    for i, (offs, cnts) in enumerate(writes):
+        n = max(cnts)
+        ld = n + 3
+        x = {k: rows_like(rng, (B, H, ld, D), dt) * (4.0 ** i if k == "K" else 1.0) for k in "KV"}   # K's scales grow
+        for k in "KV":
+            for b in range(B):
+                for h in range(H):
+                    ku.append(ref[k][0][b, h], ref[k][1][b, h], x[k][b, h, :cnts[b]], offs[b], block, fmt)
+        one = len(set(offs)) == 1 and len(set(cnts)) == 1
+        seqs = (None, None) if one else (dev(np.array(offs, np.int32)), dev(np.array(cnts, np.int32)))
+        R.rbq_quantize_kv(B, H, D, dev(x["K"], DT[dt]), dev(x["V"], DT[dt]), ld, n, max(offs), cap, block, d["K"][0], d["V"][0],
+                          d["K"][1], d["V"][1], *seqs)
+    torch.cuda.synchronize()
+    for k in "KV":
+        assert np.array_equal(d[k][1].cpu().numpy().astype(np.float64), ref[k][1]), k
+        got = codes_np(d[k][0])
+        for b in range(B):   # every row, the ones behind the last written included (left as they were)
+            assert np.array_equal(ku.decode_codes(got[b], fmt), ku.decode_codes(ref[k][0][b], fmt), equal_nan=True), (k, b)
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_extreme_values(R, dt, fmt):
+    """Blocks of zeros, of subnormals, at the type's largest and lowest value, exactly at the format's largest code, and
+    with infinities and NaN beside ordinary values; then an append that the held rows' scale does not cover."""
+    D, block = 64, 16
+    big = float(torch.finfo(DT[dt]).max)
+    fills = [0.0, 448.0, 448.0 * 2.0 ** -7, 449.0 if dt == "f32" else 450.0, big, -big, 1e-40, 2.0 ** -133, 1.0]
+    x = np.zeros((1, 1, block * len(fills), D))
+    rng = np.random.default_rng(3)
+    for i, f in enumerate(fills):
+        u = rng.uniform(-1, 1, (block, D))
+        u[0, 0] = 1.0
+        x[0, 0, i * block:(i + 1) * block] = u * f
+    x = torch.from_numpy(x).to(DT[dt]).double().numpy()
+    x[0, 0, -1, :4] = [np.inf, -np.inf, np.nan, -np.nan]
+    x[0, 0, 3, 1:3] = [np.inf, np.nan]                     # in the block of zeros
+    n = x.shape[2]
+    cap = n + block
+    codes, s = np.zeros((1, 1, cap, D), np.uint8), np.zeros((1, 1, cap // block))
+    K8, V8 = cache_of(codes, fmt), cache_of(codes, fmt)
+    ks, vs = dev(s, torch.float32), dev(s, torch.float32)
+    xt = dev(x, DT[dt])
+    R.rbq_quantize_kv(1, 1, D, xt, xt, n, n, 0, cap, block, K8, V8, ks, vs)
+    ku.append(codes[0, 0], s[0, 0], x[0, 0], 0, block, fmt)
+    more = torch.from_numpy(rng.standard_normal((1, 1, 20, D)) * 1e4).to(DT[dt]).double().numpy()
+    mt = dev(more, DT[dt])
+    R.rbq_quantize_kv(1, 1, D, mt, mt, 20, 20, n - 5, cap, block, K8, V8, ks, vs)
+    ku.append(codes[0, 0], s[0, 0], more[0, 0], n - 5, block, fmt)
+    torch.cuda.synchronize()
+    for c8, sc in ((K8, ks), (V8, vs)):
+        assert np.array_equal(sc.cpu().numpy().astype(np.float64), s)
+        assert np.array_equal(ku.decode_codes(codes_np(c8), fmt), ku.decode_codes(codes, fmt))   # (no NaN in it)
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_rows_read_back_are_code_times_scale(R, dt, fmt):
+    B, H, D, block, cap = 3, 2, 64, 32, 101
+    rng = np.random.default_rng(9)
+    codes = rng.integers(0, 256, (B, H, cap, D)).astype(np.uint8)
+    codes[(codes & 0x7F) == 0x7F] = 3
+    s = rng.uniform(0.01, 3.0, (B, H, 4)).astype(np.float32)
+    offs, cnts = [0, 37, 60], [41, 1, 0]
+    K, V = (torch.full((B, H, 50, D), 7.0, dtype=DT[dt], device="cuda") for _ in range(2))
+    R.rbq_dequantize_kv(B, H, D, cache_of(codes, fmt), cache_of(codes[::-1], fmt), block, dev(s), dev(s[::-1]), cap, 41, 60,
+                        K, V, 50, dev(np.array(offs, np.int32)), dev(np.array(cnts, np.int32)))
+    torch.cuda.synchronize()
+    for got, c, sc in ((K, codes, s), (V, codes[::-1], s[::-1])):
+        want = torch.full((B, H, 50, D), 7.0, dtype=DT[dt])
+        for b in range(B):
+            r = np.arange(offs[b], offs[b] + cnts[b])
+            v = ku.decode_codes(c[b][:, r], fmt).astype(np.float32) * sc[b][:, r // block, None]
+            want[b, :, :cnts[b]] = torch.from_numpy(v).to(DT[dt])
+        assert torch.equal(got.cpu(), want)
+
+
+# B, Hq, Hkv, D, block, cap, rows, window rows, share selected, window type
+READS = [
+    (1, 8, 2, 128, 64, 3967, [3967], [129], 0.05, "bf16"),
+    (2, 4, 4, 64, 16, 1030, [1025, 1], [0, 1], 0.3, "f32"),              # G = 1; one row; no window
+    (3, 4, 2, 128, 32, 500, [0, 500, 31], [0, 257, 4], 0.5, "bf16"),     # an empty sequence; a window of two splits
+    (1, 16, 1, 128, 256, 2100, [2049], [70], 0.02, "f32"),               # G = 16
+    (2, 16, 2, 64, 128, 700, [640, 129], [17, 300], 0.9, "bf16"),        # G = 8, D = 64
+    (2, 8, 2, 128, 16, 40, [17, 33], [0, 0], 0.2, "bf16"),
+    (1, 2, 1, 64, 64, 64, [0], [5], 0.5, "f32"),                          # the window alone
+    (9, 8, 2, 128, 64, 33000, [33000, 3, 20000, 1024, 0, 15000, 777, 32768, 9], [0, 5, 64, 1, 0, 9, 3, 8, 2], 0.02, "bf16"),
+]
+
+
+def _read_case(case, fmt):
+    B, Hq, Hkv, D, block, cap, ns, ws, share, ldt = case
+    rng = np.random.default_rng(cap + Hq)
+    nblk = (cap + block - 1) // block
+    codes, scales = {}, {}
+    for k in "KV":
+        c = rng.integers(0, 256, (B, Hkv, cap, D)).astype(np.uint8)
+        if fmt == "e4m3":
+            c = (c & 0x80) | (c & 0x3F)             # up to 2 - 1/8: no NaN
+        codes[k] = c
+        s = np.exp(rng.uniform(-1, 1, (B, Hkv, nblk))) * (0.02 if fmt == "int8" else 1.0)
+        scales[k] = (2.0 ** np.round(np.log2(s)) if fmt == "e4m3" else s).astype(np.float32)
+    keep = rng.random((B, Hq, cap)) < share
+    for b in range(B):
+        keep[b, :, ns[b]:] = False
+        if b == 0 and ns[0] > 40:
+            keep[0, 0] = False                       # a head that selects nothing
+            keep[0, -1, :ns[0]] = True               # and, unless they are one group, a head that selects everything
+    return rng, codes, scales, keep
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("case", READS, ids=[f"B{c[0]}-G{c[1] // c[2]}-D{c[3]}-block{c[4]}-n{max(c[6])}" for c in READS])
+def test_attention_over_the_cache(R, case, fmt):
+    B, Hq, Hkv, D, block, cap, ns, ws, share, ldt = case
+    print("read", case, fmt, flush=True)
+    rng, codes, scales, keep = _read_case(case, fmt)
+    G, n, w, tau = Hq // Hkv, max(ns), max(ws), 1.0 / math.sqrt(D)
+    q = rng.standard_normal((B, Hq, D)).astype(np.float32)
+    win = {k: torch.from_numpy(rng.standard_normal((B, Hkv, w + 2, D))).to(DT[ldt]) for k in "KV"}
+    val = {k: [[ku.values(codes[k][b, h], scales[k][b, h].astype(np.float64), block, fmt) for h in range(Hkv)] for b in range(B)]
+           for k in "KV"}
+    # what no head may read: rows past a sequence's own (NaN codes, NaN scales of whole blocks behind them, NaN windows)
+    for b in range(B):
+        first = (ns[b] + block - 1) // block
+        for k in "KV":
+            if fmt == "e4m3":
+                codes[k][b, :, ns[b]:] = 0x7F
+            scales[k][b, :, first:] = np.nan
+            win[k][b, :, ws[b]:] = float("nan")
+    d = {k: (cache_of(codes[k], fmt), dev(scales[k]), win[k].cuda()) for k in "KV"}
+    sel = np.zeros((B, Hq, max(n, 1)), np.int32)
+    cnt = keep.sum(axis=2).astype(np.int32)
+    for b in range(B):
+        for h in range(Hq):
+            sel[b, h, :cnt[b, h]] = np.flatnonzero(keep[b, h])
+    wsb = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+    wsb.fill_(255)                                      # (NaN patterns: nothing is read before it is written)
+    uniform = len(set(ns)) == 1 and len(set(ws)) == 1
+    seqs = (None, None) if uniform else (dev(np.array(ns, np.int32)), dev(np.array(ws, np.int32)))
+    head = (B, Hq, Hkv, D, dev(q), d["K"][0], d["V"][0], block, d["K"][1], d["V"][1], cap, n)
+    loc = (d["K"][2], d["V"][2], w + 2, w, tau)
+    res = {}
+    for kind in ("dense", "sparse"):
+        out, lse = torch.full((B, Hq, D), 9.0, device="cuda"), torch.full((B, Hq), 9.0, device="cuda")
+        if kind == "dense":
+            R.rbq_dense_decode_kv8(*head, *loc, out, lse, wsb, *seqs)
+        else:
+            R.rbq_sparse_decode_kv8(*head, dev(sel), dev(cnt), *loc, out, lse, wsb, *seqs)
+        torch.cuda.synchronize()
+        res[kind] = out.cpu().numpy(), lse.cpu().numpy()
+    for kind, (out, lse) in res.items():
+        for b in range(B):
+            for h in range(Hq):
+                if B > 4 and h not in (0, Hq - 1):
+                    continue
+                rows = np.arange(ns[b]) if kind == "dense" else np.flatnonzero(keep[b, h])
+                K, V = (np.concatenate([val[k][b][h // G][rows], win[k][b, h // G, :ws[b]].double().numpy()]) for k in "KV")
+                o, l = ku.attention(q[b, h].astype(np.float64), K, V, tau)
+                ot, lt = ku.attention_tolerance(q[b, h].astype(np.float64), K, V, tau)
+                assert np.abs(out[b, h] - o).max() <= ot, (kind, b, h, np.abs(out[b, h] - o).max(), ot)
+                assert (lse[b, h] == l if np.isinf(l) else abs(lse[b, h] - l) <= lt), (kind, b, h, lse[b, h], l, lt)
+
+
+def test_a_selection_of_everything_is_the_dense_call(R):
+    B, Hq, Hkv, D, block, n = 2, 8, 2, 128, 32, 1500
+    rng = np.random.default_rng(4)
+    c = rng.integers(0, 255, (B, Hkv, n, D)).astype(np.uint8)
+    c8 = cache_of(c, "int8")
+    s = dev(rng.uniform(0.01, 0.02, (B, Hkv, (n + block - 1) // block)).astype(np.float32))
+    q = dev(rng.standard_normal((B, Hq, D)).astype(np.float32))
+    sel = torch.arange(n, dtype=torch.int32, device="cuda").expand(B, Hq, n).contiguous()
+    cnt = torch.full((B, Hq), n, dtype=torch.int32, device="cuda")
+    ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, 0)
+    outs = []
+    for kind in (0, 1):
+        out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+        if kind:
+            R.rbq_sparse_decode_kv8(B, Hq, Hkv, D, q, c8, c8, block, s, s, n, n, sel, cnt, None, None, 0, 0, 0.09, out, lse, ws)
+        else:
+            R.rbq_dense_decode_kv8(B, Hq, Hkv, D, q, c8, c8, block, s, s, n, n, None, None, 0, 0, 0.09, out, lse, ws)
+        outs.append((out, lse))
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+def test_append_and_attend_in_a_graph_and_on_two_streams(R):
+    """A token appended and attended to, captured once and replayed with new rows and queries (the program's own work
+    between the replays), against the same calls made eagerly; and the same on a stream of its own beside another call."""
+    B, Hq, Hkv, D, block, cap, n = 2, 8, 2, 64, 16, 256, 100
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    K, V = rnd(B, Hkv, n, D), rnd(B, Hkv, n, D)
+
+    def fresh():
+        c = [torch.zeros(B, Hkv, cap, D, dtype=torch.int8, device="cuda") for _ in range(2)]
+        s = [torch.zeros(B, Hkv, cap // block, device="cuda") for _ in range(2)]
+        R.rbq_quantize_kv(B, Hkv, D, K, V, n, n, 0, cap, block, *c, *s)
+        return c, s, torch.zeros(B, Hq, D, device="cuda"), torch.zeros(B, Hq, device="cuda"), \
+            R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, cap, 0)
+
+    off = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    k1, v1, q = rnd(B, Hkv, 1, D), rnd(B, Hkv, 1, D), rnd(B, Hq, D)
+
+    def token(st, stream=None):
+        c, s, out, lse, ws = st
+        R.rbq_quantize_kv(B, Hkv, D, k1, v1, 1, 1, cap - 1, cap, block, *c, *s, off, None, stream=stream)
+        R.rbq_dense_decode_kv8(B, Hq, Hkv, D, q, *c, block, *s, cap, cap, None, None, 0, 0, 0.125, out, lse, ws, cnt, None,
+                               stream=stream)
+
+    cnt = off + 1
+    ref, cap_st = fresh(), fresh()
+    token(fresh())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        token(cap_st)
+    for i in range(5):
+        k1.copy_(rnd(B, Hkv, 1, D) * 2.0 ** i)      # (the block's scale grows)
+        v1.copy_(rnd(B, Hkv, 1, D))
+        q.copy_(rnd(B, Hq, D))
+        off.fill_(n + i)
+        cnt.fill_(n + i + 1)
+        graph.replay()
+        token(ref)
+        torch.cuda.synchronize()
+        assert torch.equal(ref[2], cap_st[2]) and torch.equal(ref[3], cap_st[3])
+        for a, b in zip(ref[0] + ref[1], cap_st[0] + cap_st[1]):
+            assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    a, b = fresh(), fresh()
+    torch.cuda.synchronize()
+    token(a, stream=side)
+    token(b)
+    torch.cuda.synchronize()
+    assert torch.equal(a[2], b[2]) and torch.equal(a[0][0], b[0][0])

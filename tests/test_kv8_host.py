@@ -1,0 +1,116 @@
+"""The 8-bit cache's calls without a GPU: argument checks on the host, workspace
+sizes, the Python binding's refusals, and the tests' own model of the formats."""
+import numpy as np
+import pytest
+import torch
+
+import kv8_util as ku
+
+FAKE = 1 << 40   # never dereferenced: every call below fails validation first
+
+
+@pytest.fixture(scope="module")
+def R():
+    from paper_2606_31519_amd import rbq
+    return rbq
+
+
+def _quant(R, back=False, **k):
+    g = k.get
+    if back:
+        return R.lib.rbq_dequantize_kv(g("B", 1), g("H", 2), g("D", 128), g("K8", FAKE), FAKE, g("fmt", 16), g("block", 64),
+                                       g("ks", FAKE), FAKE, g("cap", 100), g("n", 10), g("off", 0), g("K", FAKE), FAKE,
+                                       g("dt", 1), g("ld", 10), g("so", None), g("sn", None), 0)
+    return R.lib.rbq_quantize_kv(g("B", 1), g("H", 2), g("D", 128), g("K", FAKE), FAKE, g("dt", 1), g("ld", 10),
+                                 g("n", 10), g("off", 0), g("cap", 100), g("block", 64), g("fmt", 16), g("K8", FAKE), FAKE,
+                                 g("ks", FAKE), FAKE, g("so", None), g("sn", None), 0)
+
+
+@pytest.mark.parametrize("back", [False, True])
+def test_cache_writes_and_reads_reject_invalid_arguments(R, back):
+    E, U = R.RBQ_EINVAL, R.RBQ_EUNSUPPORTED
+    for kw, want in [(dict(B=0), E), (dict(H=0), E), (dict(D=96), U), (dict(D=100), E), (dict(dt=2), U), (dict(dt=16), U),
+                     (dict(fmt=1), U), (dict(fmt=18), U), (dict(block=0), E), (dict(block=-16), E), (dict(block=48), E),
+                     (dict(block=8), U), (dict(block=512), U), (dict(n=-1), E), (dict(off=-1), E), (dict(off=91), E),
+                     (dict(ld=9), E), (dict(ld=1 << 31), E), (dict(cap=9), E), (dict(K=None), E), (dict(K=FAKE + 8), E),
+                     (dict(K8=None), E), (dict(K8=FAKE + 4), E), (dict(ks=None), E), (dict(so=FAKE + 4), E),
+                     (dict(sn=FAKE + 8), E), (dict(cap=(1 << 31) - 1, off=1 << 24), E), (dict(B=65536), E)]:
+        assert _quant(R, back, **kw) == want, kw
+    assert _quant(R, back, n=0, K=None, K8=None, ks=None) == R.RBQ_OK   # no rows: nothing read, nothing enqueued
+
+
+def _decode(R, sparse, **k):
+    g = k.get
+    sel = (g("sel", FAKE), g("cnt", FAKE)) if sparse else ()
+    fn = R.lib.rbq_sparse_decode_kv8 if sparse else R.lib.rbq_dense_decode_kv8
+    return fn(g("B", 1), g("Hq", 8), g("Hkv", 4), g("D", 128), g("q", FAKE), g("K8", FAKE), FAKE, g("fmt", 17),
+              g("block", 32), g("ks", FAKE), FAKE, g("cap", 100), g("n", 100), *sel, g("kl", FAKE), FAKE, g("ldt", 1),
+              g("ld", 20), g("w", 10), g("tau", 0.1), g("out", FAKE), None, g("ws", FAKE), g("wsb", 1 << 30),
+              g("sn", None), g("sw", None), 0)
+
+
+@pytest.mark.parametrize("sparse", [False, True])
+def test_attention_rejects_invalid_arguments(R, sparse):
+    E, U = R.RBQ_EINVAL, R.RBQ_EUNSUPPORTED
+    cases = [(dict(B=0), E), (dict(Hq=6), E), (dict(Hq=12), U), (dict(Hq=128), U), (dict(D=96), U), (dict(fmt=0), U),
+             (dict(block=24), E), (dict(block=1024), U), (dict(n=101), E), (dict(n=-1), E), (dict(cap=99), E),
+             (dict(w=5000, ld=5000), E), (dict(w=21), E), (dict(w=-1), E), (dict(kl=None), E), (dict(kl=FAKE + 2), E),
+             (dict(ldt=16), U), (dict(tau=0.0), E), (dict(tau=float("nan")), E), (dict(tau=float("inf")), E),
+             (dict(q=None), E), (dict(K8=None), E), (dict(ks=None), E), (dict(ks=FAKE + 4), E), (dict(out=None), E),
+             (dict(ws=None), E), (dict(wsb=64), E), (dict(sn=FAKE + 4), E), (dict(sw=FAKE + 4), E),
+             (dict(n=1 << 24, cap=1 << 24), E)]
+    if sparse:
+        cases += [(dict(sel=None), E), (dict(cnt=None), E), (dict(sel=FAKE + 4), E)]
+    for kw, want in cases:
+        assert _decode(R, sparse, **kw) == want, kw
+
+
+def test_other_calls_do_not_take_the_8_bit_formats(R):
+    st = R.lib.rbq_dense_decode(1, 8, 4, 128, FAKE, FAKE, FAKE, R.RBQ_E4M3, 100, 100, None, None, 0, 0, 0.1, FAKE, None,
+                                FAKE, 1 << 30, 0)
+    assert st == R.RBQ_EUNSUPPORTED
+
+
+def test_workspace_is_that_of_the_full_precision_call(R):
+    for n, w in [(0, 0), (1, 0), (0, 5), (4000, 129), (130816, 256)]:
+        a = R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, 1, 32, 8, 128, n, w)
+        assert a > 0 and a == R.rbq_workspace_bytes(R.RBQ_OP_DENSE_DECODE, 1, 32, 8, 128, n, w)
+
+
+def test_binding_refuses_short_or_mixed_buffers(R):
+    B, H, D, cap, block = 1, 2, 64, 64, 16
+    i8 = torch.zeros(B, H, cap, D, dtype=torch.int8)
+    e4 = torch.zeros(B, H, cap, D, dtype=torch.float8_e4m3fn)
+    s = torch.zeros(B, H, cap // block)
+    x = torch.zeros(B, H, 4, D)
+    with pytest.raises(ValueError):    # two formats
+        R.rbq_quantize_kv(B, H, D, x, x, 4, 4, 0, cap, block, i8, e4, s, s)
+    with pytest.raises(ValueError):    # scales for fewer blocks
+        R.rbq_quantize_kv(B, H, D, x, x, 4, 4, 0, cap, block, i8, i8, s[:, :, :3], s)
+    with pytest.raises(ValueError):    # fewer source rows
+        R.rbq_quantize_kv(B, H, D, x, x, 5, 5, 0, cap, block, i8, i8, s, s)
+    with pytest.raises(ValueError):    # two source types
+        R.rbq_quantize_kv(B, H, D, x, x.bfloat16(), 4, 4, 0, cap, block, i8, i8, s, s)
+    with pytest.raises(ValueError):    # no 8-bit type
+        R.rbq_quantize_kv(B, H, D, x, x, 4, 4, 0, cap, block, x, x, s, s)
+    with pytest.raises(ValueError):    # outputs of fewer rows
+        R.rbq_dequantize_kv(B, H, D, i8, i8, block, s, s, cap, 8, 0, x, x, 8)
+    q, out, lse, ws = torch.zeros(B, 4, D), torch.zeros(B, 4, D), torch.zeros(B, 4), torch.zeros(1 << 16, dtype=torch.uint8)
+    with pytest.raises(ValueError):    # a window of fewer rows
+        R.rbq_dense_decode_kv8(B, 4, H, D, q, i8, i8, block, s, s, cap, cap, x, x, 5, 5, 0.1, out, lse, ws)
+    with pytest.raises(ValueError):    # a selection of fewer entries
+        R.rbq_sparse_decode_kv8(B, 4, H, D, q, i8, i8, block, s, s, cap, cap, torch.zeros(B, 4, cap - 1, dtype=torch.int32),
+                                torch.zeros(B, 4, dtype=torch.int32), None, None, 0, 0, 0.1, out, lse, ws)
+
+
+def test_the_models_e4m3_is_the_ocp_format():
+    v = np.concatenate([ku.E4M3, -ku.E4M3])
+    t = torch.from_numpy(v).float().to(torch.float8_e4m3fn)
+    assert np.array_equal(t.double().numpy(), v)
+    assert np.array_equal(t.view(torch.uint8).numpy(), ku.encode_values(v, "e4m3"))
+    x = np.random.default_rng(1).standard_normal(20000) * np.exp(np.random.default_rng(2).uniform(-9, 5, 20000))
+    x = np.clip(x.astype(np.float32), -448, 448)
+    mid = ((ku.E4M3[:-1] + ku.E4M3[1:]) / 2).astype(np.float32)   # ties
+    for y in (x, mid, -mid):
+        t = torch.from_numpy(y).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+        assert np.array_equal(t, ku.encode_values(y.astype(np.float64), "e4m3"))
