@@ -71,6 +71,7 @@ typedef enum rbq_kv8_dtype { RBQ_E4M3 = 16, RBQ_I8 = 17 } rbq_kv8_dtype;
 #define RBQ_OP_DENSE_DECODE 4
 #define RBQ_OP_DECODE_STEP 5
 #define RBQ_OP_DECODE_KV8 6       /* rbq_sparse_decode_kv8 and rbq_dense_decode_kv8 */
+#define RBQ_OP_PREFILL 7          /* rbq_prefill_attention: n = max_k, w = total_q */
 
 #define RBQ_QSCAL_STRIDE 8   /* floats per query head in qscal */
 #define RBQ_MAX_WINDOW 4096  /* largest local window accepted by the decode calls */
@@ -456,6 +457,44 @@ rbq_status rbq_sparse_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_k
                                  const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
                                  float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
                                  const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream);
+
+/*
+ * rbq_prefill_attention -- the attention of whole prompts (or of chunks of them
+ * behind rows already cached), which fills the cache that the decode calls read:
+ * softmax(q_i . k_j * sm_scale) over the keys of the query's own sequence, packed
+ * queries of sequences of different lengths in one call.
+ *   q    total_q rows of Hq heads: head h of token t at q + t * q_ld + h * D, in
+ *        `dtype` (RBQ_BF16 or RBQ_F32; K, V and out have the same)
+ *   cu_q [B + 1] int32 (device), ascending: sequence b's tokens are
+ *        [cu_q[b], cu_q[b + 1]) of q, out and lse
+ *   cu_k [B + 1] int32 (device), ascending: sequence b has Lk = cu_k[b + 1] -
+ *        cu_k[b] keys, at most max_k (more are not read)
+ *   K, V row r of KV head h of sequence b at K + r * kv_ld + h * kv_head, plus
+ *        b * kv_seq where kv_seq > 0 (every sequence has kv_rows rows of its own: for
+ *        the cache [B][Hkv][cap][D], kv_ld = D, kv_head = cap * D, kv_seq = Hkv * cap
+ *        * D, kv_rows = cap), plus cu_k[b] * kv_ld where kv_seq == 0 (packed like q,
+ *        kv_rows rows in all). Strides are in elements, multiples of 16 bytes,
+ *        kv_ld >= D, q_ld >= Hq * D, q_ld and kv_ld below 2^23.
+ *   causal: nonzero: token i of a sequence of Lq tokens sees keys j <= i + Lk - Lq
+ *        (its own key is the last it sees when the chunk's keys end the sequence);
+ *        0: every key
+ *   out  [total_q][Hq][D] in `dtype`; lse [total_q][Hq] float or NULL, natural-log
+ *        log-sum-exp of the scaled logits. A token that sees no key: out = 0, lse =
+ *        -inf. Rows of tokens outside every sequence are left as they were.
+ *   ws:  at least rbq_workspace_bytes(RBQ_OP_PREFILL, B, Hq, Hkv, D, max_k, total_q)
+ *        bytes, 0 (then NULL is allowed) unless few rows attend to long keys.
+ * Products and sums in fp32; with RBQ_BF16 the probabilities are rounded to bf16
+ * before they meet V. A NaN or infinity in a row of V may also reach tokens up to 63
+ * places before the first one that sees it. Device counts are not checked on the
+ * host: lengths outside the buffers are clamped to them. Any group size up to 16.
+ * RBQ_EUNSUPPORTED also beyond 2^24 tiles of 128 (token, head of the group) rows.
+ */
+rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                                 const void* q, int64_t q_ld, const void* K, const void* V, int32_t dtype,
+                                 int64_t kv_ld, int64_t kv_head, int64_t kv_seq, int32_t kv_rows,
+                                 const int32_t* cu_q, const int32_t* cu_k, int32_t total_q, int32_t max_k,
+                                 int32_t causal, float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes,
+                                 hipStream_t stream);
 
 /*
  * rbq_mapped_device_pointer -- the device address of pinned host memory

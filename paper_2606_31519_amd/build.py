@@ -16,7 +16,7 @@ BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "librbq.so")
 
 HIP_SOURCES = ["api.hip", "score.hip", "quantize.hip", "encode.hip", "topp.hip", "decode.hip", "kv8.hip",
-               "decode_kv8.hip"]
+               "decode_kv8.hip", "prefill.hip"]
 CXX_SOURCES = ["validate.cpp"]          # plain C++ (no HIP): host-side argument checks
 
 ARCH = "gfx950"

@@ -485,4 +485,16 @@ rbq_status rbq_sparse_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_k
                            ws, true, stream, nullptr, 0, seq_n, seq_w);
 }
 
+rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const void* q,
+                                 int64_t q_ld, const void* K, const void* V, int32_t dtype, int64_t kv_ld,
+                                 int64_t kv_head, int64_t kv_seq, int32_t kv_rows, const int32_t* cu_q,
+                                 const int32_t* cu_k, int32_t total_q, int32_t max_k, int32_t causal, float sm_scale,
+                                 void* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const PrefillArgs a{q, q_ld, K, V, kv_ld, kv_head, kv_seq, kv_rows, dtype, cu_q, cu_k, total_q, max_k, causal,
+                      sm_scale, out, lse, ws, ws_bytes};
+  const rbq_status s = check_prefill(batch, heads_q, heads_kv, head_dim, a);
+  if (s != RBQ_OK) return s;
+  return launch_prefill(batch, heads_q, heads_kv, head_dim, a, stream);
+}
+
 }  // extern "C"

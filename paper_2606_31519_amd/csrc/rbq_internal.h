@@ -56,6 +56,34 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
                             const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
                             const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w);
 
+// The prompt's attention.
+struct PrefillArgs {
+  const void* q;
+  int64_t q_ld;
+  const void *K, *V;
+  int64_t kv_ld, kv_head, kv_seq;
+  int32_t kv_rows, dtype;
+  const int32_t *cu_q, *cu_k;
+  int32_t total_q, max_k, causal;
+  float sm_scale;
+  void* out;
+  float* lse;
+  void* ws;
+  size_t ws_bytes;
+};
+rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a);
+// How it is cut: query tiles of `rows` (token, head of the group) rows of one
+// sequence and KV head, and, where those are too few for the GPU, the keys into
+// `splits` chunks of `kchunk`, joined by a second kernel.
+struct PrefillPlan {
+  int32_t rows, tiles;   // tiles: an upper bound over the sequences, per KV head
+  int32_t splits, kchunk;
+};
+PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t max_k, int32_t total_q,
+                         int32_t dtype);
+size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
+                               int32_t total_q);
+
 // ---------------------------------------------------------------- workspace layouts
 // Top-p: a row of scores of at most kSelRowMax keys is selected by one block; a
 // longer one is cut into parts of spb sub-chunks of kSelSub keys, one block of
@@ -255,5 +283,8 @@ rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, i
                              const Kv8Window& win, float sm_scale, float* out, float* lse, void* ws, bool sparse,
                              hipStream_t stream, const unsigned long long* sel_mask = nullptr, int32_t mask_words = 0,
                              const int32_t* seq_n = nullptr, const int32_t* seq_w = nullptr);
+
+rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a,
+                          hipStream_t stream);
 
 }  // namespace rbq

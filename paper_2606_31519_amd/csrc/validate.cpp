@@ -1,7 +1,9 @@
 // Host-side argument checks and workspace sizing. No HIP calls: everything
 // here runs (and is tested) without a GPU.
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "rbq_internal.h"
 
@@ -9,6 +11,9 @@ namespace rbq {
 
 namespace {
 constexpr int64_t kMaxRows = int64_t(1) << 31;
+constexpr int64_t kMaxStride = int64_t(1) << 23;   // elements: 64 rows of it are addressed with 32-bit byte offsets
+constexpr int64_t kCus = 256;                      // compute units of the GPU
+constexpr int64_t kPrefillMinKeys = 256;           // keys per split, at least
 // a required device pointer: present, and 16-byte aligned (the kernels use 16-byte vector loads)
 bool bad_ptr(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 }  // namespace
@@ -221,6 +226,59 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
   return RBQ_OK;
 }
 
+PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t max_k, int32_t total_q,
+                         int32_t dtype) {
+  const int64_t rows = int64_t(total_q) * (heads_q / heads_kv);
+  PrefillPlan p;
+  p.rows = dtype == RBQ_BF16 && rows * heads_kv >= int64_t(256) * 2 * kCus ? 256 : 128;
+  p.tiles = int32_t(rows / p.rows + batch);
+  const int64_t blocks = (rows + p.rows - 1) / p.rows * heads_kv;
+  int64_t want = blocks < kCus ? (2 * kCus + blocks - 1) / blocks : 1;
+  want = std::min<int64_t>(want, (int64_t(max_k) + kPrefillMinKeys - 1) / kPrefillMinKeys);
+  want = std::max<int64_t>(want, 1);
+  p.kchunk = int32_t(((int64_t(max_k) + want - 1) / want + 63) / 64 * 64);
+  if (p.kchunk == 0) p.kchunk = 64;
+  p.splits = std::max<int32_t>(int32_t((int64_t(max_k) + p.kchunk - 1) / p.kchunk), 1);
+  return p;
+}
+
+size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
+                               int32_t total_q) {
+  if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || max_k < 0 || total_q <= 0) return 0;
+  if (heads_q % heads_kv != 0) return 0;
+  size_t need = 0;
+  for (int32_t dtype : {RBQ_F32, RBQ_BF16}) {
+    const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, max_k, total_q, dtype);
+    if (p.splits > 1) need = std::max(need, size_t(total_q) * heads_q * p.splits * (size_t(head_dim) + 2) * sizeof(float));
+  }
+  return align_up(need, 256);
+}
+
+rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a) {
+  rbq_status s = check_heads(batch, heads_q, heads_kv, head_dim);
+  if (s != RBQ_OK) return s;
+  if (a.dtype != RBQ_F32 && a.dtype != RBQ_BF16) return RBQ_EUNSUPPORTED;
+  const int64_t align = a.dtype == RBQ_BF16 ? 8 : 4;   // elements of 16 bytes
+  if (a.total_q < 0 || a.max_k < 0 || a.kv_rows < 0) return RBQ_EINVAL;
+  if (a.q_ld < int64_t(heads_q) * head_dim || a.q_ld % align != 0) return RBQ_EINVAL;
+  if (a.kv_ld < head_dim || a.kv_ld % align != 0 || a.kv_head < 0 || a.kv_head % align != 0 || a.kv_seq < 0 ||
+      a.kv_seq % align != 0)
+    return RBQ_EINVAL;
+  if (a.q_ld >= kMaxStride || a.kv_ld >= kMaxStride) return RBQ_EUNSUPPORTED;
+  if (!std::isfinite(a.sm_scale) || !(a.sm_scale > 0.0f)) return RBQ_EINVAL;
+  if (a.total_q == 0) return RBQ_OK;
+  // the rows of a sequence (tokens times heads of a group) and the grid are 32-bit numbers
+  const int64_t rows = int64_t(a.total_q) * (heads_q / heads_kv);
+  if (rows >= kMaxRows - 256 || (rows / 128 + batch) * heads_kv >= (int64_t(1) << 24)) return RBQ_EUNSUPPORTED;
+  if (bad_ptr(a.q) || bad_ptr(a.out) || bad_ptr(a.cu_q) || bad_ptr(a.cu_k)) return RBQ_EINVAL;
+  if (a.kv_rows > 0 && a.max_k > 0 && (bad_ptr(a.K) || bad_ptr(a.V))) return RBQ_EINVAL;
+  const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, a.max_k, a.total_q, a.dtype);
+  if (p.splits > 1 &&
+      (bad_ptr(a.ws) || a.ws_bytes < prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q)))
+    return RBQ_EINVAL;
+  return RBQ_OK;
+}
+
 // Keys per lane of the score kernel: enough blocks to cover the 256 CUs
 // several times over, as many keys in flight per lane as that allows.
 int score_keys_per_lane(int32_t batch, int32_t heads_kv, int32_t n) {
@@ -266,6 +324,8 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
     case RBQ_OP_DENSE_DECODE:
     case RBQ_OP_DECODE_KV8:
       return rbq::decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
+    case RBQ_OP_PREFILL:
+      return rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_DECODE_STEP:
       if (heads_q % heads_kv != 0) return 0;
       return rbq::step_workspace(nullptr, batch, heads_q, heads_kv, head_dim, n, w).bytes;

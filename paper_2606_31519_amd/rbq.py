@@ -20,7 +20,7 @@ RBQ_F32, RBQ_BF16 = 0, 1
 RBQ_E4M3, RBQ_I8 = 16, 17   # formats of the 8-bit cache
 RBQ_ENCODE_SET_CENTROID = 1
 RBQ_OP_ENCODE, RBQ_OP_TOPP, RBQ_OP_SPARSE_DECODE, RBQ_OP_DENSE_DECODE, RBQ_OP_DECODE_STEP = 1, 2, 3, 4, 5
-RBQ_OP_DECODE_KV8 = 6
+RBQ_OP_DECODE_KV8, RBQ_OP_PREFILL = 6, 7
 QSCAL_STRIDE = 8
 RBQ_MAX_WINDOW = 4096   # largest local window accepted by the decode calls
 RBQ_NOALLOC_SCRATCH_BYTES = 16 << 20   # the static scratch of rbq_decode_step_noalloc
@@ -35,6 +35,7 @@ EXPORTED = [
     "rbq_encode_keys_f16", "rbq_score_f16", "rbq_decode_step_f16", "rbq_score_varlen_f16", "rbq_decode_step_varlen_f16",
     "rbq_decode_step_noalloc",
     "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8",
+    "rbq_prefill_attention",
 ]
 
 
@@ -94,6 +95,8 @@ def _load():
                                  f32, vp, vp, vp, sz, vp, vp, vp],
         "rbq_sparse_decode_kv8": [i32, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32,
                                   i64, i32, f32, vp, vp, vp, sz, vp, vp, vp],
+        "rbq_prefill_attention": [i32, i32, i32, i32, vp, i64, vp, vp, i32, i64, i64, i64, i32, vp, vp, i32, i32, i32,
+                                  f32, vp, vp, vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -509,3 +512,19 @@ def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, 
         _ptr(v_scale), cap, n, _ptr(sel_idx), _ptr(sel_count), _ptr(K_loc), _ptr(V_loc),
         _kv8_window(name, K_loc, V_loc), loc_ld, w, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _ptr(seq_n),
         _ptr(seq_w), _stream(stream)))
+
+
+def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_ld, kv_head, kv_seq, kv_rows, cu_q,
+                          cu_k, total_q, max_k, causal, sm_scale, out, lse, ws=None, stream=None):
+    """Attention of prompts packed along one token axis: q [total_q][Hq][D] (rows q_ld elements apart), cu_q and cu_k
+    [batch + 1] int32 device tensors; K / V rows kv_ld elements apart, heads kv_head, sequences kv_seq (0: packed)."""
+    name = "rbq_prefill_attention"
+    if not q.dtype == K.dtype == V.dtype == out.dtype:
+        raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
+    _need(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, total_q * heads_q * head_dim),
+          lse=(lse, total_q * heads_q))
+    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    _check(name, lib.rbq_prefill_attention(
+        batch, heads_q, heads_kv, head_dim, _ptr(q), q_ld, _ptr(K), _ptr(V), kv_dtype_code(K), kv_ld, kv_head, kv_seq,
+        kv_rows, _ptr(cu_q), _ptr(cu_k), total_q, max_k, int(bool(causal)), sm_scale, _ptr(out), _ptr(lse), _ptr(ws),
+        ws_bytes, _stream(stream)))

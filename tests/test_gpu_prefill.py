@@ -1,0 +1,219 @@
+"""rbq_prefill_attention against 64 bits: whole prompts and chunks over cached rows,
+packed and strided layouts, sequences of any length (none, one, many), group sizes
+that are no powers of two, rows that see nothing, keys split over blocks."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from kv8_util import attention_tolerance
+
+pytestmark = pytest.mark.gpu
+
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def R():
+    assert torch.cuda.is_available(), "GPU tests need a ROCm device"
+    from paper_2606_31519_amd import rbq
+    return rbq
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+class Inputs:
+    """Packed q / k / v of one fused projection ([tokens][Hq + 2 Hkv][D], layout "fused"), packed buffers of their own
+    ("packed"), or K and V in a cache [B][Hkv][cap][D] ("cache")."""
+
+    def __init__(self, seed, dt, Hq, Hkv, D, qs, ks, layout, lead=0, tail=0):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda *s: torch.randn(*s, device="cuda", generator=g).to(DT[dt])  # noqa: E731
+        self.dt, self.Hq, self.Hkv, self.D, self.qs, self.ks, self.layout = dt, Hq, Hkv, D, qs, ks, layout
+        B = self.B = len(qs)
+        cu_q, cu_k = (np.cumsum([s0] + list(v)).tolist() for s0, v in ((lead, qs), (lead if layout == "fused" else 0, ks)))
+        self.cu_q, self.cu_k, self.T = cu_q, cu_k, cu_q[-1] + tail
+        self.max_k = max(ks)
+        rows = max(cu_k[-1], 1)
+        if layout == "fused":
+            self.qkv = rnd(max(self.T, rows), Hq + 2 * Hkv, D)
+            self.q, self.K, self.V = self.qkv[:, :Hq], self.qkv[:, Hq:Hq + Hkv], self.qkv[:, Hq + Hkv:]
+            ld = (Hq + 2 * Hkv) * D
+            self.q_ld, self.lay = ld, (ld, D, 0, rows)
+        else:
+            self.q, self.q_ld = rnd(max(self.T, 1), Hq, D), Hq * D
+            if layout == "packed":
+                self.K, self.V = rnd(rows, Hkv, D), rnd(rows, Hkv, D)
+                self.lay = (Hkv * D, D, 0, rows)
+            else:
+                cap = self.max_k + 3
+                self.K, self.V = rnd(B, Hkv, cap, D), rnd(B, Hkv, cap, D)
+                for b in range(B):      # rows that no sequence has
+                    self.K[b, :, ks[b]:] = float("nan")
+                    self.V[b, :, ks[b]:] = float("nan")
+                self.lay = (D, cap * D, Hkv * cap * D, cap)
+        self.tau = 1.0 / math.sqrt(D)
+
+    def run(self, R, causal, ws=None, stream=None, out=None, lse=None):
+        out = torch.full((max(self.T, 1), self.Hq, self.D), 5.0, dtype=DT[self.dt], device="cuda") if out is None else out
+        lse = torch.full((max(self.T, 1), self.Hq), 5.0, device="cuda") if lse is None else lse
+        if ws is None:
+            ws = R.workspace(R.RBQ_OP_PREFILL, self.B, self.Hq, self.Hkv, self.D, self.max_k, self.T)
+            ws.fill_(255)               # NaN patterns: nothing is read before it is written
+        if not hasattr(self, "cu"):
+            self.cu = i32(self.cu_q), i32(self.cu_k)
+        R.rbq_prefill_attention(self.B, self.Hq, self.Hkv, self.D, self.q, self.q_ld, self.K, self.V, *self.lay, *self.cu,
+                                self.T, self.max_k, causal, self.tau, out, lse, ws, stream=stream)
+        return out, lse
+
+    def sequence(self, b):
+        q = self.q[self.cu_q[b]:self.cu_q[b + 1]].double().cpu().numpy()
+        if self.layout == "cache":
+            k, v = (t[b, :, :self.ks[b]].double().cpu().numpy() for t in (self.K, self.V))
+        else:
+            k, v = (t[self.cu_k[b]:self.cu_k[b + 1]].double().cpu().numpy().transpose(1, 0, 2) for t in (self.K, self.V))
+        return q, k, v
+
+
+def check(inp, out, lse, causal, heads=None):
+    out, lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    for b in range(inp.B):
+        q, k, v = inp.sequence(b)
+        nq, nk = inp.qs[b], inp.ks[b]
+        if nq == 0:
+            continue
+        for h in (range(inp.Hq) if heads is None else heads):
+            K, V = k[h // (inp.Hq // inp.Hkv)], v[h // (inp.Hq // inp.Hkv)]
+            o, l = out[inp.cu_q[b]:inp.cu_q[b + 1], h], lse[inp.cu_q[b]:inp.cu_q[b + 1], h]
+            S = q[:, h] @ K.T * inp.tau
+            if causal:
+                S = np.where(np.arange(nk)[None] <= np.arange(nq)[:, None] + nk - nq, S, -np.inf)
+            m = S.max(axis=1, initial=-np.inf)
+            some = m > -np.inf
+            p = np.exp(S - np.where(some, m, 0.0)[:, None])
+            tot = np.where(some, p.sum(axis=1), 1.0)
+            want = p @ V / tot[:, None]
+            assert np.all(o[~some] == 0) and np.all(l[~some] == -np.inf)
+            if not some.any():
+                continue
+            # (the fp32 bound of the longest row, for the sequence's largest query)
+            big = q[np.argmax((np.abs(q[:, h]) @ np.abs(K).T).max(axis=1)), h]
+            ot, lt = attention_tolerance(big, K, V, inp.tau)
+            if inp.dt == "bf16":   # each probability and the result are off by up to half a step of bf16
+                ot = ot + 2.0 ** -8 * (p @ np.abs(V) / tot[:, None] + np.abs(want))
+            assert np.all(np.abs(o - want) <= ot), (b, h, np.abs(o - want).max())
+            wl = m + np.log(tot)
+            assert np.all(np.abs(l - wl)[some] <= lt), (b, h, np.abs(l - wl)[some].max(), lt)
+
+
+# dtype, Hq, Hkv, D, tokens, keys, layout, causal
+CASES = [
+    ("bf16", 8, 2, 128, [1], [1], "packed", True),
+    ("bf16", 8, 2, 128, [257], [257], "fused", True),
+    ("bf16", 4, 4, 64, [63, 1, 0, 130, 64], [63, 1, 0, 130, 64], "fused", True),
+    ("bf16", 6, 2, 128, [100, 31, 7], [164, 31, 300], "packed", True),          # three heads a group; chunks
+    ("bf16", 16, 1, 64, [9, 40], [700, 65], "cache", True),
+    ("bf16", 5, 1, 128, [50, 3, 20], [20, 0, 20], "packed", True),              # more tokens than keys: rows that see nothing
+    ("bf16", 8, 2, 128, [33, 65], [190, 64], "cache", False),
+    ("bf16", 32, 8, 128, [300, 17, 460], [300, 17, 460], "packed", True),        # 256-row tiles
+    ("bf16", 16, 2, 64, [1100], [1100], "fused", True),
+    ("bf16", 8, 2, 128, [1, 3], [4097, 5000], "cache", True),                   # keys split over blocks
+    ("bf16", 8, 1, 64, [2], [9001], "packed", False),
+    ("f32", 8, 2, 128, [1, 40], [1, 40], "packed", True),
+    ("f32", 4, 4, 64, [33, 0, 129], [65, 5, 129], "fused", True),
+    ("f32", 6, 2, 128, [20, 5], [90, 3], "cache", True),
+    ("f32", 2, 1, 64, [31], [64], "packed", False),
+    ("f32", 4, 1, 128, [3], [3001], "cache", True),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=[f"{c[0]}-Hq{c[1]}-Hkv{c[2]}-D{c[3]}-{c[6]}-q{max(c[4])}-k{max(c[5])}" for c in CASES])
+def test_attention_of_prompts(R, case):
+    dt, Hq, Hkv, D, qs, ks, layout, causal = case
+    if layout == "fused":
+        ks = qs                       # one token axis
+    print("case", case, flush=True)
+    inp = Inputs(17, dt, Hq, Hkv, D, qs, ks, layout)
+    out, lse = inp.run(R, causal)
+    torch.cuda.synchronize()
+    check(inp, out, lse, causal)
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 128), ("f32", 64)])
+def test_many_sequences_and_rows_outside_them(R, dt, D):
+    """More sequences than a wave has lanes, empty ones among them; tokens before the first and behind the last."""
+    rng = np.random.default_rng(8)
+    qs = [int(v) for v in rng.integers(0, 40, 150)]
+    ks = [v + int(e) for v, e in zip(qs, rng.integers(0, 30, 150))]
+    inp = Inputs(5, dt, 4, 2, D, qs, ks, "packed", lead=3, tail=11)
+    out, lse = inp.run(R, True)
+    torch.cuda.synchronize()
+    assert torch.all(out[:3] == 5.0) and torch.all(out[-11:] == 5.0) and torch.all(lse[:3] == 5.0) and torch.all(lse[-11:] == 5.0)
+    check(inp, out, lse, True, heads=(0, 3))
+
+
+def test_rows_outside_the_sequences_with_split_keys(R):
+    inp = Inputs(6, "bf16", 8, 2, 128, [2, 1], [3000, 1500], "packed", lead=2, tail=3)
+    assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 2, 8, 2, 128, 3000, inp.T) > 0
+    out, lse = inp.run(R, True)
+    torch.cuda.synchronize()
+    assert torch.all(out[:2] == 5.0) and torch.all(out[-3:] == 5.0) and torch.all(lse[:2] == 5.0) and torch.all(lse[-3:] == 5.0)
+    check(inp, out, lse, True)
+
+
+def test_lengths_beyond_the_buffers_are_clamped(R):
+    """Device counts that pass max_k, the rows or the tokens read and write inside the buffers only: the results are those
+    of the clamped lengths."""
+    inp = Inputs(9, "bf16", 4, 2, 64, [40, 24], [100, 60], "cache")
+    want = inp.run(R, False)
+    inp.cu = i32([0, 40, 1000]), i32([0, 100, 160])
+    got = inp.run(R, False)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    short = Inputs(9, "bf16", 4, 2, 64, [40, 24], [70, 60], "cache")
+    short.K, short.V, short.lay = inp.K, inp.V, inp.lay
+    want = short.run(R, False)
+    inp.cu = i32([0, 40, 64]), i32([0, 100, 160])
+    inp.max_k = 70
+    got = inp.run(R, False)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_large_logits_and_a_rising_maximum(R):
+    """Keys whose logits grow along the sequence (the running maximum moves at every step) and reach thousands."""
+    inp = Inputs(10, "bf16", 4, 1, 128, [200], [900], "packed")
+    inp.K.mul_(torch.linspace(0.1, 60.0, 900, device="cuda")[:, None, None].to(torch.bfloat16))
+    out, lse = inp.run(R, True)
+    torch.cuda.synchronize()
+    check(inp, out, lse, True)
+
+
+@pytest.mark.parametrize("qs,ks", [([90, 30], [90, 95]), ([2, 1], [3000, 2000])], ids=["whole", "split"])
+def test_graph_replays_and_two_streams(R, qs, ks):
+    inp = Inputs(11, "bf16", 8, 2, 128, qs, ks, "packed")
+    want = [t.clone() for t in inp.run(R, True)]
+    again = inp.run(R, True)
+    torch.cuda.synchronize()
+    assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1])     # run to run
+    ws = R.workspace(R.RBQ_OP_PREFILL, inp.B, 8, 2, 128, inp.max_k, inp.T)
+    out, lse = torch.zeros_like(want[0]), torch.zeros_like(want[1])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        inp.run(R, True, ws=ws, out=out, lse=lse)
+    for i in range(4):
+        inp.q.copy_(torch.randn(inp.q.shape, device="cuda").to(inp.q.dtype))
+        inp.cu[1].copy_(i32([0, ks[0] - i, sum(ks) - i]))
+        graph.replay()
+        eager = inp.run(R, True)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    a = inp.run(R, True, stream=side, ws=ws, out=out, lse=lse)
+    b = inp.run(R, True)
+    torch.cuda.synchronize()
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])

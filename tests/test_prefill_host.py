@@ -1,0 +1,61 @@
+"""rbq_prefill_attention without a GPU: argument checks, workspace sizes and the
+binding's refusals."""
+import pytest
+import torch
+
+FAKE = 1 << 40   # never dereferenced: every call below fails validation first
+
+
+@pytest.fixture(scope="module")
+def R():
+    from paper_2606_31519_amd import rbq
+    return rbq
+
+
+def _call(R, **k):
+    g = k.get
+    return R.lib.rbq_prefill_attention(g("B", 2), g("Hq", 8), g("Hkv", 4), g("D", 128), g("q", FAKE), g("q_ld", 1024),
+                                       g("K", FAKE), g("V", FAKE), g("dt", 1), g("kv_ld", 512), g("kv_head", 128),
+                                       g("kv_seq", 0), g("kv_rows", 100), g("cu_q", FAKE), g("cu_k", FAKE), g("T", 100),
+                                       g("max_k", 60), 1, g("tau", 0.1), g("out", FAKE), None, g("ws", None), g("wsb", 0), 0)
+
+
+def test_invalid_arguments_are_rejected_on_the_host(R):
+    E, U = R.RBQ_EINVAL, R.RBQ_EUNSUPPORTED
+    for kw, want in [(dict(B=0), E), (dict(Hq=6), E), (dict(Hq=128), U), (dict(D=96), U), (dict(D=100), E), (dict(dt=2), U),
+                     (dict(dt=16), U), (dict(T=-1), E), (dict(max_k=-1), E), (dict(kv_rows=-1), E), (dict(q_ld=1016), E),
+                     (dict(q_ld=1028), E), (dict(q_ld=1 << 23), U), (dict(kv_ld=120), E), (dict(kv_ld=516), E),
+                     (dict(kv_ld=1 << 23), U), (dict(kv_head=-8), E), (dict(kv_head=4), E), (dict(kv_seq=-8), E),
+                     (dict(kv_seq=12), E), (dict(tau=0.0), E), (dict(tau=float("nan")), E), (dict(q=None), E),
+                     (dict(q=FAKE + 8), E), (dict(K=None), E), (dict(V=FAKE + 2), E), (dict(out=None), E),
+                     (dict(cu_q=None), E), (dict(cu_k=None), E), (dict(cu_q=FAKE + 4), E), (dict(T=1 << 30), U)]:
+        assert _call(R, **kw) == want, kw
+    assert _call(R, T=0, q=None, K=None, V=None, out=None, cu_q=None, cu_k=None) == R.RBQ_OK   # nothing to do
+
+
+def test_few_rows_over_long_keys_need_a_workspace(R):
+    assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 1, 32, 8, 128, 16000, 16000) == 0
+    need = R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 1, 32, 8, 128, 131072, 5)
+    assert need >= 5 * 32 * 130 * 4 * 2
+    kw = dict(B=1, Hq=32, Hkv=8, q_ld=4096, kv_ld=1024, kv_rows=131072, max_k=131072, T=5)
+    assert _call(R, **kw) == R.RBQ_EINVAL
+    assert _call(R, **kw, ws=FAKE, wsb=need - 256) == R.RBQ_EINVAL
+    assert _call(R, **kw, ws=FAKE + 8, wsb=need) == R.RBQ_EINVAL
+    for a in [(0, 32, 8, 128, 100, 5), (1, 32, 0, 128, 100, 5), (1, 6, 4, 128, 100, 5), (1, 32, 8, 128, -1, 5),
+              (1, 32, 8, 128, 100, 0)]:
+        assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, *a) == 0
+
+
+def test_binding_refuses_short_or_mixed_buffers(R):
+    T, H, D = 4, 2, 64
+    x, cu = torch.zeros(T, H, D), torch.tensor([0, T], dtype=torch.int32)
+    args = lambda **k: (1, H, H, D, k.get("q", x), H * D, k.get("K", x), x, H * D, D, 0, T, k.get("cu_q", cu),  # noqa: E731
+                        k.get("cu_k", cu), T, T, True, 0.1, k.get("out", torch.zeros(T, H, D)),
+                        k.get("lse", torch.zeros(T, H)))
+    for kw in (dict(q=x.bfloat16()), dict(K=x.bfloat16()), dict(out=torch.zeros(T, H, D).bfloat16()),
+               dict(out=torch.zeros(T - 1, H, D)), dict(lse=torch.zeros(T, H - 1)), dict(cu_q=cu[:1]), dict(cu_k=cu[:1])):
+        with pytest.raises(ValueError):
+            R.rbq_prefill_attention(*args(**kw))
+    half = x.half()
+    with pytest.raises(ValueError):
+        R.rbq_prefill_attention(*args(q=half, K=half, out=half)[:7], half, *args(out=half)[8:])
