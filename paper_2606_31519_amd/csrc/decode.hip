@@ -338,9 +338,6 @@ struct GroupLoads {
 // faster). Sparser blocks, and groups of 8 or 16 heads (three products per
 // 16 rows for the logits instead of one), are bound by latency and compute;
 // there the policy measured slower.
-constexpr int kSkipOffset = 0x7FFFFF00;
-constexpr int kStream = 2;   // cache-policy bits of the K / V buffer loads: nt
-constexpr int kStreamDenNum = 1, kStreamDenDen = 3;   // a third of the block's positions
 
 template <bool SPARSE, int D, int CP>
 __device__ __forceinline__ void load_group_k(GroupLoads<D>& d, int grp, bool skip, int U, const RowMap& rm,

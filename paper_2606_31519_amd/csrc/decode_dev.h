@@ -18,6 +18,12 @@ static_assert(kListCap == kDecodeListCap, "the split sizing on the host assumes 
 constexpr int kListPad = 16;                                      // a list ends on a whole group of rows
 static_assert(kListCap % kListPad == 0, "the padding fits");
 
+// K / V buffer loads: an offset past every buffer (the load is dropped), the streaming
+// policy's bits, and the share of a sparse block's positions from which on it is used.
+constexpr int kSkipOffset = 0x7FFFFF00;
+constexpr int kStream = 2;   // cache-policy bits of the K / V buffer loads: nt
+constexpr int kStreamDenNum = 1, kStreamDenDen = 3;   // a third of the block's positions
+
 // Lower bounds of x0 and x1 in the ascending a[0, cnt) (first index whose
 // value is >= x), found together by one wave: each round probes 64 evenly
 // spaced entries per search and keeps the gap where the answer lies, so a list
@@ -263,18 +269,23 @@ constexpr int kOrderMinChunk = 512;
 // blocks resident at once (256 CUs; registers, for groups of 16 heads the LDS)
 constexpr int64_t resident_blocks(int D, int G) { return 256 * (D == 64 ? (G == 16 ? 4 : 6) : (G == 16 ? 2 : 4)); }
 constexpr int kOrderHeads = 8;
-__device__ __forceinline__ int sequence_of_rank(int r, int batch, int n, int Hq, int Hkv,
-                                                const int32_t* __restrict__ sel_count,
-                                                const int32_t* __restrict__ seq_n, int& own) {
-  const int lane = lane_id(), b = min(lane, batch - 1), G = Hq / Hkv;
-  own = min(max(seq_n[b], 0), n);
+// the share of sequence b's `own` indexed keys that up to kOrderHeads of its query heads select
+__device__ __forceinline__ float selected_share(int b, int own, int Hq, int Hkv, const int32_t* __restrict__ sel_count) {
+  const int G = Hq / Hkv;
   int cnt[kOrderHeads];
 #pragma unroll
   for (int k = 0; k < kOrderHeads; ++k) cnt[k] = sel_count[b * Hq + k * Hkv / kOrderHeads * G];
   int sum = 0;
 #pragma unroll
   for (int k = 0; k < kOrderHeads; ++k) sum += cnt[k];
-  const float dens = float(sum) / float(max(own, 1));
+  return float(sum) / float(max(own, 1));
+}
+__device__ __forceinline__ int sequence_of_rank(int r, int batch, int n, int Hq, int Hkv,
+                                                const int32_t* __restrict__ sel_count,
+                                                const int32_t* __restrict__ seq_n, int& own) {
+  const int lane = lane_id(), b = min(lane, batch - 1);
+  own = min(max(seq_n[b], 0), n);
+  const float dens = selected_share(b, own, Hq, Hkv, sel_count);
   int rank = 0;
   for (int o = 0; o < batch; ++o) {
     const float d = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(dens)), o)));

@@ -30,9 +30,8 @@
 namespace rbq {
 namespace {
 
-constexpr int kScaleCap = kDecodeChunk / kMinKv8Block;   // scale pairs of a split
+constexpr int kScaleCap = kKv8DenseChunk / kMinKv8Block;   // scale pairs of a split
 constexpr int kPad8 = 32;                                // a row list ends on a whole group
-constexpr int kSkipOffset = 0x7FFFFF00;                  // past every buffer: the load is dropped
 
 constexpr int elem_bytes(int src) { return src == RBQ_F32 ? 4 : src == RBQ_BF16 ? 2 : 1; }
 constexpr int row_tiles(int src) { return elem_bytes(src) == 1 ? 2 : 1; }   // tiles of 16 rows per group
@@ -45,8 +44,6 @@ struct RowRegs {
   static constexpr int kKw = D * elem_bytes(SRC) / 16, kVw = D * elem_bytes(SRC) / 64;
   uint32_t k[row_tiles(SRC)][kKw];
   uint32_t v[row_tiles(SRC)][4][kVw];
-  uint32_t mk;        // bit 4 t + i: row 4j + i of tile t is valid and taken by head x
-  f32x2 sc[row_tiles(SRC)][4];   // its scales {ks, vs} (8-bit rows)
 };
 
 template <int WORDS, int CP>
@@ -109,6 +106,7 @@ __device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int pa
     f32x4 r = {__uint_as_float(v[0][c]), __uint_as_float(v[1][c]), __uint_as_float(v[2][c]), __uint_as_float(v[3][c])};
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
     bf16x4 p = __builtin_convertvector(r, bf16x4);
+#pragma unroll
     for (int t = 0; t < part; ++t) {
       r -= __builtin_convertvector(p, f32x4);
       p = __builtin_convertvector(r, bf16x4);
@@ -131,6 +129,7 @@ __device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int pa
 // What a block keeps in LDS for its waves.
 template <bool SPARSE, int G, int D>
 struct Shared {
+  static_assert(kScaleCap <= kDThreads, "one scale pair per thread");
   static constexpr bool kPackedQ = kQParts * G <= 16;
   static constexpr int kQOps = kPackedQ ? 1 : kQParts;
   u32x4 qB[D / 32][kQOps][kWave];   // B operands of the logits product
@@ -146,32 +145,43 @@ struct Shared {
 // One wave's online softmax over its groups of the block's U rows: row c0 + e of the
 // buffers, or lst[e]. m: head x's running maximum (log2 domain, uniform over j), lsum:
 // this lane's part of its sum; acc[c] lane (x, j), register i: head 4j + i, dimension
-// (D / 16) x + c.
+// (D / 16) x + c. begin() requests the first group, so that a block whose rows follow
+// each other has them on the way while it stages its queries.
 template <int SRC, bool LIST, int G, int D, int CP, class S>
-__device__ __forceinline__ void attend_rows(S& sh, __amdgpu_buffer_rsrc_t Kr, __amdgpu_buffer_rsrc_t Vr, int c0, int U,
-                                            int bshift, float& m, float& lsum, f32x4 (&acc)[D / 16]) {
-  constexpr int NT = row_tiles(SRC), kRows = 16 * NT, EB = elem_bytes(SRC), KB = D / 32, NP = row_parts(SRC);
-  constexpr bool kCodes = EB == 1;
-  constexpr int kQOps = S::kQOps;
+struct Rows {
+  static constexpr int NT = row_tiles(SRC), kRows = 16 * NT, EB = elem_bytes(SRC), KB = D / 32, NP = row_parts(SRC);
+  static constexpr bool kCodes = EB == 1;
+  // One group's registers are reused for the next: its K rows are requested as soon
+  // as the logits are done, its V rows as soon as the values are. (fp32 rows, four
+  // times the registers: each half is requested when its turn comes.)
+  static constexpr bool kAhead = SRC != RBQ_F32;
   using Regs = RowRegs<SRC, D>;
-  const int wave = threadIdx.x / kWave, lane = lane_id();
-  const int x = lane & 15, j = lane >> 4;
-  const int ngroups = (U + kRows - 1) / kRows;
+  S& sh;
+  const __amdgpu_buffer_rsrc_t Kr, Vr;
+  const int c0, U, bshift, wave, x, j, ngroups;
+  Regs cur;
+  uint32_t mk;                // bit 4 t + i: row 4j + i of tile t is valid and taken by head x
+  f32x2 sc[LIST ? NT : 1][4];   // its scales {ks, vs} (listed 8-bit rows)
 
-  auto load_k = [&](Regs& d, int grp, bool skip) {
+  __device__ __forceinline__ Rows(S& s, __amdgpu_buffer_rsrc_t kr, __amdgpu_buffer_rsrc_t vr, int first, int rows, int shift)
+      : sh(s), Kr(kr), Vr(vr), c0(first), U(rows), bshift(shift), wave(threadIdx.x / kWave), x(lane_id() & 15),
+        j(lane_id() >> 4), ngroups((rows + kRows - 1) / kRows) {}
+
+  __device__ __forceinline__ int row_of(int grp, int e) const { return c0 + (e < U ? e : grp * kRows); }
+  __device__ __forceinline__ void load_k(int grp, bool skip) {
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int e = grp * kRows + 16 * t + x;
       int row;
       if constexpr (LIST) row = sh.lst[e];
-      else row = c0 + (e < U ? e : grp * kRows);
+      else row = row_of(grp, e);
       const int off = skip ? kSkipOffset : row * (D * EB) + 16 * EB * j;
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i) load_words<4 * EB, CP>(&d.k[t][4 * EB * i], Kr, off + 64 * EB * i);
+      for (int i = 0; i < D / 64; ++i) load_words<4 * EB, CP>(&cur.k[t][4 * EB * i], Kr, off + 64 * EB * i);
     }
-  };
-  auto load_v = [&](Regs& d, int grp, bool skip) {
-    uint32_t mk = 0u;
+  }
+  __device__ __forceinline__ void load_v(int grp, bool skip) {
+    mk = 0u;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       const int e0 = grp * kRows + 16 * t + 4 * j;   // this lane's four entries
@@ -184,155 +194,215 @@ __device__ __forceinline__ void attend_rows(S& sh, __amdgpu_buffer_rsrc_t Kr, __
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const bool valid = e0 + i < U;
-          row[i] = c0 + (valid ? e0 + i : grp * kRows);
-          mk |= uint32_t(valid && x < G) << (4 * t + i);
+          row[i] = row_of(grp, e0 + i);
+          mk |= uint32_t(e0 + i < U && x < G) << (4 * t + i);
         }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int off = skip ? kSkipOffset : row[i] * (D * EB) + (D * EB / 16) * x;
-        load_words<Regs::kVw, CP>(d.v[t][i], Vr, off);
-      }
-      if constexpr (kCodes) {
-        if constexpr (LIST) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) d.sc[t][i] = sh.scale[(row[i] - c0) >> bshift];
-        } else {
-          d.sc[t][0] = sh.scale[(row[0] - c0) >> bshift];   // (16 rows from a multiple of 16: one token block)
-#pragma unroll
-          for (int i = 1; i < 4; ++i) d.sc[t][i] = d.sc[t][0];
-        }
+        load_words<Regs::kVw, CP>(cur.v[t][i], Vr, off);
+        if constexpr (LIST && kCodes) sc[t][i] = sh.scale[(row[i] - c0) >> bshift];
       }
     }
-    d.mk = mk;
-  };
-
-  // One group's registers are reused for the next: its K rows are requested as soon
-  // as the logits are done, its V rows as soon as the values are.
-  Regs cur;
-  int grp = wave;
-  if (grp < ngroups) {
-    load_k(cur, grp, false);
-    load_v(cur, grp, false);
   }
-  while (grp < ngroups) {
-    const int nxt = grp + kDWaves;
-    const bool last = nxt >= ngroups;
-    // (an opaque offset: the query operands are re-read from LDS every group, in
-    // registers they would cost waves per SIMD)
-    int qoff = lane;
-    asm volatile("" : "+v"(qoff));
-    const u32x4* qp = &sh.qB[0][0][0] + qoff;
-    f32x4 s[NT];
+  __device__ __forceinline__ void begin() {
+    if (kAhead && wave < ngroups) {
+      load_k(wave, false);
+      load_v(wave, false);
+    }
+  }
+
+  __device__ __forceinline__ void run(float& m, float& lsum, f32x4 (&acc)[D / 16]) {
+    constexpr int kQOps = S::kQOps;
+    int grp = wave;
+    while (grp < ngroups) {
+      const int nxt = grp + kDWaves;
+      const bool last = nxt >= ngroups;
+      if constexpr (!kAhead) load_k(grp, false);
+      // (an opaque offset: the query operands are re-read from LDS every group, in
+      // registers they would cost waves per SIMD)
+      int qoff = lane_id();
+      asm volatile("" : "+v"(qoff));
+      const u32x4* qp = &sh.qB[0][0][0] + qoff;
+      f32x2 ts[NT];   // scales of rows that follow each other: 16 from a multiple of 16 are in one token block
+      if constexpr (kCodes && !LIST) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int t = 0; t < NT; ++t) ts[t] = sh.scale[(grp * kRows + 16 * t < U ? grp * kRows + 16 * t : 0) >> bshift];
+      }
+      f32x4 s[NT];
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb) {
+      for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        bf16x8 a[NT];
+      for (int kb = 0; kb < KB; ++kb) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) a[t] = k_operand<SRC>(cur.k[t], kb, p);
+        for (int p = 0; p < NP; ++p) {
+          // (kept in this order: moved up, the operands of every group would be held at once)
+          __builtin_amdgcn_sched_barrier(0);
+          bf16x8 a[NT];
 #pragma unroll
-        for (int op = 0; op < kQOps; ++op) {
-          const bf16x8 b = __builtin_bit_cast(bf16x8, qp[(kb * kQOps + op) * kWave]);
+          for (int t = 0; t < NT; ++t) a[t] = k_operand<SRC>(cur.k[t], kb, p);
 #pragma unroll
-          for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b, s[t], 0, 0, 0);
+          for (int op = 0; op < kQOps; ++op) {
+            const bf16x8 b = __builtin_bit_cast(bf16x8, qp[(kb * kQOps + op) * kWave]);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b, s[t], 0, 0, 0);
+          }
         }
       }
-    }
-    load_k(cur, last ? grp : nxt, last);
-    // columns h + G and h + 2G hold the mid and lo parts of head h's logits (through
-    // opaque copies: hipcc 7.2 reads one element's register for all four otherwise)
-    float lg[NT][4];
-    float tmax = -INFINITY;
+      if constexpr (kAhead) load_k(last ? grp : nxt, last);
+      else load_v(grp, false);
+      // columns h + G and h + 2G hold the mid and lo parts of head h's logits (through
+      // opaque copies: hipcc 7.2 reads one element's register for all four otherwise)
+      float lg[NT][4];
+      float tmax = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float sv = s[t][i];
-        if constexpr (S::kPackedQ) {
-          asm volatile("" : "+v"(sv));
-          const int v = __builtin_bit_cast(int, sv);
-          const float mid = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, v, 0x100 + G, 0xF, 0xF, false));
-          const float lo = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, v, 0x100 + 2 * G, 0xF, 0xF, false));
-          sv = (sv + mid) + lo;
+        for (int i = 0; i < 4; ++i) {
+          float sv = s[t][i];
+          if constexpr (S::kPackedQ) {
+            asm volatile("" : "+v"(sv));
+            const int v = __builtin_bit_cast(int, sv);
+            const float mid = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, v, 0x100 + G, 0xF, 0xF, false));
+            const float lo = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, v, 0x100 + 2 * G, 0xF, 0xF, false));
+            sv = (sv + mid) + lo;
+          }
+          if constexpr (kCodes) sv *= LIST ? sc[LIST ? t : 0][i].x : ts[t].x;
+          lg[t][i] = ((mk >> (4 * t + i)) & 1u) ? sv : -INFINITY;
+          tmax = fmaxf(tmax, lg[t][i]);
         }
-        if constexpr (kCodes) sv *= cur.sc[t][i].x;
-        lg[t][i] = ((cur.mk >> (4 * t + i)) & 1u) ? sv : -INFINITY;
-        tmax = fmaxf(tmax, lg[t][i]);
       }
-    }
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 16, kWave));
-    tmax = fmaxf(tmax, __shfl_xor(tmax, 32, kWave));
-    const float mn = fmaxf(m, tmax);
-    const float mref = mn == -INFINITY ? 0.f : mn;   // (no row yet: every exponential below is that of -inf)
-    const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mref);
-    float w[NT * 4], sum = 0.f;
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 16, kWave));
+      tmax = fmaxf(tmax, __shfl_xor(tmax, 32, kWave));
+      const float mn = fmaxf(m, tmax);
+      const float mref = mn == -INFINITY ? 0.f : mn;   // (no row yet: every exponential below is that of -inf)
+      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mref);
+      float w[NT * 4], sum = 0.f;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
+      for (int t = 0; t < NT; ++t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p = __builtin_amdgcn_exp2f(lg[t][i] - mref);
-        sum += p;
-        w[4 * t + i] = kCodes ? p * cur.sc[t][i].y : p;
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(lg[t][i] - mref);
+          sum += p;
+          w[4 * t + i] = kCodes ? p * (LIST ? sc[LIST ? t : 0][i].y : ts[t].y) : p;
+        }
       }
-    }
-    lsum = fmaf(lsum, corr, sum);
-    const bool moved = mn != m;
-    m = mn;
-    if (__ballot(moved)) {
-      float cr[4];
+      lsum = fmaf(lsum, corr, sum);
+      const bool moved = mn != m;
+      m = mn;
+      if (__ballot(moved)) {
+        float cr[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) cr[i] = __shfl(corr, 4 * j + i, kWave);
+        for (int i = 0; i < 4; ++i) cr[i] = __shfl(corr, 4 * j + i, kWave);
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[c][i] *= cr[i];
+        }
+      }
+      // the weighted probabilities in three parts: A operands (row = head x; k = rows 4j .. 4j+3
+      // of both tiles, or, of one tile, the same rows in two parts)
+      bf16x8 pa[3];
+      if constexpr (NT == 2) {
+        f32x8 wv;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wv[i] = w[i];
+        split3(wv, pa);
+      } else {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        f32x4 r = {w[0], w[1], w[2], w[3]};
+        bf16x4 p3[3];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) {
+          p3[t] = __builtin_convertvector(r, bf16x4);
+          r -= __builtin_convertvector(p3[t], f32x4);
+        }
+        const bf16x4 zero = __builtin_bit_cast(bf16x4, u32x2{0u, 0u});
+        pa[0] = __builtin_shufflevector(p3[0], p3[1], 0, 1, 2, 3, 4, 5, 6, 7);
+        pa[1] = __builtin_shufflevector(p3[2], zero, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
+        if (c % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[c][i] *= cr[i];
+        for (int p = 0; p < NP; ++p) {
+          const u32x2 v0 = v_column<SRC>(cur.v[0], c, p);
+          const u32x2 v1 = NT == 2 ? v_column<SRC>(cur.v[NT - 1], c, p) : v0;
+          const bf16x8 bv = __builtin_bit_cast(bf16x8, u32x4{v0.x, v0.y, v1.x, v1.y});
+#pragma unroll
+          for (int t = 0; t < (NT == 2 ? 3 : 2); ++t)
+            acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[t], bv, acc[c], 0, 0, 0);
+        }
       }
+      if constexpr (kAhead) load_v(last ? grp : nxt, last);
+      grp = nxt;
     }
-    // the weighted probabilities in three parts: A operands (row = head x; k = rows 4j .. 4j+3
-    // of both tiles, or, of one tile, the same rows in two parts)
-    bf16x8 pa[3];
-    if constexpr (NT == 2) {
-      f32x8 wv;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) wv[i] = w[i];
-      split3(wv, pa);
-    } else {
-      typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-      f32x4 r = {w[0], w[1], w[2], w[3]};
-      bf16x4 p3[3];
-#pragma unroll
-      for (int t = 0; t < 3; ++t) {
-        p3[t] = __builtin_convertvector(r, bf16x4);
-        r -= __builtin_convertvector(p3[t], f32x4);
-      }
-      const bf16x4 zero = __builtin_bit_cast(bf16x4, u32x2{0u, 0u});
-      pa[0] = __builtin_shufflevector(p3[0], p3[1], 0, 1, 2, 3, 4, 5, 6, 7);
-      pa[1] = __builtin_shufflevector(p3[2], zero, 0, 1, 2, 3, 4, 5, 6, 7);
-    }
-#pragma unroll
-    for (int c = 0; c < D / 16; ++c) {
-#pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const u32x2 v0 = v_column<SRC>(cur.v[0], c, p);
-        const u32x2 v1 = NT == 2 ? v_column<SRC>(cur.v[NT - 1], c, p) : v0;
-        const bf16x8 bv = __builtin_bit_cast(bf16x8, u32x4{v0.x, v0.y, v1.x, v1.y});
-#pragma unroll
-        for (int t = 0; t < (NT == 2 ? 3 : 2); ++t)
-          acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[t], bv, acc[c], 0, 0, 0);
-      }
-    }
-    load_v(cur, last ? grp : nxt, last);
-    grp = nxt;
   }
+};
+
+// A block's sequence, KV head and place s among its group's blocks: idx of them over
+// the sequence's nb cached rows, then win over its wb window rows.
+struct BlockId {
+  int b, hk, s, nb, wb, idx, win;
+};
+
+// Block p of a ragged batch: sequence after sequence, each with the blocks that its own
+// lengths call for (one where it has no rows), so that the blocks that follow each other
+// are those of one sequence as in a uniform call, and the grid's unused rest comes last.
+// (One row of blocks per split, in which short sequences leave gaps: 16 sequences of 2K
+// to 32K rows, 32 / 8 heads: 117 us; this order 107.) ordered: densest sequences first (see
+// sequence_of_rank), batch <= 64. b = -1: none.
+template <bool SPARSE>
+__device__ __forceinline__ BlockId ragged_block(int p, int ordered, int batch, int n, int w, int chunk, int Hq, int Hkv,
+                                                const int32_t* __restrict__ sel_count, const int32_t* __restrict__ seq_n,
+                                                const int32_t* __restrict__ seq_w) {
+  const int lane = lane_id();
+  BlockId id{-1, 0, 0, 0, 0, 0, 0};
+  int before = 0;
+  for (int b0 = 0; b0 < batch; b0 += kWave) {
+    const int b = min(b0 + lane, batch - 1);
+    const int nb = seq_n ? min(max(seq_n[b], 0), n) : n, wb = seq_w ? min(max(seq_w[b], 0), w) : w;
+    float dens = 0.f;
+    if (SPARSE && ordered) dens = selected_share(b, nb, Hq, Hkv, sel_count);
+    const int idx = (nb + chunk - 1) / chunk, win = (wb + kDecodeWinChunk - 1) / kDecodeWinChunk;
+    const int blocks = b0 + lane < batch ? max(idx + win, 1) * Hkv : 0;
+    int first = 0;   // blocks before this lane's sequence
+    if (SPARSE && ordered) {
+      for (int o = 0; o < batch; ++o) {
+        const float d = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(dens)), o)));
+        first += d > dens || (d == dens && o < lane) ? __builtin_amdgcn_readlane(blocks, o) : 0;
+      }
+    } else {
+      int inc = blocks;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int v = __shfl_up(inc, o, kWave);
+        inc += lane >= o ? v : 0;
+      }
+      first = before + inc - blocks;
+      before += __builtin_amdgcn_readlane(inc, kWave - 1);
+    }
+    const unsigned long long mine = __ballot(p >= first && p < first + blocks);
+    if (mine != 0ull) {
+      const int l = __builtin_ctzll(mine);
+      id.b = b0 + l;
+      id.nb = __builtin_amdgcn_readlane(nb, l);
+      id.wb = __builtin_amdgcn_readlane(wb, l);
+      id.idx = __builtin_amdgcn_readlane(idx, l);
+      id.win = __builtin_amdgcn_readlane(win, l);
+      const int e = p - __builtin_amdgcn_readlane(first, l), per = max(id.idx + id.win, 1);
+      id.hk = e / per;
+      id.s = e - id.hk * per;
+      return id;
+    }
+  }
+  return id;
 }
 
 // FMT: the rows' 8-bit format; LOC: the window's type (RBQ_BF16 or RBQ_F32)
 template <int FMT, int LOC, bool SPARSE, int G, int D>
-__global__ __launch_bounds__(kDThreads) void decode_kv8_kernel(
+__global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     const float* __restrict__ q, const char* __restrict__ K8, const char* __restrict__ V8,
     const float* __restrict__ k_scale, const float* __restrict__ v_scale, int bshift, int cap, int n,
     const int32_t* __restrict__ sel_idx, const int32_t* __restrict__ sel_count,
@@ -343,22 +413,20 @@ __global__ __launch_bounds__(kDThreads) void decode_kv8_kernel(
   using S = Shared<SPARSE, G, D>;
   __shared__ S sh;
 
-  // ragged grids are split-major (ordered: a sequence's blocks after the other's, ordered = batch)
-  int split = ragged ? blockIdx.y : blockIdx.x;
-  int bh = ragged ? blockIdx.x : blockIdx.y;
-  int b = bh / Hkv, hk = bh - b * Hkv;
-  int own_n = 0;
-  if (SPARSE && ordered) {
-    const int per = Hkv * total_splits, id = blockIdx.y * gridDim.x + blockIdx.x, r = id / per, e = id - r * per;
-    b = sequence_of_rank(r, ordered, n, Hq, Hkv, sel_count, seq_n, own_n);
-    split = e / Hkv;
-    hk = e - split * Hkv;
-    bh = b * Hkv + hk;
+  BlockId id{int(blockIdx.y), 0, int(blockIdx.x), n, w, idx_splits, total_splits - idx_splits};
+  if (ragged) {
+    id = ragged_block<SPARSE>(blockIdx.x, ordered, ragged, n, w, chunk, Hq, Hkv, sel_count, seq_n, seq_w);
+    if (id.b < 0) return;
+  } else {
+    id.b = int(blockIdx.y) / Hkv;
+    id.hk = int(blockIdx.y) - id.b * Hkv;
   }
+  const int b = id.b, hk = id.hk, bh = b * Hkv + hk, nb = id.nb, wb = id.wb;
+  const bool window = id.s >= id.idx;
+  const int split = window ? idx_splits + id.s - id.idx : id.s;   // its place among the group's states
   const int row0 = b * Hq + hk * G;
   const int wave = threadIdx.x / kWave, lane = lane_id();
   const int x = lane & 15, j = lane >> 4;
-  const bool window = split >= idx_splits;
   // what does not depend on the sequence's lengths is requested first
   static_assert(G * (D / 8) <= kDThreads, "one piece of the queries per thread");
   const bool stages = int(threadIdx.x) < G * (D / 8);
@@ -374,13 +442,19 @@ __global__ __launch_bounds__(kDThreads) void decode_kv8_kernel(
     mword = load_mask_words<G>(sel_mask, mask_words, row0, split * chunk, min(n, (split + 1) * chunk));
   HeadCounts<G> hcount{};
   if constexpr (SPARSE) hcount = load_head_counts<G>(sel_count, row0);
-  const int nb = SPARSE && ordered ? __builtin_amdgcn_readlane(own_n, b) : seq_n ? min(max(seq_n[b], 0), n) : n;
-  const int wb = seq_w ? min(max(seq_w[b], 0), w) : w;
   const int lim = window ? wb : nb;
   const int c0 = window ? (split - idx_splits) * kDecodeWinChunk : split * chunk;
   const int c1 = max(c0, min(lim, c0 + (window ? kDecodeWinChunk : chunk)));
-  if (c1 == c0) {   // block-uniform: past this sequence's rows, an empty partial state
-    if (int(threadIdx.x) < G) part[(int64_t(row0 + threadIdx.x) * total_splits + split) * (D + 2)] = -INFINITY;
+  if (ragged && id.s == 0) {   // the group's first block also writes the empty states that follow the sequence's own
+    const int none = total_splits - id.idx - id.win;
+    for (int e = threadIdx.x; e < G * none; e += kDThreads) {
+      const int g = e / none, k = e - g * none;
+      const int slot = k < idx_splits - id.idx ? id.idx + k : idx_splits + id.win + k - (idx_splits - id.idx);
+      part[(int64_t(row0 + g) * total_splits + slot) * (D + 2)] = -INFINITY;
+    }
+  }
+  if (c1 == c0) {   // block-uniform: no rows (uniform calls: the one empty split; ragged: written above)
+    if (!ragged && int(threadIdx.x) < G) part[(int64_t(row0 + threadIdx.x) * total_splits + split) * (D + 2)] = -INFINITY;
     return;
   }
   constexpr int kLocEl = elem_bytes(LOC);
@@ -388,17 +462,25 @@ __global__ __launch_bounds__(kDThreads) void decode_kv8_kernel(
   const char* Vb = window ? V_loc + int64_t(bh) * loc_ld * (D * kLocEl) : V8 + int64_t(bh) * cap * D;
   const uint32_t region = uint32_t(lim) * uint32_t(window ? D * kLocEl : D);   // < 2^31
   const __amdgpu_buffer_rsrc_t Kr = make_rsrc(Kb, region), Vr = make_rsrc(Vb, region);
+  float m = -INFINITY, lsum = 0.f;
+  f32x4 acc[D / 16];
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   // the split's scales
-  if (!window && int(threadIdx.x) <= (c1 - 1 - c0) >> bshift) {
+  const bool scales = !window && int(threadIdx.x) <= (c1 - 1 - c0) >> bshift;
+  f32x2 own_scale = {0.f, 0.f};
+  if (scales) {
     const int64_t s0 = int64_t(bh) * ((int64_t(cap) + (1 << bshift) - 1) >> bshift) + (c0 >> bshift) + threadIdx.x;
-    sh.scale[threadIdx.x] = f32x2{k_scale[s0], v_scale[s0]};
+    own_scale = f32x2{k_scale[s0], v_scale[s0]};
   }
 
   // query operands, lane (column c, quarter jj) of group kb = dimensions
   // 64 (kb / 2) + 16 jj + 8 (kb % 2) .. +8. G <= 4: one operand per group, column
   // c = part * G + head; otherwise one per (group, part), column c = head.
   // (Columns without a head stay unwritten: masked, and no other column reads them.)
-  if (stages) {
+  auto stage = [&] {
+    if (scales) sh.scale[threadIdx.x] = own_scale;
+    if (!stages) return;
     const f32x8 qv = __builtin_shufflevector(qa, qb, 0, 1, 2, 3, 4, 5, 6, 7) * scale_log2e;
     bf16x8 parts[kQParts];
     split3(qv, parts);
@@ -406,23 +488,33 @@ __global__ __launch_bounds__(kDThreads) void decode_kv8_kernel(
 #pragma unroll
     for (int t = 0; t < kQParts; ++t)
       sh.qB[kb][S::kPackedQ ? 0 : t][16 * jj + (S::kPackedQ ? t * G + qh : qh)] = __builtin_bit_cast(u32x4, parts[t]);
-  }
+  };
 
-  int U = c1 - c0;
-  if (SPARSE && !window)
-    U = build_union_list<G, kDThreads, true, kPad8>(sel_idx, sel_mask, mask_words, row0, n, c0, c1, 0, 0, sh.bm, sh.lst,
-                                                    sh.hmask, sh.rng_lo, sh.rng_hi, mword, hcount);
-  else
+  // the rows' cache policy as in decode.hip: streaming where the gather is bound by bandwidth
+  if (window) {
+    Rows<LOC, false, G, D, 0, S> rows(sh, Kr, Vr, c0, c1 - c0, 0);
+    rows.begin();
+    stage();
     __syncthreads();
-
-  float m = -INFINITY, lsum = 0.f;
-  f32x4 acc[D / 16];
-#pragma unroll
-  for (int c = 0; c < D / 16; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (window)
-    attend_rows<LOC, false, G, D, 0>(sh, Kr, Vr, c0, U, 0, m, lsum, acc);
-  else
-    attend_rows<FMT, SPARSE, G, D, 0>(sh, Kr, Vr, c0, U, bshift, m, lsum, acc);
+    rows.run(m, lsum, acc);
+  } else if constexpr (SPARSE) {
+    stage();
+    const int U = build_union_list<G, kDThreads, true, kPad8>(sel_idx, sel_mask, mask_words, row0, n, c0, c1, 0, 0, sh.bm,
+                                                              sh.lst, sh.hmask, sh.rng_lo, sh.rng_hi, mword, hcount);
+    auto attend = [&](auto cp) {
+      Rows<FMT, true, G, D, decltype(cp)::value, S> rows(sh, Kr, Vr, c0, U, bshift);
+      rows.begin();
+      rows.run(m, lsum, acc);
+    };
+    if (G <= 4 && int64_t(U) * kStreamDenDen >= int64_t(c1 - c0) * kStreamDenNum) attend(std::integral_constant<int, kStream>{});
+    else attend(std::integral_constant<int, 0>{});
+  } else {
+    Rows<FMT, false, G, D, kStream, S> rows(sh, Kr, Vr, c0, c1 - c0, bshift);
+    rows.begin();
+    stage();
+    __syncthreads();
+    rows.run(m, lsum, acc);
+  }
 
   // ---- merge the waves, write this split's partial state per head
   lsum += __shfl_xor(lsum, 16, kWave);
@@ -517,15 +609,15 @@ rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, i
                              hipStream_t stream, const unsigned long long* sel_mask, int32_t mask_words,
                              const int32_t* seq_n, const int32_t* seq_w) {
   const int G = heads_q / heads_kv;
-  const DecodeSplits sp = decode_splits(batch, heads_kv, n, win.w);
+  const DecodeSplits sp = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr);
   const bool ragged = seq_n || seq_w;
-  const dim3 grid = ragged ? dim3(batch * heads_kv, sp.total()) : dim3(sp.total(), batch * heads_kv);
-  const int64_t blocks = int64_t(grid.x) * grid.y;
+  const dim3 grid = ragged ? dim3(uint32_t(batch * heads_kv * int64_t(sp.total()))) : dim3(sp.total(), batch * heads_kv);
+  const int64_t blocks = int64_t(batch) * heads_kv * sp.total();
   const int ordered = sparse && seq_n && batch > 1 && batch <= kWave && sp.chunk >= kOrderMinChunk &&
                               blocks > resident_blocks(head_dim, G) ? batch : 0;
   const Call a{grid, stream, q, cache, n, sel_idx, sel_count, sel_mask, mask_words, win, sp,
                float(double(sm_scale) * 1.4426950408889634), static_cast<float*>(ws), heads_q, heads_kv, seq_n, seq_w,
-               ragged ? 1 : 0, ordered};
+               ragged ? batch : 0, ordered};
   const bool f32 = win.dtype == RBQ_F32 && win.w > 0, i8 = cache.dtype == RBQ_I8;
   rbq_status st;
 #define RBQ_KV8(D)                                                                                          \

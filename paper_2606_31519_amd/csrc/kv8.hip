@@ -226,7 +226,7 @@ void launch_quantize_form(int pieces, dim3 grid, hipStream_t stream, const char*
     case 128: RBQ_QUANT_FORM(64, 2); break;
     case 256: RBQ_QUANT_FORM(64, 4); break;
     case 512: RBQ_QUANT_FORM(64, 8); break;
-    case 1024: RBQ_QUANT_FORM(256, 4); break;
+    case 1024: RBQ_QUANT_FORM(64, 16); break;
     case 2048: RBQ_QUANT_FORM(256, 8); break;
     default: RBQ_QUANT_FORM(256, 16); break;
   }
@@ -240,7 +240,7 @@ rbq_status launch_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim,
                               const int32_t* seq_off, const int32_t* seq_new, hipStream_t stream) {
   if (n_new == 0) return RBQ_OK;
   const int bshift = log2i(block), dshift = log2i(head_dim), pieces = block * head_dim / 8;
-  const int units = pieces <= 512 ? kQuantThreads / kWave : 1;
+  const int units = pieces <= 1024 ? kQuantThreads / kWave : 1;
   // token blocks a sequence's rows can touch (ragged: from any place in the first)
   const int64_t first = seq_off ? 0 : offset >> bshift;
   const int64_t blocks =

@@ -152,6 +152,11 @@ constexpr int kDecodeListCap = 1280;      // row-list positions of a sparse spli
 // by the chunk), provided every sequence's window fits its splits that way.
 DecodeSplits decode_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool tail_window = false,
                            bool sparse = false, bool ragged = false);
+// The splits over an 8-bit cache (no folded window: its rows are of another type).
+constexpr int kKv8DenseChunk = 2048;   // positions per dense split (at most)
+DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged);
+size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
+                                  int32_t w);
 size_t decode_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                               int32_t w);
 

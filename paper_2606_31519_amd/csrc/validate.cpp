@@ -13,6 +13,7 @@ namespace {
 constexpr int64_t kMaxRows = int64_t(1) << 31;
 constexpr int64_t kMaxStride = int64_t(1) << 23;   // elements: 64 rows of it are addressed with 32-bit byte offsets
 constexpr int64_t kCus = 256;                      // compute units of the GPU
+constexpr int64_t kKv8Resident = 4 * kCus;         // blocks of the decode over an 8-bit cache that run at once
 constexpr int64_t kPrefillMinKeys = 256;           // keys per split, at least
 // a required device pointer: present, and 16-byte aligned (the kernels use 16-byte vector loads)
 bool bad_ptr(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
@@ -177,6 +178,28 @@ rbq_status check_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_
   return RBQ_OK;
 }
 
+DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged) {
+  DecodeSplits s = decode_splits(batch, heads_kv, n, w);
+  if (sparse || s.chunk < kDecodeChunk) return s;
+  const int64_t groups = int64_t(batch) * heads_kv;
+  if (ragged) return s;
+  const int64_t rounds = (groups * (s.idx_splits + s.win_splits) + kKv8Resident / 2) / kKv8Resident;
+  const int64_t splits = (std::max<int64_t>(rounds, 1) * kKv8Resident) / groups - s.win_splits;
+  if (splits < 1) return s;
+  s.chunk = int32_t(std::min<int64_t>(((int64_t(n) + splits - 1) / splits + 63) / 64 * 64, kKv8DenseChunk));
+  s.idx_splits = int32_t((int64_t(n) + s.chunk - 1) / s.chunk);
+  return s;
+}
+
+size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
+                                  int32_t w) {
+  if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || n < 0 || w < 0) return 0;
+  int64_t total = 0;
+  for (int form = 0; form < 3; ++form)
+    total = std::max<int64_t>(total, decode_kv8_splits(batch, heads_kv, n, w, form == 2, form == 1).total());
+  return align_up(size_t(batch) * heads_q * total * (head_dim + 2) * sizeof(float), 256);
+}
+
 namespace {
 bool bad_seq(const int32_t* p) { return p != nullptr && (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 rbq_status check_kv8_form(int32_t block, int32_t kv8_dtype) {
@@ -222,7 +245,7 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
   if (win.w > 0 && (bad_ptr(win.K) || bad_ptr(win.V) || win.ld < win.w || win.ld >= kMaxRows)) return RBQ_EINVAL;
   // rows of one (sequence, KV head) are addressed with 32-bit byte offsets
   if (int64_t(n) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;
-  if (bad_ptr(ws) || ws_bytes < decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, win.w)) return RBQ_EINVAL;
+  if (bad_ptr(ws) || ws_bytes < decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, win.w)) return RBQ_EINVAL;
   return RBQ_OK;
 }
 
@@ -322,8 +345,9 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
       return rbq::topp_workspace(nullptr, int64_t(batch) * heads_q, n).bytes;
     case RBQ_OP_SPARSE_DECODE:
     case RBQ_OP_DENSE_DECODE:
-    case RBQ_OP_DECODE_KV8:
       return rbq::decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
+    case RBQ_OP_DECODE_KV8:
+      return rbq::decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_PREFILL:
       return rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_DECODE_STEP:

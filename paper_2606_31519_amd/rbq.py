@@ -190,14 +190,6 @@ def kv_dtype_code(t: torch.Tensor) -> int:
     raise ValueError(f"unsupported key/value dtype {t.dtype}")
 
 
-def kv8_dtype_code(t: torch.Tensor) -> int:
-    if t.dtype == torch.float8_e4m3fn:
-        return RBQ_E4M3
-    if t.dtype == torch.int8:
-        return RBQ_I8
-    raise ValueError(f"unsupported 8-bit cache dtype {t.dtype}")
-
-
 def rbq_workspace_bytes(op, batch, heads_q, heads_kv, head_dim, n, w=0) -> int:
     return int(lib.rbq_workspace_bytes(op, batch, heads_q, heads_kv, head_dim, n, w))
 
@@ -435,65 +427,99 @@ def rbq_decode_step_varlen_f16(batch, heads_q, heads_kv, head_dim, q, P, c_k, K,
 
 
 # ---- the 8-bit cache: K8, V8 [B][Hkv][cap][D] torch.float8_e4m3fn or torch.int8, k_scale, v_scale
-# [B][Hkv][ceil(cap / block)] float32; seq_*: per-sequence counts of ragged batches (int32 device tensors) or None
+# [B][Hkv][ceil(cap / block)] float32; seq_*: per-sequence counts of ragged batches (int32 device tensors) or None.
+# (A token's calls take the GPU 2 to 4 us: the checks are plain comparisons, and the messages, through _need, are
+# formed when one fails. Checked through _need a call took 6.8 to 9 us of the host, so 3.9 to 5.)
+
+_KV_CODES = {torch.bfloat16: RBQ_BF16, torch.float32: RBQ_F32}
+_KV8_CODES = {torch.float8_e4m3fn: RBQ_E4M3, torch.int8: RBQ_I8}
 
 
-def _need_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale):
-    if K8.dtype != V8.dtype:
-        raise ValueError(f"{name}: K8 is {K8.dtype}, V8 {V8.dtype}")
+def _pair_code(name, codes, a, K, b, V):
+    """The code of the type that two tensors share."""
+    code = codes.get(K.dtype)
+    if code is None or K.dtype != V.dtype:
+        raise ValueError(f"{name}: {a} is {K.dtype}, {b} {V.dtype}; one type of {list(codes)} is taken")
+    return code
+
+
+def _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale):
+    count = batch * heads_kv * cap * head_dim
     blocks = batch * heads_kv * ((cap + block - 1) // block) if block > 0 else 0
-    _need(name, K8=(K8, batch * heads_kv * cap * head_dim), V8=(V8, batch * heads_kv * cap * head_dim),
-          k_scale=(k_scale, blocks), v_scale=(v_scale, blocks))
+    if K8.numel() < count or V8.numel() < count or k_scale.numel() < blocks or v_scale.numel() < blocks:
+        _need(name, K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks), v_scale=(v_scale, blocks))
+
+
+def _check_rows(name, batch, heads_kv, head_dim, ld, rows, K, V):
+    """Rows [0, rows) of blocks of ld rows per (sequence, KV head)."""
+    count = ((batch * heads_kv - 1) * ld + rows) * head_dim if rows > 0 else 0
+    if K.numel() < count or V.numel() < count:
+        _need(name, K=(K, count), V=(V, count))
+
+
+def _check_seqs(name, batch, *seqs):
+    for t in seqs:
+        if t is not None and t.numel() < batch:
+            _need(name, per_sequence=(t, batch))
 
 
 def rbq_quantize_kv(batch, heads_kv, head_dim, K, V, ld, n_new, offset, cap, block, K8, V8, k_scale, v_scale,
                     seq_off=None, seq_new=None, stream=None):
     """Append rows [0, n_new) of K / V [B][Hkv][ld][D] to the 8-bit cache as rows [offset, offset + n_new)."""
-    _need_kv8("rbq_quantize_kv", batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    if K.dtype != V.dtype:
-        raise ValueError(f"rbq_quantize_kv: K is {K.dtype}, V {V.dtype}")
-    rows = ((batch * heads_kv - 1) * ld + n_new) * head_dim if n_new > 0 else 0
-    _need("rbq_quantize_kv", K=(K, rows), V=(V, rows), seq_off=(seq_off, batch), seq_new=(seq_new, batch))
-    _check("rbq_quantize_kv", lib.rbq_quantize_kv(
-        batch, heads_kv, head_dim, _ptr(K), _ptr(V), kv_dtype_code(K), ld, n_new, offset, cap, block,
-        kv8_dtype_code(K8), _ptr(K8), _ptr(V8), _ptr(k_scale), _ptr(v_scale), _ptr(seq_off), _ptr(seq_new),
-        _stream(stream)))
+    name = "rbq_quantize_kv"
+    fmt, dt = _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8), _pair_code(name, _KV_CODES, "K", K, "V", V)
+    _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    _check_rows(name, batch, heads_kv, head_dim, ld, n_new, K, V)
+    _check_seqs(name, batch, seq_off, seq_new)
+    st = lib.rbq_quantize_kv(
+        batch, heads_kv, head_dim, K.data_ptr(), V.data_ptr(), dt, ld, n_new, offset, cap, block, fmt, K8.data_ptr(),
+        V8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(seq_off), _ptr(seq_new), _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
 
 
 def rbq_dequantize_kv(batch, heads_kv, head_dim, K8, V8, block, k_scale, v_scale, cap, n_rows, offset, K, V, ld,
                       seq_off=None, seq_rows=None, stream=None):
     """Cache rows [offset, offset + n_rows) as rows [0, n_rows) of K / V [B][Hkv][ld][D] (bf16 or fp32)."""
-    _need_kv8("rbq_dequantize_kv", batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    if K.dtype != V.dtype:
-        raise ValueError(f"rbq_dequantize_kv: K is {K.dtype}, V {V.dtype}")
-    rows = ((batch * heads_kv - 1) * ld + n_rows) * head_dim if n_rows > 0 else 0
-    _need("rbq_dequantize_kv", K=(K, rows), V=(V, rows), seq_off=(seq_off, batch), seq_rows=(seq_rows, batch))
-    _check("rbq_dequantize_kv", lib.rbq_dequantize_kv(
-        batch, heads_kv, head_dim, _ptr(K8), _ptr(V8), kv8_dtype_code(K8), block, _ptr(k_scale), _ptr(v_scale), cap,
-        n_rows, offset, _ptr(K), _ptr(V), kv_dtype_code(K), ld, _ptr(seq_off), _ptr(seq_rows), _stream(stream)))
+    name = "rbq_dequantize_kv"
+    fmt, dt = _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8), _pair_code(name, _KV_CODES, "K", K, "V", V)
+    _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    _check_rows(name, batch, heads_kv, head_dim, ld, n_rows, K, V)
+    _check_seqs(name, batch, seq_off, seq_rows)
+    st = lib.rbq_dequantize_kv(
+        batch, heads_kv, head_dim, K8.data_ptr(), V8.data_ptr(), fmt, block, k_scale.data_ptr(), v_scale.data_ptr(), cap,
+        n_rows, offset, K.data_ptr(), V.data_ptr(), dt, ld, _ptr(seq_off), _ptr(seq_rows), _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
 
 
-def _kv8_window(name, K_loc, V_loc):
-    if K_loc is None or V_loc is None:
-        return RBQ_BF16
-    if K_loc.dtype != V_loc.dtype:
-        raise ValueError(f"{name}: K_loc is {K_loc.dtype}, V_loc {V_loc.dtype}")
-    return kv_dtype_code(K_loc)
+def _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc, V_loc,
+                      loc_ld, w, out, lse, seq_n, seq_w):
+    """Formats of the cache and of the window, once every buffer is large enough."""
+    _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
+    rows = batch * heads_q
+    if q.numel() < rows * head_dim or out.numel() < rows * head_dim or (lse is not None and lse.numel() < rows):
+        _need(name, q=(q, rows * head_dim), out=(out, rows * head_dim), lse=(lse, rows))
+    loc = RBQ_BF16
+    if K_loc is not None and V_loc is not None:
+        loc = _pair_code(name, _KV_CODES, "K_loc", K_loc, "V_loc", V_loc)
+        _check_rows(name, batch, heads_kv, head_dim, loc_ld, w, K_loc, V_loc)
+    _check_seqs(name, batch, seq_n, seq_w)
+    return _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8), loc
 
 
 def rbq_dense_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, n, K_loc, V_loc,
                          loc_ld, w, sm_scale, out, lse, ws, seq_n=None, seq_w=None, stream=None):
     """rbq_dense_decode over an 8-bit cache and a window [B][Hkv][loc_ld][D] in bf16 or fp32."""
     name = "rbq_dense_decode_kv8"
-    _need_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    rows = ((batch * heads_kv - 1) * loc_ld + w) * head_dim if w > 0 else 0
-    _need(name, q=(q, batch * heads_q * head_dim), K_loc=(K_loc, rows), V_loc=(V_loc, rows),
-          out=(out, batch * heads_q * head_dim), lse=(lse, batch * heads_q), seq_n=(seq_n, batch), seq_w=(seq_w, batch))
-    ws_bytes = ws.numel() * ws.element_size()
-    _check(name, lib.rbq_dense_decode_kv8(
-        batch, heads_q, heads_kv, head_dim, _ptr(q), _ptr(K8), _ptr(V8), kv8_dtype_code(K8), block, _ptr(k_scale),
-        _ptr(v_scale), cap, n, _ptr(K_loc), _ptr(V_loc), _kv8_window(name, K_loc, V_loc), loc_ld, w, sm_scale,
-        _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _ptr(seq_n), _ptr(seq_w), _stream(stream)))
+    fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
+                                 V_loc, loc_ld, w, out, lse, seq_n, seq_w)
+    st = lib.rbq_dense_decode_kv8(
+        batch, heads_q, heads_kv, head_dim, q.data_ptr(), K8.data_ptr(), V8.data_ptr(), fmt, block, k_scale.data_ptr(),
+        v_scale.data_ptr(), cap, n, _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w, sm_scale, out.data_ptr(), _ptr(lse),
+        ws.data_ptr(), ws.numel() * ws.element_size(), _ptr(seq_n), _ptr(seq_w), _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
 
 
 def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, n, sel_idx,
@@ -501,17 +527,17 @@ def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, 
                           stream=None):
     """rbq_sparse_decode over an 8-bit cache and a window [B][Hkv][loc_ld][D] in bf16 or fp32."""
     name = "rbq_sparse_decode_kv8"
-    _need_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    rows = ((batch * heads_kv - 1) * loc_ld + w) * head_dim if w > 0 else 0
-    _need(name, q=(q, batch * heads_q * head_dim), K_loc=(K_loc, rows), V_loc=(V_loc, rows),
-          sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q),
-          out=(out, batch * heads_q * head_dim), lse=(lse, batch * heads_q), seq_n=(seq_n, batch), seq_w=(seq_w, batch))
-    ws_bytes = ws.numel() * ws.element_size()
-    _check(name, lib.rbq_sparse_decode_kv8(
-        batch, heads_q, heads_kv, head_dim, _ptr(q), _ptr(K8), _ptr(V8), kv8_dtype_code(K8), block, _ptr(k_scale),
-        _ptr(v_scale), cap, n, _ptr(sel_idx), _ptr(sel_count), _ptr(K_loc), _ptr(V_loc),
-        _kv8_window(name, K_loc, V_loc), loc_ld, w, sm_scale, _ptr(out), _ptr(lse), _ptr(ws), ws_bytes, _ptr(seq_n),
-        _ptr(seq_w), _stream(stream)))
+    fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
+                                 V_loc, loc_ld, w, out, lse, seq_n, seq_w)
+    if sel_idx.numel() < batch * heads_q * n or sel_count.numel() < batch * heads_q:
+        _need(name, sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q))
+    st = lib.rbq_sparse_decode_kv8(
+        batch, heads_q, heads_kv, head_dim, q.data_ptr(), K8.data_ptr(), V8.data_ptr(), fmt, block, k_scale.data_ptr(),
+        v_scale.data_ptr(), cap, n, sel_idx.data_ptr(), sel_count.data_ptr(), _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w,
+        sm_scale, out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _ptr(seq_n), _ptr(seq_w),
+        _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
 
 
 def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_ld, kv_head, kv_seq, kv_rows, cu_q,
@@ -519,12 +545,17 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
     """Attention of prompts packed along one token axis: q [total_q][Hq][D] (rows q_ld elements apart), cu_q and cu_k
     [batch + 1] int32 device tensors; K / V rows kv_ld elements apart, heads kv_head, sequences kv_seq (0: packed)."""
     name = "rbq_prefill_attention"
-    if not q.dtype == K.dtype == V.dtype == out.dtype:
+    dt = _pair_code(name, _KV_CODES, "K", K, "V", V)
+    if q.dtype != K.dtype or out.dtype != K.dtype:
         raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
-    _need(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, total_q * heads_q * head_dim),
-          lse=(lse, total_q * heads_q))
+    rows = total_q * heads_q
+    if (cu_q.numel() <= batch or cu_k.numel() <= batch or out.numel() < rows * head_dim
+            or (lse is not None and lse.numel() < rows)):
+        _need(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    _check(name, lib.rbq_prefill_attention(
-        batch, heads_q, heads_kv, head_dim, _ptr(q), q_ld, _ptr(K), _ptr(V), kv_dtype_code(K), kv_ld, kv_head, kv_seq,
-        kv_rows, _ptr(cu_q), _ptr(cu_k), total_q, max_k, int(bool(causal)), sm_scale, _ptr(out), _ptr(lse), _ptr(ws),
-        ws_bytes, _stream(stream)))
+    st = lib.rbq_prefill_attention(
+        batch, heads_q, heads_kv, head_dim, q.data_ptr(), q_ld, K.data_ptr(), V.data_ptr(), dt, kv_ld, kv_head, kv_seq,
+        kv_rows, cu_q.data_ptr(), cu_k.data_ptr(), total_q, max_k, 1 if causal else 0, sm_scale, out.data_ptr(), _ptr(lse),
+        _ptr(ws), ws_bytes, _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)

@@ -71,10 +71,12 @@ def test_other_calls_do_not_take_the_8_bit_formats(R):
     assert st == R.RBQ_EUNSUPPORTED
 
 
-def test_workspace_is_that_of_the_full_precision_call(R):
-    for n, w in [(0, 0), (1, 0), (0, 5), (4000, 129), (130816, 256)]:
-        a = R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, 1, 32, 8, 128, n, w)
-        assert a > 0 and a == R.rbq_workspace_bytes(R.RBQ_OP_DENSE_DECODE, 1, 32, 8, 128, n, w)
+def test_workspace_covers_every_form_of_the_call(R):
+    """One size serves dense, sparse and ragged calls: at least that of the full-precision call's splits."""
+    for B, n, w in [(1, 0, 0), (1, 1, 0), (1, 0, 5), (1, 4000, 129), (1, 130816, 256), (16, 32512, 256), (64, 200, 4096)]:
+        a = R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, B, 32, 8, 128, n, w)
+        assert a >= R.rbq_workspace_bytes(R.RBQ_OP_DENSE_DECODE, B, 32, 8, 128, n, w) > 0
+    assert R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, 1, 32, 8, 128, -1, 0) == 0
 
 
 def test_binding_refuses_short_or_mixed_buffers(R):
