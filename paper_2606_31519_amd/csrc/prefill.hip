@@ -5,8 +5,6 @@
 //   over the j < Lk of the query's sequence, for causal j <= i + Lk - Lq
 //
 // One pass over the keys with the running maximum and sum of the softmax.
-#include <algorithm>
-
 #include "rbq_device.h"
 #include "rbq_internal.h"
 
@@ -28,60 +26,141 @@ constexpr float kLn2 = 0.69314718055994531f;
 // row r = token r / G, head r % G of the group.
 struct TileId {
   int b, tile;   // sequence, tile of its rows; b < 0: none
+  int split;     // of its keys
   int q0, nq;    // first token of the sequence on the packed axis, tokens
   int nk;        // keys
   int64_t k0;    // first row of the sequence's keys (packed), 0 otherwise
 };
 
-// The tile'th tile of the batch: sequences in order, each with ceil(tokens * G / BM).
-__device__ __forceinline__ TileId find_tile(int tile, int batch, int G, int BM, int total_q, int max_k, int kv_rows,
-                                            bool packed, const int32_t* __restrict__ cu_q,
+// One sequence's lengths, inside the buffers: keys inside [0, kv_rows) of the packed axis,
+// or of the sequence's own rows.
+struct Lengths {
+  int q0, nq, k0, nk, tiles;
+};
+__device__ __forceinline__ Lengths lengths_of(int b, int G, int BM, int total_q, int max_k, int kv_rows, bool packed,
+                                              const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k) {
+  Lengths s;
+  const int ka = cu_k[b], kb = cu_k[b + 1];
+  s.q0 = min(max(cu_q[b], 0), total_q);
+  s.nq = max(min(max(cu_q[b + 1], 0), total_q) - s.q0, 0);
+  s.k0 = packed ? min(max(ka, 0), kv_rows) : 0;
+  s.nk = min(min(max(kb - ka, 0), max_k), kv_rows - s.k0);
+  s.tiles = int((int64_t(s.nq) * G + BM - 1) / BM);
+  return s;
+}
+
+// What block `id` of a KV head does. Query tiles (ceil(tokens * G / BM) a sequence) are
+// ranked by their steps of kPKeys keys, the longest first: started last they would run on
+// alone. The tiles of a causal sequence see more keys one after the other, so a bisection
+// over the number of steps, each lane counting one sequence's tiles, finds the p'th. Of
+// split keys, split y is taken by the tiles that have keys there, a number L_y that lane y
+// counts, so the blocks are split 0 of L_0 tiles, split 1 of the first L_1, ...: those
+// without work all come last. (Spread among the others, as a grid of tiles x splits has
+// them, they leave whole shader engines idle, which take blocks in turn: 512 blocks of
+// 256 fp32 keys with 512 empty ones between them 84 us, in this order 52.)
+// More sequences than lanes: in the sequences' order, backwards, every split of a tile.
+__device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int kchunk, int batch, int G, int BM, int total_q, int max_k, int kv_rows,
+                                            bool packed, bool causal, const int32_t* __restrict__ cu_q,
                                             const int32_t* __restrict__ cu_k) {
   const int lane = lane_id();
-  TileId t{-1, 0, 0, 0, 0, 0};
-  int before = 0;
-  for (int b0 = 0; b0 < batch; b0 += kWave) {
-    const int b = min(b0 + lane, batch - 1);
-    const int qa = min(max(cu_q[b], 0), total_q), qb = min(max(cu_q[b + 1], 0), total_q);
-    const int ka = cu_k[b], kb = cu_k[b + 1];
-    const int nq = max(qb - qa, 0);
-    const int tiles = b0 + lane < batch ? int((int64_t(nq) * G + BM - 1) / BM) : 0;
-    int inc = tiles;
+  TileId t{-1, 0, 0, 0, 0, 0, 0};
+  auto found = [&](const Lengths& s, int b0, int l, int tile) {
+    t.b = b0 + l;
+    t.tile = tile;
+    t.q0 = __builtin_amdgcn_readlane(s.q0, l);
+    t.nq = __builtin_amdgcn_readlane(s.nq, l);
+    t.nk = __builtin_amdgcn_readlane(s.nk, l);
+    t.k0 = __builtin_amdgcn_readlane(s.k0, l);
+  };
+  auto prefix = [&](int v) {   // inclusive sum over the lanes
 #pragma unroll
     for (int o = 1; o < kWave; o <<= 1) {
-      const int v = __shfl_up(inc, o, kWave);
-      inc += lane >= o ? v : 0;
+      const int u = __shfl_up(v, o, kWave);
+      v += lane >= o ? u : 0;
     }
-    const unsigned long long mine = __ballot(tile >= before + inc - tiles && tile < before + inc);
-    if (mine != 0ull) {
-      const int l = __builtin_ctzll(mine);
-      t.b = b0 + l;
-      t.tile = tile - before - __builtin_amdgcn_readlane(inc - tiles, l);
-      t.q0 = __builtin_amdgcn_readlane(qa, l);
-      t.nq = __builtin_amdgcn_readlane(nq, l);
-      // keys inside [0, kv_rows) of the packed axis, or of the sequence's own rows
-      const int a = packed ? min(max(__builtin_amdgcn_readlane(ka, l), 0), kv_rows) : 0;
-      const int n = max(__builtin_amdgcn_readlane(kb, l) - __builtin_amdgcn_readlane(ka, l), 0);
-      t.nk = min(min(n, max_k), kv_rows - a);
-      t.k0 = a;
+    return v;
+  };
+  if (batch == 1 && splits == 1) {
+    const Lengths s = lengths_of(0, G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k);
+    if (id < s.tiles) found(s, 0, 0, s.tiles - 1 - id);
+    return t;
+  }
+  if (batch <= kWave) {
+    Lengths s = lengths_of(min(lane, batch - 1), G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k);
+    if (lane >= batch) s.nq = s.tiles = 0;
+    // this sequence's tiles of at least n steps: a causal tile's keys end at its last token's
+    auto of = [&](int nq, int nk, int tiles_b, int n) {
+      if (n <= 0) return tiles_b;
+      if (!causal) return (nk + kPKeys - 1) / kPKeys >= n ? tiles_b : 0;
+      const int64_t first = int64_t(n - 1) * kPKeys - (nk - nq);   // the token that its last token must reach
+      return first >= nq ? 0 : tiles_b - (first > 0 ? int(first * G / BM) : 0);
+    };
+    auto count = [&](int n) { return of(s.nq, s.nk, s.tiles, n); };
+    int p = id;
+    if (splits > 1) {
+      int live = 0;   // L_y of lane y
+      for (int b = 0; b < batch; ++b)
+        live += of(__builtin_amdgcn_readlane(s.nq, b), __builtin_amdgcn_readlane(s.nk, b),
+                   __builtin_amdgcn_readlane(s.tiles, b), lane > 0 ? lane * (kchunk / kPKeys) + 1 : 0);
+      if (lane >= splits) live = 0;
+      const int inc = prefix(live);
+      const unsigned long long at = __ballot(id >= inc - live && id < inc);
+      if (at == 0ull) return t;
+      t.split = __builtin_ctzll(at);
+      p -= __builtin_amdgcn_readlane(inc - live, t.split);
+    }
+    if (p >= wave_sum_i32(s.tiles)) return t;
+    int lo = 0, hi = (max_k + kPKeys - 1) / kPKeys + 1;   // more than p tiles have at least lo steps, no more than p hi
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) / 2;
+      if (wave_sum_i32(count(mid)) > p) lo = mid;
+      else hi = mid;
+    }
+    const int more = count(lo + 1), here = count(lo) - more, inc = prefix(here);
+    const int r = p - wave_sum_i32(more);
+    const int l = __builtin_ctzll(__ballot(r >= inc - here && r < inc) | (1ull << 63));
+    found(s, 0, l, __builtin_amdgcn_readlane(s.tiles - more - here, l) + r - __builtin_amdgcn_readlane(inc - here, l));
+    return t;
+  }
+  const int tile = tiles - 1 - id / splits;
+  t.split = id % splits;
+  int before = 0;
+  for (int b0 = 0; b0 < batch; b0 += kWave) {
+    const Lengths s = lengths_of(min(b0 + lane, batch - 1), G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k);
+    const int mine = b0 + lane < batch ? s.tiles : 0, inc = before + prefix(mine);
+    const unsigned long long at = __ballot(tile >= inc - mine && tile < inc);
+    if (at != 0ull) {
+      const int l = __builtin_ctzll(at);
+      found(s, b0, l, tile - __builtin_amdgcn_readlane(inc - mine, l));
       return t;
     }
-    before += __builtin_amdgcn_readlane(inc, kWave - 1);
+    before = __builtin_amdgcn_readlane(inc, kWave - 1);
   }
   return t;
 }
 
 // 16 bytes per lane from global memory straight into LDS (lane l's at lds + 16 l)
-__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, void* lds, int off) {
+__device__ __forceinline__ void load_lds16(__amdgpu_buffer_rsrc_t r, char* lds, int off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (RBQ_LDS void*)lds, 16, off, 0, 0, 0);
 }
+// Waits for this wave's loads: before the barrier that publishes them to the block.
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// The 16-byte chunk c of row r of a tile lies at chunk c ^ swizzle(r) of the row, so that the
+// lanes served together (256 bytes a clock) touch every bank once: 16 rows' same chunk of K,
+// 64 bytes of four rows that follow each other of V. Both depend on r mod 16 alone.
+template <int D>
+__device__ __forceinline__ int k_swizzle(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int v_swizzle(int r) { return D == 128 ? 4 * (r & 3) : 4 * ((r >> 1) & 1); }
 
 // A lane's part of a finished row: dimensions 32 d + 8 g + 4 h .. +4. With one split
 // the output itself, otherwise the split's state {m, l, acc}.
 template <int D, int DT, int NQ>
 __device__ __forceinline__ void store_row(const f32x16 (&o)[D / 32][NQ], int i, float m, float sum, int64_t row, int h,
-                                          void* __restrict__ out, float* __restrict__ lse, float* __restrict__ part) {
-  float* pr = part + (row * gridDim.y + blockIdx.y) * (D + 2);
+                                          void* __restrict__ out, float* __restrict__ lse, float* __restrict__ part,
+                                          int split, int splits, int none) {
+  float* pr = part + (row * splits + split) * (D + 2);
   const float scale = part ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
@@ -102,25 +181,41 @@ __device__ __forceinline__ void store_row(const f32x16 (&o)[D / 32][NQ], int i, 
       }
     }
   if (h != 0) return;
-  if (part)
+  if (part) {
     *reinterpret_cast<f32x2*>(pr) = f32x2{sum > 0.f ? m : -INFINITY, sum};
-  else if (lse)
+    // split 0 also writes the states of the splits from `none` on, which no block takes
+    for (int k = none; split == 0 && k < splits; ++k) pr[int64_t(k) * (D + 2)] = -INFINITY;
+  } else if (lse)
     lse[row] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
 }
 
-// D: head dimension; QT: 32-row query tiles per wave
-template <int D, int QT>
-__global__ __launch_bounds__(kPThreads, QT == 1 ? 2 : 1) void prefill_kernel(
+// bf16 rows. A wave holds 32 query rows as the columns of its products, so that a row's
+// maximum and sum are over its own lane and the one 32 away:
+//   S^T = K Q^T   v_mfma_f32_32x32x16_bf16, A = 32 keys, B = the queries (in registers);
+//                 lane (row x, half h), register r: key 8 (r / 4) + 4 h + r % 4
+//   O^T = V^T P^T A = 32 dimensions of V by transposing LDS reads, B = the probabilities
+//                 straight from those registers (the order of the 16 keys of a product is
+//                 free as long as both operands share it)
+// A step takes 64 keys, staged by the block's four waves into a double buffer in LDS, K a
+// step ahead of V: the products of the next step's logits run on the matrix cores while
+// the softmax of this one runs on the vector units, and K's and V's LDS reads are hidden
+// behind both. Two blocks share a compute unit: with its 128 accumulators for 64 rows a wave
+// would read LDS half as often, but alone on its SIMD it waits (16001 tokens of 32 heads:
+// 2772 us; 32 rows 2129). 2.10 TFLOP in 2060 to 2190 us is 0.96 to 1.02 PFLOP/s; the clock
+// is what the power limit leaves (1.8 of 2.4 GHz): the same call on zeros takes 1552 us, and
+// the library's 8192^3 product, in the same state, makes 1.23 PFLOP/s of its 1.70 on zeros.
+template <int D>
+__global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     const uint16_t* __restrict__ q, int64_t q_ld, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     int64_t kv_ld, int64_t kv_head, int64_t kv_seq, int kv_rows, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ cu_k, int batch, int total_q, int max_k, int causal, float scale_log2e,
-    uint16_t* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv, int tiles, int kchunk) {
-  constexpr int BM = 32 * QT * kPWaves, C = D / 8, KB = D / 16, DT = D / 32, RB = D * 2;   // chunks, k-blocks, dim tiles, row bytes
-  constexpr int KT = kPKeys / 32;
+    uint16_t* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv, int tiles, int splits, int kchunk) {
+  constexpr int BM = 32 * kPWaves, C = D / 8, KB = D / 16, DT = D / 32, RB = D * 2;   // chunks, k-blocks, dim tiles, row bytes
   __shared__ __attribute__((aligned(1024))) char ldsK[2][kPKeys * RB], ldsV[2][kPKeys * RB];
   const int G = Hq / Hkv;
   const int hk = blockIdx.x % Hkv;
-  const TileId t = find_tile(tiles - 1 - int(blockIdx.x) / Hkv, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0, cu_q, cu_k);
+  const TileId t = find_tile(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
+                             causal != 0, cu_q, cu_k);
   if (t.b < 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
   const int x = lane & 31, h = lane >> 5;
@@ -129,162 +224,134 @@ __global__ __launch_bounds__(kPThreads, QT == 1 ? 2 : 1) void prefill_kernel(
   const int shift = t.nk - t.nq;                                   // query token i sees keys <= i + shift
   auto visible = [&](int token) { return causal ? min(max(token + shift + 1, 0), t.nk) : t.nk; };
   const int kend = visible((min(row0 + BM, rows) - 1) / G);         // keys that some row of the block sees
-  const int wrow = row0 + wave * (32 * QT);
-  const int kbeg = int(blockIdx.y) * kchunk, kstop = min(kend, kbeg + kchunk);   // this block's keys
-  const int wend = wrow < rows ? visible((min(wrow + 32 * QT, rows) - 1) / G) : 0;   // of the wave
+  const int wrow = row0 + wave * 32;
+  const int kbeg = t.split * kchunk, kstop = min(kend, kbeg + kchunk);   // this block's keys
+  const int wend = wrow < rows ? visible((min(wrow + 32, rows) - 1) / G) : 0;   // of the wave
   const int wmin = visible(min(wrow, rows - 1) / G);                // keys that every row of the wave sees
 
   // queries: B operand, lane (row x, half h) holds dimensions 16 kb + 8 h .. +8
-  bf16x8 qf[QT][KB];
-  int token[QT], head[QT], lim[QT];
+  bf16x8 qf[KB];
+  const int qrow = min(wrow + x, rows - 1), token = qrow / G, head = hk * G + (qrow - token * G), lim = visible(token);
+  {
+    const uint16_t* p = q + int64_t(t.q0 + token) * q_ld + head * D + 8 * h;
 #pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    const int r = min(wrow + 32 * i + x, rows - 1);
-    token[i] = r / G;
-    head[i] = hk * G + (r - token[i] * G);
-    lim[i] = visible(token[i]);
-    const uint16_t* p = q + int64_t(t.q0 + token[i]) * q_ld + head[i] * D + 8 * h;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) qf[i][kb] = *reinterpret_cast<const bf16x8*>(p + 16 * kb);
+    for (int kb = 0; kb < KB; ++kb) qf[kb] = *reinterpret_cast<const bf16x8*>(p + 16 * kb);
   }
 
   const int64_t kvoff = (kv_seq == 0 ? t.k0 * kv_ld : int64_t(t.b) * kv_seq) + int64_t(hk) * kv_head;
   const uint16_t *Kb = K + kvoff, *Vb = V + kvoff;
-  // staging: one instruction moves 1024 bytes, 1024 / RB rows; chunk position p of row r
-  // holds chunk p ^ f(r), so that the reads below touch every bank once
+  // staging: one instruction moves 1024 bytes, 1024 / RB rows
   constexpr int kRowsPer = 1024 / RB, kIssues = kPKeys / kRowsPer / kPWaves;
   const int srow = lane / C, spos = lane % C;
-  int koff[kIssues], voff[kIssues];
-#pragma unroll
-  for (int i = 0; i < kIssues; ++i) {
-    const int r = (wave * kIssues + i) * kRowsPer + srow;
-    koff[i] = int(r * kv_ld * 2) + ((spos ^ (r & (C - 1))) * 16);
-    voff[i] = int(r * kv_ld * 2) + ((spos ^ (2 * (r & 3))) * 16);
-  }
-  auto stage = [&](int k0, int buf) {
-    const int left = min(t.nk - k0, kPKeys);
-    const uint32_t bytes = uint32_t((left - 1) * kv_ld * 2 + RB);
-    const __amdgpu_buffer_rsrc_t kr = make_rsrc(Kb + k0 * kv_ld, bytes), vr = make_rsrc(Vb + k0 * kv_ld, bytes);
-    if (left < kPKeys) {   // the last rows again in place of those behind them
-#pragma unroll
-      for (int i = 0; i < kIssues; ++i) {
-        const int r = (wave * kIssues + i) * kRowsPer + srow, at = int(min(r, left - 1) * kv_ld * 2);
-        load_lds16(kr, &ldsK[buf][(wave * kIssues + i) * 1024], at + ((spos ^ (r & (C - 1))) * 16));
-        load_lds16(vr, &ldsV[buf][(wave * kIssues + i) * 1024], at + ((spos ^ (2 * (r & 3))) * 16));
-      }
-      return;
-    }
+  auto stage = [&](const uint16_t* base, char* lds, int k0, bool v) {
+    const int left = min(t.nk - k0, kPKeys);   // (the last rows again in place of those behind them)
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base + k0 * kv_ld, uint32_t((left - 1) * kv_ld * 2 + RB));
 #pragma unroll
     for (int i = 0; i < kIssues; ++i) {
-      load_lds16(kr, &ldsK[buf][(wave * kIssues + i) * 1024], koff[i]);
-      load_lds16(vr, &ldsV[buf][(wave * kIssues + i) * 1024], voff[i]);
+      const int row = (wave * kIssues + i) * kRowsPer + srow;
+      load_lds16(r, lds + (wave * kIssues + i) * 1024,
+                 min(row, left - 1) * int(kv_ld * 2) + ((spos ^ (v ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16));
     }
   };
   // read addresses: K rows (lane: key x, chunk 2 kb + h), V columns by the transposing
   // read (16 lanes: 4 keys x 16 dimensions; lane i gives key i / 4, dimensions 4 (i % 4) .. +4)
-  const int kbase = x * RB + ((h ^ (x & (C - 1))) * 16);
+  const int kbase = x * RB + ((h ^ k_swizzle<D>(x)) * 16);
   const int i16 = lane & 15, g16 = (lane >> 4) & 1;
-  const int vbase = (4 * h + (i16 >> 2)) * RB + (((2 * g16 + ((i16 & 3) >> 1)) ^ (2 * (i16 >> 2))) * 16) + (i16 & 1) * 8;
+  const int vbase = (4 * h + (i16 >> 2)) * RB + (((2 * g16 + ((i16 & 3) >> 1)) ^ v_swizzle<D>(i16 >> 2)) * 16) + (i16 & 1) * 8;
 
-  f32x16 o[DT][QT];
-  float m[QT], l[QT];
+  f32x16 o[DT][1];
+  float m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    m[i] = -INFINITY;
-    l[i] = 0.f;
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int d = 0; d < DT; ++d)
+    for (int r = 0; r < 16; ++r) o[d][0][r] = 0.f;
+
+  auto logits = [&](f32x16& d, const char* tile) {   // of the 32 keys whose rows start at `tile`
 #pragma unroll
-      for (int r = 0; r < 16; ++r) o[d][i][r] = 0.f;
+    for (int r = 0; r < 16; ++r) d[r] = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb) {
+      const bf16x8 a = *reinterpret_cast<const bf16x8*>(tile + (kbase ^ (kb * 32)));
+      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], d, 0, 0, 0);
+    }
+  };
+  // the softmax of s (32 keys from k0) and its product with V, and the logits nx of the 32 keys after
+  auto step = [&](f32x16& s, f32x16& nx, int k0, const char* next_k, const char* tile_v) {
+    if (k0 + 32 > wmin) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[r] = k0 + 8 * (r / 4) + 4 * h + r % 4 < lim ? s[r] : -INFINITY;
+    }
+    float mx[2] = {s[0], s[1]};
+#pragma unroll
+    for (int r = 2; r < 16; ++r) mx[r & 1] = fmaxf(mx[r & 1], s[r]);
+    float top = fmaxf(mx[0], mx[1]);
+    const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
+    top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2e;
+    // the reference moves only where a row's maximum passes it by more than 2^8 (the
+    // probabilities then stay below 2^8, which costs fp32 sums and bf16's precision nothing)
+    if (__ballot(top > m + 8.f)) {
+      const float mn = fmaxf(m, top);
+      const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
+      l *= corr;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[d][0][r] *= corr;
+      m = mn;
+    }
+    const float mref = m == -INFINITY ? 0.f : m;
+    logits(nx, next_k);
+    bf16x8 p[2];
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      f32x8 e;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * g + r], scale_log2e, -mref));
+        sum[r & 1] += e[r];
+      }
+      p[g] = __builtin_convertvector(e, bf16x8);
+    }
+    l += sum[0] + sum[1];
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+      for (int d = 0; d < DT; ++d) {
+        const char* at = tile_v + g * 16 * RB + (vbase ^ (d * 64));
+        const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((RBQ_LDS s16x4*)at);
+        const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((RBQ_LDS s16x4*)(at + 8 * RB));
+        const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+        o[d][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[g], o[d][0], 0, 0, 0);
+      }
+  };
+
+  // Tile i of V holds the keys of step i, kbeg + 64 i .. +64; tile i of K those whose logits
+  // step i forms, 32 further on (the first 32 keys' come before the loop). Logits of keys
+  // behind the last are formed from whatever the tile holds and masked.
+  f32x16 sa, sb;
+  if (kbeg < kstop) {
+    stage(Kb, ldsK[1], kbeg, false);
+    stage(Vb, ldsV[0], kbeg, true);
+    if (kbeg + 32 < kstop) stage(Kb, ldsK[0], kbeg + 32, false);
+    wait_lds();
+    __syncthreads();
+    logits(sa, ldsK[1]);
   }
-
-  if (kbeg < kstop) stage(kbeg, 0);
+  const int wstop = min(wend, kstop);
   int buf = 0;
   for (int k0 = kbeg; k0 < kstop; k0 += kPKeys, buf ^= 1) {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    wait_lds();
     __syncthreads();
-    if (k0 + kPKeys < kstop) stage(k0 + kPKeys, buf ^ 1);
-    if (k0 >= wend) continue;
-    f32x16 s[KT][QT];
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int i = 0; i < QT; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[kt][i][r] = 0.f;
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int kb = 0; kb < KB; ++kb) {
-        const bf16x8 a = *reinterpret_cast<const bf16x8*>(&ldsK[buf][kt * 32 * RB + (kbase ^ (kb * 32))]);
-#pragma unroll
-        for (int i = 0; i < QT; ++i) s[kt][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[i][kb], s[kt][i], 0, 0, 0);
-      }
-    if (k0 + kPKeys > wmin) {
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int i = 0; i < QT; ++i)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s[kt][i][r] = k0 + 32 * kt + 8 * (r / 4) + 4 * h + r % 4 < lim[i] ? s[kt][i][r] : -INFINITY;
-    }
-    bf16x8 p[KT][QT][2];
-#pragma unroll
-    for (int i = 0; i < QT; ++i) {
-      float mx = s[0][i][0];
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[kt][i][r]);
-      mx = fmaxf(mx, __shfl_xor(mx, 32, kWave)) * scale_log2e;
-      const float mn = fmaxf(m[i], mx);
-      if (__ballot(mn != m[i])) {
-        const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - mn);
-        l[i] *= corr;
-#pragma unroll
-        for (int d = 0; d < DT; ++d)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) o[d][i][r] *= corr;
-        m[i] = mn;
-      }
-      const float mref = m[i] == -INFINITY ? 0.f : m[i];
-      float sum = 0.f;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) {
-          f32x8 e;
-#pragma unroll
-          for (int r = 0; r < 8; ++r) {
-            e[r] = __builtin_amdgcn_exp2f(fmaf(s[kt][i][8 * g + r], scale_log2e, -mref));
-            sum += e[r];
-          }
-          p[kt][i][g] = __builtin_convertvector(e, bf16x8);
-        }
-      l[i] += sum;
-    }
-#pragma unroll
-    for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-      for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int d = 0; d < DT; ++d) {
-          const int at = (kt * 32 + g * 16) * RB + (vbase ^ (d * 64));
-          const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((RBQ_LDS s16x4*)&ldsV[buf][at]);
-          const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((RBQ_LDS s16x4*)&ldsV[buf][at + 8 * RB]);
-          const bf16x8 a = __builtin_bit_cast(bf16x8, __builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-#pragma unroll
-          for (int i = 0; i < QT; ++i) o[d][i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[kt][i][g], o[d][i], 0, 0, 0);
-        }
+    if (k0 + kPKeys < kstop) stage(Vb, ldsV[buf ^ 1], k0 + kPKeys, true);
+    if (k0 + kPKeys + 32 < kstop) stage(Kb, ldsK[buf ^ 1], k0 + kPKeys + 32, false);
+    if (k0 < wstop) step(sa, sb, k0, ldsK[buf], ldsV[buf]);
+    if (k0 + 32 < wstop) step(sb, sa, k0 + 32, &ldsK[buf][32 * RB], &ldsV[buf][32 * RB]);
   }
 
-#pragma unroll
-  for (int i = 0; i < QT; ++i) {
-    const float sum = l[i] + __shfl_xor(l[i], 32, kWave);
-    if (wrow + 32 * i + x < rows)
-      store_row<D, RBQ_BF16>(o, i, m[i], sum, int64_t(t.q0 + token[i]) * Hq + head[i], h, out, lse, part);
-  }
+  const float sum = l + __shfl_xor(l, 32, kWave);
+  if (wrow + x < rows) store_row<D, RBQ_BF16>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part, t.split, splits,
+                      batch <= kWave ? (kend + kchunk - 1) / kchunk + (kend == 0) : splits);
 }
 
 // fp32 rows: the same on v_mfma_f32_32x32x2_f32, products and probabilities in fp32.
@@ -298,20 +365,21 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
     const float* __restrict__ q, int64_t q_ld, const float* __restrict__ K, const float* __restrict__ V, int64_t kv_ld,
     int64_t kv_head, int64_t kv_seq, int kv_rows, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
     int batch, int total_q, int max_k, int causal, float scale_log2e, float* __restrict__ out, float* __restrict__ lse,
-    float* __restrict__ part, int Hq, int Hkv, int tiles, int kchunk) {
+    float* __restrict__ part, int Hq, int Hkv, int tiles, int splits, int kchunk) {
   constexpr int BM = 32 * kPWaves, DT = D / 32, LD = D + 4;   // (padded rows: four consecutive keys in other banks)
   constexpr int kPieces = kFKeys * D / 4 / kPThreads;        // 16-byte pieces per thread and tensor
   __shared__ __attribute__((aligned(16))) float ldsK[kFKeys][LD], ldsV[kFKeys][LD];
   const int G = Hq / Hkv;
   const int hk = blockIdx.x % Hkv;
-  const TileId t = find_tile(tiles - 1 - int(blockIdx.x) / Hkv, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0, cu_q, cu_k);
+  const TileId t = find_tile(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
+                             causal != 0, cu_q, cu_k);
   if (t.b < 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
   const int x = lane & 31, h = lane >> 5;
   const int rows = t.nq * G, row0 = t.tile * BM, shift = t.nk - t.nq;
   auto visible = [&](int token) { return causal ? min(max(token + shift + 1, 0), t.nk) : t.nk; };
   const int kend = visible((min(row0 + BM, rows) - 1) / G);
-  const int kbeg = int(blockIdx.y) * kchunk, kstop = min(kend, kbeg + kchunk);
+  const int kbeg = t.split * kchunk, kstop = min(kend, kbeg + kchunk);
   const int wrow = row0 + wave * 32;
   const int wend = wrow < rows ? visible((min(wrow + 32, rows) - 1) / G) : 0;
   const int r0 = min(wrow + x, rows - 1), token = r0 / G, head = hk * G + (r0 - token * G), lim = visible(token);
@@ -353,12 +421,32 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
     f32x16 s;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
+    // LDS reads in groups of four, each requested before the last one's products (the fences
+    // keep them there)
+    f32x4 ka[2][4];
+    auto read_k = [&](int g) {
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) {
-      const f32x4 a = *reinterpret_cast<const f32x4*>(&ldsK[x][h * (D / 2) + 4 * i]);
+      for (int i = 0; i < 4; ++i) ka[g & 1][i] = *reinterpret_cast<const f32x4*>(&ldsK[x][h * (D / 2) + 4 * (4 * g + i)]);
+    };
+    read_k(0);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], qf[i][e], s, 0, 0, 0);
+    for (int g = 0; g < D / 32; ++g) {
+      if (g + 1 < D / 32) read_k(g + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s = __builtin_amdgcn_mfma_f32_32x32x2f32(ka[g & 1][i][e], qf[4 * g + i][e], s, 0, 0, 0);
     }
+    float va[2][4][DT];
+    auto read_v = [&](int g) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < DT; ++d) va[g & 1][i][d] = ldsV[8 * g + 4 * h + i][32 * d + x];
+    };
+    read_v(0);
+    __builtin_amdgcn_sched_barrier(0);
     float mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -383,38 +471,52 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
       l += s[r];
     }
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int g = 0; g < 4; ++g) {
+      if (g < 3) read_v(g + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int d = 0; d < DT; ++d)
-        o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(ldsV[8 * (r / 4) + 4 * h + r % 4][32 * d + x], s[r], o[d][0], 0, 0, 0);
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(va[g & 1][i][d], s[4 * g + i], o[d][0], 0, 0, 0);
+    }
   }
   const float sum = l + __shfl_xor(l, 32, kWave);
   if (wrow + x < rows)
-    store_row<D, RBQ_F32>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part);
+    store_row<D, RBQ_F32>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part, t.split, splits,
+                      batch <= kWave ? (kend + kchunk - 1) / kchunk + (kend == 0) : splits);
 }
 
-// Joins the splits of the rows of sequences (tokens [cu_q[0], cu_q[batch])), in order: a
-// wave per row, each lane D / 64 dimensions.
+// Joins the splits of the rows of sequences (tokens [cu_q[0], cu_q[batch])): a wave per
+// row; lane s weighs split s, then each lane adds up D / 64 dimensions in the splits' order.
 template <int D, int DT>
 __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float* __restrict__ part, int splits, int64_t rows,
                                                                     int Hq, const int32_t* __restrict__ cu_q, int batch,
                                                                     void* __restrict__ out, float* __restrict__ lse) {
-  constexpr int E = D / 64;
+  constexpr int E = D / 64, kBatch = 8;
   const int64_t row = int64_t(blockIdx.x) * kPWaves + threadIdx.x / kWave;
   if (row >= rows || row < int64_t(cu_q[0]) * Hq || row >= int64_t(cu_q[batch]) * Hq) return;
   const int lane = lane_id();
   const float* p = part + row * splits * (D + 2);
-  float M = -INFINITY;
-  for (int s = 0; s < splits; ++s) M = fmaxf(M, p[s * (D + 2)]);
-  float l = 0.f, acc[E] = {};
-  if (M != -INFINITY) {
-    for (int s = 0; s < splits; ++s) {
-      const float* ps = p + s * (D + 2);
-      const float c = __builtin_amdgcn_exp2f(ps[0] - M);
-      if (ps[0] == -INFINITY) continue;
-      l = fmaf(ps[1], c, l);
+  const f32x2 ml = *reinterpret_cast<const f32x2*>(p + min(lane, splits - 1) * (D + 2));
+  const float ms = lane < splits ? ml.x : -INFINITY;
+  const float M = wave_max(ms);
+  const float c = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
+  const float l = wave_reduce(c > 0.f ? ml.y * c : 0.f, [](float a, float b) { return a + b; });
+  float acc[E] = {};
+  for (int s0 = 0; s0 < splits; s0 += kBatch) {
+    float v[kBatch][E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) acc[e] = fmaf(ps[2 + E * lane + e], c, acc[e]);
+    for (int k = 0; k < kBatch; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[k][e] = p[min(s0 + k, splits - 1) * (D + 2) + 2 + E * lane + e];
+#pragma unroll
+    for (int k = 0; k < kBatch; ++k) {
+      const float ck = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(c)), min(s0 + k, kWave - 1))));
+      if (s0 + k < splits && ck > 0.f) {   // (a split without keys has written nothing else)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[e] = fmaf(v[k][e], ck, acc[e]);
+      }
     }
   }
   const float inv = l > 0.f ? 1.f / l : 0.f;
@@ -436,14 +538,14 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
   const PrefillPlan pl = prefill_plan(batch, heads_q, heads_kv, a.max_k, a.total_q, a.dtype);
   const float c = float(double(a.sm_scale) * 1.4426950408889634);
   float* part = pl.splits > 1 ? static_cast<float*>(a.ws) : nullptr;
-  const dim3 grid(uint32_t(int64_t(pl.tiles) * heads_kv), pl.splits);
+  const dim3 grid(uint32_t(int64_t(pl.tiles) * heads_kv * pl.splits));
   const int64_t rows = int64_t(a.total_q) * heads_q;
   const dim3 cgrid(uint32_t((rows + kPWaves - 1) / kPWaves));
 #define RBQ_PREFILL(KERNEL, T)                                                                                          \
   KERNEL<<<grid, kPThreads, 0, stream>>>(static_cast<const T*>(a.q), a.q_ld, static_cast<const T*>(a.K),                 \
                                          static_cast<const T*>(a.V), a.kv_ld, a.kv_head, a.kv_seq, a.kv_rows, a.cu_q,   \
                                          a.cu_k, batch, a.total_q, a.max_k, a.causal, c, static_cast<T*>(a.out), a.lse, \
-                                         part, heads_q, heads_kv, pl.tiles, pl.kchunk)
+                                         part, heads_q, heads_kv, pl.tiles, pl.splits, pl.kchunk)
 #define RBQ_PREFILL_JOIN(D, DT)                                                                                    \
   if (part)                                                                                                        \
   prefill_combine_kernel<D, DT><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, a.out, \
@@ -457,12 +559,10 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
       RBQ_PREFILL_JOIN(128, RBQ_F32);
     }
   } else if (head_dim == 64) {
-    if (pl.rows > 128) RBQ_PREFILL((prefill_kernel<64, 2>), uint16_t);
-    else RBQ_PREFILL((prefill_kernel<64, 1>), uint16_t);
+    RBQ_PREFILL(prefill_kernel<64>, uint16_t);
     RBQ_PREFILL_JOIN(64, RBQ_BF16);
   } else {
-    if (pl.rows > 128) RBQ_PREFILL((prefill_kernel<128, 2>), uint16_t);
-    else RBQ_PREFILL((prefill_kernel<128, 1>), uint16_t);
+    RBQ_PREFILL(prefill_kernel<128>, uint16_t);
     RBQ_PREFILL_JOIN(128, RBQ_BF16);
   }
 #undef RBQ_PREFILL_JOIN

@@ -15,6 +15,8 @@ constexpr int64_t kMaxStride = int64_t(1) << 23;   // elements: 64 rows of it ar
 constexpr int64_t kCus = 256;                      // compute units of the GPU
 constexpr int64_t kKv8Resident = 4 * kCus;         // blocks of the decode over an 8-bit cache that run at once
 constexpr int64_t kPrefillMinKeys = 256;           // keys per split, at least
+constexpr int64_t kPrefillMaxSplits = 64;          // (the joining kernel weighs a split per lane)
+constexpr int64_t kPrefillAim = 2 * kCus, kPrefillAimF32 = 4 * kCus;
 // a required device pointer: present, and 16-byte aligned (the kernels use 16-byte vector loads)
 bool bad_ptr(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 }  // namespace
@@ -253,12 +255,13 @@ PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
                          int32_t dtype) {
   const int64_t rows = int64_t(total_q) * (heads_q / heads_kv);
   PrefillPlan p;
-  p.rows = dtype == RBQ_BF16 && rows * heads_kv >= int64_t(256) * 2 * kCus ? 256 : 128;
+  p.rows = 128;
   p.tiles = int32_t(rows / p.rows + batch);
   const int64_t blocks = (rows + p.rows - 1) / p.rows * heads_kv;
-  int64_t want = blocks < kCus ? (2 * kCus + blocks - 1) / blocks : 1;
+  const int64_t aim = dtype == RBQ_F32 ? kPrefillAimF32 : kPrefillAim;
+  int64_t want = blocks < kCus ? (aim + blocks - 1) / blocks : 1;
   want = std::min<int64_t>(want, (int64_t(max_k) + kPrefillMinKeys - 1) / kPrefillMinKeys);
-  want = std::max<int64_t>(want, 1);
+  want = std::max<int64_t>(std::min<int64_t>(want, kPrefillMaxSplits), 1);
   p.kchunk = int32_t(((int64_t(max_k) + want - 1) / want + 63) / 64 * 64);
   if (p.kchunk == 0) p.kchunk = 64;
   p.splits = std::max<int32_t>(int32_t((int64_t(max_k) + p.kchunk - 1) / p.kchunk), 1);
