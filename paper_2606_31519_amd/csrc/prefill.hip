@@ -287,9 +287,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     float top = fmaxf(mx[0], mx[1]);
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2e;
-    // the reference moves only where a row's maximum passes it by more than 2^8 (the
-    // probabilities then stay below 2^8, which costs fp32 sums and bf16's precision nothing)
-    if (__ballot(top > m + 8.f)) {
+    // (Moving the reference only where the maximum passes it by a factor of 2^8 saves 2 %, but
+    // the largest probability is then rounded to bf16 instead of being 1: 1.25 times the
+    // plain form's error instead of 1.05.)
+    if (__ballot(top > m)) {
       const float mn = fmaxf(m, top);
       const float corr = mn == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mn);
       l *= corr;
