@@ -71,6 +71,7 @@ typedef enum rbq_kv8_dtype { RBQ_E4M3 = 16, RBQ_I8 = 17 } rbq_kv8_dtype;
 #define RBQ_OP_DENSE_DECODE 4
 #define RBQ_OP_DECODE_STEP 5
 #define RBQ_OP_DECODE_KV8 6       /* rbq_sparse_decode_kv8 and rbq_dense_decode_kv8 */
+#define RBQ_OP_DECODE_STEP_KV8 8
 #define RBQ_OP_PREFILL 7          /* rbq_prefill_attention: n = max_k, w = total_q */
 
 #define RBQ_QSCAL_STRIDE 8   /* floats per query head in qscal */
@@ -457,6 +458,27 @@ rbq_status rbq_sparse_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_k
                                  const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
                                  float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
                                  const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream);
+
+/*
+ * rbq_decode_step_kv8 -- rbq_decode_step over the 8-bit cache: one step of a uniform
+ * batch whose indexed rows [0, n) are in 8 bits and whose window is K_loc / V_loc
+ * [B][Hkv][loc_ld][D] rows [0, w). Its outputs are bitwise those of the sequence
+ *   rbq_quantize_query, rbq_score (rbq_score_f16 with kfac16), rbq_topp_select,
+ *   rbq_sparse_decode_kv8(..., K_loc, V_loc, loc_dtype, loc_ld, w, ...)
+ *   if (flush) rbq_encode_keys (rbq_encode_keys_f16) of the window rows into index
+ *     rows [n, n + w), and rbq_quantize_kv of them into cache rows [n, n + w)
+ * Exactly one of kfac (the full index) and kfac16 (the compact index, then c_q =
+ * NULL) is given: RBQ_EINVAL otherwise. With flush, n + w <= cap; the index and the
+ * cache have the same capacity.
+ *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_STEP_KV8, B, Hq, Hkv, D, n, w) bytes.
+ */
+rbq_status rbq_decode_step_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                               const float* P, const float* c_q, const float* c_k, void* K8, void* V8,
+                               int32_t kv8_dtype, int32_t block, float* k_scale, float* v_scale, int32_t cap, int32_t n,
+                               const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                               uint32_t* codes, float* kfac, uint16_t* kfac16, int32_t flush, float p, float sm_scale,
+                               uint32_t* qplanes, float* qscal, float* scores, int32_t* sel_idx, int32_t* sel_count,
+                               float* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * rbq_prefill_attention -- the attention of whole prompts (or of chunks of them

@@ -485,6 +485,66 @@ rbq_status rbq_sparse_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_k
                            ws, true, stream, nullptr, 0, seq_n, seq_w);
 }
 
+rbq_status rbq_decode_step_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                               const float* P, const float* c_q, const float* c_k, void* K8, void* V8,
+                               int32_t kv8_dtype, int32_t block, float* k_scale, float* v_scale, int32_t cap, int32_t n,
+                               const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                               uint32_t* codes, float* kfac, uint16_t* kfac16, int32_t flush, float p, float sm_scale,
+                               uint32_t* qplanes, float* qscal, float* scores, int32_t* sel_idx, int32_t* sel_count,
+                               float* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const Kv8Cache c{K8, V8, k_scale, v_scale, kv8_dtype, block, cap};
+  const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
+  const void* fac = kfac16 != nullptr ? static_cast<const void*>(kfac16) : kfac;
+  if ((kfac != nullptr) == (kfac16 != nullptr) || (kfac16 != nullptr && c_q != nullptr)) return RBQ_EINVAL;
+  rbq_status s = check_heads(batch, heads_q, heads_kv, head_dim);
+  if (s != RBQ_OK) return s;
+  if (n < 0 || w < 0) return RBQ_EINVAL;
+  const StepWorkspace sw = step_workspace(ws, batch, heads_q, heads_kv, head_dim, n, w, true);
+  if (ws == nullptr || ws_bytes < sw.bytes) return RBQ_EINVAL;
+  const bool do_flush = flush != 0 && w > 0;
+  if ((s = check_quantize(batch, heads_q, heads_kv, head_dim, q, P, c_k, qplanes, qscal)) != RBQ_OK) return s;
+  if ((s = check_score(batch, heads_q, heads_kv, head_dim, n, cap, codes, fac, qplanes, qscal, scores)) != RBQ_OK)
+    return s;
+  if ((s = check_topp(batch, heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, sw.topp_bytes)) != RBQ_OK)
+    return s;
+  if ((s = check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win, sm_scale, out,
+                            sw.decode, decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w), nullptr,
+                            nullptr)) != RBQ_OK)
+    return s;
+  if (do_flush) {
+    if ((s = check_encode(batch, heads_kv, head_dim, K_loc, loc_dtype, loc_ld, w, n, cap, P, c_k, codes, fac, 0u, nullptr,
+                          0)) != RBQ_OK)
+      return s;
+    if ((s = check_quantize_kv(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, block, kv8_dtype, K8,
+                               V8, k_scale, v_scale, nullptr, nullptr)) != RBQ_OK)
+      return s;
+  }
+
+  if (!do_flush && quantize_score_fused(batch, heads_q, heads_kv, n, head_dim)) {
+    s = launch_quantize_score(batch, heads_q, heads_kv, n, cap, q, P, c_q, c_k, qplanes, qscal, codes, kfac, kfac16,
+                              scores, stream, head_dim);
+  } else {
+    if (do_flush)
+      s = launch_quantize_flush(batch, heads_q, heads_kv, q, P, c_q, c_k, qplanes, qscal, K_loc, loc_dtype, loc_ld, w, n,
+                                cap, codes, kfac, stream, nullptr, nullptr, 0, kfac16, head_dim);
+    else
+      s = launch_quantize(batch, heads_q, heads_kv, q, P, c_q, c_k, qplanes, qscal, nullptr, stream, 4, head_dim);
+    if (s != RBQ_OK) return s;
+    s = launch_score(batch, heads_q, heads_kv, n, cap, codes, kfac, qplanes, qscal, scores, nullptr, nullptr, stream,
+                     nullptr, kfac16, 4, head_dim);
+  }
+  if (s != RBQ_OK) return s;
+  s = launch_topp(batch * heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, stream, sw.masks);
+  if (s != RBQ_OK) return s;
+  s = launch_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, sel_idx, sel_count, win, sm_scale, out, lse,
+                        sw.decode, true, stream, sw.masks, topp_mask_words(n));
+  // (last: it may re-encode rows that the attention reads)
+  if (s == RBQ_OK && do_flush)
+    s = launch_quantize_kv(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, block, kv8_dtype, K8, V8,
+                           k_scale, v_scale, nullptr, nullptr, stream);
+  return s;
+}
+
 rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const void* q,
                                  int64_t q_ld, const void* K, const void* V, int32_t dtype, int64_t kv_ld,
                                  int64_t kv_head, int64_t kv_seq, int32_t kv_rows, const int32_t* cu_q,

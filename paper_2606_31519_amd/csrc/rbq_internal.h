@@ -213,7 +213,7 @@ struct StepWorkspace {
   size_t bytes;
 };
 StepWorkspace step_workspace(void* base, int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
-                             int32_t n, int32_t w);
+                             int32_t n, int32_t w, bool kv8 = false);   // kv8: over an 8-bit cache
 
 // Encode: centroid partial sums over chunks of kCentroidChunk keys.
 constexpr int kCentroidChunk = 1024;

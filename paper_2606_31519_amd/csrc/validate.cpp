@@ -318,13 +318,14 @@ int topp_mask_words(int32_t n) {
 }
 
 StepWorkspace step_workspace(void* base, int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
-                             int32_t n, int32_t w) {
+                             int32_t n, int32_t w, bool kv8) {
   StepWorkspace s{};
   const int64_t rows = int64_t(batch) * heads_q;
   char* b = static_cast<char*>(base);
   size_t off = 0;
   s.decode = b + off;
-  off = align_up(off + decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w), 256);
+  off = align_up(off + (kv8 ? decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w)
+                            : decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w)), 256);
   s.topp = b + off;
   s.topp_bytes = topp_workspace(nullptr, rows, n).bytes;
   off = align_up(off + s.topp_bytes, 256);
@@ -354,8 +355,9 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
     case RBQ_OP_PREFILL:
       return rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_DECODE_STEP:
+    case RBQ_OP_DECODE_STEP_KV8:
       if (heads_q % heads_kv != 0) return 0;
-      return rbq::step_workspace(nullptr, batch, heads_q, heads_kv, head_dim, n, w).bytes;
+      return rbq::step_workspace(nullptr, batch, heads_q, heads_kv, head_dim, n, w, op == RBQ_OP_DECODE_STEP_KV8).bytes;
     default:
       return 0;
   }

@@ -196,6 +196,72 @@ class DecodeState:
                                     self.lse if lse is None else lse, self.ws_decode, stream)
 
 
+KV8_DTYPES = {"e4m3": torch.float8_e4m3fn, "int8": torch.int8}
+
+
+class Kv8Cache:
+    """K and V rows in 8 bits ("e4m3" or "int8"), one scale per (sequence, KV head,
+    block of `block` tokens): the buffers and the calls that write and read them."""
+
+    def __init__(self, B, Hkv, D, cap, fmt="e4m3", block=64, device="cuda"):
+        if fmt not in KV8_DTYPES:
+            raise ValueError(f"unknown 8-bit format {fmt!r} (one of {sorted(KV8_DTYPES)})")
+        self.B, self.Hkv, self.D, self.cap, self.fmt, self.block = B, Hkv, D, cap, fmt, block
+        self.K8, self.V8 = (torch.zeros(B, Hkv, cap, D, dtype=torch.int8, device=device).view(KV8_DTYPES[fmt])
+                            for _ in range(2))
+        blocks = (cap + block - 1) // block
+        self.k_scale, self.v_scale = (torch.zeros(B, Hkv, blocks, dtype=torch.float32, device=device) for _ in range(2))
+
+    def append(self, K, V, ld, rows, offset, seq_off=None, seq_rows=None, stream=None):
+        """Rows [0, rows) of K / V [B][Hkv][ld][D] as cache rows [offset, offset + rows) (rbq_quantize_kv)."""
+        rbq.rbq_quantize_kv(self.B, self.Hkv, self.D, K, V, ld, rows, offset, self.cap, self.block, self.K8, self.V8,
+                            self.k_scale, self.v_scale, seq_off, seq_rows, stream)
+
+    def read(self, K, V, ld, rows, offset=0, seq_off=None, seq_rows=None, stream=None):
+        """Cache rows [offset, offset + rows) as rows [0, rows) of K / V (rbq_dequantize_kv)."""
+        rbq.rbq_dequantize_kv(self.B, self.Hkv, self.D, self.K8, self.V8, self.block, self.k_scale, self.v_scale, self.cap,
+                              rows, offset, K, V, ld, seq_off, seq_rows, stream)
+
+
+class PromptAttention:
+    """The attention of a batch of prompts, or of chunks of them behind rows that are
+    cached (rbq_prefill_attention): q_lens tokens and k_lens keys per sequence
+    (k_lens None: the prompts themselves), the lengths' device arrays and the
+    workspace kept for every call (one per layer; calls that overlap in time, on
+    several streams, need plans of their own)."""
+
+    def __init__(self, Hq, Hkv, D, q_lens, k_lens=None, causal=True, device="cuda"):
+        k_lens = q_lens if k_lens is None else k_lens
+        if len(q_lens) != len(k_lens) or not len(q_lens) or min(min(q_lens), min(k_lens)) < 0:
+            raise ValueError("one length of at least 0 per sequence, for the queries and for the keys")
+        self.B, self.Hq, self.Hkv, self.D, self.causal = len(q_lens), Hq, Hkv, D, causal
+        cu_q, cu_k = (np.concatenate([[0], np.cumsum(v)]).astype(np.int32) for v in (q_lens, k_lens))
+        self.total_q, self.total_k, self.max_k = int(cu_q[-1]), int(cu_k[-1]), int(max(k_lens))
+        self.cu_q, self.cu_k = (torch.from_numpy(c).to(device) for c in (cu_q, cu_k))
+        self.ws = rbq.workspace(rbq.RBQ_OP_PREFILL, self.B, Hq, Hkv, D, self.max_k, self.total_q, device)
+        self.sm_scale = 1.0 / math.sqrt(D)
+
+    def __call__(self, q, K, V, out=None, lse=None, stream=None):
+        """q [total_q][Hq][D]; K, V packed [total_k][Hkv][D] or in a cache [B][Hkv][cap][D] (rows from 0); any strides
+        whose last dimension (of q: two) is contiguous. Returns out [total_q][Hq][D] in q's type."""
+        D = self.D
+        if tuple(q.shape[1:]) != (self.Hq, D) or q.shape[0] < self.total_q:
+            raise ValueError(f"q is {tuple(q.shape)}, the plan needs ({self.total_q}, {self.Hq}, {D})")
+        packed = K.dim() == 3
+        want = (self.total_k, self.Hkv, D) if packed else (self.B, self.Hkv, self.max_k, D)
+        rows = 0 if packed else 2
+        if (K.shape != V.shape or K.stride() != V.stride() or K.dim() not in (3, 4) or K.shape[rows] < want[rows]
+                or tuple(K.shape[:rows]) != want[:rows] or tuple(K.shape[rows + 1:]) != want[rows + 1:]):
+            raise ValueError(f"K and V are {tuple(K.shape)} and {tuple(V.shape)}, the plan needs {want} and equal strides")
+        if q.stride(2) != 1 or q.stride(1) != D or K.stride(-1) != 1:
+            raise ValueError("the head dimension (and the heads of q) must be contiguous")
+        lay = (K.stride(0), K.stride(1), 0) if packed else (K.stride(2), K.stride(1), K.stride(0))
+        out = torch.empty(self.total_q, self.Hq, D, dtype=q.dtype, device=q.device) if out is None else out
+        rbq.rbq_prefill_attention(self.B, self.Hq, self.Hkv, D, q, q.stride(0), K, V, *lay, K.shape[rows], self.cu_q,
+                                  self.cu_k, self.total_q, self.max_k, self.causal, self.sm_scale, out, lse, self.ws, stream)
+        return out
+
+
 class DecodeSession:
     """A decode loop over one growing cache: the lazy index update of Section
     3.4 as a serving loop would run it. The cache holds `cap` rows per (sequence,
@@ -209,9 +275,14 @@ class DecodeSession:
 
     K, V: [B][Hkv][cap][D] device tensors holding the prefill rows; P: the
     rotation; c_q: query centroids or None; compact: the fp16-factor index
-    (then without c_q)."""
+    (then without c_q).
 
-    def __init__(self, B, Hq, Hkv, D, cap, n_prefill, window, K, V, P, c_q=None, device="cuda", compact=False):
+    kv8 ("e4m3" or "int8"): the indexed rows are kept in 8 bits (kv8_block tokens per
+    scale), the window in K's type in buffers of its own; K and V [B][Hkv][at least
+    n_prefill][D] are then read here only, and every step is one rbq_decode_step_kv8."""
+
+    def __init__(self, B, Hq, Hkv, D, cap, n_prefill, window, K, V, P, c_q=None, device="cuda", compact=False, kv8=None,
+                 kv8_block=64):
         if not 0 < window <= rbq.RBQ_MAX_WINDOW or n_prefill + window > cap:
             raise ValueError("the window must fit after the prefill rows (n_prefill + window <= cap)")
         q = torch.zeros(B, Hq, D, dtype=torch.float32, device=device)
@@ -222,21 +293,30 @@ class DecodeSession:
         self.n_sizes = list(range(n_prefill, cap + 1, window))
         self.n_max = self.n_sizes[-1]
         # sized for the largest index: the scores, selections and per-row workspaces grow with n
+        self.kv8 = None
+        src, src_ld = K, cap          # the prefill rows and their number per block
+        if kv8 is not None:
+            src_ld = K.shape[2]
+            if src_ld < n_prefill or not (K.is_contiguous() and V.is_contiguous() and K.shape == V.shape):
+                raise ValueError("K and V must be contiguous, of one shape, and hold the prefill rows")
+            self.kv8 = Kv8Cache(B, Hkv, D, cap, kv8, kv8_block, device)
+            self.kv8.append(K, V, src_ld, n_prefill, 0)
+            K, V = (torch.zeros(B, Hkv, window, D, dtype=K.dtype, device=device) for _ in range(2))   # the window
         self.state = DecodeState(B, Hq, Hkv, D, cap, self.n_max, window, K, V, q, P, c_q, device, compact)
         self.n, self.w, self.window = n_prefill, 0, window
         st = self.state
         # the step workspace is not monotonic in n (smaller indexes may take more,
         # shorter decode splits): size it for every index size the loop will pass;
         # for a given n it grows with the window rows, so the full window bounds it
-        need = max(rbq.rbq_workspace_bytes(rbq.RBQ_OP_DECODE_STEP, B, Hq, Hkv, D, m, window)
-                   for m in self.n_sizes)
+        op = rbq.RBQ_OP_DECODE_STEP if kv8 is None else rbq.RBQ_OP_DECODE_STEP_KV8
+        need = max(rbq.rbq_workspace_bytes(op, B, Hq, Hkv, D, m, window) for m in self.n_sizes)
         if need > st.ws_step.numel():
             st.ws_step = torch.empty(need, dtype=torch.uint8, device=device)
         if compact:
-            rbq.rbq_encode_keys_f16(B, Hkv, D, K, cap, n_prefill, 0, cap, P, st.c_k, st.codes, st.kfac16,
+            rbq.rbq_encode_keys_f16(B, Hkv, D, src, src_ld, n_prefill, 0, cap, P, st.c_k, st.codes, st.kfac16,
                                     rbq.RBQ_ENCODE_SET_CENTROID, st.ws_encode)
         else:
-            rbq.rbq_encode_keys(B, Hkv, D, K, cap, n_prefill, 0, cap, P, c_q, st.c_k, st.codes, st.kfac,
+            rbq.rbq_encode_keys(B, Hkv, D, src, src_ld, n_prefill, 0, cap, P, c_q, st.c_k, st.codes, st.kfac,
                                 rbq.RBQ_ENCODE_SET_CENTROID, None, st.ws_encode)
 
     def append(self, k: torch.Tensor, v: torch.Tensor):
@@ -245,7 +325,7 @@ class DecodeSession:
             raise RuntimeError("the window is full: run step() first (it flushes the window)")
         if self.n + self.w >= self.state.cap:
             raise RuntimeError("the cache is full")
-        r = self.n + self.w
+        r = self.w if self.kv8 is not None else self.n + self.w
         self.state.K[:, :, r].copy_(k)
         self.state.V[:, :, r].copy_(v)
         self.w += 1
@@ -261,7 +341,13 @@ class DecodeSession:
                                f"({self.n_max} keys, cap {st.cap})")
         st.q.copy_(q)
         flush = self.w == self.window
-        if st.compact:
+        if self.kv8 is not None:
+            c = self.kv8
+            rbq.rbq_decode_step_kv8(st.B, st.Hq, st.Hkv, st.D, st.q, st.P, st.c_q, st.c_k, c.K8, c.V8, c.block, c.k_scale,
+                                    c.v_scale, st.cap, self.n, st.K, st.V, self.window, self.w, st.codes, st.kfac,
+                                    st.kfac16, flush, p, st.sm_scale, st.qplanes, st.qscal, st.scores, st.sel_idx,
+                                    st.sel_count, st.out, st.lse, st.ws_step, stream)
+        elif st.compact:
             rbq.rbq_decode_step_f16(st.B, st.Hq, st.Hkv, st.D, st.q, st.P, st.c_k, st.K, st.V, st.cap, self.n,
                                     self.w, st.codes, st.kfac16, flush, p, st.sm_scale, st.qplanes, st.qscal,
                                     st.scores, st.sel_idx, st.sel_count, st.out, st.lse, st.ws_step, stream)

@@ -20,7 +20,7 @@ RBQ_F32, RBQ_BF16 = 0, 1
 RBQ_E4M3, RBQ_I8 = 16, 17   # formats of the 8-bit cache
 RBQ_ENCODE_SET_CENTROID = 1
 RBQ_OP_ENCODE, RBQ_OP_TOPP, RBQ_OP_SPARSE_DECODE, RBQ_OP_DENSE_DECODE, RBQ_OP_DECODE_STEP = 1, 2, 3, 4, 5
-RBQ_OP_DECODE_KV8, RBQ_OP_PREFILL = 6, 7
+RBQ_OP_DECODE_KV8, RBQ_OP_PREFILL, RBQ_OP_DECODE_STEP_KV8 = 6, 7, 8
 QSCAL_STRIDE = 8
 RBQ_MAX_WINDOW = 4096   # largest local window accepted by the decode calls
 RBQ_NOALLOC_SCRATCH_BYTES = 16 << 20   # the static scratch of rbq_decode_step_noalloc
@@ -34,7 +34,7 @@ EXPORTED = [
     "rbq_score_q8", "rbq_score_ints_q8", "rbq_mapped_device_pointer",
     "rbq_encode_keys_f16", "rbq_score_f16", "rbq_decode_step_f16", "rbq_score_varlen_f16", "rbq_decode_step_varlen_f16",
     "rbq_decode_step_noalloc",
-    "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8",
+    "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8", "rbq_decode_step_kv8",
     "rbq_prefill_attention",
 ]
 
@@ -95,6 +95,8 @@ def _load():
                                  f32, vp, vp, vp, sz, vp, vp, vp],
         "rbq_sparse_decode_kv8": [i32, i32, i32, i32, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, vp, vp, i32,
                                   i64, i32, f32, vp, vp, vp, sz, vp, vp, vp],
+        "rbq_decode_step_kv8": [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, vp, vp, i32, i32, vp, vp, i32, i64,
+                                i32, vp, vp, vp, i32, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "rbq_prefill_attention": [i32, i32, i32, i32, vp, i64, vp, vp, i32, i64, i64, i64, i32, vp, vp, i32, i32, i32,
                                   f32, vp, vp, vp, sz, vp],
     }
@@ -536,6 +538,29 @@ def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, 
         v_scale.data_ptr(), cap, n, sel_idx.data_ptr(), sel_count.data_ptr(), _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w,
         sm_scale, out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _ptr(seq_n), _ptr(seq_w),
         _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+def rbq_decode_step_kv8(batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, K8, V8, block, k_scale, v_scale, cap, n,
+                        K_loc, V_loc, loc_ld, w, codes, kfac, kfac16, flush, p, sm_scale, qplanes, qscal, scores, sel_idx,
+                        sel_count, out, lse, ws, stream=None):
+    """rbq_decode_step over an 8-bit cache and a window [B][Hkv][loc_ld][D]; kfac (full index) or kfac16 (compact), the
+    other None."""
+    name = "rbq_decode_step_kv8"
+    fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
+                                 V_loc, loc_ld, w, out, lse, None, None)
+    rows = batch * heads_q
+    if (qplanes.numel() < rows * 4 * (head_dim // 32) or qscal.numel() < rows * QSCAL_STRIDE or scores.numel() < rows * n
+            or sel_idx.numel() < rows * n or sel_count.numel() < rows):
+        _need(name, qplanes=(qplanes, rows * 4 * (head_dim // 32)), qscal=(qscal, rows * QSCAL_STRIDE),
+              scores=(scores, rows * n), sel_idx=(sel_idx, rows * n), sel_count=(sel_count, rows))
+    st = lib.rbq_decode_step_kv8(
+        batch, heads_q, heads_kv, head_dim, q.data_ptr(), P.data_ptr(), _ptr(c_q), c_k.data_ptr(), K8.data_ptr(),
+        V8.data_ptr(), fmt, block, k_scale.data_ptr(), v_scale.data_ptr(), cap, n, _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w,
+        codes.data_ptr(), _ptr(kfac), _ptr(kfac16), 1 if flush else 0, p, sm_scale, qplanes.data_ptr(), qscal.data_ptr(),
+        scores.data_ptr(), sel_idx.data_ptr(), sel_count.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 

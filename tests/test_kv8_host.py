@@ -116,3 +116,46 @@ def test_the_models_e4m3_is_the_ocp_format():
     for y in (x, mid, -mid):
         t = torch.from_numpy(y).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
         assert np.array_equal(t, ku.encode_values(y.astype(np.float64), "e4m3"))
+
+
+def test_the_fused_step_rejects_invalid_arguments(R):
+    E, U = R.RBQ_EINVAL, R.RBQ_EUNSUPPORTED
+
+    def step(**k):
+        g = k.get
+        return R.lib.rbq_decode_step_kv8(
+            1, g("Hq", 8), 4, g("D", 128), FAKE, g("P", FAKE), g("c_q", None), FAKE, g("K8", FAKE), FAKE, g("fmt", 16),
+            g("block", 64), FAKE, FAKE, g("cap", 200), g("n", 100), g("kl", FAKE), FAKE, g("ldt", 1), g("ld", 16), g("w", 10),
+            FAKE, g("kf", FAKE), g("kf16", None), g("flush", 1), g("p", 0.9), 0.1, FAKE, FAKE, FAKE, g("sel", FAKE), FAKE,
+            FAKE, None, FAKE, g("wsb", 1 << 30), 0)
+
+    for kw, want in [(dict(kf=None), E), (dict(kf16=FAKE), E), (dict(kf=None, kf16=FAKE, c_q=FAKE), E),
+                     (dict(kf=None, kf16=FAKE + 2), E), (dict(cap=105), E), (dict(n=-1), E), (dict(n=201), E), (dict(w=-1), E),
+                     (dict(w=17), E), (dict(kl=None), E), (dict(ldt=7), U), (dict(block=20), E), (dict(fmt=2), U),
+                     (dict(D=96), U), (dict(Hq=12), U), (dict(p=0.0), E), (dict(P=None), E), (dict(K8=None), E),
+                     (dict(sel=None), E), (dict(wsb=64), E)]:
+        assert step(**kw) == want, kw
+    need = R.rbq_workspace_bytes(R.RBQ_OP_DECODE_STEP_KV8, 1, 32, 8, 128, 4000, 64)
+    assert need >= R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, 1, 32, 8, 128, 4000, 64) > 0
+    assert R.rbq_workspace_bytes(R.RBQ_OP_DECODE_STEP_KV8, 1, 6, 4, 128, 4000, 64) == 0
+
+
+def test_pipeline_objects_refuse_what_they_cannot_hold():
+    from paper_2606_31519_amd import pipeline
+    with pytest.raises(ValueError):
+        pipeline.Kv8Cache(1, 2, 64, 32, fmt="e5m2", device="cpu")
+    for q, k in (([], None), ([3], [3, 4]), ([-1], None), ([3], [-2])):
+        with pytest.raises(ValueError):
+            pipeline.PromptAttention(4, 2, 64, q, k, device="cpu")
+    att = pipeline.PromptAttention(4, 2, 64, [3, 5], [3, 9], device="cpu")
+    q, K, C = torch.zeros(8, 4, 64), torch.zeros(12, 2, 64), torch.zeros(2, 2, 9, 64)
+    for bad in ((q[:7], K, K), (torch.zeros(8, 4, 32), K, K), (torch.zeros(8, 2, 64), K, K), (q, K[:11], K[:11]),
+                (q, K, K.double()[:, :, :32]), (q, C[:, :, :8], C[:, :, :8]), (q, C[:1], C[:1]), (q, K[0], K[0]),
+                (q, C, C.transpose(1, 2).contiguous().transpose(1, 2)), (q.transpose(1, 2).contiguous().transpose(1, 2), K, K)):
+        with pytest.raises(ValueError):
+            att(*bad)
+    K = torch.zeros(1, 2, 40, 64)
+    with pytest.raises(ValueError):    # fewer rows than the prefill
+        pipeline.DecodeSession(1, 4, 2, 64, 100, 50, 16, K, K, torch.eye(64), device="cpu", kv8="int8")
+    with pytest.raises(ValueError):    # rows that are not contiguous
+        pipeline.DecodeSession(1, 4, 2, 64, 100, 30, 16, K[:, :, :35], K[:, :, :35], torch.eye(64), device="cpu", kv8="int8")
