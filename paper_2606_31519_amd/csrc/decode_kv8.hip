@@ -84,12 +84,16 @@ __device__ __forceinline__ bf16x8 k_operand(const uint32_t* k, int kb, int part)
   if constexpr (SRC == RBQ_BF16) {
     return __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
   } else if constexpr (SRC == RBQ_F32) {
-    f32x8 v;
+    f32x8 r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
-    bf16x8 p[kQParts];
-    split3(v, p);
-    return p[part];
+    for (int i = 0; i < 8; ++i) r[i] = __uint_as_float(w[i]);
+    bf16x8 p = __builtin_convertvector(r, bf16x8);
+#pragma unroll
+    for (int t = 0; t < part; ++t) {
+      r -= __builtin_convertvector(p, f32x8);
+      p = __builtin_convertvector(r, bf16x8);
+    }
+    return p;
   } else {
     return __builtin_bit_cast(bf16x8, u32x4{codes_bf16<SRC, false>(w[0]), codes_bf16<SRC, true>(w[0]),
                                             codes_bf16<SRC, false>(w[1]), codes_bf16<SRC, true>(w[1])});

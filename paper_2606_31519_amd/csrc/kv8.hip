@@ -5,10 +5,13 @@
 //         within 448; x / s is then exact and the code is its one rounding
 //   int8: s = amax / 127, code = x (1/s) rounded once to a whole number
 //
-// A token block of one tensor is held in registers by a wave (up to 64 tokens) or
+// A token block of one tensor is held in registers by a wave (up to 4096 values) or
 // by four: its new rows are read once, their largest magnitude is reduced, and the
 // codes leave from the same registers, so the bytes are those of the rows and the
-// codes. A block that holds earlier rows keeps them: where the new rows need a
+// codes, which bound it: K and V of 130816 tokens x 8 heads x 128 in bf16, 805 MB,
+// 131 us (6.1 TB/s; a plain copy on this GPU 6.2), and the same back 137. (With loads
+// that the caches keep 162; 8 codes per lane and store 159; a wave for 8192 values 134.)
+// A block that holds earlier rows keeps them: where the new rows need a
 // larger scale, the held codes are read, multiplied by the ratio of the scales and
 // written back (a rounding of at most half a step of the new scale).
 #include "rbq_device.h"
@@ -77,23 +80,19 @@ __device__ __forceinline__ void decode4(uint32_t w, float* x) {
   }
 }
 
-// 8 values of a row of DT at `p`
+// 16 values of a row of DT at `p`. (Read once: streamed past the caches.)
 template <int DT>
-__device__ __forceinline__ void load8(const char* p, u32x4* raw) {
-  raw[0] = reinterpret_cast<const u32x4*>(p)[0];
-  if constexpr (DT == RBQ_F32) raw[1] = reinterpret_cast<const u32x4*>(p)[1];
+__device__ __forceinline__ void load16(const char* p, u32x4* raw) {
+#pragma unroll
+  for (int i = 0; i < (DT == RBQ_BF16 ? 2 : 4); ++i)
+    raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
 }
 template <int DT>
-__device__ __forceinline__ void widen8(const u32x4* raw, float* x) {
-  if constexpr (DT == RBQ_BF16) {
+__device__ __forceinline__ void widen16(const u32x4* raw, float* x) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = bf16_lo(raw[0][i]);
-      x[2 * i + 1] = bf16_hi(raw[0][i]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = __uint_as_float(raw[i / 4][i % 4]);
+  for (int i = 0; i < 16; ++i) {
+    if constexpr (DT == RBQ_BF16) x[i] = i % 2 ? bf16_hi(raw[i / 8][i % 8 / 2]) : bf16_lo(raw[i / 8][i % 8 / 2]);
+    else x[i] = __uint_as_float(raw[i / 4][i % 4]);
   }
 }
 
@@ -106,13 +105,14 @@ __device__ __forceinline__ Span span_of(int b, int offset, int rows, const int32
 }
 
 // Grid (token blocks of a sequence / units per workgroup, (b, kv head), K or V).
-// T threads take a token block of D-dimension rows: CH pieces of 8 dimensions each.
+// T threads take a token block of D-dimension rows: CH pieces of 16 dimensions each, so
+// that codes leave 16 bytes per lane.
 template <int DT, int FMT, int T, int CH>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kv_kernel(
     const char* __restrict__ K, const char* __restrict__ V, int64_t ld, int n_new, int offset, int cap, int bshift,
     int dshift, uint32_t* __restrict__ K8, uint32_t* __restrict__ V8, float* __restrict__ k_scale,
     float* __restrict__ v_scale, int Hkv, const int32_t* __restrict__ seq_off, const int32_t* __restrict__ seq_new) {
-  constexpr int kEl = DT == RBQ_BF16 ? 2 : 4, kRaw = DT == RBQ_BF16 ? 1 : 2;
+  constexpr int kEl = DT == RBQ_BF16 ? 2 : 4, kRaw = DT == RBQ_BF16 ? 2 : 4;
   constexpr int kUnits = kQuantThreads / T;
   __shared__ uint32_t red[kQuantThreads / kWave];
   const int bh = blockIdx.y, b = bh / Hkv;
@@ -128,22 +128,22 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kv_kernel(
   float* scale = (blockIdx.z ? v_scale : k_scale) + sidx;
   const float old = row0 < sp.off ? *scale : 0.f;   // rows that the block holds already
 
-  const int cshift = dshift - 3;   // pieces of a row
+  const int cshift = dshift - 4;   // pieces of a row
   u32x4 raw[CH][kRaw];
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int e = c * T + t, row = row0 + (e >> cshift), dim = (e & ((1 << cshift) - 1)) * 8;
-    raw[c][0] = u32x4{0u, 0u, 0u, 0u};
-    if constexpr (kRaw == 2) raw[c][1] = raw[c][0];
-    if (row >= sp.off && row < end) load8<DT>(src + ((int64_t(row - sp.off) << dshift) + dim) * kEl, raw[c]);
+    const int e = c * T + t, row = row0 + (e >> cshift), dim = (e & ((1 << cshift) - 1)) * 16;
+#pragma unroll
+    for (int i = 0; i < kRaw; ++i) raw[c][i] = u32x4{0u, 0u, 0u, 0u};
+    if (row >= sp.off && row < end) load16<DT>(src + ((int64_t(row - sp.off) << dshift) + dim) * kEl, raw[c]);
   }
   uint32_t amax = 0u;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    float x[8];
-    widen8<DT>(raw[c], x);
+    float x[16];
+    widen16<DT>(raw[c], x);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) amax = max(amax, finite_bits(x[i]));
+    for (int i = 0; i < 16; ++i) amax = max(amax, finite_bits(x[i]));
   }
   amax = wave_max_u32(amax);
   if constexpr (T > kWave) {
@@ -158,18 +158,22 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kv_kernel(
   const float ratio = grows ? old / s : 1.f;
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
-    const int e = c * T + t, row = row0 + (e >> cshift), dim = (e & ((1 << cshift) - 1)) * 8;
-    u32x2* out = reinterpret_cast<u32x2*>(dst + ((int64_t(row) << (dshift - 2)) + dim / 4));
+    const int e = c * T + t, row = row0 + (e >> cshift), dim = (e & ((1 << cshift) - 1)) * 16;
+    u32x4* out = reinterpret_cast<u32x4*>(dst + ((int64_t(row) << (dshift - 2)) + dim / 4));
     if (row >= sp.off && row < end) {
-      float x[8];
-      widen8<DT>(raw[c], x);
-      *out = u32x2{encode4<FMT>(x, r), encode4<FMT>(x + 4, r)};
+      float x[16];
+      widen16<DT>(raw[c], x);
+      *out = u32x4{encode4<FMT>(x, r), encode4<FMT>(x + 4, r), encode4<FMT>(x + 8, r), encode4<FMT>(x + 12, r)};
     } else if (grows && row < sp.off) {
-      const u32x2 was = *out;
-      float x[8];
-      decode4<FMT>(was.x, x);
-      decode4<FMT>(was.y, x + 4);
-      *out = u32x2{encode4<FMT>(x, ratio), encode4<FMT>(x + 4, ratio)};
+      const u32x4 was = *out;
+      u32x4 now;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x[4];
+        decode4<FMT>(was[i], x);
+        now[i] = encode4<FMT>(x, ratio);
+      }
+      *out = now;
     }
   }
   if (t == 0) *scale = s;
@@ -222,13 +226,13 @@ void launch_quantize_form(int pieces, dim3 grid, hipStream_t stream, const char*
 #define RBQ_QUANT_FORM(T, CH)                                                                                     \
   quantize_kv_kernel<DT, FMT, T, CH><<<grid, kQuantThreads, 0, stream>>>(K, V, ld, n_new, offset, cap, bshift, dshift, \
                                                                          K8, V8, ks, vs, Hkv, seq_off, seq_new)
-  switch (pieces) {   // of 8 values in a token block: 64 threads up to 64 tokens, 256 above
+  switch (pieces) {   // of 16 values in a token block: 64 threads up to 256, 256 above
+    case 64: RBQ_QUANT_FORM(64, 1); break;
     case 128: RBQ_QUANT_FORM(64, 2); break;
     case 256: RBQ_QUANT_FORM(64, 4); break;
-    case 512: RBQ_QUANT_FORM(64, 8); break;
-    case 1024: RBQ_QUANT_FORM(64, 16); break;
-    case 2048: RBQ_QUANT_FORM(256, 8); break;
-    default: RBQ_QUANT_FORM(256, 16); break;
+    case 512: RBQ_QUANT_FORM(256, 2); break;
+    case 1024: RBQ_QUANT_FORM(256, 4); break;
+    default: RBQ_QUANT_FORM(256, 8); break;
   }
 #undef RBQ_QUANT_FORM
 }
@@ -239,8 +243,8 @@ rbq_status launch_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim,
                               int32_t kv8_dtype, void* K8, void* V8, float* k_scale, float* v_scale,
                               const int32_t* seq_off, const int32_t* seq_new, hipStream_t stream) {
   if (n_new == 0) return RBQ_OK;
-  const int bshift = log2i(block), dshift = log2i(head_dim), pieces = block * head_dim / 8;
-  const int units = pieces <= 1024 ? kQuantThreads / kWave : 1;
+  const int bshift = log2i(block), dshift = log2i(head_dim), pieces = block * head_dim / 16;
+  const int units = pieces <= 256 ? kQuantThreads / kWave : 1;
   // token blocks a sequence's rows can touch (ragged: from any place in the first)
   const int64_t first = seq_off ? 0 : offset >> bshift;
   const int64_t blocks =
