@@ -162,14 +162,14 @@ struct Rows {
   using Regs = RowRegs<SRC, D>;
   S& sh;
   const __amdgpu_buffer_rsrc_t Kr, Vr;
-  const int c0, U, bshift, wave, x, j, ngroups;
+  const int c0, U, bshift, in_block, wave, x, j, ngroups;   // in_block: place of row c0 in its token block
   Regs cur;
   uint32_t mk;                // bit 4 t + i: row 4j + i of tile t is valid and taken by head x
   f32x2 sc[LIST ? NT : 1][4];   // its scales {ks, vs} (listed 8-bit rows)
 
   __device__ __forceinline__ Rows(S& s, __amdgpu_buffer_rsrc_t kr, __amdgpu_buffer_rsrc_t vr, int first, int rows, int shift)
-      : sh(s), Kr(kr), Vr(vr), c0(first), U(rows), bshift(shift), wave(threadIdx.x / kWave), x(lane_id() & 15),
-        j(lane_id() >> 4), ngroups((rows + kRows - 1) / kRows) {}
+      : sh(s), Kr(kr), Vr(vr), c0(first), U(rows), bshift(shift), in_block(first & ((1 << shift) - 1)),
+        wave(threadIdx.x / kWave), x(lane_id() & 15), j(lane_id() >> 4), ngroups((rows + kRows - 1) / kRows) {}
 
   __device__ __forceinline__ int row_of(int grp, int e) const { return c0 + (e < U ? e : grp * kRows); }
   __device__ __forceinline__ void load_k(int grp, bool skip) {
@@ -206,7 +206,7 @@ struct Rows {
       for (int i = 0; i < 4; ++i) {
         const int off = skip ? kSkipOffset : row[i] * (D * EB) + (D * EB / 16) * x;
         load_words<Regs::kVw, CP>(cur.v[t][i], Vr, off);
-        if constexpr (LIST && kCodes) sc[t][i] = sh.scale[(row[i] - c0) >> bshift];
+        if constexpr (LIST && kCodes) sc[t][i] = sh.scale[(in_block + row[i] - c0) >> bshift];
       }
     }
   }
@@ -232,7 +232,7 @@ struct Rows {
       f32x2 ts[NT];   // scales of rows that follow each other: 16 from a multiple of 16 are in one token block
       if constexpr (kCodes && !LIST) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) ts[t] = sh.scale[(grp * kRows + 16 * t < U ? grp * kRows + 16 * t : 0) >> bshift];
+        for (int t = 0; t < NT; ++t) ts[t] = sh.scale[(in_block + (grp * kRows + 16 * t < U ? grp * kRows + 16 * t : 0)) >> bshift];
       }
       f32x4 s[NT];
 #pragma unroll
@@ -471,7 +471,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
 #pragma unroll
   for (int c = 0; c < D / 16; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
   // the split's scales
-  const bool scales = !window && int(threadIdx.x) <= (c1 - 1 - c0) >> bshift;
+  const bool scales = !window && int(threadIdx.x) <= ((c1 - 1) >> bshift) - (c0 >> bshift);
   f32x2 own_scale = {0.f, 0.f};
   if (scales) {
     const int64_t s0 = int64_t(bh) * ((int64_t(cap) + (1 << bshift) - 1) >> bshift) + (c0 >> bshift) + threadIdx.x;

@@ -256,8 +256,10 @@ PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
   const int64_t rows = int64_t(total_q) * (heads_q / heads_kv);
   PrefillPlan p;
   p.rows = 128;
-  p.tiles = int32_t(rows / p.rows + batch);
-  const int64_t blocks = (rows + p.rows - 1) / p.rows * heads_kv;
+  // every sequence with tokens may end in a tile of its own
+  const int64_t ends = std::min<int64_t>(batch, total_q);
+  p.tiles = int32_t(rows / p.rows + ends);
+  const int64_t blocks = std::max<int64_t>((rows + p.rows - 1) / p.rows, ends) * heads_kv;
   const int64_t aim = dtype == RBQ_F32 ? kPrefillAimF32 : kPrefillAim;
   int64_t want = blocks < kCus ? (aim + blocks - 1) / blocks : 1;
   want = std::min<int64_t>(want, (int64_t(max_k) + kPrefillMinKeys - 1) / kPrefillMinKeys);
@@ -295,7 +297,8 @@ rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
   if (a.total_q == 0) return RBQ_OK;
   // the rows of a sequence (tokens times heads of a group) and the grid are 32-bit numbers
   const int64_t rows = int64_t(a.total_q) * (heads_q / heads_kv);
-  if (rows >= kMaxRows - 256 || (rows / 128 + batch) * heads_kv >= (int64_t(1) << 24)) return RBQ_EUNSUPPORTED;
+  if (rows >= kMaxRows - 256 || (rows / 128 + std::min<int64_t>(batch, a.total_q)) * heads_kv >= (int64_t(1) << 24))
+    return RBQ_EUNSUPPORTED;
   if (bad_ptr(a.q) || bad_ptr(a.out) || bad_ptr(a.cu_q) || bad_ptr(a.cu_k)) return RBQ_EINVAL;
   if (a.kv_rows > 0 && a.max_k > 0 && (bad_ptr(a.K) || bad_ptr(a.V))) return RBQ_EINVAL;
   const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, a.max_k, a.total_q, a.dtype);

@@ -257,6 +257,8 @@ class PromptAttention:
             raise ValueError("the head dimension (and the heads of q) must be contiguous")
         lay = (K.stride(0), K.stride(1), 0) if packed else (K.stride(2), K.stride(1), K.stride(0))
         out = torch.empty(self.total_q, self.Hq, D, dtype=q.dtype, device=q.device) if out is None else out
+        if not out.is_contiguous() or (lse is not None and not lse.is_contiguous()):
+            raise ValueError("out and lse must be contiguous")
         rbq.rbq_prefill_attention(self.B, self.Hq, self.Hkv, D, q, q.stride(0), K, V, *lay, K.shape[rows], self.cu_q,
                                   self.cu_k, self.total_q, self.max_k, self.causal, self.sm_scale, out, lse, self.ws, stream)
         return out
@@ -301,7 +303,8 @@ class DecodeSession:
                 raise ValueError("K and V must be contiguous, of one shape, and hold the prefill rows")
             self.kv8 = Kv8Cache(B, Hkv, D, cap, kv8, kv8_block, device)
             self.kv8.append(K, V, src_ld, n_prefill, 0)
-            K, V = (torch.zeros(B, Hkv, window, D, dtype=K.dtype, device=device) for _ in range(2))   # the window
+            self.K_win, self.V_win = (torch.zeros(B, Hkv, window, D, dtype=K.dtype, device=device) for _ in range(2))
+            K = V = None              # (the state's calls over a full-precision cache have none to read)
         self.state = DecodeState(B, Hq, Hkv, D, cap, self.n_max, window, K, V, q, P, c_q, device, compact)
         self.n, self.w, self.window = n_prefill, 0, window
         st = self.state
@@ -325,9 +328,13 @@ class DecodeSession:
             raise RuntimeError("the window is full: run step() first (it flushes the window)")
         if self.n + self.w >= self.state.cap:
             raise RuntimeError("the cache is full")
-        r = self.w if self.kv8 is not None else self.n + self.w
-        self.state.K[:, :, r].copy_(k)
-        self.state.V[:, :, r].copy_(v)
+        if self.kv8 is not None:
+            self.K_win[:, :, self.w].copy_(k)
+            self.V_win[:, :, self.w].copy_(v)
+        else:
+            r = self.n + self.w
+            self.state.K[:, :, r].copy_(k)
+            self.state.V[:, :, r].copy_(v)
         self.w += 1
 
     def step(self, q: torch.Tensor, p: float, stream=None) -> bool:
@@ -344,7 +351,7 @@ class DecodeSession:
         if self.kv8 is not None:
             c = self.kv8
             rbq.rbq_decode_step_kv8(st.B, st.Hq, st.Hkv, st.D, st.q, st.P, st.c_q, st.c_k, c.K8, c.V8, c.block, c.k_scale,
-                                    c.v_scale, st.cap, self.n, st.K, st.V, self.window, self.w, st.codes, st.kfac,
+                                    c.v_scale, st.cap, self.n, self.K_win, self.V_win, self.window, self.w, st.codes, st.kfac,
                                     st.kfac16, flush, p, st.sm_scale, st.qplanes, st.qscal, st.scores, st.sel_idx,
                                     st.sel_count, st.out, st.lse, st.ws_step, stream)
         elif st.compact:

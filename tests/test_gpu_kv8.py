@@ -301,3 +301,25 @@ def test_append_and_attend_in_a_graph_and_on_two_streams(R):
     token(b)
     torch.cuda.synchronize()
     assert torch.equal(a[2], b[2]) and torch.equal(a[0][0], b[0][0])
+
+
+@pytest.mark.parametrize("block", [16, 128, 256])
+def test_long_splits_whose_ends_lie_inside_token_blocks(R, block):
+    """Many (sequence, KV head) groups of many rows: the dense call's splits are sized to the GPU and need not end on a
+    block of tokens. Checked by every row's own scale: K = 0 gives the mean of V."""
+    B, H, D, n = 8, 8, 64, 16500
+    cap = n + 12
+    print("long splits", block, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(block)
+    K8 = torch.zeros(B, H, cap, D, dtype=torch.int8, device="cuda")
+    V8 = torch.randint(-127, 128, (B, H, cap, D), dtype=torch.int8, device="cuda", generator=g)
+    s = torch.rand(B, H, (cap + block - 1) // block, device="cuda", generator=g) ** 4
+    q = torch.randn(B, H, D, device="cuda", generator=g)
+    out, lse = torch.empty(B, H, D, device="cuda"), torch.empty(B, H, device="cuda")
+    ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, H, H, D, n, 0)
+    R.rbq_dense_decode_kv8(B, H, H, D, q, K8, V8, block, s, s, cap, n, None, None, 0, 0, 0.125, out, lse, ws)
+    val = V8[:, :, :n].double() * s.repeat_interleave(block, dim=2)[:, :, :n, None].double()
+    # (n roundings of one addition and one product each, at most, of the mean magnitude)
+    tol = (2 * n + 64) * ku.EPS * val.abs().mean(dim=2)
+    assert torch.all((out.double() - val.mean(dim=2)).abs() <= tol)
+    assert torch.all((lse.double() - math.log(n)).abs() <= (n + 64) * ku.EPS)

@@ -59,3 +59,11 @@ def test_binding_refuses_short_or_mixed_buffers(R):
     half = x.half()
     with pytest.raises(ValueError):
         R.rbq_prefill_attention(*args(q=half, K=half, out=half)[:7], half, *args(out=half)[8:])
+
+
+def test_many_empty_sequences_do_not_split_the_keys_or_fill_the_grid(R):
+    """One token in each of many sequences has a tile of its own: no keys are split for them; sequences without tokens
+    count for nothing."""
+    assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 1000, 4, 1, 128, 5000, 1000) == 0
+    assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 65535, 4, 1, 128, 5000, 3) == \
+        R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 3, 4, 1, 128, 5000, 3) > 0
