@@ -105,7 +105,8 @@ template <int SRC, int VW>
 __device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int part) {
   if constexpr (SRC == RBQ_BF16) {
     const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-    return u32x2{__builtin_amdgcn_perm(v[1][c / 2], v[0][c / 2], sel), __builtin_amdgcn_perm(v[3][c / 2], v[2][c / 2], sel)};
+    return u32x2{__builtin_amdgcn_perm(v[1][c / 2], v[0][c / 2], sel),
+                 __builtin_amdgcn_perm(v[3][c / 2], v[2][c / 2], sel)};
   } else if constexpr (SRC == RBQ_F32) {
     f32x4 r = {__uint_as_float(v[0][c]), __uint_as_float(v[1][c]), __uint_as_float(v[2][c]), __uint_as_float(v[3][c])};
     typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -118,7 +119,8 @@ __device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int pa
     return __builtin_bit_cast(u32x2, p);
   } else if constexpr (SRC == RBQ_E4M3) {
     const uint32_t sel = (c % 4) < 2 ? 0x05010400u : 0x07030602u;   // {r0.c, r1.c, r0.c+1, r1.c+1} of an even c
-    const uint32_t a = __builtin_amdgcn_perm(v[1][c / 4], v[0][c / 4], sel), b = __builtin_amdgcn_perm(v[3][c / 4], v[2][c / 4], sel);
+    const uint32_t a = __builtin_amdgcn_perm(v[1][c / 4], v[0][c / 4], sel);
+    const uint32_t b = __builtin_amdgcn_perm(v[3][c / 4], v[2][c / 4], sel);
     return c % 2 ? u32x2{codes_bf16<SRC, true>(a), codes_bf16<SRC, true>(b)}
                  : u32x2{codes_bf16<SRC, false>(a), codes_bf16<SRC, false>(b)};
   } else {
@@ -232,7 +234,10 @@ struct Rows {
       f32x2 ts[NT];   // scales of rows that follow each other: 16 from a multiple of 16 are in one token block
       if constexpr (kCodes && !LIST) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) ts[t] = sh.scale[(in_block + (grp * kRows + 16 * t < U ? grp * kRows + 16 * t : 0)) >> bshift];
+        for (int t = 0; t < NT; ++t) {
+          const int e = grp * kRows + 16 * t;
+          ts[t] = sh.scale[(in_block + (e < U ? e : 0)) >> bshift];
+        }
       }
       f32x4 s[NT];
 #pragma unroll
@@ -524,7 +529,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
   lsum += __shfl_xor(lsum, 16, kWave);
   lsum += __shfl_xor(lsum, 32, kWave);
   if (j == 0 && x < G) {
-    sh.sm[wave][x] = m;
+    sh.sm[wave][x] = lsum == lsum ? m : lsum;   // (a NaN among the logits goes through the joins as the maximum)
     sh.sl[wave][x] = lsum;
   }
 #pragma unroll
@@ -545,19 +550,17 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     for (int v = 0; v < kDWaves; ++v) M = fmaxf(M, sh.sm[v][g]);
     f32x4 r = {0.f, 0.f, 0.f, 0.f};
     float l = 0.f;
-    if (M != -INFINITY) {
 #pragma unroll
-      for (int v = 0; v < kDWaves; ++v) {
-        if (sh.sm[v][g] != -INFINITY) {
-          const float sc = __builtin_amdgcn_exp2f(sh.sm[v][g] - M);
-          const f32x4 a = *reinterpret_cast<const f32x4*>(&sh.sacc[v][g][4 * d4]);
-          r = f32x4{fmaf(a.x, sc, r.x), fmaf(a.y, sc, r.y), fmaf(a.z, sc, r.z), fmaf(a.w, sc, r.w)};
-          l = fmaf(sh.sl[v][g], sc, l);
-        }
+    for (int v = 0; v < kDWaves; ++v) {
+      if (sh.sm[v][g] != -INFINITY) {
+        const float sc = __builtin_amdgcn_exp2f(sh.sm[v][g] - M);
+        const f32x4 a = *reinterpret_cast<const f32x4*>(&sh.sacc[v][g][4 * d4]);
+        r = f32x4{fmaf(a.x, sc, r.x), fmaf(a.y, sc, r.y), fmaf(a.z, sc, r.z), fmaf(a.w, sc, r.w)};
+        l = fmaf(sh.sl[v][g], sc, l);
       }
     }
     f32x2* o = reinterpret_cast<f32x2*>(part + (int64_t(row0 + g) * total_splits + split) * (D + 2));
-    if (d4 == 0) o[0] = f32x2{M, l};
+    if (d4 == 0) o[0] = f32x2{l == l ? M : l, l};
     o[1 + 2 * d4] = f32x2{r.x, r.y};
     o[2 + 2 * d4] = f32x2{r.z, r.w};
   }

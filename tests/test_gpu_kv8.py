@@ -323,3 +323,32 @@ def test_long_splits_whose_ends_lie_inside_token_blocks(R, block):
     tol = (2 * n + 64) * ku.EPS * val.abs().mean(dim=2)
     assert torch.all((out.double() - val.mean(dim=2)).abs() <= tol)
     assert torch.all((lse.double() - math.log(n)).abs() <= (n + 64) * ku.EPS)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,ldt", [(8, 2, 128, "bf16"), (16, 2, 64, "f32"), (2, 2, 128, "f32")])
+def test_a_nan_in_a_query_or_the_window_gives_nan(R, Hq, Hkv, D, ldt):
+    """One head's query, and one row of one KV head's window: their heads' results are NaN, the others' keep every bit."""
+    B, block, n, w, G, tau = 2, 64, 700, 40, Hq // Hkv, 0.1
+    rng = np.random.default_rng(31)
+    c8 = cache_of(rng.integers(0, 255, (B, Hkv, n, D)).astype(np.uint8), "int8")
+    s = dev(rng.uniform(0.01, 0.02, (B, Hkv, (n + block - 1) // block)).astype(np.float32))
+    q = dev(rng.standard_normal((B, Hq, D)).astype(np.float32))
+    K, V = (dev(rng.standard_normal((B, Hkv, w, D)), DT[ldt]) for _ in range(2))
+    sel = torch.arange(n, dtype=torch.int32, device="cuda").expand(B, Hq, n).contiguous()
+    cnt = torch.full((B, Hq), 300, dtype=torch.int32, device="cuda")
+    ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+
+    def run(sparse):
+        out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+        head, loc = (B, Hq, Hkv, D, q, c8, c8, block, s, s, n, n), (K, V, w, w, tau, out, lse, ws)
+        R.rbq_sparse_decode_kv8(*head, sel, cnt, *loc) if sparse else R.rbq_dense_decode_kv8(*head, *loc)
+        torch.cuda.synchronize()
+        return out, lse
+
+    clean = [run(False), run(True)]
+    q[0, 0, 5] = float("nan")
+    K[1, Hkv - 1, 7, 1] = float("nan")
+    for (out, lse), (o, l) in zip([run(False), run(True)], clean):
+        o[0, 0], l[0, 0], o[1, Hq - G:], l[1, Hq - G:] = (float("nan"),) * 4
+        assert ((out == o) | (torch.isnan(out) & torch.isnan(o))).all()
+        assert ((lse == l) | (torch.isnan(lse) & torch.isnan(l))).all()

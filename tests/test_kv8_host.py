@@ -159,3 +159,9 @@ def test_pipeline_objects_refuse_what_they_cannot_hold():
         pipeline.DecodeSession(1, 4, 2, 64, 100, 50, 16, K, K, torch.eye(64), device="cpu", kv8="int8")
     with pytest.raises(ValueError):    # rows that are not contiguous
         pipeline.DecodeSession(1, 4, 2, 64, 100, 30, 16, K[:, :, :35], K[:, :, :35], torch.eye(64), device="cpu", kv8="int8")
+
+
+@pytest.mark.parametrize("sparse", [False, True])
+def test_a_ragged_batch_of_too_many_blocks_is_refused(R, sparse):
+    kw = dict(B=16383, Hq=4, Hkv=4, D=64, n=(1 << 25) - 1, cap=(1 << 25) - 1, wsb=(1 << 63) - 1)
+    assert _decode(R, sparse, sn=FAKE, **kw) == R.RBQ_EUNSUPPORTED
