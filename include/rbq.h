@@ -443,6 +443,8 @@ rbq_status rbq_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, 
  *     cached rows and window rows, clamped to [0, n] and [0, w] (its window
  *     starts at row 0 of its block of K_loc / V_loc). A selection holds rows
  *     below seq_n[b] only.
+ *   A NaN in a query or an attended window row gives NaN.
+ *   RBQ_EUNSUPPORTED for a ragged batch also beyond 2^24 blocks (split, sequence, KV head).
  *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w) bytes.
  */
 rbq_status rbq_dense_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
@@ -506,9 +508,9 @@ rbq_status rbq_decode_step_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv,
  *   ws:  at least rbq_workspace_bytes(RBQ_OP_PREFILL, B, Hq, Hkv, D, max_k, total_q)
  *        bytes, 0 (then NULL is allowed) unless few rows attend to long keys.
  * Products and sums in fp32; with RBQ_BF16 the probabilities are rounded to bf16
- * before they meet V. A NaN or infinity in a row of V may also reach tokens up to 63
- * places before the first one that sees it. Device counts are not checked on the
- * host: lengths outside the buffers are clamped to them. Any group size up to 16.
+ * before they meet V. A NaN or infinity in a key, value or query reaches the tokens
+ * that see it and no other. Device counts are not checked on the host: lengths
+ * outside the buffers are clamped to them. Any group size up to 16.
  * RBQ_EUNSUPPORTED also beyond 2^24 tiles of 128 (token, head of the group) rows.
  */
 rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,

@@ -59,9 +59,9 @@ __device__ __forceinline__ Lengths lengths_of(int b, int G, int BM, int total_q,
 // them, they leave whole shader engines idle, which take blocks in turn: 512 blocks of
 // 256 fp32 keys with 512 empty ones between them 84 us, in this order 52.)
 // More sequences than lanes: in the sequences' order, backwards, every split of a tile.
-__device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int kchunk, int batch, int G, int BM, int total_q, int max_k, int kv_rows,
-                                            bool packed, bool causal, const int32_t* __restrict__ cu_q,
-                                            const int32_t* __restrict__ cu_k) {
+__device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int kchunk, int batch, int G, int BM,
+                                            int total_q, int max_k, int kv_rows, bool packed, bool causal,
+                                            const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k) {
   const int lane = lane_id();
   TileId t{-1, 0, 0, 0, 0, 0, 0};
   auto found = [&](const Lengths& s, int b0, int l, int tile) {
@@ -161,7 +161,7 @@ __device__ __forceinline__ void store_row(const f32x16 (&o)[D / 32][NQ], int i, 
                                           void* __restrict__ out, float* __restrict__ lse, float* __restrict__ part,
                                           int split, int splits, int none) {
   float* pr = part + (row * splits + split) * (D + 2);
-  const float scale = part ? 1.f : sum > 0.f ? 1.f / sum : 0.f;
+  const float scale = part ? 1.f : sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
 #pragma unroll
@@ -182,11 +182,11 @@ __device__ __forceinline__ void store_row(const f32x16 (&o)[D / 32][NQ], int i, 
     }
   if (h != 0) return;
   if (part) {
-    *reinterpret_cast<f32x2*>(pr) = f32x2{sum > 0.f ? m : -INFINITY, sum};
+    *reinterpret_cast<f32x2*>(pr) = f32x2{sum == 0.f ? -INFINITY : sum == sum ? m : sum, sum};   // (a NaN is kept)
     // split 0 also writes the states of the splits from `none` on, which no block takes
     for (int k = none; split == 0 && k < splits; ++k) pr[int64_t(k) * (D + 2)] = -INFINITY;
   } else if (lse)
-    lse[row] = sum > 0.f ? (m + log2f(sum)) * kLn2 : -INFINITY;
+    lse[row] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
 }
 
 // bf16 rows. A wave holds 32 query rows as the columns of its products, so that a row's
@@ -209,9 +209,11 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     const uint16_t* __restrict__ q, int64_t q_ld, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     int64_t kv_ld, int64_t kv_head, int64_t kv_seq, int kv_rows, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ cu_k, int batch, int total_q, int max_k, int causal, float scale_log2e,
-    uint16_t* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv, int tiles, int splits, int kchunk) {
-  constexpr int BM = 32 * kPWaves, C = D / 8, KB = D / 16, DT = D / 32, RB = D * 2;   // chunks, k-blocks, dim tiles, row bytes
+    uint16_t* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv, int tiles, int splits,
+    int kchunk) {
+  constexpr int BM = 32 * kPWaves, C = D / 8, KB = D / 16, DT = D / 32, RB = D * 2;   // chunks, k-blocks, dim tiles, bytes of a row
   __shared__ __attribute__((aligned(1024))) char ldsK[2][kPKeys * RB], ldsV[2][kPKeys * RB];
+  __shared__ int odd;   // values were replaced (below)
   const int G = Hq / Hkv;
   const int hk = blockIdx.x % Hkv;
   const TileId t = find_tile(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
@@ -326,6 +328,30 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
         o[d][0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, p[g], o[d][0], 0, 0, 0);
       }
   };
+  // A masked probability of 0 would carry an infinity or NaN of V to rows that do not see its
+  // key: in tiles that some row sees in part they are replaced by 0 and noted; at the end each
+  // row adds those of the keys that it sees (from kodd on).
+  const int bmin = visible(row0 / G);
+  const int kodd = bmin > kbeg ? kbeg + (bmin - kbeg) / kPKeys * kPKeys : kbeg;
+  auto finite_tile = [&](char* tile) {   // the pieces that this lane has staged, before they are published
+#pragma unroll
+    for (int i = 0; i < kIssues; ++i) {
+      u32x4* at = reinterpret_cast<u32x4*>(tile + (wave * kIssues + i) * 1024 + lane * 16);
+      u32x4 w = *at;
+      uint32_t f = 0u;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f |= (w[e] & 0x7F807F80u) + 0x00800080u;   // an exponent of ones carries
+      if (f & 0x80008000u) {
+        odd = 1;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if ((w[e] & 0x7F80u) == 0x7F80u) w[e] &= 0xFFFF0000u;
+          if ((w[e] & 0x7F800000u) == 0x7F800000u) w[e] &= 0xFFFFu;
+        }
+        *at = w;
+      }
+    }
+  };
 
   // Tile i of V holds the keys of step i, kbeg + 64 i .. +64; tile i of K those whose logits
   // step i forms, 32 further on (the first 32 keys' come before the loop). Logits of keys
@@ -335,6 +361,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     stage(Kb, ldsK[1], kbeg, false);
     stage(Vb, ldsV[0], kbeg, true);
     if (kbeg + 32 < kstop) stage(Kb, ldsK[0], kbeg + 32, false);
+    if (threadIdx.x == 0) odd = 0;
     wait_lds();
     __syncthreads();
     logits(sa, ldsK[1]);
@@ -343,6 +370,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   int buf = 0;
   for (int k0 = kbeg; k0 < kstop; k0 += kPKeys, buf ^= 1) {
     wait_lds();
+    if (k0 >= kodd) finite_tile(ldsV[buf]);
     __syncthreads();
     if (k0 + kPKeys < kstop) stage(Vb, ldsV[buf ^ 1], k0 + kPKeys, true);
     if (k0 + kPKeys + 32 < kstop) stage(Kb, ldsK[buf ^ 1], k0 + kPKeys + 32, false);
@@ -350,9 +378,24 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     if (k0 + 32 < wstop) step(sb, sa, k0 + 32, &ldsK[buf][32 * RB], &ldsV[buf][32 * RB]);
   }
 
+  if (kbeg < kstop && odd) {
+#pragma unroll 1
+    for (int key = kodd; key < min(lim, kstop); ++key) {
+#pragma unroll
+      for (int c = 0; c < 4 * DT; ++c) {   // the lane's dimensions 8 c + 4 h .. +4
+        const u32x2 w = *reinterpret_cast<const u32x2*>(Vb + key * kv_ld + 8 * c + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const float v = __uint_as_float((w[e / 2] >> (16 * (e % 2))) << 16);
+          o[c / 4][0][4 * (c % 4) + e] += fabsf(v) < INFINITY ? 0.f : v;
+        }
+      }
+    }
+  }
   const float sum = l + __shfl_xor(l, 32, kWave);
-  if (wrow + x < rows) store_row<D, RBQ_BF16>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part, t.split, splits,
-                      batch <= kWave ? (kend + kchunk - 1) / kchunk + (kend == 0) : splits);
+  if (wrow + x < rows)
+    store_row<D, RBQ_BF16>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part, t.split, splits,
+                           batch <= kWave ? (kend + kchunk - 1) / kchunk + (kend == 0) : splits);
 }
 
 // fp32 rows: the same on v_mfma_f32_32x32x2_f32, products and probabilities in fp32.
@@ -407,8 +450,22 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][0][r] = 0.f;
   float m = -INFINITY, l = 0.f;
+  // (infinities and NaN of V as in the bf16 kernel)
+  const int bmin = visible(row0 / G);
+  const int kodd = bmin > kbeg ? kbeg + (bmin - kbeg) / kFKeys * kFKeys : kbeg;
+  bool odd = false;
   if (kbeg < kstop) fetch(kbeg);
   for (int k0 = kbeg; k0 < kstop; k0 += kFKeys) {
+    if (k0 >= kodd) {
+#pragma unroll
+      for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const bool f = fabsf(vreg[i][c]) < INFINITY;
+          odd |= !f;
+          vreg[i][c] = f ? vreg[i][c] : 0.f;
+        }
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
@@ -482,6 +539,17 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
           o[d][0] = __builtin_amdgcn_mfma_f32_32x32x2f32(va[g & 1][i][d], s[4 * g + i], o[d][0], 0, 0, 0);
     }
   }
+  if (__syncthreads_or(odd)) {
+#pragma unroll 1
+    for (int key = kodd; key < min(lim, kstop); ++key) {
+#pragma unroll
+      for (int c = 0; c < 4 * DT; ++c) {
+        const f32x4 v = *reinterpret_cast<const f32x4*>(V + kvoff + key * kv_ld + 8 * c + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[c / 4][0][4 * (c % 4) + e] += fabsf(v[e]) < INFINITY ? 0.f : v[e];
+      }
+    }
+  }
   const float sum = l + __shfl_xor(l, 32, kWave);
   if (wrow + x < rows)
     store_row<D, RBQ_F32>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part, t.split, splits,
@@ -503,7 +571,7 @@ __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float*
   const float ms = lane < splits ? ml.x : -INFINITY;
   const float M = wave_max(ms);
   const float c = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
-  const float l = wave_reduce(c > 0.f ? ml.y * c : 0.f, [](float a, float b) { return a + b; });
+  const float l = wave_reduce(c == 0.f ? 0.f : ml.y * c, [](float a, float b) { return a + b; });
   float acc[E] = {};
   for (int s0 = 0; s0 < splits; s0 += kBatch) {
     float v[kBatch][E];
@@ -514,13 +582,13 @@ __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float*
 #pragma unroll
     for (int k = 0; k < kBatch; ++k) {
       const float ck = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(c)), min(s0 + k, kWave - 1))));
-      if (s0 + k < splits && ck > 0.f) {   // (a split without keys has written nothing else)
+      if (s0 + k < splits && ck != 0.f) {   // (a split without keys has written nothing else)
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = fmaf(v[k][e], ck, acc[e]);
       }
     }
   }
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
     const int64_t at = row * D + E * lane + e;
@@ -529,7 +597,7 @@ __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float*
     else
       static_cast<float*>(out)[at] = acc[e] * inv;
   }
-  if (lse && lane == 0) lse[row] = l > 0.f ? (M + log2f(l)) * kLn2 : -INFINITY;
+  if (lse && lane == 0) lse[row] = l == 0.f ? -INFINITY : (M + log2f(l)) * kLn2;
 }
 }  // namespace
 

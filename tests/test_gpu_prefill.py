@@ -217,3 +217,62 @@ def test_graph_replays_and_two_streams(R, qs, ks):
     b = inp.run(R, True)
     torch.cuda.synchronize()
     assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,qs,ks,layout", [
+    ("bf16", 8, 2, 128, [300, 70], [300, 133], "packed"),
+    ("bf16", 4, 4, 64, [150, 200], [150, 200], "cache"),
+    ("bf16", 8, 1, 128, [40, 3], [3000, 2100], "packed"),      # keys split over blocks
+    ("f32", 8, 2, 64, [90, 140], [120, 140], "packed"),
+    ("f32", 4, 1, 128, [30, 7], [2001, 50], "cache"),
+], ids=["bf16-D128", "bf16-D64", "bf16-split", "f32-D64", "f32-D128-split"])
+def test_infinities_and_nan_reach_the_tokens_that_see_them_only(R, dt, Hq, Hkv, D, qs, ks, layout):
+    """An infinity in one dimension of a value, a NaN in another value, a key of NaN, one after the other, and a query of
+    NaN: tokens that see none of them, and dimensions that hold none, keep their results to the bit."""
+    print("nan", dt, Hq, Hkv, D, qs, ks, layout, flush=True)
+    inp = Inputs(23, dt, Hq, Hkv, D, qs, ks, layout)
+    G = Hq // Hkv
+    clean, clean_lse = (t.clone() for t in inp.run(R, True))
+    marks = {}                       # sequence -> first tokens that see: the infinity, the NaN of a value, the key
+    at = lambda t, b, j: t[b, -1, j] if layout == "cache" else t[inp.cu_k[b] + j, -1]  # noqa: E731  (the last KV head)
+    for b in range(2):
+        steps = sorted({qs[b] // 3, qs[b] // 2, qs[b] - 2})
+        inf_t, nan_t, key_t = steps if len(steps) == 3 else (steps[0], steps[0], steps[-1])
+        shift = ks[b] - qs[b]
+        at(inp.V, b, inf_t + shift)[5] = -float("inf")
+        at(inp.V, b, nan_t + shift)[D - 3] = float("nan")
+        at(inp.K, b, key_t + shift)[7] = float("nan")
+        marks[b] = inf_t, nan_t, key_t
+    inp.q[inp.cu_q[0] + 1, 0, 3] = float("nan")
+    out, lse = inp.run(R, True)
+    torch.cuda.synchronize()
+    assert torch.isnan(out[1, 0]).all() and torch.isnan(lse[1, 0])
+    clean[1, 0], clean_lse[1, 0] = out[1, 0], lse[1, 0]
+    if Hkv > 1:                       # the other KV heads' groups
+        assert torch.equal(torch.nan_to_num(out[:, :-G]), torch.nan_to_num(clean[:, :-G]))
+        assert torch.equal(torch.nan_to_num(lse[:, :-G]), torch.nan_to_num(clean_lse[:, :-G]))
+    for b, (inf_t, nan_t, key_t) in marks.items():
+        o, c = out[inp.cu_q[b]:inp.cu_q[b + 1], -G:], clean[inp.cu_q[b]:inp.cu_q[b + 1], -G:].clone()
+        l, cl = lse[inp.cu_q[b]:inp.cu_q[b + 1], -G:], clean_lse[inp.cu_q[b]:inp.cu_q[b + 1], -G:].clone()
+        c[inf_t:, :, 5] = -float("inf")
+        c[nan_t:, :, D - 3] = float("nan")
+        c[key_t:] = float("nan")
+        cl[key_t:] = float("nan")
+        if b == 0 and Hkv == 1:
+            c[1, 0], cl[1, 0] = float("nan"), float("nan")
+        same = (o == c) | (torch.isnan(o) & torch.isnan(c))
+        assert same.all(), (b, (~same).nonzero()[:4])
+        assert ((l == cl) | (torch.isnan(l) & torch.isnan(cl))).all()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_an_infinity_in_the_last_value_of_a_full_mask(R, dt):
+    """Not causal, lengths that end inside a tile: every token gets the infinity, in its dimension alone."""
+    inp = Inputs(24, dt, 4, 2, 64, [33, 5], [77, 33], "packed")
+    want = inp.run(R, False)[0].clone()
+    for b in range(2):
+        inp.V[inp.cu_k[b + 1] - 1, :, 9] = float("inf")
+    want[..., 9] = float("inf")
+    got = inp.run(R, False)[0]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
