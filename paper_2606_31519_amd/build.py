@@ -9,11 +9,13 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "librbq.so")
+CALL_PATH = os.path.join(HERE, "_rbqcall.so")   # the Python binding's own (csrc/pycall.cpp)
 
 HIP_SOURCES = ["api.hip", "score.hip", "quantize.hip", "encode.hip", "topp.hip", "decode.hip", "kv8.hip",
                "decode_kv8.hip", "prefill.hip"]
@@ -53,7 +55,7 @@ def _run(cmd, verbose):
 
 
 def build(verbose: bool = False) -> str:
-    """Compile every source and link librbq.so; returns the library path."""
+    """Compile every source and link librbq.so and the binding's call module; returns the library path."""
     os.makedirs(BUILD_DIR, exist_ok=True)
     hipcc = _hipcc()
     jobs = []
@@ -69,6 +71,10 @@ def build(verbose: bool = False) -> str:
     tmp = LIB_PATH + ".tmp"
     _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB_PATH)
+    tmp = CALL_PATH + ".tmp"
+    _run(["g++", *CXX_FLAGS, "-shared", "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "pycall.cpp"), "-o",
+          tmp], verbose)
+    os.replace(tmp, CALL_PATH)
     _write_build_info()
     return LIB_PATH
 

@@ -1,0 +1,129 @@
+// The binding's calls of the C ABI for work that takes the GPU a few microseconds,
+// as CPython functions: arguments are read where they lie on the interpreter's stack,
+// without ctypes' conversion objects (an rbq_quantize_kv call with its checks: 4.3 us
+// of the host through ctypes, 2.5 here; its kernel for one token takes 3). The
+// entry points are those that the ctypes library has loaded: bind() takes their addresses.
+//
+// An argument of a pointer type is None, an address, or an object with data_ptr().
+#define PY_SSIZE_T_CLEAN
+#include <Python.h>
+
+#include <tuple>
+#include <utility>
+
+#include "../../include/rbq.h"
+
+namespace {
+
+PyObject *str_data_ptr, *str_numel;
+
+bool take(PyObject* o, int64_t& v) {
+  v = PyLong_AsLong(o);
+  return v != -1 || !PyErr_Occurred();
+}
+bool take(PyObject* o, int32_t& v) {
+  int64_t x;
+  if (!take(o, x)) return false;
+  v = int32_t(x);
+  if (v == x) return true;
+  PyErr_Format(PyExc_OverflowError, "%lld does not fit into 32 bits", (long long)x);
+  return false;
+}
+bool take(PyObject* o, size_t& v) {
+  v = PyLong_AsSize_t(o);
+  return v != size_t(-1) || !PyErr_Occurred();
+}
+bool take(PyObject* o, float& v) {
+  const double x = PyFloat_AsDouble(o);
+  v = float(x);
+  return x != -1.0 || !PyErr_Occurred();
+}
+template <class T>
+bool take(PyObject* o, T*& v) {
+  if (o == Py_None) {
+    v = nullptr;
+    return true;
+  }
+  if (PyLong_Check(o)) {
+    v = static_cast<T*>(PyLong_AsVoidPtr(o));
+  } else {
+    PyObject* p = PyObject_CallMethodNoArgs(o, str_data_ptr);
+    if (p == nullptr) return false;
+    v = static_cast<T*>(PyLong_AsVoidPtr(p));
+    Py_DECREF(p);
+  }
+  return v != nullptr || !PyErr_Occurred();
+}
+
+enum { kQuantize, kDequantize, kDense, kSparse, kStep, kPrefill, kEntries };
+void* entry[kEntries];
+
+template <class F>
+struct Entry;
+template <class... A>
+struct Entry<rbq_status (*)(A...)> {
+  template <int E, size_t... I>
+  static PyObject* call(PyObject* const* args, std::index_sequence<I...>) {
+    std::tuple<A...> v;
+    if (!(take(args[I], std::get<I>(v)) && ...)) return nullptr;
+    const auto fn = reinterpret_cast<rbq_status (*)(A...)>(entry[E]);
+    rbq_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = fn(std::get<I>(v)...);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+  }
+  template <int E>
+  static PyObject* run(PyObject*, PyObject* const* args, Py_ssize_t n) {
+    if (n != Py_ssize_t(sizeof...(A)) || entry[E] == nullptr)
+      return PyErr_Format(PyExc_TypeError, "%zd arguments, the call takes %zu", n, sizeof...(A));
+    return call<E>(args, std::index_sequence_for<A...>{});
+  }
+};
+
+// fits(buffer, elements, buffer, elements, ...): whether every buffer that knows its
+// number of elements holds as many as the call needs (None and addresses know nothing)
+PyObject* fits(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n % 2 != 0) return PyErr_Format(PyExc_TypeError, "pairs of a buffer and its elements");
+  for (Py_ssize_t i = 0; i < n; i += 2) {
+    int64_t need, have;
+    if (!take(args[i + 1], need)) return nullptr;
+    if (args[i] == Py_None || PyLong_Check(args[i])) continue;
+    PyObject* r = PyObject_CallMethodNoArgs(args[i], str_numel);
+    if (r == nullptr) return nullptr;
+    const bool ok = take(r, have);
+    Py_DECREF(r);
+    if (!ok) return nullptr;
+    if (have < need) Py_RETURN_FALSE;
+  }
+  Py_RETURN_TRUE;
+}
+
+PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
+  if (n != kEntries) return PyErr_Format(PyExc_TypeError, "%d addresses", int(kEntries));
+  for (int e = 0; e < kEntries; ++e)
+    if (!take(args[e], entry[e])) return nullptr;
+  Py_RETURN_NONE;
+}
+
+#define RBQ_ENTRY(NAME, E) \
+  {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&Entry<decltype(&NAME)>::run<E>)), METH_FASTCALL, nullptr}
+#define RBQ_HELPER(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(&NAME)), METH_FASTCALL, nullptr}
+PyMethodDef methods[] = {RBQ_ENTRY(rbq_quantize_kv, kQuantize),
+                         RBQ_ENTRY(rbq_dequantize_kv, kDequantize),
+                         RBQ_ENTRY(rbq_dense_decode_kv8, kDense),
+                         RBQ_ENTRY(rbq_sparse_decode_kv8, kSparse),
+                         RBQ_ENTRY(rbq_decode_step_kv8, kStep),
+                         RBQ_ENTRY(rbq_prefill_attention, kPrefill),
+                         RBQ_HELPER(fits),
+                         RBQ_HELPER(bind),
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_rbqcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__rbqcall(void) {
+  str_data_ptr = PyUnicode_InternFromString("data_ptr");
+  str_numel = PyUnicode_InternFromString("numel");
+  return str_data_ptr != nullptr && str_numel != nullptr ? PyModule_Create(&module_def) : nullptr;
+}

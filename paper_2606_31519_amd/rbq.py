@@ -118,6 +118,21 @@ def _load():
 lib = _load()
 
 
+def _load_calls():
+    """The call module, bound to the loaded library's entry points."""
+    try:
+        from . import _rbqcall
+    except ImportError as e:
+        raise ImportError("_rbqcall.so is not built; run paper_2606_31519_amd.build.build() first") from e
+    _rbqcall.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
+        "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8", "rbq_decode_step_kv8",
+        "rbq_prefill_attention")))
+    return _rbqcall
+
+
+_call = _load_calls()
+
+
 def status_string(s: int) -> str:
     return lib.rbq_status_string(s).decode()
 
@@ -131,6 +146,7 @@ def _ptr(t):
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _stream(stream=None):
@@ -140,7 +156,7 @@ def _stream(stream=None):
     if stream is not None:
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
     if _raw_stream is not None and torch.cuda.is_initialized():
-        return _raw_stream(torch.cuda.current_device())
+        return _raw_stream(_raw_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -178,6 +194,9 @@ class MappedHost:
 
     def data_ptr(self) -> int:
         return self._base + self._offset
+
+    def numel(self) -> int:
+        return self.tensor.numel() - self._offset // self.tensor.element_size()
 
     def rows(self, first_row: int, head_dim: int) -> "MappedHost":
         """The same buffer from row `first_row` of every block on (K + n*D: a cache tail)."""
@@ -430,8 +449,8 @@ def rbq_decode_step_varlen_f16(batch, heads_q, heads_kv, head_dim, q, P, c_k, K,
 
 # ---- the 8-bit cache: K8, V8 [B][Hkv][cap][D] torch.float8_e4m3fn or torch.int8, k_scale, v_scale
 # [B][Hkv][ceil(cap / block)] float32; seq_*: per-sequence counts of ragged batches (int32 device tensors) or None.
-# (A token's calls take the GPU 2 to 4 us: the checks are plain comparisons, and the messages, through _need, are
-# formed when one fails. Checked through _need an rbq_quantize_kv call took 6.8 us of the host, so 4.6.)
+# (A token's calls take the GPU 2 to 4 us, so they go through the call module, and the messages of _pair_code and _need
+# are formed when a check has failed.)
 
 _KV_CODES = {torch.bfloat16: RBQ_BF16, torch.float32: RBQ_F32}
 _KV8_CODES = {torch.float8_e4m3fn: RBQ_E4M3, torch.int8: RBQ_I8}
@@ -445,37 +464,42 @@ def _pair_code(name, codes, a, K, b, V):
     return code
 
 
-def _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale):
-    count = batch * heads_kv * cap * head_dim
-    blocks = batch * heads_kv * ((cap + block - 1) // block) if block > 0 else 0
-    if K8.numel() < count or V8.numel() < count or k_scale.numel() < blocks or v_scale.numel() < blocks:
-        _need(name, K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks), v_scale=(v_scale, blocks))
+def _too_small(name, **sizes):
+    """Refuse the call: one of these buffers holds fewer elements than it needs."""
+    _need(name, **sizes)
+    raise ValueError(f"{name}: a mapped host buffer holds fewer elements than the call needs")
 
 
-def _check_rows(name, batch, heads_kv, head_dim, ld, rows, K, V):
-    """Rows [0, rows) of blocks of ld rows per (sequence, KV head)."""
-    count = ((batch * heads_kv - 1) * ld + rows) * head_dim if rows > 0 else 0
-    if K.numel() < count or V.numel() < count:
-        _need(name, K=(K, count), V=(V, count))
+def _rows_count(groups, head_dim, ld, rows):
+    """Elements that rows [0, rows) of `groups` blocks of ld rows reach to."""
+    return ((groups - 1) * ld + rows) * head_dim if rows > 0 else 0
 
 
-def _check_seqs(name, batch, *seqs):
-    for t in seqs:
-        if t is not None and t.numel() < batch:
-            _need(name, per_sequence=(t, batch))
+def _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, block, K8, V8, k_scale, v_scale, seq_off,
+                      seq_rows):
+    """Formats of the cache and of the rows, once every buffer is large enough."""
+    fmt, dt, groups = _KV8_CODES.get(K8.dtype), _KV_CODES.get(K.dtype), batch * heads_kv
+    if fmt is None or dt is None or K8.dtype is not V8.dtype or K.dtype is not V.dtype:
+        _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8)
+        _pair_code(name, _KV_CODES, "K", K, "V", V)
+    count, need = groups * cap * head_dim, _rows_count(groups, head_dim, ld, rows)
+    blocks = groups * ((cap + block - 1) // block) if block > 0 else 0
+    if not _call.fits(K8, count, V8, count, k_scale, blocks, v_scale, blocks, K, need, V, need, seq_off, batch, seq_rows,
+                      batch):
+        _too_small(name, K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks), v_scale=(v_scale, blocks),
+                   K=(K, need), V=(V, need), seq_off=(seq_off, batch), seq_rows=(seq_rows, batch))
+    return fmt, dt
 
 
 def rbq_quantize_kv(batch, heads_kv, head_dim, K, V, ld, n_new, offset, cap, block, K8, V8, k_scale, v_scale,
                     seq_off=None, seq_new=None, stream=None):
     """Append rows [0, n_new) of K / V [B][Hkv][ld][D] to the 8-bit cache as rows [offset, offset + n_new)."""
     name = "rbq_quantize_kv"
-    fmt, dt = _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8), _pair_code(name, _KV_CODES, "K", K, "V", V)
-    _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    _check_rows(name, batch, heads_kv, head_dim, ld, n_new, K, V)
-    _check_seqs(name, batch, seq_off, seq_new)
-    st = lib.rbq_quantize_kv(
-        batch, heads_kv, head_dim, K.data_ptr(), V.data_ptr(), dt, ld, n_new, offset, cap, block, fmt, K8.data_ptr(),
-        V8.data_ptr(), k_scale.data_ptr(), v_scale.data_ptr(), _ptr(seq_off), _ptr(seq_new), _stream(stream))
+    fmt, dt = _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, n_new, cap, block, K8, V8, k_scale, v_scale,
+                                seq_off, seq_new)
+    st = _call.rbq_quantize_kv(
+        batch, heads_kv, head_dim, K, V, dt, ld, n_new, offset, cap, block, fmt, K8, V8, k_scale, v_scale, seq_off,
+        seq_new, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -484,13 +508,11 @@ def rbq_dequantize_kv(batch, heads_kv, head_dim, K8, V8, block, k_scale, v_scale
                       seq_off=None, seq_rows=None, stream=None):
     """Cache rows [offset, offset + n_rows) as rows [0, n_rows) of K / V [B][Hkv][ld][D] (bf16 or fp32)."""
     name = "rbq_dequantize_kv"
-    fmt, dt = _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8), _pair_code(name, _KV_CODES, "K", K, "V", V)
-    _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    _check_rows(name, batch, heads_kv, head_dim, ld, n_rows, K, V)
-    _check_seqs(name, batch, seq_off, seq_rows)
-    st = lib.rbq_dequantize_kv(
-        batch, heads_kv, head_dim, K8.data_ptr(), V8.data_ptr(), fmt, block, k_scale.data_ptr(), v_scale.data_ptr(), cap,
-        n_rows, offset, K.data_ptr(), V.data_ptr(), dt, ld, _ptr(seq_off), _ptr(seq_rows), _stream(stream))
+    fmt, dt = _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, n_rows, cap, block, K8, V8, k_scale, v_scale,
+                                seq_off, seq_rows)
+    st = _call.rbq_dequantize_kv(
+        batch, heads_kv, head_dim, K8, V8, fmt, block, k_scale, v_scale, cap, n_rows, offset, K, V, dt, ld, seq_off,
+        seq_rows, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -498,16 +520,19 @@ def rbq_dequantize_kv(batch, heads_kv, head_dim, K8, V8, block, k_scale, v_scale
 def _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc, V_loc,
                       loc_ld, w, out, lse, seq_n, seq_w):
     """Formats of the cache and of the window, once every buffer is large enough."""
-    _check_kv8(name, batch, heads_kv, head_dim, cap, block, K8, V8, k_scale, v_scale)
-    rows = batch * heads_q
-    if q.numel() < rows * head_dim or out.numel() < rows * head_dim or (lse is not None and lse.numel() < rows):
-        _need(name, q=(q, rows * head_dim), out=(out, rows * head_dim), lse=(lse, rows))
-    loc = RBQ_BF16
+    fmt, loc, groups, rows = _KV8_CODES.get(K8.dtype), RBQ_BF16, batch * heads_kv, batch * heads_q
+    if fmt is None or K8.dtype is not V8.dtype:
+        _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8)
     if K_loc is not None and V_loc is not None:
         loc = _pair_code(name, _KV_CODES, "K_loc", K_loc, "V_loc", V_loc)
-        _check_rows(name, batch, heads_kv, head_dim, loc_ld, w, K_loc, V_loc)
-    _check_seqs(name, batch, seq_n, seq_w)
-    return _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8), loc
+    count, need = groups * cap * head_dim, _rows_count(groups, head_dim, loc_ld, w)
+    blocks = groups * ((cap + block - 1) // block) if block > 0 else 0
+    if not _call.fits(K8, count, V8, count, k_scale, blocks, v_scale, blocks, K_loc, need, V_loc, need, q, rows * head_dim,
+                      out, rows * head_dim, lse, rows, seq_n, batch, seq_w, batch):
+        _too_small(name, K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks), v_scale=(v_scale, blocks),
+                   K_loc=(K_loc, need), V_loc=(V_loc, need), q=(q, rows * head_dim), out=(out, rows * head_dim),
+                   lse=(lse, rows), seq_n=(seq_n, batch), seq_w=(seq_w, batch))
+    return fmt, loc
 
 
 def rbq_dense_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, n, K_loc, V_loc,
@@ -516,10 +541,9 @@ def rbq_dense_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k
     name = "rbq_dense_decode_kv8"
     fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
                                  V_loc, loc_ld, w, out, lse, seq_n, seq_w)
-    st = lib.rbq_dense_decode_kv8(
-        batch, heads_q, heads_kv, head_dim, q.data_ptr(), K8.data_ptr(), V8.data_ptr(), fmt, block, k_scale.data_ptr(),
-        v_scale.data_ptr(), cap, n, _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w, sm_scale, out.data_ptr(), _ptr(lse),
-        ws.data_ptr(), ws.numel() * ws.element_size(), _ptr(seq_n), _ptr(seq_w), _stream(stream))
+    st = _call.rbq_dense_decode_kv8(
+        batch, heads_q, heads_kv, head_dim, q, K8, V8, fmt, block, k_scale, v_scale, cap, n, K_loc, V_loc, loc, loc_ld,
+        w, sm_scale, out, lse, ws, ws.numel() * ws.element_size(), seq_n, seq_w, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -531,13 +555,11 @@ def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, 
     name = "rbq_sparse_decode_kv8"
     fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
                                  V_loc, loc_ld, w, out, lse, seq_n, seq_w)
-    if sel_idx.numel() < batch * heads_q * n or sel_count.numel() < batch * heads_q:
-        _need(name, sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q))
-    st = lib.rbq_sparse_decode_kv8(
-        batch, heads_q, heads_kv, head_dim, q.data_ptr(), K8.data_ptr(), V8.data_ptr(), fmt, block, k_scale.data_ptr(),
-        v_scale.data_ptr(), cap, n, sel_idx.data_ptr(), sel_count.data_ptr(), _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w,
-        sm_scale, out.data_ptr(), _ptr(lse), ws.data_ptr(), ws.numel() * ws.element_size(), _ptr(seq_n), _ptr(seq_w),
-        _stream(stream))
+    if not _call.fits(sel_idx, batch * heads_q * n, sel_count, batch * heads_q):
+        _too_small(name, sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q))
+    st = _call.rbq_sparse_decode_kv8(
+        batch, heads_q, heads_kv, head_dim, q, K8, V8, fmt, block, k_scale, v_scale, cap, n, sel_idx, sel_count, K_loc,
+        V_loc, loc, loc_ld, w, sm_scale, out, lse, ws, ws.numel() * ws.element_size(), seq_n, seq_w, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -551,16 +573,14 @@ def rbq_decode_step_kv8(batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, K8, 
     fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
                                  V_loc, loc_ld, w, out, lse, None, None)
     rows = batch * heads_q
-    if (qplanes.numel() < rows * 4 * (head_dim // 32) or qscal.numel() < rows * QSCAL_STRIDE or scores.numel() < rows * n
-            or sel_idx.numel() < rows * n or sel_count.numel() < rows):
-        _need(name, qplanes=(qplanes, rows * 4 * (head_dim // 32)), qscal=(qscal, rows * QSCAL_STRIDE),
-              scores=(scores, rows * n), sel_idx=(sel_idx, rows * n), sel_count=(sel_count, rows))
-    st = lib.rbq_decode_step_kv8(
-        batch, heads_q, heads_kv, head_dim, q.data_ptr(), P.data_ptr(), _ptr(c_q), c_k.data_ptr(), K8.data_ptr(),
-        V8.data_ptr(), fmt, block, k_scale.data_ptr(), v_scale.data_ptr(), cap, n, _ptr(K_loc), _ptr(V_loc), loc, loc_ld, w,
-        codes.data_ptr(), _ptr(kfac), _ptr(kfac16), 1 if flush else 0, p, sm_scale, qplanes.data_ptr(), qscal.data_ptr(),
-        scores.data_ptr(), sel_idx.data_ptr(), sel_count.data_ptr(), out.data_ptr(), _ptr(lse), ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream(stream))
+    if not _call.fits(qplanes, rows * 4 * (head_dim // 32), qscal, rows * QSCAL_STRIDE, scores, rows * n, sel_idx, rows * n,
+                      sel_count, rows):
+        _too_small(name, qplanes=(qplanes, rows * 4 * (head_dim // 32)), qscal=(qscal, rows * QSCAL_STRIDE),
+                   scores=(scores, rows * n), sel_idx=(sel_idx, rows * n), sel_count=(sel_count, rows))
+    st = _call.rbq_decode_step_kv8(
+        batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, K8, V8, fmt, block, k_scale, v_scale, cap, n, K_loc, V_loc,
+        loc, loc_ld, w, codes, kfac, kfac16, 1 if flush else 0, p, sm_scale, qplanes, qscal, scores, sel_idx, sel_count,
+        out, lse, ws, ws.numel() * ws.element_size(), _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -574,13 +594,11 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
     if q.dtype != K.dtype or out.dtype != K.dtype:
         raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
     rows = total_q * heads_q
-    if (cu_q.numel() <= batch or cu_k.numel() <= batch or out.numel() < rows * head_dim
-            or (lse is not None and lse.numel() < rows)):
-        _need(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
+    if not _call.fits(cu_q, batch + 1, cu_k, batch + 1, out, rows * head_dim, lse, rows):
+        _too_small(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
     ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
-    st = lib.rbq_prefill_attention(
-        batch, heads_q, heads_kv, head_dim, q.data_ptr(), q_ld, K.data_ptr(), V.data_ptr(), dt, kv_ld, kv_head, kv_seq,
-        kv_rows, cu_q.data_ptr(), cu_k.data_ptr(), total_q, max_k, 1 if causal else 0, sm_scale, out.data_ptr(), _ptr(lse),
-        _ptr(ws), ws_bytes, _stream(stream))
+    st = _call.rbq_prefill_attention(
+        batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, dt, kv_ld, kv_head, kv_seq, kv_rows, cu_q, cu_k, total_q,
+        max_k, 1 if causal else 0, sm_scale, out, lse, ws, ws_bytes, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)

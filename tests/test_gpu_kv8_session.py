@@ -201,3 +201,33 @@ def test_prompt_cache_session_and_next_chunk(mods, fmt, block, D, compact, dt):
     else:                                     # (int8 values are rounded to fp32: half a step of each)
         ot = ot + 2 * 2.0 ** -24 * np.abs(Vd).max() + 2 * 2.0 ** -24 * np.abs(Kd).max() * np.abs(qd).sum() * tau * np.abs(Vd).max()
     assert np.all(np.abs(out[b * chunk + i, h].double().cpu().numpy() - o) <= ot)
+
+
+def test_rows_in_mapped_host_memory(mods):
+    """K and V in pinned host memory, read over PCIe: written into the cache, as a window, and as a prompt's keys, bitwise
+    as from device memory; buffers that are too small are refused."""
+    R = mods[0]
+    B, Hq, Hkv, D, n, w, cap, block = 1, 4, 2, 64, 200, 24, 256, 32
+    g = torch.Generator().manual_seed(3)
+    host = [torch.randn(B, Hkv, n, D, generator=g).to(torch.bfloat16).pin_memory() for _ in range(2)]
+    q = torch.randn(B, Hq, D, generator=g).cuda()
+    prompt = torch.randn(5, Hq, D, generator=g).to(torch.bfloat16).cuda()
+    res = []
+    for rows in ([t.cuda() for t in host], [R.MappedHost(t) for t in host]):
+        c = [torch.zeros(B, Hkv, cap, D, dtype=torch.int8, device="cuda") for _ in range(2)]
+        s = [torch.zeros(B, Hkv, cap // block, device="cuda") for _ in range(2)]
+        R.rbq_quantize_kv(B, Hkv, D, *rows, n, n, 0, cap, block, *c, *s)
+        out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+        ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+        R.rbq_dense_decode_kv8(B, Hq, Hkv, D, q, *c, block, *s, cap, n, *rows, n, w, 0.1, out, lse, ws)
+        po = torch.empty_like(prompt)
+        cu_q, cu_k = (torch.tensor(v, dtype=torch.int32, device="cuda") for v in ([0, 5], [0, n]))
+        pw = R.workspace(R.RBQ_OP_PREFILL, B, Hq, Hkv, D, n, 5)
+        R.rbq_prefill_attention(B, Hq, Hkv, D, prompt, Hq * D, *rows, D, n * D, Hkv * n * D, n, cu_q, cu_k, 5, n, True, 0.1, po,
+                                None, pw)
+        torch.cuda.synchronize()
+        res.append((*c, *s, out, lse, po))
+        with pytest.raises(ValueError, match="rbq_quantize_kv"):
+            R.rbq_quantize_kv(B, Hkv, D, *rows, n + 1, n, 0, cap, block, *c, *s)
+    for a, b in zip(*res):
+        assert torch.equal(a, b)
