@@ -62,6 +62,43 @@ __device__ __forceinline__ void wave_lower_bounds(const int32_t* __restrict__ a,
   r1 = lo1;
 }
 
+// Lower bounds of x in H lists a[h][0, cnt[h]) at once: their rounds of loads overlap.
+template <int H>
+__device__ __forceinline__ void wave_lower_bound_of(const int32_t* const (&a)[H], const int (&cnt)[H], int x,
+                                                    int (&lo)[H]) {
+  const int lane = lane_id();
+  int hi[H];
+  bool open = false;
+#pragma unroll
+  for (int h = 0; h < H; ++h) {
+    lo[h] = 0;
+    hi[h] = cnt[h];
+    open |= cnt[h] > 0;
+  }
+  while (open) {
+    int v[H], st[H];
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      st[h] = (hi[h] - lo[h] + kWave - 1) / kWave;
+      v[h] = a[h][max(min(lo[h] + lane * st[h], cnt[h] - 1), 0)];   // (clamped into the row: some list holds an entry)
+    }
+    open = false;
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      const int k = __popcll(__ballot(lo[h] + lane * st[h] < hi[h] && v[h] < x));   // the first k probes are below x
+      if (hi[h] > lo[h]) {
+        if (k == 0) {
+          hi[h] = lo[h];
+        } else {
+          lo[h] += (k - 1) * st[h] + 1;
+          hi[h] = min(hi[h], lo[h] - 1 + st[h]);
+        }
+      }
+      open |= hi[h] > lo[h];
+    }
+  }
+}
+
 // This lane's words of the split's selection bitmaps: word l % 16 (keys
 // c0 + 64 (l % 16) .. + 64) of heads l / 16 + 4k. Every wave of the block reads
 // the same words; the matrix-core kernel requests them at its start so that the
@@ -118,7 +155,12 @@ __device__ __forceinline__ HeadCounts<G> load_head_counts(const int32_t* __restr
 // [lower bound of c0, lower bound of c1) of its heads' selection lists (their
 // counts in hc), and the entries, loaded all at once, are marked in per-head
 // LDS bitmaps that then serve as the words.
-template <int G, int kThreads, bool PRE, int kPad = kListPad>
+// ONE (the 8-bit decode): only the lower bound of c0 is searched for, of a wave's heads
+// together, and the entries are read on from there until they pass c1. A round of probes
+// touches 64 lines per wave, which costs more than entries read in vain: the call over
+// 128K rows, a fifth per head 45.0 -> 43.9 us, 8 x 2-32K of 64 heads 37.2 -> 34.3, 64K at
+// D = 64 16.3 -> 15.4. (More probes per round, to save one: 51, 38.2 and 17.1.)
+template <int G, int kThreads, bool PRE, int kPad = kListPad, bool ONE = false>
 __device__ __forceinline__ int build_union_list(const int32_t* __restrict__ sel_idx,
                                 const unsigned long long* __restrict__ sel_mask, int mask_words, int row0,
                                 int n, int c0, int c1, int nwin, int wshift, uint32_t (*bm)[kBmWords], int32_t* lst,
@@ -129,17 +171,36 @@ __device__ __forceinline__ int build_union_list(const int32_t* __restrict__ sel_
   const int wd = lane & 15;
   if (sel_mask == nullptr) {
     static_assert(kWaves == kDWaves, "the preloaded counts assume the decode block");
+    constexpr int kHeads = (G + kWaves - 1) / kWaves;   // of a wave
+    if constexpr (ONE) {
+      const int32_t* rows[kHeads];
+      int cnts[kHeads], at[kHeads];
 #pragma unroll
-    for (int i = 0; i < (G + kWaves - 1) / kWaves; ++i) {
-      const int g = wave + kWaves * i;
-      if (g >= G) break;   // (wave-uniform)
-      const int32_t* sel = sel_idx + int64_t(row0 + g) * n;
-      const int cnt = min(max(hc.c[i], 0), n);
-      int lo, hi;
-      wave_lower_bounds(sel, cnt, c0, c1, lo, hi);
-      if (lane == 0) {
-        rng_lo[g] = lo;
-        rng_hi[g] = hi;
+      for (int i = 0; i < kHeads; ++i) {
+        rows[i] = sel_idx + int64_t(row0 + min(wave + kWaves * i, G - 1)) * n;
+        cnts[i] = min(max(__builtin_amdgcn_readfirstlane(hc.c[i]), 0), n);
+      }
+      wave_lower_bound_of<kHeads>(rows, cnts, c0, at);
+#pragma unroll
+      for (int i = 0; i < kHeads; ++i) {
+        if (lane == 0 && wave + kWaves * i < G) {
+          rng_lo[wave + kWaves * i] = at[i];
+          rng_hi[wave + kWaves * i] = cnts[i];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kHeads; ++i) {
+        const int g = wave + kWaves * i;
+        if (g >= G) break;   // (wave-uniform)
+        const int32_t* sel = sel_idx + int64_t(row0 + g) * n;
+        const int cnt = min(max(hc.c[i], 0), n);
+        int lo, hi;
+        wave_lower_bounds(sel, cnt, c0, c1, lo, hi);
+        if (lane == 0) {
+          rng_lo[g] = lo;
+          rng_hi[g] = hi;
+        }
       }
     }
     for (int e = t; e < G * kBmWords; e += kThreads) bm[e / kBmWords][e % kBmWords] = 0u;
@@ -149,6 +210,33 @@ __device__ __forceinline__ int build_union_list(const int32_t* __restrict__ sel_
     constexpr int kHB = G < 4 ? G : 4;                      // heads per batch of loads
 #pragma unroll
     for (int g0 = 0; g0 < G; g0 += kHB) {
+      if constexpr (ONE) {
+        // a first round of every head's entries, then on for those whose last one lies in the split
+        int v[kHB], from[kHB], end[kHB];
+#pragma unroll
+        for (int gg = 0; gg < kHB; ++gg) {
+          from[gg] = rng_lo[g0 + gg];
+          end[gg] = min(rng_hi[g0 + gg], from[gg] + (c1 - c0));
+        }
+        bool more = true;
+        for (int u = 0; more; u += kThreads) {
+          int last[kHB];
+#pragma unroll
+          for (int gg = 0; gg < kHB; ++gg) {
+            const int32_t* sel = sel_idx + int64_t(row0 + g0 + gg) * n;
+            v[gg] = sel[max(min(from[gg] + u + t, end[gg] - 1), 0)];
+            last[gg] = sel[max(min(from[gg] + u + kThreads - 1, end[gg] - 1), 0)];
+          }
+          more = false;
+#pragma unroll
+          for (int gg = 0; gg < kHB; ++gg) {
+            const int pos = from[gg] + u + t < end[gg] ? v[gg] - c0 : -1;
+            if (pos >= 0 && pos < c1 - c0) atomicOr(&bm[g0 + gg][pos >> 5], 1u << (pos & 31));
+            more |= from[gg] + u + kThreads < end[gg] && last[gg] < c1;
+          }
+        }
+        continue;
+      }
       int pv[kHB][kPer];
 #pragma unroll
       for (int gg = 0; gg < kHB; ++gg) {

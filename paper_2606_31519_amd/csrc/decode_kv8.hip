@@ -508,7 +508,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     rows.run(m, lsum, acc);
   } else if constexpr (SPARSE) {
     stage();
-    const int U = build_union_list<G, kDThreads, true, kPad8>(sel_idx, sel_mask, mask_words, row0, n, c0, c1, 0, 0, sh.bm,
+    const int U = build_union_list<G, kDThreads, true, kPad8, true>(sel_idx, sel_mask, mask_words, row0, n, c0, c1, 0, 0, sh.bm,
                                                               sh.lst, sh.hmask, sh.rng_lo, sh.rng_hi, mword, hcount);
     auto attend = [&](auto cp) {
       Rows<FMT, true, G, D, decltype(cp)::value, S> rows(sh, Kr, Vr, c0, U, bshift);
