@@ -680,8 +680,7 @@ __device__ __forceinline__ void lse_merge(float& m, float& l, float& o, float ms
 }
 
 // (D = 128: 32 dimensions per block, 8 groups; D = 64: 16 dimensions, 16 groups)
-// NANS: states whose sum is NaN hold NaN as their maximum, and give NaN.
-template <int D = kHeadDim, bool NANS = false>
+template <int D = kHeadDim>
 __global__ __launch_bounds__(kCombThreads) void decode_combine_kernel(const float* __restrict__ part, int splits,
                                                                       float* __restrict__ out,
                                                                       float* __restrict__ lse) {
@@ -707,16 +706,15 @@ __global__ __launch_bounds__(kCombThreads) void decode_combine_kernel(const floa
 #pragma unroll
     for (int k = 0; k < kCombBatch; ++k) lse_merge(m, l, o, ms[k], ls[k], os[k]);
   }
-  gm[grp][dl] = NANS && l != l ? l : m;
+  gm[grp][dl] = m;
   gl[grp][dl] = l;
   go[grp][dl] = o;
   __syncthreads();
   if (grp == 0) {
 #pragma unroll
     for (int g = 1; g < kCombGroups; ++g) lse_merge(m, l, o, gm[g][dl], gl[g][dl], go[g][dl]);
-    const bool some = l > 0.f || (NANS && l != l);
-    out[int64_t(row) * D + d] = some ? o / l : 0.f;
-    if (lse && slice == 0 && dl == 0) lse[row] = some ? (m + log2f(l)) * kLn2 : -INFINITY;
+    out[int64_t(row) * D + d] = l > 0.f ? o / l : 0.f;
+    if (lse && slice == 0 && dl == 0) lse[row] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
@@ -825,15 +823,6 @@ rbq_status launch_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, const
   if (st != RBQ_OK) return st;
   decode_combine_kernel<kHeadDim><<<dim3(batch * heads_q, kCombSlices), kCombThreads, 0, stream>>>(part, sp.total(),
                                                                                                      out, lse);
-  return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
-}
-
-rbq_status launch_decode_combine(int32_t rows, int32_t head_dim, int32_t splits, const float* part, float* out, float* lse,
-                                 hipStream_t stream) {
-  if (head_dim == 64)
-    decode_combine_kernel<64, true><<<dim3(rows, kCombSlices), kCombThreads, 0, stream>>>(part, splits, out, lse);
-  else
-    decode_combine_kernel<kHeadDim, true><<<dim3(rows, kCombSlices), kCombThreads, 0, stream>>>(part, splits, out, lse);
   return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
 }
 

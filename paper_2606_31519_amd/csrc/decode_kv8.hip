@@ -31,6 +31,7 @@ namespace rbq {
 namespace {
 
 constexpr int kScaleCap = kKv8DenseChunk / kMinKv8Block;   // scale pairs of a split
+constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kPad8 = 32;                                // a row list ends on a whole group
 
 constexpr int elem_bytes(int src) { return src == RBQ_F32 ? 4 : src == RBQ_BF16 ? 2 : 1; }
@@ -566,6 +567,77 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
   }
 }
 
+// Joins the splits of query head blockIdx.x (states {m in the log2 domain, l, acc[D]}), a quarter
+// of its dimensions per block: a thread takes one dimension of every kGroups'th split, BATCH
+// at once, their common maximum first so that the weights do not wait for each other; the
+// groups are then added in order. (A state without rows holds m = -inf and nothing else.)
+template <int D, int BATCH>
+__global__ __launch_bounds__(kDThreads) void join_kv8_kernel(const float* __restrict__ part, int splits,
+                                                             float* __restrict__ out, float* __restrict__ lse) {
+  constexpr int kDims = D / 4, kGroups = kDThreads / kDims;
+  __shared__ float gm[kGroups][kDims], gl[kGroups][kDims], go[kGroups][kDims];
+  const int row = blockIdx.x, dl = threadIdx.x % kDims, grp = threadIdx.x / kDims, d = blockIdx.y * kDims + dl;
+  const float* pr = part + int64_t(row) * splits * (D + 2);
+  auto weight = [](float m, float top) { return m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top); };
+  float m = -INFINITY, l = 0.f, o = 0.f;
+  for (int s0 = grp; s0 < splits; s0 += kGroups * BATCH) {
+    float ms[BATCH], ls[BATCH], os[BATCH];
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const int s = s0 + kGroups * k;
+      const float* ps = pr + int64_t(min(s, splits - 1)) * (D + 2);
+      ms[k] = ps[0];
+      ls[k] = ps[1];
+      os[k] = ps[2 + d];
+      if (s >= splits) ms[k] = -INFINITY;
+    }
+    float top = m;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) top = fmaxf(top, ms[k]);
+    const float w0 = weight(m, top);
+    l *= w0;
+    o *= w0;
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k) {
+      const float w = weight(ms[k], top);
+      l = fmaf(w, ms[k] == -INFINITY ? 0.f : ls[k], l);
+      o = fmaf(w, ms[k] == -INFINITY ? 0.f : os[k], o);
+    }
+    m = top;
+  }
+  gm[grp][dl] = l == l ? m : l;
+  gl[grp][dl] = l;
+  go[grp][dl] = o;
+  __syncthreads();
+  if (grp != 0) return;
+  float top = -INFINITY;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) top = fmaxf(top, gm[g][dl]);
+  l = o = 0.f;
+#pragma unroll
+  for (int g = 0; g < kGroups; ++g) {
+    const float w = weight(gm[g][dl], top);
+    l = fmaf(w, gl[g][dl], l);
+    o = fmaf(w, go[g][dl], o);
+  }
+  out[int64_t(row) * D + d] = l == 0.f ? 0.f : o / l;
+  if (lse && d == 0) lse[row] = l == 0.f ? -INFINITY : (top + log2f(l)) * kLn2;
+}
+
+// The smallest batch that takes a thread's splits in one round: with 18 throughout, 512 heads
+// of 33 splits take 7.8 us instead of 4.8, 32 heads of 19 3.4 instead of 2.8. (The
+// full-precision decode's join, whose weights wait for each other, 6.3 and 4.2.)
+template <int D>
+void launch_join(int rows, int splits, const float* part, float* out, float* lse, hipStream_t stream) {
+  constexpr int kGroups = kDThreads / (D / 4);
+  const dim3 grid(rows, 4);
+  const int own = (splits + kGroups - 1) / kGroups;
+  if (own <= 2) join_kv8_kernel<D, 2><<<grid, kDThreads, 0, stream>>>(part, splits, out, lse);
+  else if (own <= 5) join_kv8_kernel<D, 5><<<grid, kDThreads, 0, stream>>>(part, splits, out, lse);
+  else if (own <= 10) join_kv8_kernel<D, 10><<<grid, kDThreads, 0, stream>>>(part, splits, out, lse);
+  else join_kv8_kernel<D, 18><<<grid, kDThreads, 0, stream>>>(part, splits, out, lse);
+}
+
 struct Call {
   dim3 grid;
   hipStream_t stream;
@@ -633,7 +705,9 @@ rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, i
   st = head_dim == 64 ? RBQ_KV8(64) : RBQ_KV8(128);
 #undef RBQ_KV8
   if (st != RBQ_OK) return st;
-  return launch_decode_combine(batch * heads_q, head_dim, sp.total(), a.part, out, lse, stream);
+  if (head_dim == 64) launch_join<64>(batch * heads_q, sp.total(), a.part, out, lse, stream);
+  else launch_join<128>(batch * heads_q, sp.total(), a.part, out, lse, stream);
+  return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
 }
 
 }  // namespace rbq

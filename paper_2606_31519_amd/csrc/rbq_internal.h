@@ -272,9 +272,6 @@ rbq_status launch_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, const
 // (ragged: seq_n / seq_w [B] indexed and window rows per sequence, the window
 // being the sequence's cache tail; K_loc, V_loc and loc_ld are then ignored)
 
-// joins the splits of each of `rows` query heads: part [rows][splits][D + 2] {m (log2 domain), l, acc}
-rbq_status launch_decode_combine(int32_t rows, int32_t head_dim, int32_t splits, const float* part, float* out,
-                                 float* lse, hipStream_t stream);
 rbq_status launch_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
                               int32_t dtype, int64_t ld, int32_t n_new, int32_t offset, int32_t cap, int32_t block,
                               int32_t kv8_dtype, void* K8, void* V8, float* k_scale, float* v_scale,
