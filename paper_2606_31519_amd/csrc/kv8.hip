@@ -5,12 +5,15 @@
 //         within 448; x / s is then exact and the code is its one rounding
 //   int8: s = amax / 127, code = x (1/s) rounded once to a whole number
 //
-// A token block of one tensor is held in registers by a wave (up to 4096 values) or
+// A token block of one tensor is held in registers by a wave (below 4096 values) or
 // by four: its new rows are read once, their largest magnitude is reduced, and the
 // codes leave from the same registers, so the bytes are those of the rows and the
 // codes, which bound it: K and V of 130816 tokens x 8 heads x 128 in bf16, 805 MB,
-// 131 us (6.1 TB/s; a plain copy on this GPU 6.2), and the same back 137. (With loads
-// that the caches keep 162; 8 codes per lane and store 159; a wave for 8192 values 134.)
+// 129 us (6.2 TB/s, a plain copy's rate on this GPU), and the same back 138; half as
+// many tokens in fp32, 670 MB, 113 us. (With loads that the caches keep 162; 8 codes
+// per lane and store 159; one wave for 4096 values 133, and 163 in fp32, whose loads of
+// 16 values per lane do not follow each other; bounds by branches instead of by the
+// buffers' ends 131 and 157.)
 // A block that holds earlier rows keeps them: where the new rows need a
 // larger scale, the held codes are read, multiplied by the ratio of the scales and
 // written back (a rounding of at most half a step of the new scale).
@@ -22,6 +25,7 @@ namespace {
 
 constexpr int kQuantThreads = 256;
 constexpr float kE4m3Max = 448.f, kI8Max = 127.f;
+constexpr int kPast = 0x7FFFFF00;      // an offset past the end of every buffer here
 constexpr float kRound = 12582912.f;   // 1.5 * 2^23: adding it rounds to a whole number, kept in the low bits
 
 // bits of |x|, 0 for an infinity or NaN: the order of magnitudes is the order of the bits
@@ -80,19 +84,23 @@ __device__ __forceinline__ void decode4(uint32_t w, float* x) {
   }
 }
 
-// 16 values of a row of DT at `p`. (Read once: streamed past the caches.)
+// Values of a row that a thread takes at once: 16 in bf16, so that their codes leave 16
+// bytes per lane, 4 in fp32, so that a wave's loads follow each other.
 template <int DT>
-__device__ __forceinline__ void load16(const char* p, u32x4* raw) {
+constexpr int kTake = DT == RBQ_BF16 ? 16 : 4;
+// kTake values of DT, 0 past the buffer's ends. (Read once: streamed past the caches.)
+template <int DT>
+__device__ __forceinline__ void load_values(__amdgpu_buffer_rsrc_t r, int off, u32x4* raw) {
 #pragma unroll
-  for (int i = 0; i < (DT == RBQ_BF16 ? 2 : 4); ++i)
-    raw[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p) + i);
+  for (int i = 0; i < (DT == RBQ_BF16 ? 2 : 1); ++i)
+    raw[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off + 16 * i, 0, 2));
 }
 template <int DT>
-__device__ __forceinline__ void widen16(const u32x4* raw, float* x) {
+__device__ __forceinline__ void widen(const u32x4* raw, float* x) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) {
+  for (int i = 0; i < kTake<DT>; ++i) {
     if constexpr (DT == RBQ_BF16) x[i] = i % 2 ? bf16_hi(raw[i / 8][i % 8 / 2]) : bf16_lo(raw[i / 8][i % 8 / 2]);
-    else x[i] = __uint_as_float(raw[i / 4][i % 4]);
+    else x[i] = __uint_as_float(raw[0][i]);
   }
 }
 
@@ -105,45 +113,47 @@ __device__ __forceinline__ Span span_of(int b, int offset, int rows, const int32
 }
 
 // Grid (token blocks of a sequence / units per workgroup, (b, kv head), K or V).
-// T threads take a token block of D-dimension rows: CH pieces of 16 dimensions each, so
-// that codes leave 16 bytes per lane.
+// T threads take a token block of D-dimension rows, 16 CH values each.
 template <int DT, int FMT, int T, int CH>
 __global__ __launch_bounds__(kQuantThreads) void quantize_kv_kernel(
     const char* __restrict__ K, const char* __restrict__ V, int64_t ld, int n_new, int offset, int cap, int bshift,
-    int dshift, uint32_t* __restrict__ K8, uint32_t* __restrict__ V8, float* __restrict__ k_scale,
-    float* __restrict__ v_scale, int Hkv, const int32_t* __restrict__ seq_off, const int32_t* __restrict__ seq_new) {
-  constexpr int kEl = DT == RBQ_BF16 ? 2 : 4, kRaw = DT == RBQ_BF16 ? 2 : 4;
+    int dshift, char* __restrict__ K8, char* __restrict__ V8, float* __restrict__ k_scale, float* __restrict__ v_scale,
+    int Hkv, const int32_t* __restrict__ seq_off, const int32_t* __restrict__ seq_new) {
+  constexpr int kEl = DT == RBQ_BF16 ? 2 : 4, kRaw = DT == RBQ_BF16 ? 2 : 1;
+  constexpr int kVals = kTake<DT>, kPieces = CH * 16 / kVals;
   constexpr int kUnits = kQuantThreads / T;
   __shared__ uint32_t red[kQuantThreads / kWave];
   const int bh = blockIdx.y, b = bh / Hkv;
   const Span sp = span_of(b, offset, n_new, seq_off, seq_new);
-  const int t = threadIdx.x % T;
-  const int blk = (sp.off >> bshift) + int(blockIdx.x) * kUnits + int(threadIdx.x) / T;
+  const int t = threadIdx.x % T;   // (a unit is whole waves)
+  const int blk = (sp.off >> bshift) + int(blockIdx.x) * kUnits + __builtin_amdgcn_readfirstlane(threadIdx.x / T);
   const int row0 = blk << bshift;
   const int end = sp.off + sp.cnt;
-  if (kUnits == 1 ? row0 >= end : __builtin_amdgcn_readfirstlane(row0) >= end) return;   // (a unit is whole waves)
-  const char* src = (blockIdx.z ? V : K) + int64_t(bh) * ld * (int64_t(kEl) << dshift);
-  uint32_t* dst = (blockIdx.z ? V8 : K8) + ((int64_t(bh) * cap) << (dshift - 2));
+  if (row0 >= end) return;
+  // value e of the token block; [first, last) are the new ones, those before them held. Loads and
+  // stores of the others lie past the ends of the buffers: they give 0 and are dropped.
+  const int first = max(sp.off - row0, 0) << dshift, last = min(end - row0, 1 << bshift) << dshift;
+  const char* rows = (blockIdx.z ? V : K) + ((int64_t(bh) * ld + max(row0 - sp.off, 0)) << dshift) * kEl;
+  const __amdgpu_buffer_rsrc_t src = make_rsrc(rows, uint32_t(last - first) * kEl);
+  char* codes = (blockIdx.z ? V8 : K8) + ((int64_t(bh) * cap + row0) << dshift);
+  const __amdgpu_buffer_rsrc_t dst = make_rsrc(codes + first, uint32_t(last - first));
   const int64_t sidx = int64_t(bh) * ((int64_t(cap) + (1 << bshift) - 1) >> bshift) + blk;
   float* scale = (blockIdx.z ? v_scale : k_scale) + sidx;
   const float old = row0 < sp.off ? *scale : 0.f;   // rows that the block holds already
 
-  const int cshift = dshift - 4;   // pieces of a row
-  u32x4 raw[CH][kRaw];
+  u32x4 raw[kPieces][kRaw];
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int e = c * T + t, row = row0 + (e >> cshift), dim = (e & ((1 << cshift) - 1)) * 16;
-#pragma unroll
-    for (int i = 0; i < kRaw; ++i) raw[c][i] = u32x4{0u, 0u, 0u, 0u};
-    if (row >= sp.off && row < end) load16<DT>(src + ((int64_t(row - sp.off) << dshift) + dim) * kEl, raw[c]);
+  for (int c = 0; c < kPieces; ++c) {
+    const int e = (c * T + t) * kVals;
+    load_values<DT>(src, e >= first ? (e - first) * kEl : kPast, raw[c]);
   }
   uint32_t amax = 0u;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    float x[16];
-    widen16<DT>(raw[c], x);
+  for (int c = 0; c < kPieces; ++c) {
+    float x[kVals];
+    widen<DT>(raw[c], x);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) amax = max(amax, finite_bits(x[i]));
+    for (int i = 0; i < kVals; ++i) amax = max(amax, finite_bits(x[i]));
   }
   amax = wave_max_u32(amax);
   if constexpr (T > kWave) {
@@ -154,26 +164,25 @@ __global__ __launch_bounds__(kQuantThreads) void quantize_kv_kernel(
   }
   const float s = fmaxf(block_scale<FMT>(amax), old);
   const float r = s > 0.f ? 1.f / s : 0.f;
-  const bool grows = row0 < sp.off && s > old;
-  const float ratio = grows ? old / s : 1.f;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    const int e = c * T + t, row = row0 + (e >> cshift), dim = (e & ((1 << cshift) - 1)) * 16;
-    u32x4* out = reinterpret_cast<u32x4*>(dst + ((int64_t(row) << (dshift - 2)) + dim / 4));
-    if (row >= sp.off && row < end) {
-      float x[16];
-      widen16<DT>(raw[c], x);
-      *out = u32x4{encode4<FMT>(x, r), encode4<FMT>(x + 4, r), encode4<FMT>(x + 8, r), encode4<FMT>(x + 12, r)};
-    } else if (grows && row < sp.off) {
-      const u32x4 was = *out;
-      u32x4 now;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        float x[4];
-        decode4<FMT>(was[i], x);
-        now[i] = encode4<FMT>(x, ratio);
-      }
-      *out = now;
+  for (int c = 0; c < kPieces; ++c) {
+    const int e = (c * T + t) * kVals, at = e >= first ? e - first : kPast;
+    float x[kVals];
+    widen<DT>(raw[c], x);
+    if constexpr (kVals == 16) {
+      const u32x4 now = {encode4<FMT>(x, r), encode4<FMT>(x + 4, r), encode4<FMT>(x + 8, r), encode4<FMT>(x + 12, r)};
+      __builtin_amdgcn_raw_buffer_store_b128(now, dst, at, 0, 0);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b32(encode4<FMT>(x, r), dst, at, 0, 0);
+    }
+  }
+  if (row0 < sp.off && s > old) {   // the held rows under the larger scale
+    const float ratio = old / s;
+    for (int e = 4 * t; e < first; e += 4 * T) {
+      uint32_t* at = reinterpret_cast<uint32_t*>(codes + e);
+      float x[4];
+      decode4<FMT>(*at, x);
+      *at = encode4<FMT>(x, ratio);
     }
   }
   if (t == 0) *scale = s;
@@ -221,15 +230,15 @@ int log2i(int x) { return __builtin_ctz(unsigned(x)); }
 
 template <int DT, int FMT>
 void launch_quantize_form(int pieces, dim3 grid, hipStream_t stream, const char* K, const char* V, int64_t ld, int n_new,
-                          int offset, int cap, int bshift, int dshift, uint32_t* K8, uint32_t* V8, float* ks, float* vs,
+                          int offset, int cap, int bshift, int dshift, char* K8, char* V8, float* ks, float* vs,
                           int Hkv, const int32_t* seq_off, const int32_t* seq_new) {
 #define RBQ_QUANT_FORM(T, CH)                                                                                     \
   quantize_kv_kernel<DT, FMT, T, CH><<<grid, kQuantThreads, 0, stream>>>(K, V, ld, n_new, offset, cap, bshift, dshift, \
                                                                          K8, V8, ks, vs, Hkv, seq_off, seq_new)
-  switch (pieces) {   // of 16 values in a token block: 64 threads up to 256, 256 above
+  switch (pieces) {   // of 16 values in a token block: 64 threads below 256, 256 from there on
     case 64: RBQ_QUANT_FORM(64, 1); break;
     case 128: RBQ_QUANT_FORM(64, 2); break;
-    case 256: RBQ_QUANT_FORM(64, 4); break;
+    case 256: RBQ_QUANT_FORM(256, 1); break;
     case 512: RBQ_QUANT_FORM(256, 2); break;
     case 1024: RBQ_QUANT_FORM(256, 4); break;
     default: RBQ_QUANT_FORM(256, 8); break;
@@ -244,14 +253,14 @@ rbq_status launch_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim,
                               const int32_t* seq_off, const int32_t* seq_new, hipStream_t stream) {
   if (n_new == 0) return RBQ_OK;
   const int bshift = log2i(block), dshift = log2i(head_dim), pieces = block * head_dim / 16;
-  const int units = pieces <= 256 ? kQuantThreads / kWave : 1;
+  const int units = pieces < 256 ? kQuantThreads / kWave : 1;
   // token blocks a sequence's rows can touch (ragged: from any place in the first)
   const int64_t first = seq_off ? 0 : offset >> bshift;
   const int64_t blocks =
       seq_off ? (int64_t(block) - 1 + n_new + block - 1) >> bshift : ((int64_t(offset) + n_new - 1) >> bshift) - first + 1;
   const dim3 grid((blocks + units - 1) / units, batch * heads_kv, 2);
   const char *k = static_cast<const char*>(K), *v = static_cast<const char*>(V);
-  uint32_t *k8 = static_cast<uint32_t*>(K8), *v8 = static_cast<uint32_t*>(V8);
+  char *k8 = static_cast<char*>(K8), *v8 = static_cast<char*>(V8);
 #define RBQ_QUANT(DT, FMT)                                                                                              \
   launch_quantize_form<DT, FMT>(pieces, grid, stream, k, v, ld, n_new, offset, cap, bshift, dshift, k8, v8, k_scale, \
                                 v_scale, heads_kv, seq_off, seq_new)
