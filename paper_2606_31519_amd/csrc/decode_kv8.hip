@@ -417,7 +417,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     const float* __restrict__ k_scale, const float* __restrict__ v_scale, int bshift, int cap, int n,
     const int32_t* __restrict__ sel_idx, const int32_t* __restrict__ sel_count,
     const unsigned long long* __restrict__ sel_mask, int mask_words, const char* __restrict__ K_loc,
-    const char* __restrict__ V_loc, int64_t loc_ld, int w, int chunk, int idx_splits, int total_splits,
+    const char* __restrict__ V_loc, int64_t loc_ld, int w, int chunk, int idx_splits, int total_splits, int fold_s0,
     float scale_log2e, float* __restrict__ part, int Hq, int Hkv, const int32_t* __restrict__ seq_n,
     const int32_t* __restrict__ seq_w, int ragged, int ordered) {
   using S = Shared<SPARSE, G, D>;
@@ -468,8 +468,9 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     return;
   }
   constexpr int kLocEl = elem_bytes(LOC);
-  const char* Kb = window ? K_loc + int64_t(bh) * loc_ld * (D * kLocEl) : K8 + int64_t(bh) * cap * D;
-  const char* Vb = window ? V_loc + int64_t(bh) * loc_ld * (D * kLocEl) : V8 + int64_t(bh) * cap * D;
+  const int64_t locb = int64_t(bh) * loc_ld * (D * kLocEl);
+  const char* Kb = window ? K_loc + locb : K8 + int64_t(bh) * cap * D;
+  const char* Vb = window ? V_loc + locb : V8 + int64_t(bh) * cap * D;
   const uint32_t region = uint32_t(lim) * uint32_t(window ? D * kLocEl : D);   // < 2^31
   const __amdgpu_buffer_rsrc_t Kr = make_rsrc(Kb, region), Vr = make_rsrc(Vb, region);
   float m = -INFINITY, lsum = 0.f;
@@ -518,6 +519,13 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     };
     if (G <= 4 && int64_t(U) * kStreamDenDen >= int64_t(c1 - c0) * kStreamDenNum) attend(std::integral_constant<int, kStream>{});
     else attend(std::integral_constant<int, 0>{});
+    if (split >= fold_s0) {   // the window rows that this split takes along (see decode_kv8_splits)
+      const int f0 = (split - fold_s0) * kDecodeWinChunk, f1 = min(w, f0 + kDecodeWinChunk);
+      const uint32_t size = uint32_t(w) * uint32_t(D * kLocEl);
+      Rows<LOC, false, G, D, 0, S> rows(sh, make_rsrc(K_loc + locb, size), make_rsrc(V_loc + locb, size), f0, f1 - f0, 0);
+      rows.begin();
+      rows.run(m, lsum, acc);
+    }
   } else {
     Rows<FMT, false, G, D, kStream, S> rows(sh, Kr, Vr, c0, c1 - c0, bshift);
     rows.begin();
@@ -662,7 +670,8 @@ void launch(const Call& a) {
       a.q, static_cast<const char*>(a.c.K8), static_cast<const char*>(a.c.V8), a.c.k_scale, a.c.v_scale,
       __builtin_ctz(unsigned(a.c.block)), a.c.cap, a.n, a.sel_idx, a.sel_count, a.sel_mask, a.mask_words,
       static_cast<const char*>(a.win.K), static_cast<const char*>(a.win.V), a.win.ld, a.win.w, a.sp.chunk,
-      a.sp.idx_splits, a.sp.total(), a.scale_log2e, a.part, a.Hq, a.Hkv, a.seq_n, a.seq_w, a.ragged, a.ordered);
+      a.sp.idx_splits, a.sp.total(), a.sp.fold_wq > 0 ? a.sp.fold_s0 : INT32_MAX, a.scale_log2e, a.part, a.Hq, a.Hkv,
+      a.seq_n, a.seq_w, a.ragged, a.ordered);
 }
 template <int FMT, int LOC, bool SPARSE, int D>
 rbq_status launch_g(int G, const Call& a) {

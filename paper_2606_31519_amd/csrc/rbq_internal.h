@@ -152,7 +152,17 @@ constexpr int kDecodeListCap = 1280;      // row-list positions of a sparse spli
 // by the chunk), provided every sequence's window fits its splits that way.
 DecodeSplits decode_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool tail_window = false,
                            bool sparse = false, bool ragged = false);
-// The splits over an 8-bit cache (no folded window: its rows are of another type).
+// The splits over an 8-bit cache. A uniform dense call in whole rounds of resident blocks
+// where there are rows for one: 8 x 8K rows of 8 KV heads 33.2 us, by halves of 1024 36.3;
+// 100K rows 41.0 and 43.2. A uniform sparse call in blocks twice as long as those of a
+// bf16 cache, whose rows are twice the bytes beside the same search and list: chunks
+// halved below 512 blocks instead of 1024: 120K rows, a fifth per head 38.2 and 46.4 us,
+// 64K rows, 2 % 13.4 and 17.7, 32K rows, a tenth 16.5 and 19.4; 100K in groups of 16 41.0
+// and 57.8 (below 256 blocks: 17.0 at 32K, the others alike). Where only the window's
+// blocks (its rows are of another type) would start a second round, the last splits take
+// them along (fold_s0): 128K rows and 256 of the window 41.8 us, 44.4 without.
+constexpr int kDecodeMinChunk = 256;
+constexpr int kKv8SparseBlocks = 512;
 constexpr int kKv8DenseChunk = 2048;   // positions per dense split (at most)
 DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged);
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,

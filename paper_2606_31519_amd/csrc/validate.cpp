@@ -182,14 +182,28 @@ rbq_status check_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_
 
 DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged) {
   DecodeSplits s = decode_splits(batch, heads_kv, n, w);
-  if (sparse || s.chunk < kDecodeChunk) return s;
+  if (ragged || n <= 0) return s;
   const int64_t groups = int64_t(batch) * heads_kv;
-  if (ragged) return s;
-  const int64_t rounds = (groups * (s.idx_splits + s.win_splits) + kKv8Resident / 2) / kKv8Resident;
-  const int64_t splits = (std::max<int64_t>(rounds, 1) * kKv8Resident) / groups - s.win_splits;
+  auto take = [&](int64_t chunk) {
+    s.chunk = int32_t(chunk);
+    s.idx_splits = int32_t((int64_t(n) + chunk - 1) / chunk);
+  };
+  if (sparse) {
+    take(kDecodeChunk);
+    while (s.chunk > kDecodeMinChunk && groups * s.idx_splits < kKv8SparseBlocks) take(s.chunk / 2);
+    if (s.win_splits <= s.idx_splits && groups * s.idx_splits <= kKv8Resident && groups * s.total() > kKv8Resident) {
+      s.fold_s0 = s.idx_splits - s.win_splits;
+      s.fold_wq = kDecodeWinChunk;
+      s.win_splits = 0;
+    }
+    return s;
+  }
+  if (groups * n < kKv8Resident * kDecodeMinChunk) return s;
+  const int64_t rounds = (groups * s.total() + kKv8Resident / 2) / kKv8Resident;
+  const int64_t splits = std::max<int64_t>(rounds, 1) * kKv8Resident / groups - s.win_splits;
   if (splits < 1) return s;
-  s.chunk = int32_t(std::min<int64_t>(((int64_t(n) + splits - 1) / splits + 63) / 64 * 64, kKv8DenseChunk));
-  s.idx_splits = int32_t((int64_t(n) + s.chunk - 1) / s.chunk);
+  const int64_t chunk = ((int64_t(n) + splits - 1) / splits + 63) / 64 * 64;
+  take(std::max<int64_t>(std::min<int64_t>(chunk, kKv8DenseChunk), kDecodeMinChunk));
   return s;
 }
 
@@ -197,8 +211,8 @@ size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_
                                   int32_t w) {
   if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || n < 0 || w < 0) return 0;
   int64_t total = 0;
-  for (int form = 0; form < 3; ++form)
-    total = std::max<int64_t>(total, decode_kv8_splits(batch, heads_kv, n, w, form == 2, form == 1).total());
+  for (int form = 0; form < 4; ++form)
+    total = std::max<int64_t>(total, decode_kv8_splits(batch, heads_kv, n, w, form & 1, form >> 1).total());
   return align_up(size_t(batch) * heads_q * total * (head_dim + 2) * sizeof(float), 256);
 }
 

@@ -352,3 +352,43 @@ def test_a_nan_in_a_query_or_the_window_gives_nan(R, Hq, Hkv, D, ldt):
         o[0, 0], l[0, 0], o[1, Hq - G:], l[1, Hq - G:] = (float("nan"),) * 4
         assert ((out == o) | (torch.isnan(out) & torch.isnan(o))).all()
         assert ((lse == l) | (torch.isnan(lse) & torch.isnan(l))).all()
+
+
+@pytest.mark.parametrize("Hq,Hkv,D,w,ldt", [(8, 8, 64, 300, "bf16"), (32, 8, 128, 1, "f32"), (64, 8, 64, 511, "bf16")])
+def test_windows_taken_along_by_the_last_splits(R, Hq, Hkv, D, w, ldt):
+    """As many index splits as run at once and a window of one or two splits beside them: its rows count once, in every
+    (sequence, KV head), also where the last splits hold no selected row."""
+    B, block, n, tau, G = 8, 32, 15700, 0.09, Hq // Hkv
+    print("fold", Hq, Hkv, D, w, ldt, flush=True)
+    rng = np.random.default_rng(w)
+    codes = {k: rng.integers(0, 256, (B, Hkv, n, D)).astype(np.uint8) for k in "KV"}
+    for k in "KV":
+        codes[k][codes[k] == 128] = 129
+    scales = {k: rng.uniform(0.005, 0.02, (B, Hkv, (n + block - 1) // block)).astype(np.float32) for k in "KV"}
+    win = {k: torch.from_numpy(rng.standard_normal((B, Hkv, w + 1, D))).to(DT[ldt]) for k in "KV"}
+    for k in "KV":
+        win[k][:, :, w:] = float("nan")
+    keep = rng.random((B, Hq, n)) < 0.02
+    keep[1, :, n - 3000:] = False                        # nothing in the last splits
+    keep[2] = False                                      # the window alone
+    sel, cnt = np.zeros((B, Hq, n), np.int32), keep.sum(axis=2).astype(np.int32)
+    for b in range(B):
+        for h in range(Hq):
+            sel[b, h, :cnt[b, h]] = np.flatnonzero(keep[b, h])
+    q = rng.standard_normal((B, Hq, D)).astype(np.float32)
+    d = {k: (cache_of(codes[k], "int8"), dev(scales[k]), win[k].cuda()) for k in "KV"}
+    out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+    ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+    ws.fill_(255)
+    R.rbq_sparse_decode_kv8(B, Hq, Hkv, D, dev(q), d["K"][0], d["V"][0], block, d["K"][1], d["V"][1], n, n, dev(sel), dev(cnt),
+                            d["K"][2], d["V"][2], w + 1, w, tau, out, lse, ws)
+    torch.cuda.synchronize()
+    out, lse = out.cpu().numpy(), lse.cpu().numpy()
+    for b in range(B):
+        for h in (0, Hq // 2, Hq - 1):
+            rows, hk = np.flatnonzero(keep[b, h]), h // G
+            K, V = (np.concatenate([ku.values(codes[k][b, hk], scales[k][b, hk].astype(np.float64), block, "int8")[rows],
+                                    win[k][b, hk, :w].double().numpy()]) for k in "KV")
+            o, l = ku.attention(q[b, h].astype(np.float64), K, V, tau)
+            ot, lt = ku.attention_tolerance(q[b, h].astype(np.float64), K, V, tau)
+            assert np.abs(out[b, h] - o).max() <= ot and abs(lse[b, h] - l) <= lt, (b, h)

@@ -165,3 +165,13 @@ def test_pipeline_objects_refuse_what_they_cannot_hold():
 def test_a_ragged_batch_of_too_many_blocks_is_refused(R, sparse):
     kw = dict(B=16383, Hq=4, Hkv=4, D=64, n=(1 << 25) - 1, cap=(1 << 25) - 1, wsb=(1 << 63) - 1)
     assert _decode(R, sparse, sn=FAKE, **kw) == R.RBQ_EUNSUPPORTED
+
+
+def test_workspace_of_every_length_covers_shorter_windows(R):
+    """The splits' number goes by rules on the sizes: the workspace of a call is that of its own sizes, and every size of a
+    growing cache has one."""
+    for Hkv, D in [(8, 128), (4, 64), (1, 128)]:
+        for n in list(range(0, 3000, 97)) + list(range(3000, 200000, 7919)):
+            for w in (0, 1, 256, 700):
+                a = R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, 1, 4 * Hkv, Hkv, D, n, w)
+                assert a > 0 and a % 256 == 0 and a <= (4 * Hkv) * (D + 2) * 4 * ((n + 255) // 256 + 4 + (w + 255) // 256) + 256, (n, w)
