@@ -66,6 +66,7 @@ class Setup:
     (1, 8, 2, 128, 40000, 64, "int8", 128, torch.bfloat16, True),
     (1, 16, 1, 64, 2000, 0, "e4m3", 256, torch.bfloat16, True),
     (2, 4, 4, 128, 1, 7, "e4m3", 32, torch.float32, False),
+    (8, 16, 8, 64, 15700, 300, "int8", 64, torch.bfloat16, False),     # windows taken along by the last splits
 ])
 def test_fused_step_is_its_separate_calls(mods, B, Hq, Hkv, D, n, w, fmt, block, loc, compact, flush):
     R, _ = mods
