@@ -196,14 +196,18 @@ __device__ __forceinline__ void store_row(const f32x16 (&o)[D / 32][NQ], int i, 
 //   O^T = V^T P^T A = 32 dimensions of V by transposing LDS reads, B = the probabilities
 //                 straight from those registers (the order of the 16 keys of a product is
 //                 free as long as both operands share it)
-// A step takes 64 keys, staged by the block's four waves into a double buffer in LDS, K a
-// step ahead of V: the products of the next step's logits run on the matrix cores while
+// A step takes 64 keys, staged by the block's four waves into double buffers in LDS, K a
+// tile ahead of V: the products of the next step's logits run on the matrix cores while
 // the softmax of this one runs on the vector units, and K's and V's LDS reads are hidden
-// behind both. Two blocks share a compute unit: with its 128 accumulators for 64 rows a wave
-// would read LDS half as often, but alone on its SIMD it waits (16001 tokens of 32 heads:
-// 2772 us; 32 rows 2129). 2.10 TFLOP in 2060 to 2190 us is 0.96 to 1.02 PFLOP/s; the clock
-// is what the power limit leaves (1.8 of 2.4 GHz): the same call on zeros takes 1552 us, and
-// the library's 8192^3 product, in the same state, makes 1.23 PFLOP/s of its 1.70 on zeros.
+// behind both. (32 keys at a time, with a maximum and a rescaling for each: 2000 tokens of
+// 32 heads 58.9 us, now 55.0; 16001 2056 and 2004; 4000 of D = 64 98 and 91; 8 x 43..650
+// 34.5 and 34.9, of D = 64 20.9 and 22.8.) Two blocks share a compute unit: with its 128
+// accumulators for 64 rows a wave would read LDS half as often, but alone on its SIMD it
+// waits (16001 tokens: 2772 us; 32 rows 2129). A step of a block takes 1.2 us alone on a
+// compute unit and 1.5 beside another, chained by the softmax; in long prompts the power
+// limit bounds it: 2.10 TFLOP in 2000 to 2150 us is 0.98 to 1.05 PFLOP/s at the clock that
+// it leaves (1.8 of 2.4 GHz); the library's 8192^3 product, in the same state, makes 1.23
+// PFLOP/s of its 1.70 on zeros.
 template <int D>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     const uint16_t* __restrict__ q, int64_t q_ld, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
@@ -277,16 +281,20 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
       d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], d, 0, 0, 0);
     }
   };
-  // the softmax of s (32 keys from k0) and its product with V, and the logits nx of the 32 keys after
-  auto step = [&](f32x16& s, f32x16& nx, int k0, const char* next_k, const char* tile_v) {
-    if (k0 + 32 > wmin) {
+  // the softmax of s (64 keys from k0) and its product with V, and the logits nx of the 64 keys after
+  auto step = [&](f32x16 (&s)[2], f32x16 (&nx)[2], int k0, const char* next_k, const char* tile_v) {
+    if (k0 + kPKeys > wmin) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] = k0 + 8 * (r / 4) + 4 * h + r % 4 < lim ? s[r] : -INFINITY;
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = k0 + 32 * t + 8 * (r / 4) + 4 * h + r % 4 < lim ? s[t][r] : -INFINITY;
     }
-    float mx[2] = {s[0], s[1]};
+    float mx[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
 #pragma unroll
-    for (int r = 2; r < 16; ++r) mx[r & 1] = fmaxf(mx[r & 1], s[r]);
-    float top = fmaxf(mx[0], mx[1]);
+    for (int r = 2; r < 16; ++r)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) mx[2 * t + (r & 1)] = fmaxf(mx[2 * t + (r & 1)], s[t][r]);
+    float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3]));
     const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(top), __float_as_uint(top), false, false);
     top = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1])) * scale_log2e;
     // (Moving the reference only where the maximum passes it by a factor of 2^8 saves 2 %, but
@@ -303,22 +311,25 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
       m = mn;
     }
     const float mref = m == -INFINITY ? 0.f : m;
-    logits(nx, next_k);
-    bf16x8 p[2];
-    float sum[2] = {0.f, 0.f};
+    bf16x8 p[4];
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      f32x8 e;
+    for (int t = 0; t < 2; ++t) {
+      logits(nx[t], next_k + t * 32 * RB);
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        e[r] = __builtin_amdgcn_exp2f(fmaf(s[8 * g + r], scale_log2e, -mref));
-        sum[r & 1] += e[r];
+      for (int g = 0; g < 2; ++g) {
+        f32x8 e;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) {
+          e[r] = __builtin_amdgcn_exp2f(fmaf(s[t][8 * g + r], scale_log2e, -mref));
+          sum[2 * t + (r & 1)] += e[r];
+        }
+        p[2 * t + g] = __builtin_convertvector(e, bf16x8);
       }
-      p[g] = __builtin_convertvector(e, bf16x8);
     }
-    l += sum[0] + sum[1];
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
-    for (int g = 0; g < 2; ++g)
+    for (int g = 0; g < 4; ++g)
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
         const char* at = tile_v + g * 16 * RB + (vbase ^ (d * 64));
@@ -353,29 +364,34 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     }
   };
 
-  // Tile i of V holds the keys of step i, kbeg + 64 i .. +64; tile i of K those whose logits
-  // step i forms, 32 further on (the first 32 keys' come before the loop). Logits of keys
-  // behind the last are formed from whatever the tile holds and masked.
-  f32x16 sa, sb;
+  // Tile i of K and of V holds the keys kbeg + 64 i .. +64, in buffer i % 2; step i reads tile i
+  // of V and tile i + 1 of K. Logits of keys behind the last are formed from whatever the tile
+  // holds and masked.
+  f32x16 sa[2], sb[2];
   if (kbeg < kstop) {
-    stage(Kb, ldsK[1], kbeg, false);
+    stage(Kb, ldsK[0], kbeg, false);
     stage(Vb, ldsV[0], kbeg, true);
-    if (kbeg + 32 < kstop) stage(Kb, ldsK[0], kbeg + 32, false);
+    if (kbeg + kPKeys < kstop) stage(Kb, ldsK[1], kbeg + kPKeys, false);
     if (threadIdx.x == 0) odd = 0;
     wait_lds();
     __syncthreads();
-    logits(sa, ldsK[1]);
+    logits(sa[0], ldsK[0]);
+    logits(sa[1], &ldsK[0][32 * RB]);
   }
   const int wstop = min(wend, kstop);
-  int buf = 0;
-  for (int k0 = kbeg; k0 < kstop; k0 += kPKeys, buf ^= 1) {
+  auto publish = [&](int k0, int buf) {   // tile i of V and i + 1 of K have arrived; the ones after are requested
     wait_lds();
     if (k0 >= kodd) finite_tile(ldsV[buf]);
     __syncthreads();
     if (k0 + kPKeys < kstop) stage(Vb, ldsV[buf ^ 1], k0 + kPKeys, true);
-    if (k0 + kPKeys + 32 < kstop) stage(Kb, ldsK[buf ^ 1], k0 + kPKeys + 32, false);
-    if (k0 < wstop) step(sa, sb, k0, ldsK[buf], ldsV[buf]);
-    if (k0 + 32 < wstop) step(sb, sa, k0 + 32, &ldsK[buf][32 * RB], &ldsV[buf][32 * RB]);
+    if (k0 + 2 * kPKeys < kstop) stage(Kb, ldsK[buf], k0 + 2 * kPKeys, false);
+  };
+  for (int k0 = kbeg; k0 < kstop; k0 += 2 * kPKeys) {
+    publish(k0, 0);
+    if (k0 < wstop) step(sa, sb, k0, ldsK[1], ldsV[0]);
+    if (k0 + kPKeys >= kstop) break;
+    publish(k0 + kPKeys, 1);
+    if (k0 + kPKeys < wstop) step(sb, sa, k0 + kPKeys, ldsK[0], ldsV[1]);
   }
 
   if (kbeg < kstop && odd) {
@@ -557,30 +573,36 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
 }
 
 // Joins the splits of the rows of sequences (tokens [cu_q[0], cu_q[batch])): a wave per
-// row; lane s weighs split s, then each lane adds up D / 64 dimensions in the splits' order.
-template <int D, int DT>
+// row; lane s weighs split s, then each lane adds up D / 64 dimensions in the splits' order,
+// up to the last one with keys, BATCH at once.
+template <int D, int DT, int BATCH>
 __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float* __restrict__ part, int splits, int64_t rows,
                                                                     int Hq, const int32_t* __restrict__ cu_q, int batch,
                                                                     void* __restrict__ out, float* __restrict__ lse) {
-  constexpr int E = D / 64, kBatch = 8;
+  constexpr int E = D / 64;
+  typedef float vec __attribute__((ext_vector_type(E)));
   const int64_t row = int64_t(blockIdx.x) * kPWaves + threadIdx.x / kWave;
   if (row >= rows || row < int64_t(cu_q[0]) * Hq || row >= int64_t(cu_q[batch]) * Hq) return;
   const int lane = lane_id();
   const float* p = part + row * splits * (D + 2);
   const f32x2 ml = *reinterpret_cast<const f32x2*>(p + min(lane, splits - 1) * (D + 2));
+  vec v[BATCH];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int k = 0; k < BATCH; ++k)
+      v[k] = *reinterpret_cast<const vec*>(p + min(s0 + k, splits - 1) * (D + 2) + 2 + E * lane);
+  };
+  load(0);
   const float ms = lane < splits ? ml.x : -INFINITY;
   const float M = wave_max(ms);
   const float c = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - M);
   const float l = wave_reduce(c == 0.f ? 0.f : ml.y * c, [](float a, float b) { return a + b; });
-  float acc[E] = {};
-  for (int s0 = 0; s0 < splits; s0 += kBatch) {
-    float v[kBatch][E];
+  const int live = kWave - __builtin_clzll(__ballot(c != 0.f) | 1ull);
+  vec acc = {};
+  for (int s0 = 0; s0 < live; s0 += BATCH) {
+    if (s0 > 0) load(s0);
 #pragma unroll
-    for (int k = 0; k < kBatch; ++k)
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[k][e] = p[min(s0 + k, splits - 1) * (D + 2) + 2 + E * lane + e];
-#pragma unroll
-    for (int k = 0; k < kBatch; ++k) {
+    for (int k = 0; k < BATCH; ++k) {
       const float ck = __uint_as_float(uint32_t(__builtin_amdgcn_readlane(int(__float_as_uint(c)), min(s0 + k, kWave - 1))));
       if (s0 + k < splits && ck != 0.f) {   // (a split without keys has written nothing else)
 #pragma unroll
@@ -604,7 +626,7 @@ __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float*
 rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a,
                           hipStream_t stream) {
   if (a.total_q == 0) return RBQ_OK;
-  const PrefillPlan pl = prefill_plan(batch, heads_q, heads_kv, a.max_k, a.total_q, a.dtype);
+  const PrefillPlan pl = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype);
   const float c = float(double(a.sm_scale) * 1.4426950408889634);
   float* part = pl.splits > 1 ? static_cast<float*>(a.ws) : nullptr;
   const dim3 grid(uint32_t(int64_t(pl.tiles) * heads_kv * pl.splits));
@@ -616,9 +638,12 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
                                          a.cu_k, batch, a.total_q, a.max_k, a.causal, c, static_cast<T*>(a.out), a.lse, \
                                          part, heads_q, heads_kv, pl.tiles, pl.splits, pl.kchunk)
 #define RBQ_PREFILL_JOIN(D, DT)                                                                                    \
-  if (part)                                                                                                        \
-  prefill_combine_kernel<D, DT><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, a.out, \
-                                                                 a.lse)
+  if (part && pl.splits <= 4)                                                                                      \
+    prefill_combine_kernel<D, DT, 4><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, \
+                                                                      a.out, a.lse);                               \
+  else if (part)                                                                                                   \
+    prefill_combine_kernel<D, DT, 8><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, \
+                                                                      a.out, a.lse)
   if (a.dtype == RBQ_F32) {
     if (head_dim == 64) {
       RBQ_PREFILL(prefill_f32_kernel<64>, float);

@@ -74,13 +74,16 @@ struct PrefillArgs {
 rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a);
 // How it is cut: query tiles of `rows` (token, head of the group) rows of one
 // sequence and KV head, and, where those are too few for the GPU, the keys into
-// `splits` chunks of `kchunk`, joined by a second kernel.
+// `splits` chunks of `kchunk`, joined by a second kernel: as many as the kernels' own times
+// make fastest (prefill_cost). Whole prompts of 400 to 700 tokens stay whole (660 tokens of
+// 32 / 8 heads 19.7 us; in chunks of 256 keys 26.3), 200 tokens over 3000 rows take 4 chunks
+// (34.2 us, in 9 39.8), 8 over 5000 twenty (16.8 us, in 10 20.5).
 struct PrefillPlan {
   int32_t rows, tiles;   // tiles: an upper bound over the sequences, per KV head
   int32_t splits, kchunk;
 };
-PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t max_k, int32_t total_q,
-                         int32_t dtype);
+PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
+                         int32_t total_q, int32_t dtype);
 size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
                                int32_t total_q);
 

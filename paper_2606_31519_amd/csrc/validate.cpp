@@ -14,9 +14,6 @@ constexpr int64_t kMaxRows = int64_t(1) << 31;
 constexpr int64_t kMaxStride = int64_t(1) << 23;   // elements: 64 rows of it are addressed with 32-bit byte offsets
 constexpr int64_t kCus = 256;                      // compute units of the GPU
 constexpr int64_t kKv8Resident = 4 * kCus;         // blocks of the decode over an 8-bit cache that run at once
-constexpr int64_t kPrefillMinKeys = 256;           // keys per split, at least
-constexpr int64_t kPrefillMaxSplits = 64;          // (the joining kernel weighs a split per lane)
-constexpr int64_t kPrefillAim = 2 * kCus, kPrefillAimF32 = 4 * kCus;
 // a required device pointer: present, and 16-byte aligned (the kernels use 16-byte vector loads)
 bool bad_ptr(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 }  // namespace
@@ -268,7 +265,24 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
   return RBQ_OK;
 }
 
-PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t max_k, int32_t total_q,
+namespace {
+// Time of a prompt call in us, but for what every choice takes, with the keys in chunks of
+// `kchunk`: the steps of 64 keys that a block takes one after the other, by the blocks of a
+// compute unit (the longest sequence's length stands for the others': with many, for half of
+// theirs), and the states' way through memory and the joining kernel.
+double prefill_cost(int64_t blocks, int32_t batch, int64_t rows, int32_t head_dim, int64_t max_k, int32_t dtype,
+                    int64_t kchunk) {
+  const int64_t splits = (max_k + kchunk - 1) / kchunk;
+  const double per_cu = double(blocks * splits) * (0.5 + 1.0 / (batch + 1.0)) / kCus;
+  double step;
+  if (dtype == RBQ_F32) step = head_dim == 64 ? 2.8 + 2.4 * std::ceil(per_cu) : 2.4 + 9.0 * std::ceil(per_cu);
+  else step = (head_dim == 64 ? 0.7 : 1.0) * (per_cu <= 1.0 ? 1.2 : 1.5 * std::max(1.0, per_cu / 2.0));
+  const double states = splits > 1 ? 3.5 + 0.27e-6 * double(rows * splits) * (head_dim + 2) * sizeof(float) : 0.0;
+  return double(kchunk / 64) * step + states;
+}
+}  // namespace
+
+PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k, int32_t total_q,
                          int32_t dtype) {
   const int64_t rows = int64_t(total_q) * (heads_q / heads_kv);
   PrefillPlan p;
@@ -277,12 +291,20 @@ PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
   const int64_t ends = std::min<int64_t>(batch, total_q);
   p.tiles = int32_t(rows / p.rows + ends);
   const int64_t blocks = std::max<int64_t>((rows + p.rows - 1) / p.rows, ends) * heads_kv;
-  const int64_t aim = dtype == RBQ_F32 ? kPrefillAimF32 : kPrefillAim;
-  int64_t want = blocks < kCus ? (aim + blocks - 1) / blocks : 1;
-  want = std::min<int64_t>(want, (int64_t(max_k) + kPrefillMinKeys - 1) / kPrefillMinKeys);
-  want = std::max<int64_t>(std::min<int64_t>(want, kPrefillMaxSplits), 1);
-  p.kchunk = int32_t(((int64_t(max_k) + want - 1) / want + 63) / 64 * 64);
-  if (p.kchunk == 0) p.kchunk = 64;
+  auto chunk_of = [&](int64_t splits) { return std::max<int64_t>(((int64_t(max_k) + splits - 1) / splits + 63) / 64 * 64, 64); };
+  int64_t kchunk = chunk_of(1);
+  if (blocks < kCus) {
+    double best = prefill_cost(blocks, batch, int64_t(total_q) * heads_q, head_dim, max_k, dtype, kchunk);
+    for (int64_t want : {2, 3, 4, 5, 6, 8, 10, 12, 14, 17, 20, 24, 28, 34, 40, 48, 64}) {   // (the joining kernel weighs a split per lane: 64)
+      const int64_t c = chunk_of(want);
+      const double t = prefill_cost(blocks, batch, int64_t(total_q) * heads_q, head_dim, max_k, dtype, c);
+      if (t < 0.97 * best) {
+        best = t;
+        kchunk = c;
+      }
+    }
+  }
+  p.kchunk = int32_t(std::min<int64_t>(kchunk, (int64_t(1) << 31) - 64));
   p.splits = std::max<int32_t>(int32_t((int64_t(max_k) + p.kchunk - 1) / p.kchunk), 1);
   return p;
 }
@@ -293,7 +315,7 @@ size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv,
   if (heads_q % heads_kv != 0) return 0;
   size_t need = 0;
   for (int32_t dtype : {RBQ_F32, RBQ_BF16}) {
-    const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, max_k, total_q, dtype);
+    const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, head_dim, max_k, total_q, dtype);
     if (p.splits > 1) need = std::max(need, size_t(total_q) * heads_q * p.splits * (size_t(head_dim) + 2) * sizeof(float));
   }
   return align_up(need, 256);
@@ -318,7 +340,7 @@ rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
     return RBQ_EUNSUPPORTED;
   if (bad_ptr(a.q) || bad_ptr(a.out) || bad_ptr(a.cu_q) || bad_ptr(a.cu_k)) return RBQ_EINVAL;
   if (a.kv_rows > 0 && a.max_k > 0 && (bad_ptr(a.K) || bad_ptr(a.V))) return RBQ_EINVAL;
-  const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, a.max_k, a.total_q, a.dtype);
+  const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype);
   if (p.splits > 1 &&
       (bad_ptr(a.ws) || a.ws_bytes < prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q)))
     return RBQ_EINVAL;
