@@ -276,3 +276,26 @@ def test_an_infinity_in_the_last_value_of_a_full_mask(R, dt):
     got = inp.run(R, False)[0]
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_no_keys_at_all(R, dt):
+    """max_k = 0, without K and V or with an empty one: every token of every sequence sees nothing."""
+    q = torch.randn(5, 4, 64, device="cuda").to(DT[dt])
+    empty = torch.empty(0, 2, 64, device="cuda", dtype=DT[dt])
+    for causal in (False, True):
+        out, lse = torch.full_like(q, 3.0), torch.full((5, 4), 3.0, device="cuda")
+        R.rbq_prefill_attention(2, 4, 2, 64, q, 256, empty, empty, 128, 64, 0, 0, i32([0, 2, 5]), i32([0, 0, 0]), 5, 0, causal,
+                                0.1, out, lse)
+        torch.cuda.synchronize()
+        assert torch.all(out == 0) and torch.all(lse == -float("inf"))
+
+
+def test_plans_of_every_size_agree_with_whole_keys(R):
+    """The number of splits goes by rules on the sizes: from one token to many, every plan gives the attention's value."""
+    for tokens in (1, 2, 5, 17, 60, 150, 333):
+        for keys in (64, 700, 2049):
+            inp = Inputs(tokens + keys, "bf16", 8, 2, 64, [tokens], [max(keys, tokens)], "packed")
+            out, lse = inp.run(R, True)
+            torch.cuda.synchronize()
+            check(inp, out, lse, True, heads=(0, 7))

@@ -67,3 +67,26 @@ def test_many_empty_sequences_do_not_split_the_keys_or_fill_the_grid(R):
     assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 1000, 4, 1, 128, 5000, 1000) == 0
     assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 65535, 4, 1, 128, 5000, 3) == \
         R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 3, 4, 1, 128, 5000, 3) > 0
+
+
+def test_a_plan_without_tokens_enqueues_nothing(R):
+    from paper_2606_31519_amd import pipeline
+    plan = pipeline.PromptAttention(4, 2, 64, [0, 0], [3, 0], device="cpu")
+    k = torch.zeros(3, 2, 64)
+    assert plan(torch.zeros(0, 4, 64), k, k, stream=0).shape == (0, 4, 64)
+    with pytest.raises(ValueError):
+        pipeline.PromptAttention(4, 2, 64, [1, -1], device="cpu")
+    with pytest.raises(ValueError):
+        pipeline.PromptAttention(4, 2, 64, [], device="cpu")
+
+
+def test_workspaces_of_every_size_are_bounded(R):
+    """At most 64 splits, none without keys for them, and the same size for the same call."""
+    for T in (1, 7, 40, 300, 2000):
+        for k in (0, 1, 64, 65, 1000, 9001, 131072, (1 << 31) - 1):
+            for Hq, Hkv, D in ((8, 8, 64), (32, 8, 128), (6, 2, 128)):
+                a = R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 1, Hq, Hkv, D, k, T)
+                assert a == R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 1, Hq, Hkv, D, k, T)
+                assert a <= T * Hq * min(64, (k + 63) // 64) * (D + 2) * 4 + 256, (T, k, Hq)
+                if k <= 64:
+                    assert a == 0
