@@ -188,6 +188,7 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
   if (sparse) {
     take(kDecodeChunk);
     while (s.chunk > kDecodeMinChunk && groups * s.idx_splits < kKv8SparseBlocks) take(s.chunk / 2);
+    if (groups * s.idx_splits < kCus) take(kDecodeMinChunk / 2);
     if (s.win_splits <= s.idx_splits && groups * s.idx_splits <= kKv8Resident && groups * s.total() > kKv8Resident) {
       s.fold_s0 = s.idx_splits - s.win_splits;
       s.fold_wq = kDecodeWinChunk;
@@ -195,7 +196,10 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
     }
     return s;
   }
-  if (groups * n < kKv8Resident * kDecodeMinChunk) return s;
+  if (groups * n < kKv8Resident * kDecodeMinChunk) {
+    if (groups * s.idx_splits < kCus) take(kDecodeMinChunk / 2);
+    return s;
+  }
   const int64_t rounds = (groups * s.total() + kKv8Resident / 2) / kKv8Resident;
   const int64_t splits = std::max<int64_t>(rounds, 1) * kKv8Resident / groups - s.win_splits;
   if (splits < 1) return s;
