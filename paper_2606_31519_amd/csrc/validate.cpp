@@ -262,9 +262,10 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
   if (win.w > 0 && (bad_ptr(win.K) || bad_ptr(win.V) || win.ld < win.w || win.ld >= kMaxRows)) return RBQ_EINVAL;
   // rows of one (sequence, KV head) are addressed with 32-bit byte offsets
   if (int64_t(n) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;
-  if (bad_ptr(ws) || ws_bytes < decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, win.w)) return RBQ_EINVAL;
-  // a ragged batch's blocks are numbered along one dimension of the grid
+  // (what this form of the call needs: rbq_workspace_bytes gives the largest of the forms')
   const int64_t splits = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr).total();
+  if (bad_ptr(ws) || ws_bytes < size_t(batch) * heads_q * splits * (size_t(head_dim) + 2) * sizeof(float)) return RBQ_EINVAL;
+  // a ragged batch's blocks are numbered along one dimension of the grid
   if ((seq_n || seq_w) && int64_t(batch) * heads_kv * splits >= (int64_t(1) << 24)) return RBQ_EUNSUPPORTED;
   return RBQ_OK;
 }

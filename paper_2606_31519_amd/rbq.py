@@ -470,11 +470,6 @@ def _too_small(name, **sizes):
     raise ValueError(f"{name}: a mapped host buffer holds fewer elements than the call needs")
 
 
-def _rows_count(groups, head_dim, ld, rows):
-    """Elements that rows [0, rows) of `groups` blocks of ld rows reach to."""
-    return ((groups - 1) * ld + rows) * head_dim if rows > 0 else 0
-
-
 def _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, block, K8, V8, k_scale, v_scale, seq_off,
                       seq_rows):
     """Formats of the cache and of the rows, once every buffer is large enough."""
@@ -482,7 +477,7 @@ def _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, bloc
     if fmt is None or dt is None or K8.dtype is not V8.dtype or K.dtype is not V.dtype:
         _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8)
         _pair_code(name, _KV_CODES, "K", K, "V", V)
-    count, need = groups * cap * head_dim, _rows_count(groups, head_dim, ld, rows)
+    count, need = groups * cap * head_dim, ((groups - 1) * ld + rows) * head_dim if rows > 0 else 0
     blocks = groups * ((cap + block - 1) // block) if block > 0 else 0
     if not _call.fits(K8, count, V8, count, k_scale, blocks, v_scale, blocks, K, need, V, need, seq_off, batch, seq_rows,
                       batch):
@@ -523,9 +518,12 @@ def _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block
     fmt, loc, groups, rows = _KV8_CODES.get(K8.dtype), RBQ_BF16, batch * heads_kv, batch * heads_q
     if fmt is None or K8.dtype is not V8.dtype:
         _pair_code(name, _KV8_CODES, "K8", K8, "V8", V8)
+    count, need = groups * cap * head_dim, 0
     if K_loc is not None and V_loc is not None:
-        loc = _pair_code(name, _KV_CODES, "K_loc", K_loc, "V_loc", V_loc)
-    count, need = groups * cap * head_dim, _rows_count(groups, head_dim, loc_ld, w)
+        loc = _KV_CODES.get(K_loc.dtype)
+        if loc is None or K_loc.dtype is not V_loc.dtype:
+            _pair_code(name, _KV_CODES, "K_loc", K_loc, "V_loc", V_loc)
+        need = ((groups - 1) * loc_ld + w) * head_dim if w > 0 else 0
     blocks = groups * ((cap + block - 1) // block) if block > 0 else 0
     if not _call.fits(K8, count, V8, count, k_scale, blocks, v_scale, blocks, K_loc, need, V_loc, need, q, rows * head_dim,
                       out, rows * head_dim, lse, rows, seq_n, batch, seq_w, batch):
@@ -543,7 +541,7 @@ def rbq_dense_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k
                                  V_loc, loc_ld, w, out, lse, seq_n, seq_w)
     st = _call.rbq_dense_decode_kv8(
         batch, heads_q, heads_kv, head_dim, q, K8, V8, fmt, block, k_scale, v_scale, cap, n, K_loc, V_loc, loc, loc_ld,
-        w, sm_scale, out, lse, ws, ws.numel() * ws.element_size(), seq_n, seq_w, _stream(stream))
+        w, sm_scale, out, lse, ws, ws.nbytes, seq_n, seq_w, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -559,7 +557,7 @@ def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, 
         _too_small(name, sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q))
     st = _call.rbq_sparse_decode_kv8(
         batch, heads_q, heads_kv, head_dim, q, K8, V8, fmt, block, k_scale, v_scale, cap, n, sel_idx, sel_count, K_loc,
-        V_loc, loc, loc_ld, w, sm_scale, out, lse, ws, ws.numel() * ws.element_size(), seq_n, seq_w, _stream(stream))
+        V_loc, loc, loc_ld, w, sm_scale, out, lse, ws, ws.nbytes, seq_n, seq_w, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -580,7 +578,7 @@ def rbq_decode_step_kv8(batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, K8, 
     st = _call.rbq_decode_step_kv8(
         batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, K8, V8, fmt, block, k_scale, v_scale, cap, n, K_loc, V_loc,
         loc, loc_ld, w, codes, kfac, kfac16, 1 if flush else 0, p, sm_scale, qplanes, qscal, scores, sel_idx, sel_count,
-        out, lse, ws, ws.numel() * ws.element_size(), _stream(stream))
+        out, lse, ws, ws.nbytes, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
 
@@ -596,7 +594,7 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
     rows = total_q * heads_q
     if not _call.fits(cu_q, batch + 1, cu_k, batch + 1, out, rows * head_dim, lse, rows):
         _too_small(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
-    ws_bytes = 0 if ws is None else ws.numel() * ws.element_size()
+    ws_bytes = 0 if ws is None else ws.nbytes
     st = _call.rbq_prefill_attention(
         batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, dt, kv_ld, kv_head, kv_seq, kv_rows, cu_q, cu_k, total_q,
         max_k, 1 if causal else 0, sm_scale, out, lse, ws, ws_bytes, _stream(stream))
