@@ -392,3 +392,54 @@ def test_windows_taken_along_by_the_last_splits(R, Hq, Hkv, D, w, ldt):
             o, l = ku.attention(q[b, h].astype(np.float64), K, V, tau)
             ot, lt = ku.attention_tolerance(q[b, h].astype(np.float64), K, V, tau)
             assert np.abs(out[b, h] - o).max() <= ot and abs(lse[b, h] - l) <= lt, (b, h)
+
+
+@pytest.mark.parametrize("sparse", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D,ldt", [(8, 2, 128, "bf16"), (16, 1, 64, "f32"), (2, 2, 128, "f32"), (16, 2, 64, "bf16")])
+def test_short_contexts(R, Hq, Hkv, D, ldt, sparse):
+    """Every mix of empty and held rows and windows around one block's, in uniform and ragged batches."""
+    block, tau, G = 16, 0.11, Hq // Hkv
+    cases = [([n], [w]) for n, w in [(1, 0), (0, 0), (0, 1), (0, 256), (3, 256), (512, 255), (512, 257), (513, 256), (511, 1),
+                                     (64, 64), (0, 300)]]
+    cases += [([0, 512, 7, 100], [0, 3, 256, 0]), ([5, 0, 0], [0, 9, 0]), ([0, 0], [0, 40]), ([512, 1], [0, 0]),
+              ([300, 513], [256, 0])]
+    for ns, ws in cases:
+        print("short", ns, ws, sparse, flush=True)
+        B, n, w, cap = len(ns), max(ns), max(ws), max(ns) + 3
+        rng = np.random.default_rng(n * 7 + w)
+        codes = {k: rng.integers(1, 128, (B, Hkv, cap, D)).astype(np.uint8) for k in "KV"}
+        scales = {k: rng.uniform(0.005, 0.02, (B, Hkv, (cap + block - 1) // block)).astype(np.float32) for k in "KV"}
+        win = {k: torch.from_numpy(rng.standard_normal((B, Hkv, w + 1, D))).to(DT[ldt]) for k in "KV"}
+        for k in "KV":
+            for b in range(B):
+                win[k][b, :, ws[b]:] = float("nan")
+        keep = rng.random((B, Hq, cap)) < (0.3 if sparse else 2.0)
+        for b in range(B):
+            keep[b, :, ns[b]:] = False
+        if sparse:
+            keep[0, -1] = False
+        cnt = keep.sum(axis=2).astype(np.int32)
+        sel = np.zeros((B, Hq, max(n, 1)), np.int32)
+        for b in range(B):
+            for h in range(Hq):
+                sel[b, h, :cnt[b, h]] = np.flatnonzero(keep[b, h])
+        q = rng.standard_normal((B, Hq, D)).astype(np.float32)
+        d = {k: (cache_of(codes[k], "int8"), dev(scales[k]), win[k].cuda()) for k in "KV"}
+        out, lse = torch.full((B, Hq, D), 9.0, device="cuda"), torch.full((B, Hq), 9.0, device="cuda")
+        wsb = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+        wsb.fill_(255)
+        seqs = (None, None) if B == 1 else (dev(np.array(ns, np.int32)), dev(np.array(ws, np.int32)))
+        head = (B, Hq, Hkv, D, dev(q), d["K"][0], d["V"][0], block, d["K"][1], d["V"][1], cap, n)
+        loc = (d["K"][2], d["V"][2], w + 1, w, tau, out, lse, wsb)
+        R.rbq_sparse_decode_kv8(*head, dev(sel), dev(cnt), *loc, *seqs) if sparse else R.rbq_dense_decode_kv8(*head, *loc, *seqs)
+        torch.cuda.synchronize()
+        o_, l_ = out.cpu().numpy(), lse.cpu().numpy()
+        for b in range(B):
+            for h in range(Hq):
+                rows, hk = np.flatnonzero(keep[b, h]), h // G
+                K, V = (np.concatenate([ku.values(codes[k][b, hk], scales[k][b, hk].astype(np.float64), block, "int8")[rows],
+                                        win[k][b, hk, :ws[b]].double().numpy()]) for k in "KV")
+                o, l = ku.attention(q[b, h].astype(np.float64), K, V, tau)
+                ot, lt = ku.attention_tolerance(q[b, h].astype(np.float64), K, V, tau)
+                assert np.abs(o_[b, h] - o).max() <= ot, (ns, ws, b, h)
+                assert (l_[b, h] == l if np.isinf(l) else abs(l_[b, h] - l) <= lt), (ns, ws, b, h)
