@@ -10,18 +10,22 @@
 // fp32, with the queries and the weighted probabilities in three bf16 parts (24
 // bits; fp32 outputs keep fp32's accuracy, two parts would leave 2^-17).
 //
-// The split over the keys, the row lists and the joining of splits are decode.hip's;
-// a wave takes groups of 32 rows (the bytes of 16 rows in bf16) so that the softmax's
-// cross-lane steps and the second product serve twice the rows:
+// The split over the keys and the row lists are decode.hip's, by rules of their own
+// (decode_kv8_splits); a wave takes groups of 32 rows (the bytes of 16 rows in bf16) so
+// that the softmax's cross-lane steps and the second product serve twice the rows:
 //   logits  v_mfma_f32_16x16x32_bf16 on two tiles of 16 rows: A = rows (lane (x, j)
 //           holds row x, dimensions 64 i + 16 j .. +16: each lane's 16 bytes are one
 //           load), B = the queries in the same order of dimensions
 //   values  one v_mfma_f32_16x16x32_bf16 per 16 columns and part over all 32 rows:
 //           C's layout gives a lane rows 4j .. 4j+3 of both tiles, which is the k
 //           order of A (its probabilities) and of B (its columns of those rows)
-// The split's scales (at most 64 pairs) are staged in LDS beside its row list.
-// Window rows take the same path in blocks of their own, 16 rows at a time; fp32 rows
-// are split into three bf16 parts as the queries are.
+// The split's scales (at most 128 pairs) are staged in LDS beside its row list.
+// Window rows take the same path in blocks of their own (or behind the last splits' rows),
+// 16 rows at a time; fp32 rows are split into three bf16 parts as the queries are.
+// Bound by the bytes where rows follow each other: 128K rows of 8 heads, 268 MB, 46 us
+// (5.9 TB/s) and 4 of the join. Scattered rows of 128 bytes make 4.6 TB/s (a fifth of 128K
+// per head: 37.7 us, 6 of them before the first row arrives), few rows the chain search,
+// list, rows, join (64K rows of D = 64, 2 %: 9.6 and 3.1 us).
 #include <cmath>
 #include <type_traits>
 

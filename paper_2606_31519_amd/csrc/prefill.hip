@@ -418,7 +418,9 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
 // Lane half h of the logits product takes dimensions h D / 2 .. +D / 2 (the order of the
 // dimensions is free as long as K and the queries share it), so both read four at once;
 // register r of the result is key 8 (r / 4) + 4 h + r % 4, which is row k = h of step r of
-// the second product.
+// the second product. Bound by the matrix cores (500 tokens of 8 heads of 64 over 6000 rows:
+// 56 us and 6 of the join, the cores busy for 0.64 of the time that blocks run, the rest
+// uneven numbers of blocks per compute unit).
 constexpr int kFKeys = 32;
 template <int D>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
