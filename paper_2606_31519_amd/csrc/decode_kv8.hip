@@ -701,7 +701,7 @@ rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, i
                              hipStream_t stream, const unsigned long long* sel_mask, int32_t mask_words,
                              const int32_t* seq_n, const int32_t* seq_w) {
   const int G = heads_q / heads_kv;
-  const DecodeSplits sp = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr);
+  const DecodeSplits sp = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr);
   const bool ragged = seq_n || seq_w;
   const dim3 grid = ragged ? dim3(uint32_t(batch * heads_kv * int64_t(sp.total()))) : dim3(sp.total(), batch * heads_kv);
   const int64_t blocks = int64_t(batch) * heads_kv * sp.total();

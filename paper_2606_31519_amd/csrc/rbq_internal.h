@@ -169,7 +169,10 @@ DecodeSplits decode_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w
 constexpr int kDecodeMinChunk = 256;
 constexpr int kKv8SparseBlocks = 512;
 constexpr int kKv8DenseChunk = 2048;   // positions per dense split (at most)
-DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged);
+// (ragged: the sequences have row counts of their own, own_windows: window lengths of their own,
+// which the host does not know: then no split takes window rows along)
+DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
+                               bool own_windows);
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                                   int32_t w);
 size_t decode_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,

@@ -177,7 +177,8 @@ rbq_status check_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_
   return RBQ_OK;
 }
 
-DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged) {
+DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
+                               bool own_windows) {
   DecodeSplits s = decode_splits(batch, heads_kv, n, w);
   if (ragged || n <= 0) return s;
   const int64_t groups = int64_t(batch) * heads_kv;
@@ -189,7 +190,8 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
     take(kDecodeChunk);
     while (s.chunk > kDecodeMinChunk && groups * s.idx_splits < kKv8SparseBlocks) take(s.chunk / 2);
     if (groups * s.idx_splits < kCus) take(kDecodeMinChunk / 2);
-    if (s.win_splits <= s.idx_splits && groups * s.idx_splits <= kKv8Resident && groups * s.total() > kKv8Resident) {
+    if (!own_windows && s.win_splits <= s.idx_splits && groups * s.idx_splits <= kKv8Resident &&
+        groups * s.total() > kKv8Resident) {
       s.fold_s0 = s.idx_splits - s.win_splits;
       s.fold_wq = kDecodeWinChunk;
       s.win_splits = 0;
@@ -212,8 +214,8 @@ size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_
                                   int32_t w) {
   if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || n < 0 || w < 0) return 0;
   int64_t total = 0;
-  for (int form = 0; form < 4; ++form)
-    total = std::max<int64_t>(total, decode_kv8_splits(batch, heads_kv, n, w, form & 1, form >> 1).total());
+  for (int form = 0; form < 8; ++form)
+    total = std::max<int64_t>(total, decode_kv8_splits(batch, heads_kv, n, w, form & 1, form & 2, form & 4).total());
   return align_up(size_t(batch) * heads_q * total * (head_dim + 2) * sizeof(float), 256);
 }
 
@@ -263,7 +265,7 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
   // rows of one (sequence, KV head) are addressed with 32-bit byte offsets
   if (int64_t(n) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;
   // (what this form of the call needs: rbq_workspace_bytes gives the largest of the forms')
-  const int64_t splits = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr).total();
+  const int64_t splits = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr).total();
   if (bad_ptr(ws) || ws_bytes < size_t(batch) * heads_q * splits * (size_t(head_dim) + 2) * sizeof(float)) return RBQ_EINVAL;
   // a ragged batch's blocks are numbered along one dimension of the grid
   if ((seq_n || seq_w) && int64_t(batch) * heads_kv * splits >= (int64_t(1) << 24)) return RBQ_EUNSUPPORTED;

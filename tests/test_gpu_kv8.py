@@ -443,3 +443,74 @@ def test_short_contexts(R, Hq, Hkv, D, ldt, sparse):
                 ot, lt = ku.attention_tolerance(q[b, h].astype(np.float64), K, V, tau)
                 assert np.abs(o_[b, h] - o).max() <= ot, (ns, ws, b, h)
                 assert (l_[b, h] == l if np.isinf(l) else abs(l_[b, h] - l) <= lt), (ns, ws, b, h)
+
+
+@pytest.mark.parametrize("sparse", [False, True])
+@pytest.mark.parametrize("B,Hq,Hkv,D,n,w,ws,ldt", [
+    (8, 64, 8, 64, 15700, 300, [300, 0, 1, 256, 257, 17, 299, 128], "bf16"),     # a uniform sparse call takes the windows along
+    (1, 8, 8, 128, 130816, 256, [200], "f32"),                                    # (the same)
+    (3, 8, 2, 128, 700, 600, [0, 512, 600], "f32"),
+    (2, 4, 4, 64, 0, 300, [0, 257], "bf16"),
+], ids=["B8", "B1-128K", "B3", "no-rows"])
+def test_windows_of_their_own_beside_equal_row_counts(R, B, Hq, Hkv, D, n, w, ws, ldt, sparse):
+    """seq_w without seq_n: every sequence n rows and a window of its own, whose rows count once and whose other rows are not
+    read; captured, with windows that grow on the device between the replays, as eager."""
+    print("seq_w", B, Hq, Hkv, D, n, w, sparse, flush=True)
+    block, tau, G, cap = 32, 0.09, Hq // Hkv, n + 2
+    rng = np.random.default_rng(w + B)
+    codes = {k: rng.integers(1, 128, (B, Hkv, cap, D)).astype(np.uint8) for k in "KV"}
+    scales = {k: rng.uniform(0.005, 0.02, (B, Hkv, (cap + block - 1) // block)).astype(np.float32) for k in "KV"}
+    win = {k: torch.from_numpy(rng.standard_normal((B, Hkv, w, D))).to(DT[ldt]) for k in "KV"}
+    keep = rng.random((B, Hq, n)) < (0.02 if sparse else 2.0)
+    cnt = keep.sum(axis=2).astype(np.int32)
+    sel = np.zeros((B, Hq, max(n, 1)), np.int32)
+    for b in range(B):
+        for h in range(Hq):
+            sel[b, h, :cnt[b, h]] = np.flatnonzero(keep[b, h])
+    q = rng.standard_normal((B, Hq, D)).astype(np.float32)
+    d = {k: (cache_of(codes[k], "int8"), dev(scales[k]), win[k].cuda()) for k in "KV"}
+    seq_w, head = dev(np.array(ws, np.int32)), (B, Hq, Hkv, D, dev(q), d["K"][0], d["V"][0], block, d["K"][1], d["V"][1], cap, n)
+    pick = (dev(sel), dev(cnt)) if sparse else ()
+    call = R.rbq_sparse_decode_kv8 if sparse else R.rbq_dense_decode_kv8
+
+    def state():
+        wsb = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+        wsb.fill_(255)
+        return torch.full((B, Hq, D), 9.0, device="cuda"), torch.full((B, Hq), 9.0, device="cuda"), wsb
+
+    def run(st):
+        call(*head, *pick, d["K"][2], d["V"][2], w, w, tau, *st, None, seq_w)
+
+    def check(out, lse, lens):
+        o_, l_ = out.cpu().numpy(), lse.cpu().numpy()
+        for b in range(B):
+            for h in sorted({0, Hq // 2, Hq - 1}):
+                rows, hk = np.flatnonzero(keep[b, h]), h // G
+                K, V = (np.concatenate([ku.values(codes[k][b, hk], scales[k][b, hk].astype(np.float64), block, "int8")[rows],
+                                        win[k][b, hk, :lens[b]].double().numpy()]) for k in "KV")
+                o, l = ku.attention(q[b, h].astype(np.float64), K, V, tau)
+                ot, lt = ku.attention_tolerance(q[b, h].astype(np.float64), K, V, tau)
+                assert np.abs(o_[b, h] - o).max() <= ot, (b, h, np.abs(o_[b, h] - o).max(), ot)
+                assert (l_[b, h] == l if np.isinf(l) else abs(l_[b, h] - l) <= lt), (b, h)
+
+    full = d["K"][2].clone(), d["V"][2].clone()
+    for b in range(B):                         # rows behind a window: no call may read them
+        d["K"][2][b, :, ws[b]:], d["V"][2][b, :, ws[b]:] = float("nan"), float("nan")
+    eager = state()
+    run(eager)
+    torch.cuda.synchronize()
+    check(*eager[:2], ws)
+    d["K"][2].copy_(full[0])
+    d["V"][2].copy_(full[1])
+    captured = state()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(captured)
+    for lens in ([0] * B, [min(v + 1, w) for v in ws], [w] * B, [w + 9] * B):
+        seq_w.copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        eager = state()
+        run(eager)
+        torch.cuda.synchronize()
+        assert torch.equal(captured[0], eager[0]) and torch.equal(captured[1], eager[1])
+        check(*captured[:2], [min(v, w) for v in lens])

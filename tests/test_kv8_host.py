@@ -177,3 +177,16 @@ def test_workspace_of_every_length_covers_shorter_windows(R):
                 # a split has at least 128 rows, a window's 256, and a call without rows one: so many states of D + 2 floats
                 most = (n + 127) // 128 + (w + 255) // 256 + 1
                 assert a > 0 and a % 256 == 0 and a <= (4 * Hkv) * (D + 2) * 4 * most + 256, (n, w)
+
+
+def test_windows_of_their_own_take_splits_of_their_own(R):
+    """seq_w without seq_n: the window's length is the device's, so its rows are no part of the last splits (as they are
+    where w is every sequence's). The call needs the states of the windows' splits, and the workspace has them."""
+    for kw, idx, win in [(dict(B=1, Hq=32, Hkv=8, D=128, n=130816, cap=130816, w=256, ld=256), 128, 1),
+                         (dict(B=8, Hq=64, Hkv=8, D=64, n=15700, cap=15700, w=300, ld=300), 16, 2),
+                         (dict(B=4, Hq=8, Hkv=8, D=128, n=32768, cap=32768, w=200, ld=200), 32, 1)]:
+        state = kw["B"] * kw["Hq"] * (kw["D"] + 2) * 4
+        assert _decode(R, True, **kw, wsb=idx * state - 1) == R.RBQ_EINVAL          # (the windows are taken along)
+        assert _decode(R, True, **kw, sw=FAKE, wsb=(idx + win) * state - 1) == R.RBQ_EINVAL, kw
+        assert R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, *(kw[k] for k in ("B", "Hq", "Hkv", "D", "n", "w"))) >= \
+            (idx + win) * state
