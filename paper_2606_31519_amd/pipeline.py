@@ -242,8 +242,9 @@ class PromptAttention:
         self.sm_scale = 1.0 / math.sqrt(D)
 
     def __call__(self, q, K, V, out=None, lse=None, stream=None):
-        """q [total_q][Hq][D]; K, V packed [total_k][Hkv][D] or in a cache [B][Hkv][cap][D] (rows from 0); any strides
-        whose last dimension (of q: two) is contiguous. Returns out [total_q][Hq][D] in q's type."""
+        """q [total_q][Hq][D]; K, V packed [total_k][Hkv][D] or in a cache [B][Hkv][cap][D] (rows from 0, of each sequence
+        its own: a cache expanded over several is refused); any strides whose last dimension (of q: two) is contiguous.
+        Returns out [total_q][Hq][D] in q's type."""
         D = self.D
         if tuple(q.shape[1:]) != (self.Hq, D) or q.shape[0] < self.total_q:
             raise ValueError(f"q is {tuple(q.shape)}, the plan needs ({self.total_q}, {self.Hq}, {D})")
@@ -255,6 +256,8 @@ class PromptAttention:
             raise ValueError(f"K and V are {tuple(K.shape)} and {tuple(V.shape)}, the plan needs {want} and equal strides")
         if q.stride(2) != 1 or q.stride(1) != D or K.stride(-1) != 1:
             raise ValueError("the head dimension (and the heads of q) must be contiguous")
+        if not packed and self.B > 1 and K.stride(0) == 0:   # (the call takes a stride of 0 for packed rows)
+            raise ValueError("K and V are expanded over the sequences: each needs rows of its own")
         lay = (K.stride(0), K.stride(1), 0) if packed else (K.stride(2), K.stride(1), K.stride(0))
         out = torch.empty(self.total_q, self.Hq, D, dtype=q.dtype, device=q.device) if out is None else out
         if not out.is_contiguous() or (lse is not None and not lse.is_contiguous()):

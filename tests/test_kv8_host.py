@@ -190,3 +190,12 @@ def test_windows_of_their_own_take_splits_of_their_own(R):
         assert _decode(R, True, **kw, sw=FAKE, wsb=(idx + win) * state - 1) == R.RBQ_EINVAL, kw
         assert R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV8, *(kw[k] for k in ("B", "Hq", "Hkv", "D", "n", "w"))) >= \
             (idx + win) * state
+
+
+def test_prompt_attention_refuses_one_cache_for_several_sequences():
+    """A cache expanded over the sequences has no stride from one to the next, which the call takes for packed rows."""
+    from paper_2606_31519_amd import pipeline
+    att = pipeline.PromptAttention(4, 2, 64, [3, 5], [7, 9], device="cpu")
+    q, C = torch.zeros(8, 4, 64), torch.zeros(1, 2, 9, 64).expand(2, -1, -1, -1)
+    with pytest.raises(ValueError, match="rows of its own"):
+        att(q, C, C, stream=0)
