@@ -445,7 +445,8 @@ rbq_status rbq_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, 
  *     below seq_n[b] only.
  *   A NaN in a query or an attended window row gives NaN.
  *   RBQ_EUNSUPPORTED for a ragged batch also beyond 2^24 blocks (split, sequence, KV head).
- *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w) bytes.
+ *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w) bytes (for one n,
+ *     the size for a window serves every shorter one; so with RBQ_OP_DECODE_STEP_KV8).
  */
 rbq_status rbq_dense_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
                                 const void* K8, const void* V8, int32_t kv8_dtype, int32_t block,

@@ -508,8 +508,8 @@ rbq_status rbq_decode_step_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv,
   if ((s = check_topp(batch, heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, sw.topp_bytes)) != RBQ_OK)
     return s;
   if ((s = check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win, sm_scale, out,
-                            sw.decode, decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w), nullptr,
-                            nullptr)) != RBQ_OK)
+                            sw.decode, decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w, true),
+                            nullptr, nullptr)) != RBQ_OK)
     return s;
   if (do_flush) {
     if ((s = check_encode(batch, heads_kv, head_dim, K_loc, loc_dtype, loc_ld, w, n, cap, P, c_k, codes, fac, 0u, nullptr,

@@ -177,6 +177,13 @@ rbq_status check_decode(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_
   return RBQ_OK;
 }
 
+namespace {
+// blocks of a dense call over the 8-bit cache that are planned for: those of `blocks` in whole rounds
+int64_t kv8_round_blocks(int64_t blocks) {
+  return std::max<int64_t>((blocks + kKv8Resident / 2) / kKv8Resident, 1) * kKv8Resident;
+}
+}  // namespace
+
 DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
                                bool own_windows) {
   DecodeSplits s = decode_splits(batch, heads_kv, n, w);
@@ -202,8 +209,7 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
     if (groups * s.idx_splits < kCus) take(kDecodeMinChunk / 2);
     return s;
   }
-  const int64_t rounds = (groups * s.total() + kKv8Resident / 2) / kKv8Resident;
-  const int64_t splits = std::max<int64_t>(rounds, 1) * kKv8Resident / groups - s.win_splits;
+  const int64_t splits = kv8_round_blocks(groups * s.total()) / groups - s.win_splits;
   if (splits < 1) return s;
   const int64_t chunk = ((int64_t(n) + splits - 1) / splits + 63) / 64 * 64;
   take(std::max<int64_t>(std::min<int64_t>(chunk, kKv8DenseChunk), kDecodeMinChunk));
@@ -211,11 +217,16 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
 }
 
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
-                                  int32_t w) {
+                                  int32_t w, bool step) {
   if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || n < 0 || w < 0) return 0;
-  int64_t total = 0;
-  for (int form = 0; form < 8; ++form)
-    total = std::max<int64_t>(total, decode_kv8_splits(batch, heads_kv, n, w, form & 1, form & 2, form & 4).total());
+  // sparse: chunks that do not depend on the window, and its splits beside them
+  int64_t total = decode_kv8_splits(batch, heads_kv, n, w, true, false, true).total();
+  if (!step) {
+    // ragged: the same; dense: of its own, or of a shorter window's the most that whole rounds leave
+    const int64_t groups = int64_t(batch) * heads_kv, ragged = decode_splits(batch, heads_kv, n, w).total();
+    total = std::max<int64_t>({total, ragged, decode_kv8_splits(batch, heads_kv, n, w, false, false, false).total()});
+    if (groups * n >= kKv8Resident * kDecodeMinChunk) total = std::max(total, kv8_round_blocks(groups * ragged) / groups);
+  }
   return align_up(size_t(batch) * heads_q * total * (head_dim + 2) * sizeof(float), 256);
 }
 
@@ -373,7 +384,7 @@ StepWorkspace step_workspace(void* base, int32_t batch, int32_t heads_q, int32_t
   char* b = static_cast<char*>(base);
   size_t off = 0;
   s.decode = b + off;
-  off = align_up(off + (kv8 ? decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w)
+  off = align_up(off + (kv8 ? decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w, true)
                             : decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w)), 256);
   s.topp = b + off;
   s.topp_bytes = topp_workspace(nullptr, rows, n).bytes;

@@ -199,3 +199,32 @@ def test_prompt_attention_refuses_one_cache_for_several_sequences():
     q, C = torch.zeros(8, 4, 64), torch.zeros(1, 2, 9, 64).expand(2, -1, -1, -1)
     with pytest.raises(ValueError, match="rows of its own"):
         att(q, C, C, stream=0)
+
+
+@pytest.mark.parametrize("op", ["DECODE_KV8", "DECODE_STEP_KV8"])
+def test_a_workspace_serves_every_shorter_window(R, op):
+    """A decode loop holds one workspace for each index length, sized with the full window, and passes every window from
+    none to it: the size must not shrink as the window grows."""
+    op = getattr(R, "RBQ_OP_" + op)
+    rng = np.random.default_rng(2)
+    # B, Hkv, D, n, window: first lengths at which the splits of a shorter window are more
+    cases = [(2, 8, 128, 56490, 512), (2, 8, 128, 103519, 1024), (1, 8, 128, 96953, 1024), (1, 8, 128, 195923, 128)]
+    cases += [(int(2 ** rng.uniform(0, 5)), int(2 ** rng.integers(0, 4)), int(rng.choice([64, 128])),
+               int(np.exp(rng.uniform(0, np.log(400000)))), int(rng.integers(1, 4097))) for _ in range(3000)]
+    for B, Hkv, D, n, window in cases:
+        need = [R.rbq_workspace_bytes(op, B, 4 * Hkv, Hkv, D, n, w) for w in sorted({0, 1, *range(256, window, 256),
+                                                                                     *range(257, window, 256), window})]
+        assert need == sorted(need), (B, Hkv, D, n, window)
+
+
+def test_a_session_in_8_bits_is_never_refused_a_step(R):
+    """The call's own check, with the workspace that DecodeSession would hold, at every index length and window of it."""
+    for B, n0, window, cap in [(2, 54954, 512, 57002), (2, 103519, 1024, 107615), (1, 92857, 1024, 96953),
+                               (1, 195923, 128, 196435)]:
+        size = lambda n, w: R.rbq_workspace_bytes(R.RBQ_OP_DECODE_STEP_KV8, B, 32, 8, 128, n, w)  # noqa: E731
+        sizes = list(range(n0, cap + 1, window))
+        held = max([size(n, window) for n in sizes] +
+                   [R.rbq_workspace_bytes(R.RBQ_OP_DECODE_STEP, B, 32, 8, 128, sizes[-1], window)])
+        for n in sizes:
+            for w in [0, 1, *range(256, window + 1, 256), *range(257, window + 1, 256)]:
+                assert size(n, w) <= held, (B, n, w)
