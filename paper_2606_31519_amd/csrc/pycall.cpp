@@ -15,7 +15,7 @@
 
 namespace {
 
-PyObject *str_data_ptr, *str_numel;
+PyObject *str_data_ptr, *str_numel, *str_shape, *str_stride, *str_contiguous;
 
 bool take(PyObject* o, int64_t& v) {
   v = PyLong_AsLong(o);
@@ -81,19 +81,53 @@ struct Entry<rbq_status (*)(A...)> {
   }
 };
 
-// fits(buffer, elements, buffer, elements, ...): whether every buffer that knows its
-// number of elements holds as many as the call needs (None and addresses know nothing)
+// elements of a buffer
+bool elements_of(PyObject* o, int64_t& have) {
+  PyObject* r = PyObject_CallMethodNoArgs(o, str_numel);
+  if (r == nullptr) return false;
+  const bool ok = take(r, have);
+  Py_DECREF(r);
+  return ok;
+}
+
+// elements from a view's first to its last, gaps included: 1 + sum (size - 1) stride
+bool span_of(PyObject* o, int64_t& have) {
+  PyObject* shape = PyObject_GetAttr(o, str_shape);
+  PyObject* stride = shape != nullptr ? PyObject_CallMethodNoArgs(o, str_stride) : nullptr;
+  bool ok = stride != nullptr && PyTuple_Check(shape) && PyTuple_Check(stride) &&
+            PyTuple_GET_SIZE(shape) == PyTuple_GET_SIZE(stride);
+  int64_t last = 0;
+  for (Py_ssize_t d = 0; ok && d < PyTuple_GET_SIZE(shape); ++d) {
+    int64_t size, step;
+    ok = take(PyTuple_GET_ITEM(shape, d), size) && take(PyTuple_GET_ITEM(stride, d), step);
+    if (ok) last += (size - 1) * step;
+  }
+  Py_XDECREF(shape);
+  Py_XDECREF(stride);
+  if (ok) have = 1 + last;
+  else if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "a buffer without sizes and strides");
+  return ok;
+}
+
+// fits(rows, buffer, elements, buffer, elements, ...): whether every buffer that knows its size
+// reaches as far as the call needs (None and addresses know nothing). The first `rows` buffers
+// are judged by what they span, more than their elements where a view has gaps between its
+// rows, less where it repeats them; the others by their elements.
 PyObject* fits(PyObject*, PyObject* const* args, Py_ssize_t n) {
-  if (n % 2 != 0) return PyErr_Format(PyExc_TypeError, "pairs of a buffer and its elements");
-  for (Py_ssize_t i = 0; i < n; i += 2) {
+  if (n % 2 == 0) return PyErr_Format(PyExc_TypeError, "a number, and pairs of a buffer and its elements");
+  int64_t rows;
+  if (!take(args[0], rows)) return nullptr;
+  for (Py_ssize_t i = 1; i < n; i += 2) {
     int64_t need, have;
     if (!take(args[i + 1], need)) return nullptr;
     if (args[i] == Py_None || PyLong_Check(args[i])) continue;
-    PyObject* r = PyObject_CallMethodNoArgs(args[i], str_numel);
-    if (r == nullptr) return nullptr;
-    const bool ok = take(r, have);
-    Py_DECREF(r);
-    if (!ok) return nullptr;
+    if (!elements_of(args[i], have)) return nullptr;
+    if (i < 2 * rows && have > 0) {
+      PyObject* c = PyObject_CallMethodNoArgs(args[i], str_contiguous);
+      if (c == nullptr) return nullptr;
+      Py_DECREF(c);
+      if (c != Py_True && !span_of(args[i], have)) return nullptr;
+    }
     if (have < need) Py_RETURN_FALSE;
   }
   Py_RETURN_TRUE;
@@ -125,5 +159,8 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_rbqcall", nullptr, -1, method
 PyMODINIT_FUNC PyInit__rbqcall(void) {
   str_data_ptr = PyUnicode_InternFromString("data_ptr");
   str_numel = PyUnicode_InternFromString("numel");
-  return str_data_ptr != nullptr && str_numel != nullptr ? PyModule_Create(&module_def) : nullptr;
+  str_shape = PyUnicode_InternFromString("shape");
+  str_stride = PyUnicode_InternFromString("stride");
+  str_contiguous = PyUnicode_InternFromString("is_contiguous");
+  return str_data_ptr && str_numel && str_shape && str_stride && str_contiguous ? PyModule_Create(&module_def) : nullptr;
 }

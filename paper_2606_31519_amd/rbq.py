@@ -198,6 +198,9 @@ class MappedHost:
     def numel(self) -> int:
         return self.tensor.numel() - self._offset // self.tensor.element_size()
 
+    def is_contiguous(self) -> bool:
+        return True
+
     def rows(self, first_row: int, head_dim: int) -> "MappedHost":
         """The same buffer from row `first_row` of every block on (K + n*D: a cache tail)."""
         return MappedHost(self.tensor, self._base, self._offset + first_row * head_dim * self.tensor.element_size())
@@ -464,10 +467,12 @@ def _pair_code(name, codes, a, K, b, V):
     return code
 
 
-def _too_small(name, **sizes):
-    """Refuse the call: one of these buffers holds fewer elements than it needs."""
-    _need(name, **sizes)
-    raise ValueError(f"{name}: a mapped host buffer holds fewer elements than the call needs")
+def _too_small(name, rows=(), **sizes):
+    """Refuse the call: one of these buffers holds fewer elements than it needs, or, of those named in `rows` (views
+    of longer buffers among them), spans fewer."""
+    for arg, (t, count) in sizes.items():
+        if not _call.fits(int(arg in rows), t, count):
+            raise ValueError(f"{name}: {arg} ends before the {count} elements that the call needs")
 
 
 def _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, block, K8, V8, k_scale, v_scale, seq_off,
@@ -479,10 +484,10 @@ def _check_cache_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, bloc
         _pair_code(name, _KV_CODES, "K", K, "V", V)
     count, need = groups * cap * head_dim, ((groups - 1) * ld + rows) * head_dim if rows > 0 else 0
     blocks = groups * ((cap + block - 1) // block) if block > 0 else 0
-    if not _call.fits(K8, count, V8, count, k_scale, blocks, v_scale, blocks, K, need, V, need, seq_off, batch, seq_rows,
+    if not _call.fits(2, K, need, V, need, K8, count, V8, count, k_scale, blocks, v_scale, blocks, seq_off, batch, seq_rows,
                       batch):
-        _too_small(name, K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks), v_scale=(v_scale, blocks),
-                   K=(K, need), V=(V, need), seq_off=(seq_off, batch), seq_rows=(seq_rows, batch))
+        _too_small(name, ("K", "V"), K=(K, need), V=(V, need), K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks),
+                   v_scale=(v_scale, blocks), seq_off=(seq_off, batch), seq_rows=(seq_rows, batch))
     return fmt, dt
 
 
@@ -525,10 +530,10 @@ def _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block
             _pair_code(name, _KV_CODES, "K_loc", K_loc, "V_loc", V_loc)
         need = ((groups - 1) * loc_ld + w) * head_dim if w > 0 else 0
     blocks = groups * ((cap + block - 1) // block) if block > 0 else 0
-    if not _call.fits(K8, count, V8, count, k_scale, blocks, v_scale, blocks, K_loc, need, V_loc, need, q, rows * head_dim,
+    if not _call.fits(2, K_loc, need, V_loc, need, K8, count, V8, count, k_scale, blocks, v_scale, blocks, q, rows * head_dim,
                       out, rows * head_dim, lse, rows, seq_n, batch, seq_w, batch):
-        _too_small(name, K8=(K8, count), V8=(V8, count), k_scale=(k_scale, blocks), v_scale=(v_scale, blocks),
-                   K_loc=(K_loc, need), V_loc=(V_loc, need), q=(q, rows * head_dim), out=(out, rows * head_dim),
+        _too_small(name, ("K_loc", "V_loc"), K_loc=(K_loc, need), V_loc=(V_loc, need), K8=(K8, count), V8=(V8, count),
+                   k_scale=(k_scale, blocks), v_scale=(v_scale, blocks), q=(q, rows * head_dim), out=(out, rows * head_dim),
                    lse=(lse, rows), seq_n=(seq_n, batch), seq_w=(seq_w, batch))
     return fmt, loc
 
@@ -553,7 +558,7 @@ def rbq_sparse_decode_kv8(batch, heads_q, heads_kv, head_dim, q, K8, V8, block, 
     name = "rbq_sparse_decode_kv8"
     fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
                                  V_loc, loc_ld, w, out, lse, seq_n, seq_w)
-    if not _call.fits(sel_idx, batch * heads_q * n, sel_count, batch * heads_q):
+    if not _call.fits(0, sel_idx, batch * heads_q * n, sel_count, batch * heads_q):
         _too_small(name, sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q))
     st = _call.rbq_sparse_decode_kv8(
         batch, heads_q, heads_kv, head_dim, q, K8, V8, fmt, block, k_scale, v_scale, cap, n, sel_idx, sel_count, K_loc,
@@ -571,8 +576,8 @@ def rbq_decode_step_kv8(batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, K8, 
     fmt, loc = _check_decode_kv8(name, batch, heads_q, heads_kv, head_dim, q, K8, V8, block, k_scale, v_scale, cap, K_loc,
                                  V_loc, loc_ld, w, out, lse, None, None)
     rows = batch * heads_q
-    if not _call.fits(qplanes, rows * 4 * (head_dim // 32), qscal, rows * QSCAL_STRIDE, scores, rows * n, sel_idx, rows * n,
-                      sel_count, rows):
+    if not _call.fits(0, qplanes, rows * 4 * (head_dim // 32), qscal, rows * QSCAL_STRIDE, scores, rows * n, sel_idx,
+                      rows * n, sel_count, rows):
         _too_small(name, qplanes=(qplanes, rows * 4 * (head_dim // 32)), qscal=(qscal, rows * QSCAL_STRIDE),
                    scores=(scores, rows * n), sel_idx=(sel_idx, rows * n), sel_count=(sel_count, rows))
     st = _call.rbq_decode_step_kv8(
@@ -592,7 +597,7 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
     if q.dtype != K.dtype or out.dtype != K.dtype:
         raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
     rows = total_q * heads_q
-    if not _call.fits(cu_q, batch + 1, cu_k, batch + 1, out, rows * head_dim, lse, rows):
+    if not _call.fits(0, cu_q, batch + 1, cu_k, batch + 1, out, rows * head_dim, lse, rows):
         _too_small(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
     ws_bytes = 0 if ws is None else ws.nbytes
     st = _call.rbq_prefill_attention(

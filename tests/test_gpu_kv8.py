@@ -514,3 +514,39 @@ def test_windows_of_their_own_beside_equal_row_counts(R, B, Hq, Hkv, D, n, w, ws
         torch.cuda.synchronize()
         assert torch.equal(captured[0], eager[0]) and torch.equal(captured[1], eager[1])
         check(*captured[:2], [min(v, w) for v in lens])
+
+
+@pytest.mark.parametrize("dt,D", [("bf16", 128), ("f32", 64)])
+def test_rows_at_the_tail_of_a_longer_cache(R, dt, D):
+    """New rows, rows read back and the window as rows [n, n + w) of full-precision caches (views, ld = cap): bitwise as
+    from buffers of their own, and nothing else of the caches is touched."""
+    B, Hq, Hkv, block, cap, n, w = 2, 8, 2, 32, 300, 260, 37
+    print("tail", dt, D, flush=True)
+    g = torch.Generator(device="cuda").manual_seed(8)
+    K, V = (torch.randn(B, Hkv, cap, D, device="cuda", generator=g).to(DT[dt]) for _ in range(2))
+    q = torch.randn(B, Hq, D, device="cuda", generator=g)
+    sel = torch.arange(n, dtype=torch.int32, device="cuda").expand(B, Hq, n).contiguous()
+    cnt = torch.full((B, Hq), 77, dtype=torch.int32, device="cuda")
+    res = []
+    for ld, kt, vt in ((cap, K[:, :, n:], V[:, :, n:]), (w, K[:, :, n:n + w].contiguous(), V[:, :, n:n + w].contiguous())):
+        c = [torch.zeros(B, Hkv, cap, D, dtype=torch.int8, device="cuda") for _ in range(2)]
+        s = [torch.zeros(B, Hkv, (cap + block - 1) // block, device="cuda") for _ in range(2)]
+        R.rbq_quantize_kv(B, Hkv, D, K, V, cap, n, 0, cap, block, *c, *s)
+        outs = []
+        for sparse in (False, True):
+            out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+            ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+            head, loc = (B, Hq, Hkv, D, q, *c, block, *s, cap, n), (kt, vt, ld, w, 0.1, out, lse, ws)
+            R.rbq_sparse_decode_kv8(*head, sel, cnt, *loc) if sparse else R.rbq_dense_decode_kv8(*head, *loc)
+            outs += [out, lse]
+        R.rbq_quantize_kv(B, Hkv, D, kt, vt, ld, w, n, cap, block, *c, *s)
+        back = [torch.full((B, Hkv, cap if ld == cap else w, D), 7.0, dtype=DT[dt], device="cuda") for _ in range(2)]
+        view = [t[:, :, n:] for t in back] if ld == cap else back
+        R.rbq_dequantize_kv(B, Hkv, D, *c, block, *s, cap, w, n, *view, ld)
+        torch.cuda.synchronize()
+        for t in back:
+            if ld == cap:
+                assert torch.all(t[:, :, :n] == 7.0) and torch.all(t[:, :, n + w:] == 7.0)
+        res.append((*c, *s, *outs, *(t[:, :, :w] for t in view)))
+    for a, b in zip(*res):
+        assert torch.equal(a, b)

@@ -228,3 +228,26 @@ def test_a_session_in_8_bits_is_never_refused_a_step(R):
         for n in sizes:
             for w in [0, 1, *range(256, window + 1, 256), *range(257, window + 1, 256)]:
                 assert size(n, w) <= held, (B, n, w)
+
+
+def test_rows_may_be_the_tail_of_a_longer_buffer(R):
+    """K + n * D with ld = cap, as the calls allow: the view has gaps between the heads and holds fewer elements than it
+    reaches over. The binding lets it through (to the library's own refusal here); views that end too early it refuses."""
+    B, H, D, cap, block, n, w = 2, 2, 64, 64, 16, 48, 16
+    i8, s = torch.zeros(B, H, cap, D, dtype=torch.int8), torch.zeros(B, H, cap // block)
+    x = torch.zeros(B, H, cap, D)
+    tail = x[:, :, n:]
+    q, out, lse, ws = torch.zeros(B, 4, D), torch.zeros(B, 4, D), torch.zeros(B, 4), torch.zeros(1 << 16, dtype=torch.uint8)
+    calls = {
+        "write": lambda t, m: R.rbq_quantize_kv(B, H, D, t, t, cap, m, cap, cap, block, i8, i8, s, s, stream=0),
+        "read": lambda t, m: R.rbq_dequantize_kv(B, H, D, i8, i8, block, s, s, cap, m, cap, t, t, cap, stream=0),
+        "window": lambda t, m: R.rbq_dense_decode_kv8(B, 4, H, D, q, i8, i8, block, s, s, cap, cap, t, t, cap, m, -1.0, out,
+                                                      lse, ws, stream=0),
+    }
+    for name, call in calls.items():
+        with pytest.raises(R.RbqError) as e:      # (rows past the cache's capacity, a negative scale)
+            call(tail, w)
+        assert e.value.status == R.RBQ_EINVAL, name
+        for short in (x[:, :, n + 1:], x[:1, :, n:], tail.contiguous(), x[:1].expand(B, -1, -1, -1)):
+            with pytest.raises(ValueError):
+                call(short, w)
