@@ -597,8 +597,12 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
     if q.dtype != K.dtype or out.dtype != K.dtype:
         raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
     rows = total_q * heads_q
-    if not _call.fits(0, cu_q, batch + 1, cu_k, batch + 1, out, rows * head_dim, lse, rows):
-        _too_small(name, cu_q=(cu_q, batch + 1), cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
+    need_q = (total_q - 1) * q_ld + heads_q * head_dim if total_q > 0 else 0
+    need = ((kv_rows - 1) * kv_ld + (heads_kv - 1) * kv_head + (batch - 1) * kv_seq + head_dim
+            if total_q > 0 and kv_rows > 0 and max_k > 0 else 0)
+    if not _call.fits(3, q, need_q, K, need, V, need, cu_q, batch + 1, cu_k, batch + 1, out, rows * head_dim, lse, rows):
+        _too_small(name, ("q", "K", "V"), q=(q, need_q), K=(K, need), V=(V, need), cu_q=(cu_q, batch + 1),
+                   cu_k=(cu_k, batch + 1), out=(out, rows * head_dim), lse=(lse, rows))
     ws_bytes = 0 if ws is None else ws.nbytes
     st = _call.rbq_prefill_attention(
         batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, dt, kv_ld, kv_head, kv_seq, kv_rows, cu_q, cu_k, total_q,

@@ -90,3 +90,31 @@ def test_workspaces_of_every_size_are_bounded(R):
                 assert a <= T * Hq * min(64, (k + 63) // 64) * (D + 2) * 4 + 256, (T, k, Hq)
                 if k <= 64:
                     assert a == 0
+
+
+def test_binding_refuses_rows_that_end_early(R):
+    """q, K and V by the rows and strides that the call is given: buffers and views that end before the last row."""
+    T, H, D = 4, 2, 64
+    cu, out = torch.tensor([0, T], dtype=torch.int32), torch.zeros(T, H, D)
+    fused, cache = torch.zeros(T, 3 * H, D), torch.zeros(2, H, T, D)
+
+    def call(q, K, V, lay, rows=T, q_ld=H * D, B=1, tau=-1.0):
+        R.rbq_prefill_attention(B, H, H, D, q, q_ld, K, V, *lay, rows, torch.zeros(B + 1, dtype=torch.int32) if B > 1 else cu,
+                                cu if B == 1 else torch.zeros(B + 1, dtype=torch.int32), T, T, True, tau, out, None, stream=0)
+
+    x, packed, held, fl = torch.zeros(T, H, D), (H * D, D, 0), (D, T * D, H * T * D), (3 * H * D, D, 0)
+    views = [fused[:, i * H:(i + 1) * H] for i in range(3)]
+    for kw in (dict(q=x, K=x, V=x, lay=packed), dict(q=views[0], K=views[1], V=views[2], lay=fl, q_ld=3 * H * D),
+               dict(q=x, K=cache, V=cache, lay=held, B=2), dict(q=x, K=None, V=None, lay=packed, rows=0)):
+        if kw["K"] is None:
+            kw["K"] = kw["V"] = torch.zeros(0, H, D)
+        with pytest.raises(R.RbqError) as e:      # (large enough: to the library's refusal of a negative scale)
+            call(**kw)
+        assert e.value.status == R.RBQ_EINVAL
+    for kw in (dict(q=x[1:], K=x, V=x, lay=packed), dict(q=x, K=x[1:], V=x, lay=packed), dict(q=x, K=x, V=x[:3], lay=packed),
+               dict(q=x, K=x, V=x, lay=packed, rows=T + 1), dict(q=x, K=x, V=x, lay=packed, q_ld=H * D + 8),
+               dict(q=views[0][1:], K=views[1], V=views[2], lay=fl, q_ld=3 * H * D),
+               dict(q=x, K=cache[:1], V=cache, lay=held, B=2), dict(q=x, K=cache, V=cache[:1].expand(2, -1, -1, -1), lay=held, B=2),
+               dict(q=x, K=cache, V=cache, lay=held, B=2, rows=T + 1)):
+        with pytest.raises(ValueError):
+            call(**kw)
