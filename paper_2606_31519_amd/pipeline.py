@@ -241,6 +241,13 @@ class PromptAttention:
         self.ws = rbq.workspace(rbq.RBQ_OP_PREFILL, self.B, Hq, Hkv, D, self.max_k, self.total_q, device)
         self.sm_scale = 1.0 / math.sqrt(D)
 
+    def _strides(self, t):
+        """Of K or V: from a row, a head and a sequence to the next (0: packed, or the only sequence). A dimension of one
+        entry has no stride that means anything, so it takes that of contiguous rows."""
+        rows = 0 if t.dim() == 3 else 2
+        row = t.stride(rows) if t.shape[rows] > 1 else self.D if rows else self.Hkv * self.D
+        return row, t.stride(1) if self.Hkv > 1 else self.D, t.stride(0) if rows and self.B > 1 else 0
+
     def __call__(self, q, K, V, out=None, lse=None, stream=None):
         """q [total_q][Hq][D]; K, V packed [total_k][Hkv][D] or in a cache [B][Hkv][cap][D] (rows from 0, of each sequence
         its own: a cache expanded over several is refused); any strides whose last dimension (of q: two) is contiguous.
@@ -251,18 +258,19 @@ class PromptAttention:
         packed = K.dim() == 3
         want = (self.total_k, self.Hkv, D) if packed else (self.B, self.Hkv, self.max_k, D)
         rows = 0 if packed else 2
-        if (K.shape != V.shape or K.stride() != V.stride() or K.dim() not in (3, 4) or K.shape[rows] < want[rows]
-                or tuple(K.shape[:rows]) != want[:rows] or tuple(K.shape[rows + 1:]) != want[rows + 1:]):
+        if (K.shape != V.shape or K.dim() not in (3, 4) or K.shape[rows] < want[rows]
+                or tuple(K.shape[:rows]) != want[:rows] or tuple(K.shape[rows + 1:]) != want[rows + 1:]
+                or self._strides(K) != self._strides(V)):
             raise ValueError(f"K and V are {tuple(K.shape)} and {tuple(V.shape)}, the plan needs {want} and equal strides")
-        if q.stride(2) != 1 or q.stride(1) != D or K.stride(-1) != 1:
+        if q.stride(2) != 1 or (self.Hq > 1 and q.stride(1) != D) or K.stride(-1) != 1 or V.stride(-1) != 1:
             raise ValueError("the head dimension (and the heads of q) must be contiguous")
         if not packed and self.B > 1 and K.stride(0) == 0:   # (the call takes a stride of 0 for packed rows)
             raise ValueError("K and V are expanded over the sequences: each needs rows of its own")
-        lay = (K.stride(0), K.stride(1), 0) if packed else (K.stride(2), K.stride(1), K.stride(0))
+        q_ld = q.stride(0) if self.total_q > 1 else self.Hq * D
         out = torch.empty(self.total_q, self.Hq, D, dtype=q.dtype, device=q.device) if out is None else out
         if not out.is_contiguous() or (lse is not None and not lse.is_contiguous()):
             raise ValueError("out and lse must be contiguous")
-        rbq.rbq_prefill_attention(self.B, self.Hq, self.Hkv, D, q, q.stride(0), K, V, *lay, K.shape[rows], self.cu_q,
+        rbq.rbq_prefill_attention(self.B, self.Hq, self.Hkv, D, q, q_ld, K, V, *self._strides(K), K.shape[rows], self.cu_q,
                                   self.cu_k, self.total_q, self.max_k, self.causal, self.sm_scale, out, lse, self.ws, stream)
         return out
 

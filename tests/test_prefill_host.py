@@ -118,3 +118,28 @@ def test_binding_refuses_rows_that_end_early(R):
                dict(q=x, K=cache, V=cache, lay=held, B=2, rows=T + 1)):
         with pytest.raises(ValueError):
             call(**kw)
+
+
+def test_a_dimension_of_one_entry_may_have_any_stride(R, monkeypatch):
+    """One token, one key row, one KV head or one sequence, cut from larger tensors: their strides say nothing, and the
+    call is given those of contiguous rows."""
+    from paper_2606_31519_amd import pipeline
+    seen = {}
+    monkeypatch.setattr(R, "rbq_prefill_attention", lambda *a: seen.update(q_ld=a[5], lay=a[8:12], rows=a[11]))
+    H, D = 2, 64
+
+    def strides(q, K, V, q_lens, k_lens, Hq=4, Hkv=H):
+        pipeline.PromptAttention(Hq, Hkv, D, q_lens, k_lens, device="cpu")(q, K, V, stream=0)
+        return seen["q_ld"], seen["lay"]
+
+    q1 = torch.zeros(4, 1, D).transpose(0, 1)                                # [1][4][D], strides (D, D, 1)
+    far = torch.zeros(1, 1 << 16, 4, D)[:, 7]                                # [1][4][D], a row stride of 2^24
+    k1 = torch.zeros(H, 1, D).transpose(0, 1)                                # [1][2][D]
+    assert strides(q1, k1, k1, [1], [1]) == (4 * D, (H * D, D, 0, 1))
+    assert strides(far, k1, k1.contiguous(), [1], [1]) == (4 * D, (H * D, D, 0, 1))
+    c = torch.zeros(1, H, 5, D).as_strided((1, H, 5, D), (3, 5 * D, D, 1))   # one sequence
+    assert strides(q1, c, torch.zeros(1, H, 5, D), [1], [5]) == (4 * D, (D, 5 * D, 0, 5))
+    m = torch.zeros(5, 1, D).as_strided((5, 1, D), (D, 1, 1))                # one KV head
+    assert strides(q1, m, m, [1], [5], Hkv=1) == (4 * D, (D, D, 0, 5))
+    with pytest.raises(ValueError):                                          # (two heads a key apart are no such case)
+        strides(q1, c, torch.zeros(1, 5, H, D).transpose(1, 2), [1], [5])
