@@ -299,3 +299,38 @@ def test_plans_of_every_size_agree_with_whole_keys(R):
             out, lse = inp.run(R, True)
             torch.cuda.synchronize()
             check(inp, out, lse, True, heads=(0, 7))
+
+
+@pytest.mark.parametrize("dt,Hq,Hkv,D,layout", [("bf16", 4, 1, 128, "packed"), ("f32", 2, 1, 64, "cache"), ("bf16", 6, 2, 64, "cache")])
+def test_more_sequences_than_lanes_with_split_keys(R, dt, Hq, Hkv, D, layout):
+    """Few tokens in each of many sequences, over anything from no keys to thousands: the keys are split, and every split of
+    a tile runs, also behind its last key."""
+    print("many split", dt, Hq, Hkv, D, layout, flush=True)
+    rng = np.random.default_rng(12)
+    qs = [int(v) for v in rng.integers(0, 3, 70)]
+    ks = [int(v) for v in rng.choice([0, 1, 2, 63, 64, 65, 700, 1500, 2999, 4100], 70)]
+    qs[:3], ks[:3], qs[-2:], ks[-2:] = [2, 2, 1], [0, 1, 4100], [1, 2], [4100, 2]
+    inp = Inputs(31, dt, Hq, Hkv, D, qs, ks, layout)
+    assert R.rbq_workspace_bytes(R.RBQ_OP_PREFILL, 70, Hq, Hkv, D, inp.max_k, inp.T) > 0
+    for causal in (True, False):
+        out, lse = inp.run(R, causal)
+        torch.cuda.synchronize()
+        check(inp, out, lse, causal)
+
+
+def test_strides_of_single_tokens_and_rows(R):
+    """One token of a long sequence of projections, one key row, one sequence of a cache: bitwise as contiguous."""
+    from paper_2606_31519_amd import pipeline
+    Hq, Hkv, D = 4, 2, 64
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn(1, 1 << 15, Hq, D, device="cuda", generator=g).to(torch.bfloat16)
+    K, V = (torch.randn(1, Hkv, 90, D, device="cuda", generator=g).to(torch.bfloat16) for _ in range(2))
+    odd = [t.as_strided(t.shape, (0, 90 * D, D, 1)) for t in (K, V)]
+    att = pipeline.PromptAttention(Hq, Hkv, D, [1], [90])
+    got, want = att(x[:, 7], *odd), att(x[:, 7].contiguous(), K, V)
+    k1, v1 = (t[0, :, 5:6].transpose(0, 1) for t in (K, V))
+    one = pipeline.PromptAttention(Hq, Hkv, D, [1])
+    a, b = one(x[:, 9], k1, v1), one(x[:, 9].contiguous(), k1.contiguous(), v1.contiguous())
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(a, b)
+    assert torch.equal(a[0], v1[0].repeat_interleave(Hq // Hkv, dim=0))
