@@ -443,7 +443,10 @@ rbq_status rbq_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, 
  *     cached rows and window rows, clamped to [0, n] and [0, w] (its window
  *     starts at row 0 of its block of K_loc / V_loc). A selection holds rows
  *     below seq_n[b] only.
- *   A NaN in a query or an attended window row gives NaN.
+ *   A NaN or infinity in a query or an attended window key gives NaN in its heads, a NaN
+ *   in an attended window value NaN in its dimension, an infinity there that infinity
+ *   (NaN where its probability is 0). fp32 window values of 2^128 (1 - 2^-9) and more
+ *   count as infinities.
  *   RBQ_EUNSUPPORTED for a ragged batch also beyond 2^24 blocks (split, sequence, KV head).
  *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w) bytes (for one n,
  *     the size for a window serves every shorter one; so with RBQ_OP_DECODE_STEP_KV8).

@@ -37,6 +37,7 @@ namespace {
 constexpr int kScaleCap = kKv8DenseChunk / kMinKv8Block;   // scale pairs of a split
 constexpr float kLn2 = 0.69314718055994531f;
 constexpr int kPad8 = 32;                                // a row list ends on a whole group
+constexpr float kBf16Over = 0x1.FFp127f;                 // rounded to bf16, an infinity (from here on)
 
 constexpr int elem_bytes(int src) { return src == RBQ_F32 ? 4 : src == RBQ_BF16 ? 2 : 1; }
 constexpr int row_tiles(int src) { return elem_bytes(src) == 1 ? 2 : 1; }   // tiles of 16 rows per group
@@ -283,6 +284,7 @@ struct Rows {
             sv = (sv + mid) + lo;
           }
           if constexpr (kCodes) sv *= LIST ? sc[LIST ? t : 0][i].x : ts[t].x;
+          else sv = fmaf(sv, 0.f, sv);   // (an infinite key's, whatever the signs of the query's parts: NaN)
           lg[t][i] = ((mk >> (4 * t + i)) & 1u) ? sv : -INFINITY;
           tmax = fmaxf(tmax, lg[t][i]);
         }
@@ -354,6 +356,37 @@ struct Rows {
     }
   }
 };
+
+// An infinity in a value of the window meets the parts of a probability, of either sign, and
+// the zeros of the padding: NaN. Where a sum has come out so, it is the sum of the infinities
+// and NaN of its dimension, over the window rows [f0, f1) at V that the block has taken.
+template <int LOC, int D>
+__device__ __forceinline__ void infinite_values(const char* __restrict__ V, int f0, int f1, f32x4 (&acc)[D / 16]) {
+  float t = 0.f;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t = fmaf(acc[c][i], 0.f, t);
+  if (!__ballot(t != t)) return;
+  float odd[D / 16];
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) odd[c] = 0.f;
+  const int first = D / 16 * (lane_id() & 15);   // the lane's dimensions
+#pragma unroll 1
+  for (int r = f0; r < f1; ++r) {
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) {
+      float v;
+      if constexpr (LOC == RBQ_F32) v = reinterpret_cast<const float*>(V)[r * D + first + c];
+      else v = __uint_as_float(uint32_t(reinterpret_cast<const uint16_t*>(V)[r * D + first + c]) << 16);
+      odd[c] += fabsf(v) < kBf16Over ? 0.f : v == v ? copysignf(INFINITY, v) : v;
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc[c][i] = fabsf(acc[c][i]) < INFINITY || odd[c] == 0.f ? acc[c][i] : odd[c];
+}
 
 // A block's sequence, KV head and place s among its group's blocks: idx of them over
 // the sequence's nb cached rows, then win over its wb window rows.
@@ -512,6 +545,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
     stage();
     __syncthreads();
     rows.run(m, lsum, acc);
+    infinite_values<LOC, D>(Vb, c0, c1, acc);
   } else if constexpr (SPARSE) {
     stage();
     const int U = build_union_list<G, kDThreads, true, kPad8, true>(sel_idx, sel_mask, mask_words, row0, n, c0, c1, 0, 0, sh.bm,
@@ -529,6 +563,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_kv8_kernel(
       Rows<LOC, false, G, D, 0, S> rows(sh, make_rsrc(K_loc + locb, size), make_rsrc(V_loc + locb, size), f0, f1 - f0, 0);
       rows.begin();
       rows.run(m, lsum, acc);
+      infinite_values<LOC, D>(V_loc + locb, f0, f1, acc);
     }
   } else {
     Rows<FMT, false, G, D, kStream, S> rows(sh, Kr, Vr, c0, c1 - c0, bshift);

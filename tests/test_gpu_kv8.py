@@ -550,3 +550,70 @@ def test_rows_at_the_tail_of_a_longer_cache(R, dt, D):
         res.append((*c, *s, *outs, *(t[:, :, :w] for t in view)))
     for a, b in zip(*res):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,D,n,w,ldt", [
+    (2, 8, 2, 128, 700, 40, "bf16"),
+    (2, 16, 2, 64, 700, 300, "f32"),
+    (1, 16, 1, 128, 0, 17, "f32"),
+    (2, 2, 2, 128, 100, 1, "bf16"),
+    (8, 32, 8, 64, 15700, 300, "bf16"),      # sparse: windows taken along by the last splits
+    (8, 8, 8, 128, 15700, 200, "f32"),
+])
+def test_infinities_in_the_window(R, B, Hq, Hkv, D, n, w, ldt):
+    """An infinity in a value of the window is the result in its dimension (one of each sign, or a NaN: NaN), and every
+    other dimension, and every other KV head, keeps its bits; one in a key or a query gives its heads NaN."""
+    print("inf", B, Hq, Hkv, D, n, w, ldt, flush=True)
+    block, G, tau = 64, Hq // Hkv, 0.05
+    rng = np.random.default_rng(D + w)
+    cap = n + 1
+    c8 = cache_of(rng.integers(0, 128, (B, Hkv, cap, D)).astype(np.uint8), "int8")
+    s = dev(rng.uniform(0.005, 0.01, (B, Hkv, (cap + block - 1) // block)).astype(np.float32))
+    q = dev(rng.standard_normal((B, Hq, D)).astype(np.float32))
+    K, V = (dev(rng.standard_normal((B, Hkv, w, D)), DT[ldt]) for _ in range(2))
+    sel = torch.arange(max(n, 1), dtype=torch.int32, device="cuda").expand(B, Hq, max(n, 1)).contiguous()
+    cnt = torch.full((B, Hq), n // 3, dtype=torch.int32, device="cuda")
+    seq_w = torch.full((B,), w, dtype=torch.int32, device="cuda")
+
+    def run():
+        res = []
+        for sparse in (False, True):
+            for ragged in (False, True):
+                out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+                ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+                head, loc = (B, Hq, Hkv, D, q, c8, c8, block, s, s, cap, n), (K, V, w, w, tau, out, lse, ws)
+                seqs = (None, seq_w) if ragged else (None, None)
+                if sparse:
+                    R.rbq_sparse_decode_kv8(*head, sel, cnt, *loc, *seqs)
+                else:
+                    R.rbq_dense_decode_kv8(*head, *loc, *seqs)
+                torch.cuda.synchronize()
+                res.append((out, lse))
+        return res
+
+    same = lambda a, b: bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())  # noqa: E731
+    inf, nan = float("inf"), float("nan")
+    clean = run()
+    b, hk = B - 1, Hkv - 1
+    heads = slice(hk * G, (hk + 1) * G)
+    V[b, hk, w // 2, 5], V[b, hk, w - 1, D - 1], V[b, hk, 0, 6] = inf, -inf, nan
+    marks = {5: inf, D - 1: -inf, 6: nan}
+    if w > 1:
+        V[b, hk, 0, 7], V[b, hk, w - 1, 7] = inf, -inf
+        marks[7] = nan
+    if ldt == "f32":
+        V[b, hk, w // 3, 8] = -3.4e38        # beyond bf16's range: counts as an infinity
+        marks[8] = -inf
+    got = run()
+    for (out, lse), (o, l) in zip(got, clean):
+        want = o.clone()
+        for d, v in marks.items():
+            want[b, heads, d] = v
+        assert same(out, want) and torch.equal(lse, l)
+    K[b, hk, w // 2, 3] = -inf
+    q[0, 0, 1] = inf
+    for (out, lse), (o, l) in zip(run(), got):
+        want, wl = o.clone(), l.clone()
+        for t in (want, wl):
+            t[b, heads], t[0, 0] = nan, nan
+        assert same(out, want) and same(lse, wl)
