@@ -71,11 +71,11 @@ def build(verbose: bool = False) -> str:
     tmp = LIB_PATH + ".tmp"
     _run([hipcc, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs], verbose)
     os.replace(tmp, LIB_PATH)
-    tmp = CALL_PATH + ".tmp"
+    _write_build_info()
+    tmp = CALL_PATH + ".tmp"   # (last: the library serves without it, but for the calls that go through it)
     _run(["g++", *CXX_FLAGS, "-shared", "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "pycall.cpp"), "-o",
           tmp], verbose)
     os.replace(tmp, CALL_PATH)
-    _write_build_info()
     return LIB_PATH
 
 

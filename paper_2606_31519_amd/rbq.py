@@ -118,12 +118,19 @@ def _load():
 lib = _load()
 
 
+class _NoCalls:
+    """In the call module's place where it is not built: the calls that go through it raise ImportError."""
+
+    def __getattr__(self, name):
+        raise ImportError("_rbqcall.so is not built (it takes CPython's headers); run paper_2606_31519_amd.build.build() first")
+
+
 def _load_calls():
     """The call module, bound to the loaded library's entry points."""
     try:
         from . import _rbqcall
-    except ImportError as e:
-        raise ImportError("_rbqcall.so is not built; run paper_2606_31519_amd.build.build() first") from e
+    except ImportError:
+        return _NoCalls()
     _rbqcall.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8", "rbq_decode_step_kv8",
         "rbq_prefill_attention")))

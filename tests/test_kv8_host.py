@@ -251,3 +251,25 @@ def test_rows_may_be_the_tail_of_a_longer_buffer(R):
         for short in (x[:, :, n + 1:], x[:1, :, n:], tail.contiguous(), x[:1].expand(B, -1, -1, -1)):
             with pytest.raises(ValueError):
                 call(short, w)
+
+
+def test_without_its_call_module_the_binding_has_the_other_calls():
+    """The library's calls through ctypes do not need the call module: it is asked for where a call goes through it."""
+    import subprocess
+    import sys
+    code = """if True:
+        import sys
+        sys.modules["paper_2606_31519_amd._rbqcall"] = None      # (an import of it fails)
+        import torch
+        from paper_2606_31519_amd import pipeline, rbq
+        assert rbq.rbq_version() > 0 and rbq.rbq_workspace_bytes(rbq.RBQ_OP_TOPP, 1, 8, 2, 128, 100) > 0
+        x, c, s = torch.zeros(1, 1, 4, 64), torch.zeros(1, 1, 16, 64, dtype=torch.int8), torch.zeros(1, 1, 1)
+        try:
+            rbq.rbq_quantize_kv(1, 1, 64, x, x, 4, 4, 0, 16, 16, c, c, s, s)
+        except ImportError as e:
+            assert "_rbqcall" in str(e)
+            print("refused")
+    """
+    from conftest import ROOT
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "refused", r.stderr
