@@ -617,3 +617,27 @@ def test_infinities_in_the_window(R, B, Hq, Hkv, D, n, w, ldt):
         for t in (want, wl):
             t[b, heads], t[0, 0] = nan, nan
         assert same(out, want) and same(lse, wl)
+
+
+@pytest.mark.parametrize("sparse", [False, True])
+def test_row_counts_of_their_own_beside_equal_windows(R, sparse):
+    """seq_n without seq_w: every sequence has all w window rows, bitwise as where seq_w says so."""
+    B, Hq, Hkv, D, block, n, w, tau = 3, 8, 2, 64, 16, 900, 270, 0.1
+    g = torch.Generator(device="cuda").manual_seed(6)
+    c8 = torch.randint(-127, 128, (B, Hkv, n, D), dtype=torch.int8, device="cuda", generator=g)
+    s = 0.01 + 0.01 * torch.rand(B, Hkv, (n + block - 1) // block, device="cuda", generator=g)
+    K, V = (torch.randn(B, Hkv, w, D, device="cuda", generator=g) for _ in range(2))
+    q = torch.randn(B, Hq, D, device="cuda", generator=g)
+    sel = torch.arange(n, dtype=torch.int32, device="cuda").expand(B, Hq, n).contiguous()
+    seq_n = torch.tensor([900, 0, 511], dtype=torch.int32, device="cuda")
+    cnt = (seq_n // 5)[:, None].expand(B, Hq).contiguous()
+    outs = []
+    for seq_w in (None, torch.full((B,), w, dtype=torch.int32, device="cuda")):
+        out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+        ws = R.workspace(R.RBQ_OP_DECODE_KV8, B, Hq, Hkv, D, n, w)
+        ws.fill_(255)
+        head, loc = (B, Hq, Hkv, D, q, c8, c8, block, s, s, n, n), (K, V, w, w, tau, out, lse, ws, seq_n, seq_w)
+        R.rbq_sparse_decode_kv8(*head, sel, cnt, *loc) if sparse else R.rbq_dense_decode_kv8(*head, *loc)
+        outs.append((out, lse))
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1]) and torch.isfinite(outs[0][0]).all()
