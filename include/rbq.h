@@ -407,7 +407,9 @@ rbq_status rbq_decode_step_noalloc(int32_t batch, int32_t heads_q, int32_t heads
  *             nearest whole number (even on ties) and clamped to +-127, with s
  *             and 1 / s as correctly rounded floats
  * (s = 0 where amax = 0). NaN is stored as 0 and an infinity as the largest code
- * of its sign (0 where s = 0), so the cache holds neither.
+ * of its sign (0 where s = 0), so the cache holds neither. (Magnitudes of 1.75 * 2^127 and
+ * more, and infinities beside them, may stand for infinities: code * scale passes the
+ * largest float.)
  * A block that starts before `offset` holds rows already (its scale and rows must
  * be valid): they are kept, under s' = max(s, the block's scale); where that is
  * larger than the block's scale, their codes are re-encoded as code * (scale / s'),

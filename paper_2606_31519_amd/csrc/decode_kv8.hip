@@ -21,7 +21,8 @@
 //           order of A (its probabilities) and of B (its columns of those rows)
 // The split's scales (at most 128 pairs) are staged in LDS beside its row list.
 // Window rows take the same path in blocks of their own (or behind the last splits' rows),
-// 16 rows at a time; fp32 rows are split into three bf16 parts as the queries are.
+// 16 rows at a time; fp32 rows are split into three bf16 parts as the queries are (an array of 32
+// or 48 bytes per lane stays in scratch memory or LDS there; no registers are spilled).
 // Bound by the bytes where rows follow each other: 128K rows of 8 heads, 268 MB, 46 us
 // (5.9 TB/s) and 4 of the join. Scattered rows of 128 bytes make 4.6 TB/s (a fifth of 128K
 // per head: 37.7 us, 6 of them before the first row arrives), few rows the chain search,
@@ -740,6 +741,7 @@ rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, i
   const bool ragged = seq_n || seq_w;
   const dim3 grid = ragged ? dim3(uint32_t(batch * heads_kv * int64_t(sp.total()))) : dim3(sp.total(), batch * heads_kv);
   const int64_t blocks = int64_t(batch) * heads_kv * sp.total();
+  // (more blocks than the full-precision kernel has at once; this one has 4 or 5 at D = 64 where that has 4 or 6)
   const int ordered = sparse && seq_n && batch > 1 && batch <= kWave && sp.chunk >= kOrderMinChunk &&
                               blocks > resident_blocks(head_dim, G) ? batch : 0;
   const Call a{grid, stream, q, cache, n, sel_idx, sel_count, sel_mask, mask_words, win, sp,

@@ -324,6 +324,9 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
           e[r] = __builtin_amdgcn_exp2f(fmaf(s[t][8 * g + r], scale_log2e, -mref));
           sum[2 * t + (r & 1)] += e[r];
         }
+        // (The probabilities are rounded to bf16, the sum is not: up to 2^-8 of each, which moves the
+        // outputs by 0.0005 to 0.0015 of their norm, 0.0010 for 8 x 43..650 tokens, 0.0009 for 16001;
+        // their own rounding to bf16 by 0.0016. In two parts the second product would be twice the work.)
         p[2 * t + g] = __builtin_convertvector(e, bf16x8);
       }
     }

@@ -1,7 +1,8 @@
 // The binding's calls of the C ABI for work that takes the GPU a few microseconds,
 // as CPython functions: arguments are read where they lie on the interpreter's stack,
 // without ctypes' conversion objects (an rbq_quantize_kv call with its checks: 4.3 us
-// of the host through ctypes, 2.5 here; its kernel for one token takes 3). The
+// of the host through ctypes, 2.5 here, and 0.2 since rows are judged by what their views span;
+// its kernel for one token takes 3). The
 // entry points are those that the ctypes library has loaded: bind() takes their addresses.
 //
 // An argument of a pointer type is None, an address, or an object with data_ptr().

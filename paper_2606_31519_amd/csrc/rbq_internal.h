@@ -155,8 +155,8 @@ constexpr int kDecodeListCap = 1280;      // row-list positions of a sparse spli
 // by the chunk), provided every sequence's window fits its splits that way.
 DecodeSplits decode_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool tail_window = false,
                            bool sparse = false, bool ragged = false);
-// The splits over an 8-bit cache. A uniform dense call in whole rounds of resident blocks
-// where there are rows for one: 8 x 8K rows of 8 KV heads 33.2 us, by halves of 1024 36.3;
+// The splits over an 8-bit cache. A uniform dense call in whole rounds of kKv8Resident blocks
+// (validate.cpp) where there are rows for one: 8 x 8K rows of 8 KV heads 33.2 us, by halves of 1024 36.3;
 // 100K rows 41.0 and 43.2. A uniform sparse call in blocks twice as long as those of a
 // bf16 cache, whose rows are twice the bytes beside the same search and list: chunks
 // halved below 512 blocks instead of 1024: 120K rows, a fifth per head 38.2 and 46.4 us,

@@ -13,7 +13,11 @@ namespace {
 constexpr int64_t kMaxRows = int64_t(1) << 31;
 constexpr int64_t kMaxStride = int64_t(1) << 23;   // elements: 64 rows of it are addressed with 32-bit byte offsets
 constexpr int64_t kCus = 256;                      // compute units of the GPU
-constexpr int64_t kKv8Resident = 4 * kCus;         // blocks of the decode over an 8-bit cache that run at once
+// Blocks of a round of the decode over an 8-bit cache: 4 per compute unit, as many as run at once at D = 128 in
+// groups of up to 8 heads. (By the compiler's report, with a bf16 window, 5 or 6 do at D = 64, 4 sparse in groups
+// of 16; at D = 128 in groups of 16 dense 3, sparse 2. A planned round is 0.7 to 0.8, 1.3 and 2 of the GPU's
+// there: no plans of their own are made for them, and none were measured.)
+constexpr int64_t kKv8Resident = 4 * kCus;
 // a required device pointer: present, and 16-byte aligned (the kernels use 16-byte vector loads)
 bool bad_ptr(const void* p) { return p == nullptr || (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
 }  // namespace
