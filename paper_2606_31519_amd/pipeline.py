@@ -235,6 +235,8 @@ class PromptAttention:
         if len(q_lens) != len(k_lens) or not len(q_lens) or min(min(q_lens), min(k_lens)) < 0:
             raise ValueError("one length of at least 0 per sequence, for the queries and for the keys")
         self.B, self.Hq, self.Hkv, self.D, self.causal = len(q_lens), Hq, Hkv, D, causal
+        if max(sum(map(int, q_lens)), sum(map(int, k_lens))) >= 1 << 31:   # (the call counts in int32)
+            raise ValueError("2^31 tokens or keys and more")
         cu_q, cu_k = (np.concatenate([[0], np.cumsum(v)]).astype(np.int32) for v in (q_lens, k_lens))
         self.total_q, self.total_k, self.max_k = int(cu_q[-1]), int(cu_k[-1]), int(max(k_lens))
         self.cu_q, self.cu_k = (torch.from_numpy(c).to(device) for c in (cu_q, cu_k))

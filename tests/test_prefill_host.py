@@ -143,3 +143,10 @@ def test_a_dimension_of_one_entry_may_have_any_stride(R, monkeypatch):
     assert strides(q1, m, m, [1], [5], Hkv=1) == (4 * D, (D, D, 0, 5))
     with pytest.raises(ValueError):                                          # (two heads a key apart are no such case)
         strides(q1, c, torch.zeros(1, 5, H, D).transpose(1, 2), [1], [5])
+
+
+def test_a_plan_of_more_tokens_than_the_call_counts_is_refused():
+    from paper_2606_31519_amd import pipeline
+    for q, k in (([1 << 31], None), ([1 << 30, 1 << 30], None), ([1, 1], [1 << 30, 1 << 30])):
+        with pytest.raises(ValueError, match="2\\^31"):
+            pipeline.PromptAttention(4, 2, 64, q, k, device="cpu")
