@@ -60,6 +60,8 @@ typedef enum rbq_dtype { RBQ_F32 = 0, RBQ_BF16 = 1 } rbq_dtype;
 
 /* formats of the 8-bit cache (arguments named kv8_dtype; no other call takes them) */
 typedef enum rbq_kv8_dtype { RBQ_E4M3 = 16, RBQ_I8 = 17 } rbq_kv8_dtype;
+/* formats of the 4-bit cache (arguments named kv4_dtype; no other call takes them) */
+typedef enum rbq_kv4_dtype { RBQ_FP4 = 32, RBQ_I4 = 33 } rbq_kv4_dtype;
 
 /* flags of rbq_encode_keys */
 #define RBQ_ENCODE_SET_CENTROID 1u
@@ -73,6 +75,9 @@ typedef enum rbq_kv8_dtype { RBQ_E4M3 = 16, RBQ_I8 = 17 } rbq_kv8_dtype;
 #define RBQ_OP_DECODE_KV8 6       /* rbq_sparse_decode_kv8 and rbq_dense_decode_kv8 */
 #define RBQ_OP_DECODE_STEP_KV8 8
 #define RBQ_OP_PREFILL 7          /* rbq_prefill_attention: n = max_k, w = total_q */
+#define RBQ_OP_DECODE_KV4 9       /* rbq_sparse_decode_kv4 and rbq_dense_decode_kv4 */
+#define RBQ_OP_DECODE_STEP_KV4 10
+#define RBQ_OP_PREFILL_KV4 11     /* rbq_prefill_attention_kv4: n = its n, w = total_q */
 
 #define RBQ_QSCAL_STRIDE 8   /* floats per query head in qscal */
 #define RBQ_MAX_WINDOW 4096  /* largest local window accepted by the decode calls */
@@ -525,6 +530,106 @@ rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_k
                                  const int32_t* cu_q, const int32_t* cu_k, int32_t total_q, int32_t max_k,
                                  int32_t causal, float sm_scale, void* out, float* lse, void* ws, size_t ws_bytes,
                                  hipStream_t stream);
+
+/*
+ * The 4-bit cache -- K and V rows as four bits per value with scales of each row's own: a
+ * quarter of a bf16 cache's bytes (D + 8 per row and KV head). As with the 8-bit cache the
+ * newest rows stay in full precision in the local window and enter when it is flushed; a row
+ * stands by itself, so writing rows changes no others.
+ *   KV4  [B][Hkv][cap][D] bytes: a row's record, D / 2 bytes of K's codes, then D / 2 of V's
+ *   par  [B][Hkv][cap][2] uint32: the words of K's and of V's row
+ * In format kv4_dtype:
+ *   RBQ_FP4  e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), dimension d in bits
+ *            4 (d % 2) .. +4 of byte d / 2. Byte g of the word is the exponent (e8m0) of the
+ *            D / 4 dimensions from g D / 4 on: a value is e2m1 * 2^(byte - 127) (0 where the byte is 0).
+ *   RBQ_I4   whole numbers c of 0 to 15, dimension d in nibble (d % 8) / 2 + 4 (d % 2) of the
+ *            32-bit word d / 8 (even dimensions in its low half). The low half of the row's word
+ *            is a bf16 step s, the high half a bf16 base m: a value is c s + m, as a float.
+ *
+ * rbq_quantize_kv4 writes n_new rows per (b, kv-head), K_new / V_new [B][Hkv][ld][D] rows
+ * [0, n_new) in dtype RBQ_F32 or RBQ_BF16, as cache rows [offset, offset + n_new):
+ *   RBQ_FP4: per group, amax is its largest finite magnitude, e the smallest exponent of -126
+ *            to 125 such that amax <= 7 * 2^e (125 if there is none); codes are x / 2^e rounded
+ *            to nearest even, at most 6 (a group without a finite value other than 0: byte 0,
+ *            codes 0)
+ *   RBQ_I4:  lo and hi are the row's smallest and largest finite values (0 without any), each
+ *            clamped to +-2^126; m is lo rounded down to bf16, d = hi - m, s is d / 15 rounded up to
+ *            bf16 and at least 2^-126 (0 where d = 0); codes are (x - m) * (1 / s) rounded to the nearest
+ *            whole number (even on ties) and clamped to 0 .. 15, with d, d / 15, x - m and
+ *            1 / s as correctly rounded floats
+ * NaN is stored as 0 (RBQ_I4: as the code nearest to 0), an infinity as the last code on its
+ * side (0 in a group of zeros; RBQ_I4: 0 where s = 0), so that a cache holds finite values only.
+ *   seq_off, seq_new: NULL, or [B] int32 (device): sequence b's own offset and
+ *     count, clamped to [0, offset] and [0, n_new].
+ *   RBQ_EINVAL also where (offset + n_new) * D >= 2^31.
+ */
+rbq_status rbq_quantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K_new, const void* V_new,
+                            int32_t dtype, int64_t ld, int32_t n_new, int32_t offset, int32_t cap, int32_t kv4_dtype,
+                            void* KV4, uint32_t* par, const int32_t* seq_off, const int32_t* seq_new,
+                            hipStream_t stream);
+
+/* rbq_dequantize_kv4 -- cache rows [offset, offset + n_rows) back as rows [0, n_rows) of K / V
+ * [B][Hkv][ld][D] in dtype RBQ_F32 or RBQ_BF16 (the values as floats, those rounded to bf16).
+ * seq_off, seq_rows: as seq_off, seq_new of rbq_quantize_kv4; rows behind a sequence's own
+ * are left as they were. */
+rbq_status rbq_dequantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* KV4, const uint32_t* par,
+                              int32_t kv4_dtype, int32_t cap, int32_t n_rows, int32_t offset, void* K, void* V,
+                              int32_t dtype, int64_t ld, const int32_t* seq_off, const int32_t* seq_rows,
+                              hipStream_t stream);
+
+/*
+ * rbq_dense_decode_kv4 / rbq_sparse_decode_kv4 -- rbq_dense_decode_kv8 and
+ * rbq_sparse_decode_kv8 over the 4-bit cache: exact attention (fp32 accumulation) over the
+ * values that its rows [0, n), or the selected ones, stand for, plus the window. Everything
+ * else as in those calls, ws: RBQ_OP_DECODE_KV4.
+ */
+rbq_status rbq_dense_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                const void* KV4, const uint32_t* par, int32_t kv4_dtype, int32_t cap, int32_t n,
+                                const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                                float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                                const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream);
+rbq_status rbq_sparse_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                 const void* KV4, const uint32_t* par, int32_t kv4_dtype, int32_t cap, int32_t n,
+                                 const int32_t* sel_idx, const int32_t* sel_count,
+                                 const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                                 float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                                 const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream);
+
+/*
+ * rbq_decode_step_kv4 -- rbq_decode_step_kv8 over the 4-bit cache: its outputs are bitwise
+ * those of the sequence of calls named there with rbq_sparse_decode_kv4 and rbq_quantize_kv4.
+ *   ws: at least rbq_workspace_bytes(RBQ_OP_DECODE_STEP_KV4, B, Hq, Hkv, D, n, w) bytes.
+ */
+rbq_status rbq_decode_step_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                               const float* P, const float* c_q, const float* c_k, void* KV4, uint32_t* par,
+                               int32_t kv4_dtype, int32_t cap, int32_t n,
+                               const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                               uint32_t* codes, float* kfac, uint16_t* kfac16, int32_t flush, float p, float sm_scale,
+                               uint32_t* qplanes, float* qscal, float* scores, int32_t* sel_idx, int32_t* sel_count,
+                               float* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream);
+
+/*
+ * rbq_prefill_attention_kv4 -- rbq_prefill_attention of chunks of prompts whose earlier rows
+ * are in the 4-bit cache: token i of sequence b attends over its cached rows [0, n_b) and the
+ * rows of its own chunk in full precision, those of tokens j <= i (causal) or all of them. So a
+ * session's next turn, or drafted tokens that are to be checked, need no full-precision
+ * copy of the cache.
+ *   q, q_ld, cu_q, total_q, dtype, out, lse, sm_scale: as in rbq_prefill_attention
+ *   K, V   the chunks' rows, packed like q: KV head h of token t at K + t * kv_ld + h * kv_head (kv_ld >= D)
+ *   KV4, par, kv4_dtype, cap: the cache; n: the most rows that a sequence has there (n <= cap);
+ *   seq_n  NULL (n rows each), or [B] int32 (device): n_b, clamped to [0, n]
+ *   ws:    at least rbq_workspace_bytes(RBQ_OP_PREFILL_KV4, B, Hq, Hkv, D, n, total_q) bytes,
+ *          0 (then NULL is allowed) unless few rows attend to long keys.
+ * With RBQ_BF16 the cached values (RBQ_I4) and the probabilities are rounded to bf16 before
+ * they meet the products. Everything else as in rbq_prefill_attention. RBQ_EINVAL also where
+ * n * D >= 2^31.
+ */
+rbq_status rbq_prefill_attention_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                                     const void* q, int64_t q_ld, const void* K, const void* V, int32_t dtype,
+                                     int64_t kv_ld, int64_t kv_head, const int32_t* cu_q, int32_t total_q,
+                                     const void* KV4, const uint32_t* par, int32_t kv4_dtype, int32_t cap, int32_t n,
+                                     const int32_t* seq_n, int32_t causal, float sm_scale, void* out, float* lse,
+                                     void* ws, size_t ws_bytes, hipStream_t stream);
 
 /*
  * rbq_mapped_device_pointer -- the device address of pinned host memory

@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(HERE, "librbq.so")
 CALL_PATH = os.path.join(HERE, "_rbqcall.so")   # the Python binding's own (csrc/pycall.cpp)
 
 HIP_SOURCES = ["api.hip", "score.hip", "quantize.hip", "encode.hip", "topp.hip", "decode.hip", "kv8.hip",
-               "decode_kv8.hip", "prefill.hip"]
+               "decode_kv8.hip", "prefill.hip", "kv4.hip", "decode_kv4.hip"]
 CXX_SOURCES = ["validate.cpp"]          # plain C++ (no HIP): host-side argument checks
 
 ARCH = "gfx950"
@@ -37,10 +37,10 @@ HIP_FLAGS = [
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
 ]
 CXX_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-Wall"]
-# per-source additions: the decode kernels (of both caches) keep their MFMA accumulators in
+# per-source additions: the decode kernels (of every cache) keep their MFMA accumulators in
 # ordinary VGPRs (the softmax rescales them with vector ALU ops; accumulation
 # registers would cost copies and a wave per SIMD)
-EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("decode.hip", "decode_kv8.hip")}
+EXTRA_FLAGS = {src: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for src in ("decode.hip", "decode_kv8.hip", "decode_kv4.hip")}
 
 
 def _run(cmd, verbose):

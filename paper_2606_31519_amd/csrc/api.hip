@@ -430,6 +430,61 @@ rbq_status rbq_decode_step_varlen_f16(int32_t batch, int32_t heads_q, int32_t he
 
 }  // extern "C"
 
+namespace {
+// rbq_decode_step over a cache of quantised rows and a window of its own buffers: the cache's
+// checks and launches of its attention and of the flush's rows are the caller's.
+template <class CheckDecode, class CheckWrite, class Decode, class Write>
+rbq_status decode_step_over(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                            const float* P, const float* c_q, const float* c_k, int32_t cap, int32_t n,
+                            const Kv8Window& win, uint32_t* codes, float* kfac, uint16_t* kfac16, int32_t flush, float p,
+                            float sm_scale, uint32_t* qplanes, float* qscal, float* scores, int32_t* sel_idx,
+                            int32_t* sel_count, void* ws, size_t ws_bytes, hipStream_t stream, CheckDecode check_dec,
+                            CheckWrite check_write, Decode decode, Write write) {
+  const int32_t w = win.w;
+  const void* fac = kfac16 != nullptr ? static_cast<const void*>(kfac16) : kfac;
+  if ((kfac != nullptr) == (kfac16 != nullptr) || (kfac16 != nullptr && c_q != nullptr)) return RBQ_EINVAL;
+  rbq_status s = check_heads(batch, heads_q, heads_kv, head_dim);
+  if (s != RBQ_OK) return s;
+  if (n < 0 || w < 0) return RBQ_EINVAL;
+  const StepWorkspace sw = step_workspace(ws, batch, heads_q, heads_kv, head_dim, n, w, true);
+  if (ws == nullptr || ws_bytes < sw.bytes) return RBQ_EINVAL;
+  const bool do_flush = flush != 0 && w > 0;
+  if ((s = check_quantize(batch, heads_q, heads_kv, head_dim, q, P, c_k, qplanes, qscal)) != RBQ_OK) return s;
+  if ((s = check_score(batch, heads_q, heads_kv, head_dim, n, cap, codes, fac, qplanes, qscal, scores)) != RBQ_OK)
+    return s;
+  if ((s = check_topp(batch, heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, sw.topp_bytes)) != RBQ_OK)
+    return s;
+  if ((s = check_dec(sw, decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w, true))) != RBQ_OK) return s;
+  if (do_flush) {
+    if ((s = check_encode(batch, heads_kv, head_dim, win.K, win.dtype, win.ld, w, n, cap, P, c_k, codes, fac, 0u, nullptr,
+                          0)) != RBQ_OK)
+      return s;
+    if ((s = check_write()) != RBQ_OK) return s;
+  }
+
+  if (!do_flush && quantize_score_fused(batch, heads_q, heads_kv, n, head_dim)) {
+    s = launch_quantize_score(batch, heads_q, heads_kv, n, cap, q, P, c_q, c_k, qplanes, qscal, codes, kfac, kfac16,
+                              scores, stream, head_dim);
+  } else {
+    if (do_flush)
+      s = launch_quantize_flush(batch, heads_q, heads_kv, q, P, c_q, c_k, qplanes, qscal, win.K, win.dtype, win.ld, w, n,
+                                cap, codes, kfac, stream, nullptr, nullptr, 0, kfac16, head_dim);
+    else
+      s = launch_quantize(batch, heads_q, heads_kv, q, P, c_q, c_k, qplanes, qscal, nullptr, stream, 4, head_dim);
+    if (s != RBQ_OK) return s;
+    s = launch_score(batch, heads_q, heads_kv, n, cap, codes, kfac, qplanes, qscal, scores, nullptr, nullptr, stream,
+                     nullptr, kfac16, 4, head_dim);
+  }
+  if (s != RBQ_OK) return s;
+  s = launch_topp(batch * heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, stream, sw.masks);
+  if (s != RBQ_OK) return s;
+  s = decode(sw);
+  // (last: it may re-encode rows that the attention reads)
+  if (s == RBQ_OK && do_flush) s = write();
+  return s;
+}
+}  // namespace
+
 extern "C" {
 
 rbq_status rbq_quantize_kv(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K_new, const void* V_new,
@@ -494,55 +549,106 @@ rbq_status rbq_decode_step_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv,
                                float* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
   const Kv8Cache c{K8, V8, k_scale, v_scale, kv8_dtype, block, cap};
   const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
-  const void* fac = kfac16 != nullptr ? static_cast<const void*>(kfac16) : kfac;
-  if ((kfac != nullptr) == (kfac16 != nullptr) || (kfac16 != nullptr && c_q != nullptr)) return RBQ_EINVAL;
-  rbq_status s = check_heads(batch, heads_q, heads_kv, head_dim);
-  if (s != RBQ_OK) return s;
-  if (n < 0 || w < 0) return RBQ_EINVAL;
-  const StepWorkspace sw = step_workspace(ws, batch, heads_q, heads_kv, head_dim, n, w, true);
-  if (ws == nullptr || ws_bytes < sw.bytes) return RBQ_EINVAL;
-  const bool do_flush = flush != 0 && w > 0;
-  if ((s = check_quantize(batch, heads_q, heads_kv, head_dim, q, P, c_k, qplanes, qscal)) != RBQ_OK) return s;
-  if ((s = check_score(batch, heads_q, heads_kv, head_dim, n, cap, codes, fac, qplanes, qscal, scores)) != RBQ_OK)
-    return s;
-  if ((s = check_topp(batch, heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, sw.topp_bytes)) != RBQ_OK)
-    return s;
-  if ((s = check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win, sm_scale, out,
-                            sw.decode, decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w, true),
-                            nullptr, nullptr)) != RBQ_OK)
-    return s;
-  if (do_flush) {
-    if ((s = check_encode(batch, heads_kv, head_dim, K_loc, loc_dtype, loc_ld, w, n, cap, P, c_k, codes, fac, 0u, nullptr,
-                          0)) != RBQ_OK)
-      return s;
-    if ((s = check_quantize_kv(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, block, kv8_dtype, K8,
-                               V8, k_scale, v_scale, nullptr, nullptr)) != RBQ_OK)
-      return s;
-  }
+  return decode_step_over(
+      batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, cap, n, win, codes, kfac, kfac16, flush, p, sm_scale, qplanes,
+      qscal, scores, sel_idx, sel_count, ws, ws_bytes, stream,
+      [&](const StepWorkspace& sw, size_t bytes) {
+        return check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win, sm_scale, out,
+                                sw.decode, bytes, nullptr, nullptr);
+      },
+      [&] {
+        return check_quantize_kv(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, block, kv8_dtype,
+                                 K8, V8, k_scale, v_scale, nullptr, nullptr);
+      },
+      [&](const StepWorkspace& sw) {
+        return launch_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, sel_idx, sel_count, win, sm_scale, out, lse,
+                                 sw.decode, true, stream, sw.masks, topp_mask_words(n));
+      },
+      [&] {
+        return launch_quantize_kv(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, block, kv8_dtype,
+                                  K8, V8, k_scale, v_scale, nullptr, nullptr, stream);
+      });
+}
 
-  if (!do_flush && quantize_score_fused(batch, heads_q, heads_kv, n, head_dim)) {
-    s = launch_quantize_score(batch, heads_q, heads_kv, n, cap, q, P, c_q, c_k, qplanes, qscal, codes, kfac, kfac16,
-                              scores, stream, head_dim);
-  } else {
-    if (do_flush)
-      s = launch_quantize_flush(batch, heads_q, heads_kv, q, P, c_q, c_k, qplanes, qscal, K_loc, loc_dtype, loc_ld, w, n,
-                                cap, codes, kfac, stream, nullptr, nullptr, 0, kfac16, head_dim);
-    else
-      s = launch_quantize(batch, heads_q, heads_kv, q, P, c_q, c_k, qplanes, qscal, nullptr, stream, 4, head_dim);
-    if (s != RBQ_OK) return s;
-    s = launch_score(batch, heads_q, heads_kv, n, cap, codes, kfac, qplanes, qscal, scores, nullptr, nullptr, stream,
-                     nullptr, kfac16, 4, head_dim);
-  }
+rbq_status rbq_quantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K_new, const void* V_new,
+                            int32_t dtype, int64_t ld, int32_t n_new, int32_t offset, int32_t cap, int32_t kv4_dtype,
+                            void* KV4, uint32_t* par, const int32_t* seq_off, const int32_t* seq_new,
+                            hipStream_t stream) {
+  const Kv4Cache c{KV4, par, kv4_dtype, cap};
+  const rbq_status s =
+      check_quantize_kv4(batch, heads_kv, head_dim, K_new, V_new, dtype, ld, n_new, offset, c, seq_off, seq_new);
   if (s != RBQ_OK) return s;
-  s = launch_topp(batch * heads_q, n, scores, p, sm_scale, sel_idx, sel_count, sw.topp, stream, sw.masks);
+  return launch_quantize_kv4(batch, heads_kv, head_dim, K_new, V_new, dtype, ld, n_new, offset, cap, kv4_dtype, KV4, par,
+                             seq_off, seq_new, stream);
+}
+
+rbq_status rbq_dequantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* KV4, const uint32_t* par,
+                              int32_t kv4_dtype, int32_t cap, int32_t n_rows, int32_t offset, void* K, void* V,
+                              int32_t dtype, int64_t ld, const int32_t* seq_off, const int32_t* seq_rows,
+                              hipStream_t stream) {
+  const Kv4Cache c{KV4, par, kv4_dtype, cap};
+  const rbq_status s = check_quantize_kv4(batch, heads_kv, head_dim, K, V, dtype, ld, n_rows, offset, c, seq_off, seq_rows);
   if (s != RBQ_OK) return s;
-  s = launch_decode_kv8(batch, heads_q, heads_kv, head_dim, q, c, n, sel_idx, sel_count, win, sm_scale, out, lse,
-                        sw.decode, true, stream, sw.masks, topp_mask_words(n));
-  // (last: it may re-encode rows that the attention reads)
-  if (s == RBQ_OK && do_flush)
-    s = launch_quantize_kv(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, block, kv8_dtype, K8, V8,
-                           k_scale, v_scale, nullptr, nullptr, stream);
-  return s;
+  return launch_dequantize_kv4(batch, heads_kv, head_dim, KV4, par, kv4_dtype, cap, n_rows, offset, K, V, dtype, ld,
+                               seq_off, seq_rows, stream);
+}
+
+rbq_status rbq_dense_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                const void* KV4, const uint32_t* par, int32_t kv4_dtype, int32_t cap, int32_t n,
+                                const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                                float sm_scale, float* out, float* lse, void* ws, size_t ws_bytes,
+                                const int32_t* seq_n, const int32_t* seq_w, hipStream_t stream) {
+  const Kv4Cache c{KV4, par, kv4_dtype, cap};
+  const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
+  const rbq_status s = check_decode_kv4(batch, heads_q, heads_kv, head_dim, q, c, n, false, nullptr, nullptr, win,
+                                        sm_scale, out, ws, ws_bytes, seq_n, seq_w);
+  if (s != RBQ_OK) return s;
+  return launch_decode_kv4(batch, heads_q, heads_kv, head_dim, q, c, n, nullptr, nullptr, win, sm_scale, out, lse, ws,
+                           false, stream, nullptr, 0, seq_n, seq_w);
+}
+
+rbq_status rbq_sparse_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                                 const void* KV4, const uint32_t* par, int32_t kv4_dtype, int32_t cap, int32_t n,
+                                 const int32_t* sel_idx, const int32_t* sel_count, const void* K_loc,
+                                 const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w, float sm_scale,
+                                 float* out, float* lse, void* ws, size_t ws_bytes, const int32_t* seq_n,
+                                 const int32_t* seq_w, hipStream_t stream) {
+  const Kv4Cache c{KV4, par, kv4_dtype, cap};
+  const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
+  const rbq_status s = check_decode_kv4(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win,
+                                        sm_scale, out, ws, ws_bytes, seq_n, seq_w);
+  if (s != RBQ_OK) return s;
+  return launch_decode_kv4(batch, heads_q, heads_kv, head_dim, q, c, n, sel_idx, sel_count, win, sm_scale, out, lse, ws,
+                           true, stream, nullptr, 0, seq_n, seq_w);
+}
+
+rbq_status rbq_decode_step_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                               const float* P, const float* c_q, const float* c_k, void* KV4, uint32_t* par,
+                               int32_t kv4_dtype, int32_t cap, int32_t n,
+                               const void* K_loc, const void* V_loc, int32_t loc_dtype, int64_t loc_ld, int32_t w,
+                               uint32_t* codes, float* kfac, uint16_t* kfac16, int32_t flush, float p, float sm_scale,
+                               uint32_t* qplanes, float* qscal, float* scores, int32_t* sel_idx, int32_t* sel_count,
+                               float* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const Kv4Cache c{KV4, par, kv4_dtype, cap};
+  const Kv8Window win{K_loc, V_loc, loc_dtype, loc_ld, w};
+  return decode_step_over(
+      batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, cap, n, win, codes, kfac, kfac16, flush, p, sm_scale, qplanes,
+      qscal, scores, sel_idx, sel_count, ws, ws_bytes, stream,
+      [&](const StepWorkspace& sw, size_t bytes) {
+        return check_decode_kv4(batch, heads_q, heads_kv, head_dim, q, c, n, true, sel_idx, sel_count, win, sm_scale, out,
+                                sw.decode, bytes, nullptr, nullptr);
+      },
+      [&] {
+        return check_quantize_kv4(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, c, nullptr, nullptr);
+      },
+      [&](const StepWorkspace& sw) {
+        return launch_decode_kv4(batch, heads_q, heads_kv, head_dim, q, c, n, sel_idx, sel_count, win, sm_scale, out, lse,
+                                 sw.decode, true, stream, sw.masks, topp_mask_words(n));
+      },
+      [&] {
+        return launch_quantize_kv4(batch, heads_kv, head_dim, K_loc, V_loc, loc_dtype, loc_ld, w, n, cap, kv4_dtype, KV4,
+                                   par, nullptr, nullptr, stream);
+      });
 }
 
 rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const void* q,
@@ -551,7 +657,24 @@ rbq_status rbq_prefill_attention(int32_t batch, int32_t heads_q, int32_t heads_k
                                  const int32_t* cu_k, int32_t total_q, int32_t max_k, int32_t causal, float sm_scale,
                                  void* out, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
   const PrefillArgs a{q, q_ld, K, V, kv_ld, kv_head, kv_seq, kv_rows, dtype, cu_q, cu_k, total_q, max_k, causal,
-                      sm_scale, out, lse, ws, ws_bytes};
+                      sm_scale, out, lse, ws, ws_bytes, nullptr, 0, nullptr};
+  const rbq_status s = check_prefill(batch, heads_q, heads_kv, head_dim, a);
+  if (s != RBQ_OK) return s;
+  return launch_prefill(batch, heads_q, heads_kv, head_dim, a, stream);
+}
+
+rbq_status rbq_prefill_attention_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
+                                     const void* q, int64_t q_ld, const void* K, const void* V, int32_t dtype,
+                                     int64_t kv_ld, int64_t kv_head, const int32_t* cu_q, int32_t total_q,
+                                     const void* KV4, const uint32_t* par, int32_t kv4_dtype, int32_t cap, int32_t n,
+                                     const int32_t* seq_n, int32_t causal, float sm_scale, void* out, float* lse,
+                                     void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (n < 0 || total_q < 0) return RBQ_EINVAL;
+  const int64_t keys = prefill_kv4_keys(n, total_q);
+  if (keys >= (int64_t(1) << 31) - 64) return RBQ_EUNSUPPORTED;
+  const Kv4Cache c{KV4, par, kv4_dtype, cap};
+  const PrefillArgs a{q,   q_ld, K,  V,        kv_ld, kv_head, 0, total_q, dtype, cu_q, cu_q, total_q, int32_t(keys),
+                      causal, sm_scale, out, lse, ws, ws_bytes, &c, n, seq_n};
   const rbq_status s = check_prefill(batch, heads_q, heads_kv, head_dim, a);
   if (s != RBQ_OK) return s;
   return launch_prefill(batch, heads_q, heads_kv, head_dim, a, stream);

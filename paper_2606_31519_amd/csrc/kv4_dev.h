@@ -1,0 +1,60 @@
+// Reading the rows of the 4-bit cache: what the kernels that turn them into values share.
+#pragma once
+
+#include "rbq_device.h"
+#include "rbq_internal.h"
+
+namespace rbq {
+namespace {
+
+// The place of dimension i of eight in a word of codes
+template <int FMT>
+constexpr int nibble_shift(int i) {
+  return 4 * (FMT == RBQ_FP4 ? i : i / 2 + 4 * (i % 2));
+}
+
+// fp4's scale of a group, int4's step and base, from a row's word
+template <int FMT>
+__device__ __forceinline__ f32x2 row_scale(uint32_t word, int group) {
+  if constexpr (FMT == RBQ_FP4) return f32x2{__uint_as_float((word >> (8 * group) & 255u) << 23), 0.f};
+  return f32x2{__uint_as_float(word << 16), __uint_as_float(word & 0xFFFF0000u)};
+}
+
+// A code's value
+template <int FMT>
+__device__ __forceinline__ float code_value(uint32_t c, f32x2 sc) {
+  if constexpr (FMT == RBQ_FP4) {
+    // its exponent and mantissa as a float's, which is 2^-126 of it
+    return __uint_as_float((c & 8u) << 28 | (c & 7u) << 22) * 0x1p126f * sc.x;
+  } else {
+    return fmaf(float(c), sc.x, sc.y);
+  }
+}
+
+// The 8 values of a word of codes as bf16, in their order
+template <int FMT>
+__device__ __forceinline__ u32x4 word_bf16(uint32_t w, f32x2 sc) {
+  u32x4 r;
+  if constexpr (FMT == RBQ_FP4) {
+    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 0));
+    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 1));
+    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 2));
+    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 3));
+  } else {
+    typedef float f32x2v __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const uint32_t even = w & 0x0F0F0F0Fu, odd = w >> 4 & 0x0F0F0F0Fu;   // nibbles 0 2 4 6 (dimensions 0 4 1 5), 1 3 5 7 (2 6 3 7)
+    auto value = [&](uint32_t v, int byte) { return fmaf(float(uint8_t(v >> (8 * byte))), sc.x, sc.y); };
+    auto pair = [&](float a, float b) {
+      return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{a, b}), bf16x2));
+    };
+    r[0] = pair(value(even, 0), value(even, 2));
+    r[1] = pair(value(odd, 0), value(odd, 2));
+    r[2] = pair(value(even, 1), value(even, 3));
+    r[3] = pair(value(odd, 1), value(odd, 3));
+  }
+  return r;
+}
+
+}  // namespace
+}  // namespace rbq

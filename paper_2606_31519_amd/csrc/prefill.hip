@@ -5,8 +5,11 @@
 //   over the j < Lk of the query's sequence, for causal j <= i + Lk - Lq
 //
 // One pass over the keys with the running maximum and sum of the softmax.
-#include "rbq_device.h"
-#include "rbq_internal.h"
+//
+// rbq_prefill_attention_kv4: the same of chunks whose earlier keys are rows of the 4-bit cache
+// (FMT, its format). A sequence's keys are then its cached rows, up to a whole step of kPKeys
+// (the places behind the last row are masked), and its chunk's own rows after them.
+#include "kv4_dev.h"
 
 namespace rbq {
 namespace {
@@ -30,16 +33,37 @@ struct TileId {
   int q0, nq;    // first token of the sequence on the packed axis, tokens
   int nk;        // keys
   int64_t k0;    // first row of the sequence's keys (packed), 0 otherwise
+  int nb;        // 4-bit rows before them
+};
+
+// The 4-bit rows that come before a chunk's own: n of each sequence, or n_b of seq_n.
+struct Cached {
+  const char* KV4;
+  const uint32_t* par;
+  const int32_t* seq_n;
+  int cap, n;
 };
 
 // One sequence's lengths, inside the buffers: keys inside [0, kv_rows) of the packed axis,
-// or of the sequence's own rows.
+// or of the sequence's own rows; behind 4-bit rows (FMT) as many as it has tokens. nb: 4-bit rows.
 struct Lengths {
-  int q0, nq, k0, nk, tiles;
+  int q0, nq, k0, nk, tiles, nb;
 };
+template <int FMT>
 __device__ __forceinline__ Lengths lengths_of(int b, int G, int BM, int total_q, int max_k, int kv_rows, bool packed,
-                                              const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k) {
+                                              const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
+                                              const Cached& c4) {
   Lengths s;
+  if constexpr (FMT != 0) {
+    s.nb = c4.seq_n ? min(max(c4.seq_n[b], 0), c4.n) : c4.n;
+    s.q0 = min(max(cu_q[b], 0), total_q);
+    s.nq = max(min(max(cu_q[b + 1], 0), total_q) - s.q0, 0);
+    s.k0 = s.q0;
+    s.nk = (s.nb + kPKeys - 1) / kPKeys * kPKeys + s.nq;
+    s.tiles = int((int64_t(s.nq) * G + BM - 1) / BM);
+    return s;
+  }
+  s.nb = 0;
   const int ka = cu_k[b], kb = cu_k[b + 1];
   s.q0 = min(max(cu_q[b], 0), total_q);
   s.nq = max(min(max(cu_q[b + 1], 0), total_q) - s.q0, 0);
@@ -59,11 +83,13 @@ __device__ __forceinline__ Lengths lengths_of(int b, int G, int BM, int total_q,
 // them, they leave whole shader engines idle, which take blocks in turn: 512 blocks of
 // 256 fp32 keys with 512 empty ones between them 84 us, in this order 52.)
 // More sequences than lanes: in the sequences' order, backwards, every split of a tile.
+template <int FMT>
 __device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int kchunk, int batch, int G, int BM,
                                             int total_q, int max_k, int kv_rows, bool packed, bool causal,
-                                            const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k) {
+                                            const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
+                                            const Cached& c4) {
   const int lane = lane_id();
-  TileId t{-1, 0, 0, 0, 0, 0, 0};
+  TileId t{-1, 0, 0, 0, 0, 0, 0, 0};
   auto found = [&](const Lengths& s, int b0, int l, int tile) {
     t.b = b0 + l;
     t.tile = tile;
@@ -71,6 +97,7 @@ __device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int k
     t.nq = __builtin_amdgcn_readlane(s.nq, l);
     t.nk = __builtin_amdgcn_readlane(s.nk, l);
     t.k0 = __builtin_amdgcn_readlane(s.k0, l);
+    t.nb = FMT != 0 ? __builtin_amdgcn_readlane(s.nb, l) : 0;
   };
   auto prefix = [&](int v) {   // inclusive sum over the lanes
 #pragma unroll
@@ -81,12 +108,12 @@ __device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int k
     return v;
   };
   if (batch == 1 && splits == 1) {
-    const Lengths s = lengths_of(0, G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k);
+    const Lengths s = lengths_of<FMT>(0, G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k, c4);
     if (id < s.tiles) found(s, 0, 0, s.tiles - 1 - id);
     return t;
   }
   if (batch <= kWave) {
-    Lengths s = lengths_of(min(lane, batch - 1), G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k);
+    Lengths s = lengths_of<FMT>(min(lane, batch - 1), G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k, c4);
     if (lane >= batch) s.nq = s.tiles = 0;
     // this sequence's tiles of at least n steps: a causal tile's keys end at its last token's
     auto of = [&](int nq, int nk, int tiles_b, int n) {
@@ -126,7 +153,7 @@ __device__ __forceinline__ TileId find_tile(int id, int tiles, int splits, int k
   t.split = id % splits;
   int before = 0;
   for (int b0 = 0; b0 < batch; b0 += kWave) {
-    const Lengths s = lengths_of(min(b0 + lane, batch - 1), G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k);
+    const Lengths s = lengths_of<FMT>(min(b0 + lane, batch - 1), G, BM, total_q, max_k, kv_rows, packed, cu_q, cu_k, c4);
     const int mine = b0 + lane < batch ? s.tiles : 0, inc = before + prefix(mine);
     const unsigned long long at = __ballot(tile >= inc - mine && tile < inc);
     if (at != 0ull) {
@@ -208,20 +235,20 @@ __device__ __forceinline__ void store_row(const f32x16 (&o)[D / 32][NQ], int i, 
 // limit bounds it: 2.10 TFLOP in 2000 to 2150 us is 0.98 to 1.05 PFLOP/s at the clock that
 // it leaves (1.8 of 2.4 GHz); the library's 8192^3 product, in the same state, makes 1.23
 // PFLOP/s of its 1.70 on zeros.
-template <int D>
+template <int D, int FMT = 0>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     const uint16_t* __restrict__ q, int64_t q_ld, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
     int64_t kv_ld, int64_t kv_head, int64_t kv_seq, int kv_rows, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ cu_k, int batch, int total_q, int max_k, int causal, float scale_log2e,
     uint16_t* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv, int tiles, int splits,
-    int kchunk) {
+    int kchunk, Cached c4) {
   constexpr int BM = 32 * kPWaves, C = D / 8, KB = D / 16, DT = D / 32, RB = D * 2;   // chunks, k-blocks, dim tiles, bytes of a row
   __shared__ __attribute__((aligned(1024))) char ldsK[2][kPKeys * RB], ldsV[2][kPKeys * RB];
   __shared__ int odd;   // values were replaced (below)
   const int G = Hq / Hkv;
   const int hk = blockIdx.x % Hkv;
-  const TileId t = find_tile(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
-                             causal != 0, cu_q, cu_k);
+  const TileId t = find_tile<FMT>(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
+                             causal != 0, cu_q, cu_k, c4);
   if (t.b < 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
   const int x = lane & 31, h = lane >> 5;
@@ -234,6 +261,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   const int kbeg = t.split * kchunk, kstop = min(kend, kbeg + kchunk);   // this block's keys
   const int wend = wrow < rows ? visible((min(wrow + 32, rows) - 1) / G) : 0;   // of the wave
   const int wmin = visible(min(wrow, rows - 1) / G);                // keys that every row of the wave sees
+  const int cached = t.nb;
 
   // queries: B operand, lane (row x, half h) holds dimensions 16 kb + 8 h .. +8
   bf16x8 qf[KB];
@@ -249,15 +277,49 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   // staging: one instruction moves 1024 bytes, 1024 / RB rows
   constexpr int kRowsPer = 1024 / RB, kIssues = kPKeys / kRowsPer / kPWaves;
   const int srow = lane / C, spos = lane % C;
+  const int nbp = FMT != 0 ? (t.nb + kPKeys - 1) / kPKeys * kPKeys : 0;   // first of the chunk's own keys
   auto stage = [&](const uint16_t* base, char* lds, int k0, bool v) {
+    if (FMT != 0 && k0 < nbp) return;
     const int left = min(t.nk - k0, kPKeys);   // (the last rows again in place of those behind them)
-    const __amdgpu_buffer_rsrc_t r = make_rsrc(base + k0 * kv_ld, uint32_t((left - 1) * kv_ld * 2 + RB));
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(base + (k0 - nbp) * kv_ld, uint32_t((left - 1) * kv_ld * 2 + RB));
 #pragma unroll
     for (int i = 0; i < kIssues; ++i) {
       const int row = (wave * kIssues + i) * kRowsPer + srow;
       load_lds16(r, lds + (wave * kIssues + i) * 1024,
                  min(row, left - 1) * int(kv_ld * 2) + ((spos ^ (v ? v_swizzle<D>(row) : k_swizzle<D>(row))) * 16));
     }
+  };
+  // 4-bit tiles: a thread takes a quarter of a row of K and of V, which are on their way while a
+  // step is computed and go into LDS as bf16 before the barrier after it
+  constexpr int kQuarter = D / 32;   // words
+  struct Quarter {
+    uint32_t w[kQuarter], word;
+  };
+  const int64_t first = FMT != 0 ? (int64_t(t.b) * Hkv + hk) * c4.cap : 0;
+  const __amdgpu_buffer_rsrc_t rec = make_rsrc(c4.KV4 + first * D, uint32_t(t.nb) * D);   // < 2^31
+  const __amdgpu_buffer_rsrc_t words = make_rsrc(c4.par + 2 * first, uint32_t(t.nb) * 8u);
+  const int prow = threadIdx.x / 4, pq = threadIdx.x % 4;
+  auto request = [&](Quarter& r, int k0, bool v) {
+    if (FMT == 0 || k0 >= nbp) return;
+    const int row = min(k0 + prow, t.nb - 1), at = row * D + (v ? D / 2 : 0) + 4 * kQuarter * pq;
+    if constexpr (D == 128) {
+      const u32x4 x = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rec, at, 0, 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r.w[i] = x[i];
+    } else {
+      const u32x2 x = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(rec, at, 0, 0));
+      r.w[0] = x.x;
+      r.w[1] = x.y;
+    }
+    r.word = __builtin_amdgcn_raw_buffer_load_b32(words, row * 8 + (v ? 4 : 0), 0, 0);
+  };
+  auto deliver = [&](const Quarter& r, char* lds, int k0, bool v) {
+    if (FMT == 0 || k0 >= nbp) return;
+    const f32x2 sc = row_scale<FMT>(r.word, pq);
+#pragma unroll
+    for (int i = 0; i < kQuarter; ++i)
+      *reinterpret_cast<u32x4*>(lds + prow * RB + ((pq * kQuarter + i) ^ (v ? v_swizzle<D>(prow) : k_swizzle<D>(prow))) * 16) =
+          word_bf16<FMT>(r.w[i], sc);
   };
   // read addresses: K rows (lane: key x, chunk 2 kb + h), V columns by the transposing
   // read (16 lanes: 4 keys x 16 dimensions; lane i gives key i / 4, dimensions 4 (i % 4) .. +4)
@@ -288,6 +350,12 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[t][r] = k0 + 32 * t + 8 * (r / 4) + 4 * h + r % 4 < lim ? s[t][r] : -INFINITY;
+    }
+    if (FMT != 0 && k0 < nbp && k0 + kPKeys > cached) {   // places behind the last 4-bit row
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = k0 + 32 * t + 8 * (r / 4) + 4 * h + r % 4 < cached ? s[t][r] : -INFINITY;
     }
     float mx[4] = {s[0][0], s[0][1], s[1][0], s[1][1]};
 #pragma unroll
@@ -371,10 +439,18 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   // of V and tile i + 1 of K. Logits of keys behind the last are formed from whatever the tile
   // holds and masked.
   f32x16 sa[2], sb[2];
+  Quarter kr, vr;
   if (kbeg < kstop) {
+    Quarter k1;
+    request(kr, kbeg, false);
+    request(vr, kbeg, true);
+    if (kbeg + kPKeys < kstop) request(k1, kbeg + kPKeys, false);
     stage(Kb, ldsK[0], kbeg, false);
     stage(Vb, ldsV[0], kbeg, true);
     if (kbeg + kPKeys < kstop) stage(Kb, ldsK[1], kbeg + kPKeys, false);
+    deliver(kr, ldsK[0], kbeg, false);
+    deliver(vr, ldsV[0], kbeg, true);
+    if (kbeg + kPKeys < kstop) deliver(k1, ldsK[1], kbeg + kPKeys, false);
     if (threadIdx.x == 0) odd = 0;
     wait_lds();
     __syncthreads();
@@ -383,11 +459,21 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   }
   const int wstop = min(wend, kstop);
   auto publish = [&](int k0, int buf) {   // tile i of V and i + 1 of K have arrived; the ones after are requested
+    if (FMT != 0 && k0 > kbeg) {
+      deliver(vr, ldsV[buf], k0, true);
+      if (k0 + kPKeys < kstop) deliver(kr, ldsK[buf ^ 1], k0 + kPKeys, false);
+    }
     wait_lds();
-    if (k0 >= kodd) finite_tile(ldsV[buf]);
+    if (k0 >= kodd && k0 >= nbp) finite_tile(ldsV[buf]);
     __syncthreads();
-    if (k0 + kPKeys < kstop) stage(Vb, ldsV[buf ^ 1], k0 + kPKeys, true);
-    if (k0 + 2 * kPKeys < kstop) stage(Kb, ldsK[buf], k0 + 2 * kPKeys, false);
+    if (k0 + kPKeys < kstop) {
+      request(vr, k0 + kPKeys, true);
+      stage(Vb, ldsV[buf ^ 1], k0 + kPKeys, true);
+    }
+    if (k0 + 2 * kPKeys < kstop) {
+      request(kr, k0 + 2 * kPKeys, false);
+      stage(Kb, ldsK[buf], k0 + 2 * kPKeys, false);
+    }
   };
   for (int k0 = kbeg; k0 < kstop; k0 += 2 * kPKeys) {
     publish(k0, 0);
@@ -399,10 +485,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
 
   if (kbeg < kstop && odd) {
 #pragma unroll 1
-    for (int key = kodd; key < min(lim, kstop); ++key) {
+    for (int key = max(kodd, nbp); key < min(lim, kstop); ++key) {   // (4-bit values are finite)
 #pragma unroll
       for (int c = 0; c < 4 * DT; ++c) {   // the lane's dimensions 8 c + 4 h .. +4
-        const u32x2 w = *reinterpret_cast<const u32x2*>(Vb + key * kv_ld + 8 * c + 4 * h);
+        const u32x2 w = *reinterpret_cast<const u32x2*>(Vb + (key - nbp) * kv_ld + 8 * c + 4 * h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           const float v = __uint_as_float((w[e / 2] >> (16 * (e % 2))) << 16);
@@ -425,19 +511,19 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
 // 56 us and 6 of the join, the cores busy for 0.64 of the time that blocks run, the rest
 // uneven numbers of blocks per compute unit).
 constexpr int kFKeys = 32;
-template <int D>
+template <int D, int FMT = 0>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
     const float* __restrict__ q, int64_t q_ld, const float* __restrict__ K, const float* __restrict__ V, int64_t kv_ld,
     int64_t kv_head, int64_t kv_seq, int kv_rows, const int32_t* __restrict__ cu_q, const int32_t* __restrict__ cu_k,
     int batch, int total_q, int max_k, int causal, float scale_log2e, float* __restrict__ out, float* __restrict__ lse,
-    float* __restrict__ part, int Hq, int Hkv, int tiles, int splits, int kchunk) {
+    float* __restrict__ part, int Hq, int Hkv, int tiles, int splits, int kchunk, Cached c4) {
   constexpr int BM = 32 * kPWaves, DT = D / 32, LD = D + 4;   // (padded rows: four consecutive keys in other banks)
   constexpr int kPieces = kFKeys * D / 4 / kPThreads;        // 16-byte pieces per thread and tensor
   __shared__ __attribute__((aligned(16))) float ldsK[kFKeys][LD], ldsV[kFKeys][LD];
   const int G = Hq / Hkv;
   const int hk = blockIdx.x % Hkv;
-  const TileId t = find_tile(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
-                             causal != 0, cu_q, cu_k);
+  const TileId t = find_tile<FMT>(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
+                             causal != 0, cu_q, cu_k, c4);
   if (t.b < 0) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = lane_id();
   const int x = lane & 31, h = lane >> 5;
@@ -456,11 +542,27 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
   }
   const int64_t kvoff = (kv_seq == 0 ? t.k0 * kv_ld : int64_t(t.b) * kv_seq) + int64_t(hk) * kv_head;
   f32x4 kreg[kPieces], vreg[kPieces];
+  const int nbp = FMT != 0 ? (t.nb + kPKeys - 1) / kPKeys * kPKeys : 0;   // first of the chunk's own keys
   auto fetch = [&](int k0) {
+    if constexpr (FMT != 0) {
+      if (k0 < nbp) {   // 4-bit rows: the words of the piece's codes and of its row, for now
+        const int64_t first = (int64_t(t.b) * Hkv + hk) * c4.cap;
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          const int e = i * kPThreads + threadIdx.x, r = e / (D / 4), c = e % (D / 4);
+          const int64_t row = first + min(k0 + r, t.nb - 1);
+          const uint32_t* w = reinterpret_cast<const uint32_t*>(c4.KV4 + row * D) + c / 2;
+          const u32x2 p = reinterpret_cast<const u32x2*>(c4.par)[row];
+          kreg[i] = f32x4{__uint_as_float(w[0]), __uint_as_float(p.x), 0.f, 0.f};
+          vreg[i] = f32x4{__uint_as_float(w[D / 8]), __uint_as_float(p.y), 0.f, 0.f};
+        }
+        return;
+      }
+    }
 #pragma unroll
     for (int i = 0; i < kPieces; ++i) {
       const int e = i * kPThreads + threadIdx.x, r = e / (D / 4), c = e % (D / 4);
-      const int64_t at = kvoff + int64_t(min(k0 + r, t.nk - 1)) * kv_ld + 4 * c;
+      const int64_t at = kvoff + int64_t(min(k0 + r, t.nk - 1) - nbp) * kv_ld + 4 * c;
       kreg[i] = *reinterpret_cast<const f32x4*>(K + at);
       vreg[i] = *reinterpret_cast<const f32x4*>(V + at);
     }
@@ -477,6 +579,23 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
   bool odd = false;
   if (kbeg < kstop) fetch(kbeg);
   for (int k0 = kbeg; k0 < kstop; k0 += kFKeys) {
+    if constexpr (FMT != 0) {
+      if (k0 < nbp) {
+        auto values = [&](f32x4& v) {
+          const int dim = 4 * (threadIdx.x % (D / 4));   // (256 is a multiple of D / 4)
+          const f32x2 sc = row_scale<FMT>(__float_as_uint(v.y), dim / (D / 4));
+          const uint32_t w = __float_as_uint(v.x);
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = code_value<FMT>((dim % 8 ? w >> nibble_shift<FMT>(4 + e) : w >> nibble_shift<FMT>(e)) & 15u, sc);
+        };
+#pragma unroll
+        for (int i = 0; i < kPieces; ++i) {
+          values(kreg[i]);
+          values(vreg[i]);
+        }
+      }
+    }
     if (k0 >= kodd) {
 #pragma unroll
       for (int i = 0; i < kPieces; ++i)
@@ -529,7 +648,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
     float mx = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = k0 + 8 * (r / 4) + 4 * h + r % 4 < lim ? s[r] : -INFINITY;
+      const int key = k0 + 8 * (r / 4) + 4 * h + r % 4;
+      s[r] = key < lim && (FMT == 0 || key < t.nb || key >= nbp) ? s[r] : -INFINITY;
       mx = fmaxf(mx, s[r]);
     }
     mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
@@ -562,10 +682,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
   }
   if (__syncthreads_or(odd)) {
 #pragma unroll 1
-    for (int key = kodd; key < min(lim, kstop); ++key) {
+    for (int key = max(kodd, nbp); key < min(lim, kstop); ++key) {
 #pragma unroll
       for (int c = 0; c < 4 * DT; ++c) {
-        const f32x4 v = *reinterpret_cast<const f32x4*>(V + kvoff + key * kv_ld + 8 * c + 4 * h);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(V + kvoff + (key - nbp) * kv_ld + 8 * c + 4 * h);
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[c / 4][0][4 * (c % 4) + e] += fabsf(v[e]) < INFINITY ? 0.f : v[e];
       }
@@ -633,6 +753,9 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
   if (a.total_q == 0) return RBQ_OK;
   const PrefillPlan pl = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype);
   const float c = float(double(a.sm_scale) * 1.4426950408889634);
+  Cached c4{};
+  if (a.cache != nullptr)
+    c4 = Cached{static_cast<const char*>(a.cache->KV4), a.cache->par, a.seq_n, a.cache->cap, a.cached};
   float* part = pl.splits > 1 ? static_cast<float*>(a.ws) : nullptr;
   const dim3 grid(uint32_t(int64_t(pl.tiles) * heads_kv * pl.splits));
   const int64_t rows = int64_t(a.total_q) * heads_q;
@@ -641,7 +764,13 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
   KERNEL<<<grid, kPThreads, 0, stream>>>(static_cast<const T*>(a.q), a.q_ld, static_cast<const T*>(a.K),                 \
                                          static_cast<const T*>(a.V), a.kv_ld, a.kv_head, a.kv_seq, a.kv_rows, a.cu_q,   \
                                          a.cu_k, batch, a.total_q, a.max_k, a.causal, c, static_cast<T*>(a.out), a.lse, \
-                                         part, heads_q, heads_kv, pl.tiles, pl.splits, pl.kchunk)
+                                         part, heads_q, heads_kv, pl.tiles, pl.splits, pl.kchunk, c4)
+#define RBQ_PREFILL_OF(KERNEL, D, T)                                     \
+  do {                                                                   \
+    if (a.cache == nullptr) RBQ_PREFILL((KERNEL<D, 0>), T);              \
+    else if (a.cache->dtype == RBQ_FP4) RBQ_PREFILL((KERNEL<D, RBQ_FP4>), T); \
+    else RBQ_PREFILL((KERNEL<D, RBQ_I4>), T);                            \
+  } while (0)
 #define RBQ_PREFILL_JOIN(D, DT)                                                                                    \
   if (part && pl.splits <= 4)                                                                                      \
     prefill_combine_kernel<D, DT, 4><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, \
@@ -651,20 +780,21 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
                                                                       a.out, a.lse)
   if (a.dtype == RBQ_F32) {
     if (head_dim == 64) {
-      RBQ_PREFILL(prefill_f32_kernel<64>, float);
+      RBQ_PREFILL_OF(prefill_f32_kernel, 64, float);
       RBQ_PREFILL_JOIN(64, RBQ_F32);
     } else {
-      RBQ_PREFILL(prefill_f32_kernel<128>, float);
+      RBQ_PREFILL_OF(prefill_f32_kernel, 128, float);
       RBQ_PREFILL_JOIN(128, RBQ_F32);
     }
   } else if (head_dim == 64) {
-    RBQ_PREFILL(prefill_kernel<64>, uint16_t);
+    RBQ_PREFILL_OF(prefill_kernel, 64, uint16_t);
     RBQ_PREFILL_JOIN(64, RBQ_BF16);
   } else {
-    RBQ_PREFILL(prefill_kernel<128>, uint16_t);
+    RBQ_PREFILL_OF(prefill_kernel, 128, uint16_t);
     RBQ_PREFILL_JOIN(128, RBQ_BF16);
   }
 #undef RBQ_PREFILL_JOIN
+#undef RBQ_PREFILL_OF
 #undef RBQ_PREFILL
   return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
 }

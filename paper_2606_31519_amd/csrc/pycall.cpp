@@ -56,7 +56,11 @@ bool take(PyObject* o, T*& v) {
   return v != nullptr || !PyErr_Occurred();
 }
 
-enum { kQuantize, kDequantize, kDense, kSparse, kStep, kPrefill, kEntries };
+enum {
+  kQuantize, kDequantize, kDense, kSparse, kStep, kPrefill,
+  kQuantize4, kDequantize4, kDense4, kSparse4, kStep4, kPrefill4,
+  kEntries
+};
 void* entry[kEntries];
 
 template <class F>
@@ -150,6 +154,12 @@ PyMethodDef methods[] = {RBQ_ENTRY(rbq_quantize_kv, kQuantize),
                          RBQ_ENTRY(rbq_sparse_decode_kv8, kSparse),
                          RBQ_ENTRY(rbq_decode_step_kv8, kStep),
                          RBQ_ENTRY(rbq_prefill_attention, kPrefill),
+                         RBQ_ENTRY(rbq_quantize_kv4, kQuantize4),
+                         RBQ_ENTRY(rbq_dequantize_kv4, kDequantize4),
+                         RBQ_ENTRY(rbq_dense_decode_kv4, kDense4),
+                         RBQ_ENTRY(rbq_sparse_decode_kv4, kSparse4),
+                         RBQ_ENTRY(rbq_decode_step_kv4, kStep4),
+                         RBQ_ENTRY(rbq_prefill_attention_kv4, kPrefill4),
                          RBQ_HELPER(fits),
                          RBQ_HELPER(bind),
                          {nullptr, nullptr, 0, nullptr}};

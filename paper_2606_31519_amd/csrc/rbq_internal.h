@@ -56,6 +56,20 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
                             const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
                             const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w);
 
+// The 4-bit cache.
+struct Kv4Cache {
+  const void* KV4;
+  const uint32_t* par;   // [B][Hkv][cap][2]
+  int32_t dtype, cap;
+};
+rbq_status check_quantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
+                              int32_t dtype, int64_t ld, int32_t rows, int32_t offset, const Kv4Cache& c,
+                              const int32_t* seq_off, const int32_t* seq_rows);
+rbq_status check_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                            const Kv4Cache& c, int32_t n, bool sparse, const int32_t* sel_idx,
+                            const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
+                            const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w);
+
 // The prompt's attention.
 struct PrefillArgs {
   const void* q;
@@ -70,7 +84,14 @@ struct PrefillArgs {
   float* lse;
   void* ws;
   size_t ws_bytes;
+  // chunks over 4-bit rows: the cache, the most rows of a sequence there, and the sequences' own (then
+  // kv_seq = 0, kv_rows = total_q, cu_k = cu_q and max_k = prefill_kv4_keys)
+  const Kv4Cache* cache;
+  int32_t cached;
+  const int32_t* seq_n;
 };
+// the most keys of a sequence of such a call, its cached rows up to a whole step of 64; at least 2^31: too many
+inline int64_t prefill_kv4_keys(int32_t n, int32_t total_q) { return (int64_t(n) + 63) / 64 * 64 + total_q; }
 rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a);
 // How it is cut: query tiles of `rows` (token, head of the group) rows of one
 // sequence and KV head, and, where those are too few for the GPU, the keys into
@@ -302,6 +323,20 @@ rbq_status launch_dequantize_kv(int32_t batch, int32_t heads_kv, int32_t head_di
                                 int64_t ld, const int32_t* seq_off, const int32_t* seq_rows, hipStream_t stream);
 rbq_status launch_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
                              const Kv8Cache& cache, int32_t n, const int32_t* sel_idx, const int32_t* sel_count,
+                             const Kv8Window& win, float sm_scale, float* out, float* lse, void* ws, bool sparse,
+                             hipStream_t stream, const unsigned long long* sel_mask = nullptr, int32_t mask_words = 0,
+                             const int32_t* seq_n = nullptr, const int32_t* seq_w = nullptr);
+
+rbq_status launch_quantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
+                               int32_t dtype, int64_t ld, int32_t n_new, int32_t offset, int32_t cap, int32_t kv4_dtype,
+                               void* KV4, uint32_t* par, const int32_t* seq_off, const int32_t* seq_new,
+                               hipStream_t stream);
+rbq_status launch_dequantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* KV4, const uint32_t* par,
+                                 int32_t kv4_dtype, int32_t cap, int32_t n_rows, int32_t offset, void* K, void* V,
+                                 int32_t dtype, int64_t ld, const int32_t* seq_off, const int32_t* seq_rows,
+                                 hipStream_t stream);
+rbq_status launch_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                             const Kv4Cache& cache, int32_t n, const int32_t* sel_idx, const int32_t* sel_count,
                              const Kv8Window& win, float sm_scale, float* out, float* lse, void* ws, bool sparse,
                              hipStream_t stream, const unsigned long long* sel_mask = nullptr, int32_t mask_words = 0,
                              const int32_t* seq_n = nullptr, const int32_t* seq_w = nullptr);

@@ -288,6 +288,40 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
 }
 
 namespace {
+rbq_status check_kv4_form(int32_t kv4_dtype) {
+  return kv4_dtype == RBQ_FP4 || kv4_dtype == RBQ_I4 ? RBQ_OK : RBQ_EUNSUPPORTED;
+}
+}  // namespace
+
+rbq_status check_quantize_kv4(int32_t batch, int32_t heads_kv, int32_t head_dim, const void* K, const void* V,
+                              int32_t dtype, int64_t ld, int32_t rows, int32_t offset, const Kv4Cache& c,
+                              const int32_t* seq_off, const int32_t* seq_rows) {
+  rbq_status s = check_heads(batch, heads_kv, heads_kv, head_dim);
+  if (s != RBQ_OK) return s;
+  if (dtype != RBQ_F32 && dtype != RBQ_BF16) return RBQ_EUNSUPPORTED;
+  if ((s = check_kv4_form(c.dtype)) != RBQ_OK) return s;
+  if (rows < 0 || offset < 0 || c.cap < 0 || ld < rows || ld >= kMaxRows) return RBQ_EINVAL;
+  if (int64_t(offset) + rows > c.cap) return RBQ_EINVAL;
+  if ((int64_t(offset) + rows) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;   // as the calls that read them
+  if (bad_seq(seq_off) || bad_seq(seq_rows)) return RBQ_EINVAL;
+  if (rows > 0 && (bad_ptr(K) || bad_ptr(V) || bad_ptr(c.KV4) || bad_ptr(c.par))) return RBQ_EINVAL;
+  return RBQ_OK;
+}
+
+rbq_status check_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const float* q,
+                            const Kv4Cache& c, int32_t n, bool sparse, const int32_t* sel_idx,
+                            const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
+                            const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w) {
+  const rbq_status s = check_kv4_form(c.dtype);
+  if (s != RBQ_OK) return s;
+  // the same call over another cache: a row's record takes the bytes that K's row takes there, and the splits are its
+  const float* par = reinterpret_cast<const float*>(c.par);
+  const Kv8Cache as{c.KV4, c.KV4, par, par, RBQ_E4M3, kMinKv8Block, c.cap};
+  return check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, as, n, sparse, sel_idx, sel_count, win, sm_scale, out,
+                          ws, ws_bytes, seq_n, seq_w);
+}
+
+namespace {
 // Time of a prompt call in us, but for what every choice takes, with the keys in chunks of
 // `kchunk`: the steps of 64 keys that a block takes one after the other, by the blocks of a
 // compute unit (the longest sequence's length stands for the others': with many, for half of
@@ -346,6 +380,12 @@ size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv,
 rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a) {
   rbq_status s = check_heads(batch, heads_q, heads_kv, head_dim);
   if (s != RBQ_OK) return s;
+  if (a.cache != nullptr) {
+    if ((s = check_kv4_form(a.cache->dtype)) != RBQ_OK) return s;
+    if (a.cached < 0 || a.cache->cap < 0 || a.cached > a.cache->cap || a.total_q < 0 || bad_seq(a.seq_n)) return RBQ_EINVAL;
+    if (int64_t(a.cached) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;   // as the decode calls
+    if (a.cached > 0 && (bad_ptr(a.cache->KV4) || bad_ptr(a.cache->par))) return RBQ_EINVAL;
+  }
   if (a.dtype != RBQ_F32 && a.dtype != RBQ_BF16) return RBQ_EUNSUPPORTED;
   const int64_t align = a.dtype == RBQ_BF16 ? 8 : 4;   // elements of 16 bytes
   if (a.total_q < 0 || a.max_k < 0 || a.kv_rows < 0) return RBQ_EINVAL;
@@ -415,13 +455,20 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
     case RBQ_OP_DENSE_DECODE:
       return rbq::decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_DECODE_KV8:
+    case RBQ_OP_DECODE_KV4:
       return rbq::decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_PREFILL:
       return rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
+    case RBQ_OP_PREFILL_KV4: {
+      const int64_t keys = rbq::prefill_kv4_keys(n, w);
+      return keys < rbq::kMaxRows - 64
+                 ? rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, int32_t(keys), w) : 0;
+    }
     case RBQ_OP_DECODE_STEP:
     case RBQ_OP_DECODE_STEP_KV8:
+    case RBQ_OP_DECODE_STEP_KV4:
       if (heads_q % heads_kv != 0) return 0;
-      return rbq::step_workspace(nullptr, batch, heads_q, heads_kv, head_dim, n, w, op == RBQ_OP_DECODE_STEP_KV8).bytes;
+      return rbq::step_workspace(nullptr, batch, heads_q, heads_kv, head_dim, n, w, op != RBQ_OP_DECODE_STEP).bytes;
     default:
       return 0;
   }

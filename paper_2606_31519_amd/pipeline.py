@@ -223,6 +223,28 @@ class Kv8Cache:
                               rows, offset, K, V, ld, seq_off, seq_rows, stream)
 
 
+class Kv4Cache:
+    """K and V rows in 4 bits ("fp4" or "int4"), each row with scales of its own: the buffers and the calls that
+    write and read them."""
+
+    def __init__(self, B, Hkv, D, cap, fmt="fp4", device="cuda"):
+        if fmt not in rbq.KV4_FORMATS:
+            raise ValueError(f"unknown 4-bit format {fmt!r} (one of {sorted(rbq.KV4_FORMATS)})")
+        self.B, self.Hkv, self.D, self.cap, self.fmt, self.code = B, Hkv, D, cap, fmt, rbq.KV4_FORMATS[fmt]
+        self.kv4 = torch.zeros(B, Hkv, cap, D, dtype=torch.uint8, device=device)
+        self.par = torch.zeros(B, Hkv, cap, 2, dtype=torch.int32, device=device)
+
+    def append(self, K, V, ld, rows, offset, seq_off=None, seq_rows=None, stream=None):
+        """Rows [0, rows) of K / V [B][Hkv][ld][D] as cache rows [offset, offset + rows) (rbq_quantize_kv4)."""
+        rbq.rbq_quantize_kv4(self.B, self.Hkv, self.D, K, V, ld, rows, offset, self.cap, self.code, self.kv4, self.par,
+                             seq_off, seq_rows, stream)
+
+    def read(self, K, V, ld, rows, offset=0, seq_off=None, seq_rows=None, stream=None):
+        """Cache rows [offset, offset + rows) as rows [0, rows) of K / V (rbq_dequantize_kv4)."""
+        rbq.rbq_dequantize_kv4(self.B, self.Hkv, self.D, self.kv4, self.par, self.code, self.cap, rows, offset, K, V, ld,
+                               seq_off, seq_rows, stream)
+
+
 class PromptAttention:
     """The attention of a batch of prompts, or of chunks of them behind rows that are
     cached (rbq_prefill_attention): q_lens tokens and k_lens keys per sequence
@@ -277,6 +299,47 @@ class PromptAttention:
         return out
 
 
+class ChunkAttention:
+    """The attention of chunks of prompts whose earlier rows are in a Kv4Cache (rbq_prefill_attention_kv4): q_lens tokens
+    and n_lens cached rows per sequence of the cache; the lengths' device arrays and the workspace are kept for every
+    call (calls that overlap in time, on several streams, need plans of their own)."""
+
+    def __init__(self, Hq, cache, q_lens, n_lens, causal=True):
+        if len(q_lens) != cache.B or len(n_lens) != cache.B or min(min(q_lens), min(n_lens)) < 0:
+            raise ValueError("one length of at least 0 per sequence of the cache, for the tokens and for the cached rows")
+        if max(n_lens) > cache.cap:
+            raise ValueError(f"{max(n_lens)} cached rows, the cache holds {cache.cap}")
+        if sum(map(int, q_lens)) >= 1 << 31:   # (the call counts in int32)
+            raise ValueError("2^31 tokens and more")
+        self.cache, self.Hq, self.causal, device = cache, Hq, causal, cache.kv4.device
+        cu = np.concatenate([[0], np.cumsum(q_lens)]).astype(np.int32)
+        self.total_q, self.n = int(cu[-1]), int(max(n_lens))
+        self.cu_q, self.seq_n = (torch.from_numpy(np.asarray(v, np.int32)).to(device) for v in (cu, n_lens))
+        self.ws = rbq.workspace(rbq.RBQ_OP_PREFILL_KV4, cache.B, Hq, cache.Hkv, cache.D, self.n, self.total_q, device)
+        self.sm_scale = 1.0 / math.sqrt(cache.D)
+
+    def __call__(self, q, K, V, out=None, lse=None, stream=None):
+        """q [total_q][Hq][D]; K, V [total_q][Hkv][D], the chunks' own rows; any strides whose last dimension (of q: two)
+        is contiguous. Returns out [total_q][Hq][D] in q's type."""
+        c, T = self.cache, self.total_q
+        if tuple(q.shape[1:]) != (self.Hq, c.D) or q.shape[0] < T:
+            raise ValueError(f"q is {tuple(q.shape)}, the plan needs ({T}, {self.Hq}, {c.D})")
+        if K.shape != V.shape or tuple(K.shape[1:]) != (c.Hkv, c.D) or K.shape[0] < T or K.stride() != V.stride():
+            raise ValueError(f"K and V are {tuple(K.shape)} and {tuple(V.shape)}, the plan needs ({T}, {c.Hkv}, {c.D}) and "
+                             "equal strides")
+        if q.stride(2) != 1 or (self.Hq > 1 and q.stride(1) != c.D) or K.stride(2) != 1:
+            raise ValueError("the head dimension (and the heads of q) must be contiguous")
+        # (a dimension of one entry has no stride that means anything)
+        q_ld = q.stride(0) if T > 1 else self.Hq * c.D
+        kv_ld, kv_head = K.stride(0) if T > 1 else c.Hkv * c.D, K.stride(1) if c.Hkv > 1 else c.D
+        out = torch.empty(T, self.Hq, c.D, dtype=q.dtype, device=q.device) if out is None else out
+        if not out.is_contiguous() or (lse is not None and not lse.is_contiguous()):
+            raise ValueError("out and lse must be contiguous")
+        rbq.rbq_prefill_attention_kv4(c.B, self.Hq, c.Hkv, c.D, q, q_ld, K, V, kv_ld, kv_head, self.cu_q, T, c.kv4, c.par,
+                                      c.code, c.cap, self.n, self.seq_n, self.causal, self.sm_scale, out, lse, self.ws, stream)
+        return out
+
+
 class DecodeSession:
     """A decode loop over one growing cache: the lazy index update of Section
     3.4 as a serving loop would run it. The cache holds `cap` rows per (sequence,
@@ -294,10 +357,14 @@ class DecodeSession:
 
     kv8 ("e4m3" or "int8"): the indexed rows are kept in 8 bits (kv8_block tokens per
     scale), the window in K's type in buffers of its own; K and V [B][Hkv][at least
-    n_prefill][D] are then read here only, and every step is one rbq_decode_step_kv8."""
+    n_prefill][D] are then read here only, and every step is one rbq_decode_step_kv8.
+
+    kv4 ("fp4" or "int4"): the same in 4 bits, every step one rbq_decode_step_kv4."""
 
     def __init__(self, B, Hq, Hkv, D, cap, n_prefill, window, K, V, P, c_q=None, device="cuda", compact=False, kv8=None,
-                 kv8_block=64):
+                 kv8_block=64, kv4=None):
+        if kv8 is not None and kv4 is not None:
+            raise ValueError("the indexed rows are kept in 8 bits or in 4, not both")
         if not 0 < window <= rbq.RBQ_MAX_WINDOW or n_prefill + window > cap:
             raise ValueError("the window must fit after the prefill rows (n_prefill + window <= cap)")
         q = torch.zeros(B, Hq, D, dtype=torch.float32, device=device)
@@ -308,14 +375,17 @@ class DecodeSession:
         self.n_sizes = list(range(n_prefill, cap + 1, window))
         self.n_max = self.n_sizes[-1]
         # sized for the largest index: the scores, selections and per-row workspaces grow with n
-        self.kv8 = None
+        self.kv8 = self.kv4 = None
         src, src_ld = K, cap          # the prefill rows and their number per block
-        if kv8 is not None:
+        if kv8 is not None or kv4 is not None:
             src_ld = K.shape[2]
             if src_ld < n_prefill or not (K.is_contiguous() and V.is_contiguous() and K.shape == V.shape):
                 raise ValueError("K and V must be contiguous, of one shape, and hold the prefill rows")
-            self.kv8 = Kv8Cache(B, Hkv, D, cap, kv8, kv8_block, device)
-            self.kv8.append(K, V, src_ld, n_prefill, 0)
+            if kv8 is not None:
+                self.kv8 = Kv8Cache(B, Hkv, D, cap, kv8, kv8_block, device)
+            else:
+                self.kv4 = Kv4Cache(B, Hkv, D, cap, kv4, device)
+            (self.kv8 or self.kv4).append(K, V, src_ld, n_prefill, 0)
             self.K_win, self.V_win = (torch.zeros(B, Hkv, window, D, dtype=K.dtype, device=device) for _ in range(2))
             K = V = None              # (the state's calls over a full-precision cache have none to read)
         self.state = DecodeState(B, Hq, Hkv, D, cap, self.n_max, window, K, V, q, P, c_q, device, compact)
@@ -324,7 +394,8 @@ class DecodeSession:
         # the step workspace is not monotonic in n (smaller indexes may take more,
         # shorter decode splits): size it for every index size the loop will pass;
         # for a given n it grows with the window rows, so the full window bounds it
-        op = rbq.RBQ_OP_DECODE_STEP if kv8 is None else rbq.RBQ_OP_DECODE_STEP_KV8
+        op = (rbq.RBQ_OP_DECODE_STEP_KV8 if kv8 is not None else
+              rbq.RBQ_OP_DECODE_STEP_KV4 if kv4 is not None else rbq.RBQ_OP_DECODE_STEP)
         need = max(rbq.rbq_workspace_bytes(op, B, Hq, Hkv, D, m, window) for m in self.n_sizes)
         if need > st.ws_step.numel():
             st.ws_step = torch.empty(need, dtype=torch.uint8, device=device)
@@ -341,7 +412,7 @@ class DecodeSession:
             raise RuntimeError("the window is full: run step() first (it flushes the window)")
         if self.n + self.w >= self.state.cap:
             raise RuntimeError("the cache is full")
-        if self.kv8 is not None:
+        if self.kv8 is not None or self.kv4 is not None:
             self.K_win[:, :, self.w].copy_(k)
             self.V_win[:, :, self.w].copy_(v)
         else:
@@ -367,6 +438,12 @@ class DecodeSession:
                                     c.v_scale, st.cap, self.n, self.K_win, self.V_win, self.window, self.w, st.codes, st.kfac,
                                     st.kfac16, flush, p, st.sm_scale, st.qplanes, st.qscal, st.scores, st.sel_idx,
                                     st.sel_count, st.out, st.lse, st.ws_step, stream)
+        elif self.kv4 is not None:
+            c = self.kv4
+            rbq.rbq_decode_step_kv4(st.B, st.Hq, st.Hkv, st.D, st.q, st.P, st.c_q, st.c_k, c.kv4, c.par, c.code, st.cap, self.n,
+                                    self.K_win, self.V_win, self.window, self.w, st.codes, st.kfac, st.kfac16, flush, p,
+                                    st.sm_scale, st.qplanes, st.qscal, st.scores, st.sel_idx, st.sel_count, st.out, st.lse,
+                                    st.ws_step, stream)
         elif st.compact:
             rbq.rbq_decode_step_f16(st.B, st.Hq, st.Hkv, st.D, st.q, st.P, st.c_k, st.K, st.V, st.cap, self.n,
                                     self.w, st.codes, st.kfac16, flush, p, st.sm_scale, st.qplanes, st.qscal,

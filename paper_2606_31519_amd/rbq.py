@@ -18,9 +18,12 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "librbq.so")
 RBQ_OK, RBQ_EINVAL, RBQ_EUNSUPPORTED, RBQ_EDEVICE = 0, 1, 2, 3
 RBQ_F32, RBQ_BF16 = 0, 1
 RBQ_E4M3, RBQ_I8 = 16, 17   # formats of the 8-bit cache
+RBQ_FP4, RBQ_I4 = 32, 33    # formats of the 4-bit cache
+KV4_FORMATS = {"fp4": RBQ_FP4, "int4": RBQ_I4}
 RBQ_ENCODE_SET_CENTROID = 1
 RBQ_OP_ENCODE, RBQ_OP_TOPP, RBQ_OP_SPARSE_DECODE, RBQ_OP_DENSE_DECODE, RBQ_OP_DECODE_STEP = 1, 2, 3, 4, 5
 RBQ_OP_DECODE_KV8, RBQ_OP_PREFILL, RBQ_OP_DECODE_STEP_KV8 = 6, 7, 8
+RBQ_OP_DECODE_KV4, RBQ_OP_DECODE_STEP_KV4, RBQ_OP_PREFILL_KV4 = 9, 10, 11
 QSCAL_STRIDE = 8
 RBQ_MAX_WINDOW = 4096   # largest local window accepted by the decode calls
 RBQ_NOALLOC_SCRATCH_BYTES = 16 << 20   # the static scratch of rbq_decode_step_noalloc
@@ -36,6 +39,8 @@ EXPORTED = [
     "rbq_decode_step_noalloc",
     "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8", "rbq_decode_step_kv8",
     "rbq_prefill_attention",
+    "rbq_quantize_kv4", "rbq_dequantize_kv4", "rbq_dense_decode_kv4", "rbq_sparse_decode_kv4", "rbq_decode_step_kv4",
+    "rbq_prefill_attention_kv4",
 ]
 
 
@@ -99,6 +104,17 @@ def _load():
                                 i32, vp, vp, vp, i32, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
         "rbq_prefill_attention": [i32, i32, i32, i32, vp, i64, vp, vp, i32, i64, i64, i64, i32, vp, vp, i32, i32, i32,
                                   f32, vp, vp, vp, sz, vp],
+        # the 4-bit cache
+        "rbq_quantize_kv4": [i32, i32, i32, vp, vp, i32, i64, i32, i32, i32, i32, vp, vp, vp, vp, vp],
+        "rbq_dequantize_kv4": [i32, i32, i32, vp, vp, i32, i32, i32, i32, vp, vp, i32, i64, vp, vp, vp],
+        "rbq_dense_decode_kv4": [i32, i32, i32, i32, vp, vp, vp, i32, i32, i32, vp, vp, i32, i64, i32, f32, vp, vp, vp,
+                                 sz, vp, vp, vp],
+        "rbq_sparse_decode_kv4": [i32, i32, i32, i32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, i32, i64, i32, f32, vp,
+                                  vp, vp, sz, vp, vp, vp],
+        "rbq_decode_step_kv4": [i32, i32, i32, i32, vp, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, i32, i64, i32, vp, vp,
+                                vp, i32, f32, f32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp],
+        "rbq_prefill_attention_kv4": [i32, i32, i32, i32, vp, i64, vp, vp, i32, i64, i64, vp, i32, vp, vp, i32, i32, i32,
+                                      vp, i32, f32, vp, vp, vp, sz, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -133,7 +149,8 @@ def _load_calls():
         return _NoCalls()
     _rbqcall.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in (
         "rbq_quantize_kv", "rbq_dequantize_kv", "rbq_dense_decode_kv8", "rbq_sparse_decode_kv8", "rbq_decode_step_kv8",
-        "rbq_prefill_attention")))
+        "rbq_prefill_attention", "rbq_quantize_kv4", "rbq_dequantize_kv4", "rbq_dense_decode_kv4", "rbq_sparse_decode_kv4",
+        "rbq_decode_step_kv4", "rbq_prefill_attention_kv4")))
     return _rbqcall
 
 
@@ -614,5 +631,142 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
     st = _call.rbq_prefill_attention(
         batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, dt, kv_ld, kv_head, kv_seq, kv_rows, cu_q, cu_k, total_q,
         max_k, 1 if causal else 0, sm_scale, out, lse, ws, ws_bytes, _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+# ---- the 4-bit cache: kv4 [B][Hkv][cap][D] torch.uint8 (records), par [B][Hkv][cap][2] torch.int32 (words), fmt RBQ_FP4
+# or RBQ_I4 (KV4_FORMATS by name); seq_*: as above.
+
+def _check_kv4(name, groups, head_dim, cap, kv4, par):
+    """The types of the cache's buffers."""
+    for arg, t, dt in (("kv4", kv4, torch.uint8), ("par", par, torch.int32)):
+        if t.dtype is not dt:
+            raise ValueError(f"{name}: {arg} is {t.dtype}, {dt} is taken")
+    return groups * cap * head_dim, groups * cap * 2
+
+
+def _check_kv4_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, kv4, par, seq_off, seq_rows):
+    """Types of the cache and of the rows, once every buffer is large enough."""
+    groups, dt = batch * heads_kv, _KV_CODES.get(K.dtype)
+    count, words = _check_kv4(name, groups, head_dim, cap, kv4, par)
+    if dt is None or K.dtype is not V.dtype:
+        _pair_code(name, _KV_CODES, "K", K, "V", V)
+    need = ((groups - 1) * ld + rows) * head_dim if rows > 0 else 0
+    if not _call.fits(2, K, need, V, need, kv4, count, par, words, seq_off, batch, seq_rows, batch):
+        _too_small(name, ("K", "V"), K=(K, need), V=(V, need), kv4=(kv4, count), par=(par, words), seq_off=(seq_off, batch),
+                   seq_rows=(seq_rows, batch))
+    return dt
+
+
+def rbq_quantize_kv4(batch, heads_kv, head_dim, K, V, ld, n_new, offset, cap, fmt, kv4, par, seq_off=None, seq_new=None,
+                     stream=None):
+    """Write rows [0, n_new) of K / V [B][Hkv][ld][D] into the 4-bit cache as rows [offset, offset + n_new)."""
+    name = "rbq_quantize_kv4"
+    dt = _check_kv4_rows(name, batch, heads_kv, head_dim, K, V, ld, n_new, cap, kv4, par, seq_off, seq_new)
+    st = _call.rbq_quantize_kv4(batch, heads_kv, head_dim, K, V, dt, ld, n_new, offset, cap, fmt, kv4, par, seq_off, seq_new,
+                                _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+def rbq_dequantize_kv4(batch, heads_kv, head_dim, kv4, par, fmt, cap, n_rows, offset, K, V, ld, seq_off=None,
+                       seq_rows=None, stream=None):
+    """Cache rows [offset, offset + n_rows) as rows [0, n_rows) of K / V [B][Hkv][ld][D] (bf16 or fp32)."""
+    name = "rbq_dequantize_kv4"
+    dt = _check_kv4_rows(name, batch, heads_kv, head_dim, K, V, ld, n_rows, cap, kv4, par, seq_off, seq_rows)
+    st = _call.rbq_dequantize_kv4(batch, heads_kv, head_dim, kv4, par, fmt, cap, n_rows, offset, K, V, dt, ld, seq_off,
+                                  seq_rows, _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+def _check_decode_kv4(name, batch, heads_q, heads_kv, head_dim, q, kv4, par, cap, K_loc, V_loc, loc_ld, w, out, lse, seq_n,
+                      seq_w):
+    """Types of the cache and of the window, once every buffer is large enough."""
+    loc, groups, rows, need = RBQ_BF16, batch * heads_kv, batch * heads_q, 0
+    count, words = _check_kv4(name, groups, head_dim, cap, kv4, par)
+    if K_loc is not None and V_loc is not None:
+        loc = _KV_CODES.get(K_loc.dtype)
+        if loc is None or K_loc.dtype is not V_loc.dtype:
+            _pair_code(name, _KV_CODES, "K_loc", K_loc, "V_loc", V_loc)
+        need = ((groups - 1) * loc_ld + w) * head_dim if w > 0 else 0
+    if not _call.fits(2, K_loc, need, V_loc, need, kv4, count, par, words, q, rows * head_dim, out, rows * head_dim, lse,
+                      rows, seq_n, batch, seq_w, batch):
+        _too_small(name, ("K_loc", "V_loc"), K_loc=(K_loc, need), V_loc=(V_loc, need), kv4=(kv4, count), par=(par, words),
+                   q=(q, rows * head_dim), out=(out, rows * head_dim), lse=(lse, rows), seq_n=(seq_n, batch),
+                   seq_w=(seq_w, batch))
+    return loc
+
+
+def rbq_dense_decode_kv4(batch, heads_q, heads_kv, head_dim, q, kv4, par, fmt, cap, n, K_loc, V_loc, loc_ld, w, sm_scale,
+                         out, lse, ws, seq_n=None, seq_w=None, stream=None):
+    """rbq_dense_decode over a 4-bit cache and a window [B][Hkv][loc_ld][D] in bf16 or fp32."""
+    name = "rbq_dense_decode_kv4"
+    loc = _check_decode_kv4(name, batch, heads_q, heads_kv, head_dim, q, kv4, par, cap, K_loc, V_loc, loc_ld, w, out, lse,
+                            seq_n, seq_w)
+    st = _call.rbq_dense_decode_kv4(
+        batch, heads_q, heads_kv, head_dim, q, kv4, par, fmt, cap, n, K_loc, V_loc, loc, loc_ld, w, sm_scale, out, lse, ws,
+        ws.nbytes, seq_n, seq_w, _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+def rbq_sparse_decode_kv4(batch, heads_q, heads_kv, head_dim, q, kv4, par, fmt, cap, n, sel_idx, sel_count, K_loc, V_loc,
+                          loc_ld, w, sm_scale, out, lse, ws, seq_n=None, seq_w=None, stream=None):
+    """rbq_sparse_decode over a 4-bit cache and a window [B][Hkv][loc_ld][D] in bf16 or fp32."""
+    name = "rbq_sparse_decode_kv4"
+    loc = _check_decode_kv4(name, batch, heads_q, heads_kv, head_dim, q, kv4, par, cap, K_loc, V_loc, loc_ld, w, out, lse,
+                            seq_n, seq_w)
+    if not _call.fits(0, sel_idx, batch * heads_q * n, sel_count, batch * heads_q):
+        _too_small(name, sel_idx=(sel_idx, batch * heads_q * n), sel_count=(sel_count, batch * heads_q))
+    st = _call.rbq_sparse_decode_kv4(
+        batch, heads_q, heads_kv, head_dim, q, kv4, par, fmt, cap, n, sel_idx, sel_count, K_loc, V_loc, loc, loc_ld, w,
+        sm_scale, out, lse, ws, ws.nbytes, seq_n, seq_w, _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+def rbq_decode_step_kv4(batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, kv4, par, fmt, cap, n, K_loc, V_loc, loc_ld, w,
+                        codes, kfac, kfac16, flush, p, sm_scale, qplanes, qscal, scores, sel_idx, sel_count, out, lse, ws,
+                        stream=None):
+    """rbq_decode_step over a 4-bit cache and a window [B][Hkv][loc_ld][D]; kfac (full index) or kfac16 (compact), the
+    other None."""
+    name = "rbq_decode_step_kv4"
+    loc = _check_decode_kv4(name, batch, heads_q, heads_kv, head_dim, q, kv4, par, cap, K_loc, V_loc, loc_ld, w, out, lse,
+                            None, None)
+    rows = batch * heads_q
+    if not _call.fits(0, qplanes, rows * 4 * (head_dim // 32), qscal, rows * QSCAL_STRIDE, scores, rows * n, sel_idx,
+                      rows * n, sel_count, rows):
+        _too_small(name, qplanes=(qplanes, rows * 4 * (head_dim // 32)), qscal=(qscal, rows * QSCAL_STRIDE),
+                   scores=(scores, rows * n), sel_idx=(sel_idx, rows * n), sel_count=(sel_count, rows))
+    st = _call.rbq_decode_step_kv4(
+        batch, heads_q, heads_kv, head_dim, q, P, c_q, c_k, kv4, par, fmt, cap, n, K_loc, V_loc, loc, loc_ld, w, codes, kfac,
+        kfac16, 1 if flush else 0, p, sm_scale, qplanes, qscal, scores, sel_idx, sel_count, out, lse, ws, ws.nbytes,
+        _stream(stream))
+    if st != RBQ_OK:
+        raise RbqError(name, st)
+
+
+def rbq_prefill_attention_kv4(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_ld, kv_head, cu_q, total_q, kv4, par,
+                              fmt, cap, n, seq_n, causal, sm_scale, out, lse, ws=None, stream=None):
+    """rbq_prefill_attention of chunks over rows in a 4-bit cache (sequence b's first seq_n[b], n without seq_n) and the
+    chunks' own K / V, packed like q: rows kv_ld elements apart, heads kv_head."""
+    name = "rbq_prefill_attention_kv4"
+    dt = _pair_code(name, _KV_CODES, "K", K, "V", V)
+    if q.dtype != K.dtype or out.dtype != K.dtype:
+        raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
+    count, words = _check_kv4(name, batch * heads_kv, head_dim, cap, kv4, par)
+    rows = total_q * heads_q
+    need_q = (total_q - 1) * q_ld + heads_q * head_dim if total_q > 0 else 0
+    need = (total_q - 1) * kv_ld + (heads_kv - 1) * kv_head + head_dim if total_q > 0 else 0
+    if not _call.fits(3, q, need_q, K, need, V, need, kv4, count, par, words, cu_q, batch + 1, seq_n, batch, out,
+                      rows * head_dim, lse, rows):
+        _too_small(name, ("q", "K", "V"), q=(q, need_q), K=(K, need), V=(V, need), kv4=(kv4, count), par=(par, words),
+                   cu_q=(cu_q, batch + 1), seq_n=(seq_n, batch), out=(out, rows * head_dim), lse=(lse, rows))
+    ws_bytes = 0 if ws is None else ws.nbytes
+    st = _call.rbq_prefill_attention_kv4(
+        batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, dt, kv_ld, kv_head, cu_q, total_q, kv4, par, fmt, cap, n, seq_n,
+        1 if causal else 0, sm_scale, out, lse, ws, ws_bytes, _stream(stream))
     if st != RBQ_OK:
         raise RbqError(name, st)
