@@ -29,12 +29,10 @@ constexpr int row_bytes(int src, int D) { return is_kv4(src) ? D : D * elem_bits
 constexpr int k_span(int fmt, int D) { return is_kv4(fmt) ? D / 4 : 16; }
 
 // One group's rows as one lane (x, j) sees them, raw: row x of each tile (its dimensions, see
-// k_span) and dimensions (D / 16) x .. +D / 16 of rows 4j .. 4j+3 (4 bits at D = 64: the word
-// that holds them).
+// k_span) and dimensions (D / 16) x .. +D / 16 of rows 4j .. 4j+3.
 template <int SRC, int D>
 struct RowRegs {
-  static constexpr int kKw = D * elem_bits(SRC) / 128;
-  static constexpr int kVw = D * elem_bits(SRC) / 512 > 0 ? D * elem_bits(SRC) / 512 : 1;
+  static constexpr int kKw = D * elem_bits(SRC) / 128, kVw = D * elem_bits(SRC) / 512;
   uint32_t k[row_tiles(SRC)][kKw];
   uint32_t v[row_tiles(SRC)][4][kVw];
 };
@@ -70,26 +68,9 @@ __device__ __forceinline__ uint32_t codes_bf16(uint32_t w) {
   }
 }
 
-// Eight 4-bit codes as eight bf16: e2m1 codes times a power of two (exact, as far as bf16
-// reaches), in pairs of a byte's two; whole numbers c as 16 + c, by their bits (the mantissa's
-// top four), in pairs of nibbles p and p + 4. Either way the eight come in their dimensions' order.
-template <int SRC>
-__device__ __forceinline__ u32x4 nibbles_bf16(uint32_t w, float scale) {
-  if constexpr (SRC == RBQ_FP4) {
-    return u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
-                 __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
-  } else {
-    constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
-    return u32x4{(w << 3 & kMask) | kSixteen, (w >> 1 & kMask) | kSixteen, (w >> 5 & kMask) | kSixteen,
-                 (w >> 9 & kMask) | kSixteen};
-  }
-}
-
 // a lane's 8 dimensions (group kb of the logits product) of a row as an operand, part `part`
 template <int SRC>
-__device__ __forceinline__ bf16x8 k_operand(const uint32_t* k, int kb, int part, float scale) {
+__device__ __forceinline__ bf16x8 k_operand(const uint32_t* k, int kb, int part) {
   const uint32_t* w = k + kb * elem_bits(SRC) / 4;
   if constexpr (SRC == RBQ_BF16) {
     return __builtin_bit_cast(bf16x8, u32x4{w[0], w[1], w[2], w[3]});
@@ -104,8 +85,6 @@ __device__ __forceinline__ bf16x8 k_operand(const uint32_t* k, int kb, int part,
       p = __builtin_convertvector(r, bf16x8);
     }
     return p;
-  } else if constexpr (is_kv4(SRC)) {
-    return __builtin_bit_cast(bf16x8, nibbles_bf16<SRC>(*w, scale));
   } else {
     return __builtin_bit_cast(bf16x8, u32x4{codes_bf16<SRC, false>(w[0]), codes_bf16<SRC, true>(w[0]),
                                             codes_bf16<SRC, false>(w[1]), codes_bf16<SRC, true>(w[1])});
@@ -114,18 +93,8 @@ __device__ __forceinline__ bf16x8 k_operand(const uint32_t* k, int kb, int part,
 
 // column c (of the lane's D / 16) of the lane's four rows as two pairs of bf16, part `part`
 template <int SRC, int VW>
-__device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int part, const float* scale) {
-  if constexpr (SRC == RBQ_FP4) {
-    uint32_t p[4];   // columns c and c + 1 (of an even c) of each row
-#pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = nibbles_bf16<SRC>(v[i][0], scale[i])[c / 2];
-    const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-    return u32x2{__builtin_amdgcn_perm(p[1], p[0], sel), __builtin_amdgcn_perm(p[3], p[2], sel)};
-  } else if constexpr (SRC == RBQ_I4) {   // the even columns are in a word's low half, the odd ones in the high half
-    const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
-    return u32x2{nibbles_bf16<SRC>(__builtin_amdgcn_perm(v[1][0], v[0][0], sel), 0.f)[c / 2],
-                 nibbles_bf16<SRC>(__builtin_amdgcn_perm(v[3][0], v[2][0], sel), 0.f)[c / 2]};
-  } else if constexpr (SRC == RBQ_BF16) {
+__device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int part) {
+  if constexpr (SRC == RBQ_BF16) {
     const uint32_t sel = c % 2 ? 0x07060302u : 0x05040100u;
     return u32x2{__builtin_amdgcn_perm(v[1][c / 2], v[0][c / 2], sel),
                  __builtin_amdgcn_perm(v[3][c / 2], v[2][c / 2], sel)};
@@ -158,9 +127,16 @@ __device__ __forceinline__ u32x2 v_column(const uint32_t (*v)[VW], int c, int pa
 template <int FMT, bool SPARSE, int G, int D>
 struct Shared {
   static_assert(kScaleCap <= kDThreads, "one scale pair per thread");
+  // Columns of the logits product: 8-bit rows, part * G + head where the three parts fit (one operand),
+  // head otherwise (one operand per part); 4-bit rows, slots of G heads, part kSlots op + slot in slot
+  // `slot` of operand op, zeros behind the last.
+  static constexpr bool kSlotted = is_kv4(FMT);
+  static constexpr int kSlots = 16 / G;
   static constexpr bool kPackedQ = kQParts * G <= 16;
-  static constexpr int kQOps = kPackedQ ? 1 : kQParts;
+  static constexpr int kQOps = kSlotted ? (kQParts + kSlots - 1) / kSlots : kPackedQ ? 1 : kQParts;
   static constexpr int kSpan = k_span(FMT, D);
+  // Rows of a wave's sums: a head's, or, slotted, a head's in kSums parts (4 and 8 heads' are added before)
+  static constexpr int kSums = kSlotted && G <= 2 ? kQParts : 1;
   static constexpr bool kBase = FMT == RBQ_I4;   // rows have a base beside their codes
   u32x4 qB[D / 32][kQOps][kWave];   // B operands of the logits product
   f32x2 scale[is_kv4(FMT) ? 1 : kScaleCap];   // {ks, vs} of the split's token blocks
@@ -171,20 +147,60 @@ struct Shared {
   __attribute__((aligned(16))) uint16_t hmask[SPARSE ? kListCap : 8];
   int rng_lo[G], rng_hi[G];
   float sm[kDWaves][G], sl[kDWaves][G];
-  __attribute__((aligned(16))) float sacc[kDWaves][G][D];
+  __attribute__((aligned(16))) float sacc[kDWaves][kSums * G][D];
 };
 
-// The word of lane i of this lane's four (lanes 4 (x / 4) .. +4)
-template <int I>
-__device__ __forceinline__ float quad_lane(float v) {
-  return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), 0x55 * I, 0xF, 0xF, true));
+// Slotted columns: the sum over the slots of this lane's head, in every one of its columns
+template <int G>
+__device__ __forceinline__ float slots_sum(float v) {
+  if constexpr (G <= 8) v += RBQ_DPP(v, 0x128);   // row_ror:8
+  if constexpr (G <= 4) v += RBQ_DPP(v, 0x124);
+  if constexpr (G <= 2) v += RBQ_DPP(v, 0x122);
+  if constexpr (G <= 1) v += RBQ_DPP(v, 0x121);
+  return v;
 }
-
-__device__ __forceinline__ void spread4(float v, float* to) {
-  to[0] = quad_lane<0>(v);
-  to[1] = quad_lane<1>(v);
-  to[2] = quad_lane<2>(v);
-  to[3] = quad_lane<3>(v);
+// N probabilities, weighed, of this lane's head as the operands of the second product, its rows
+// slotted like those columns: slot p holds part p of three (8 bits each; exact in 24), so that up
+// to five heads' parts share a product; 8 heads: hi and lo, mid; 16: one operand per part. Rows of
+// further slots repeat part 2 and are not summed.
+template <int G, int N>
+__device__ __forceinline__ void slot_parts(const float* w, uint32_t (*pa)[N / 2]) {
+  const int slot = (lane_id() & 15) / G;
+  auto top = [](float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); };
+  auto put = [](uint32_t* to, const float* v) {   // the top halves
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) to[i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
+  };
+  float r[N];
+  if constexpr (G <= 4) {
+    const uint32_t m1 = slot >= 1 ? 0xFFFF0000u : 0u, m2 = slot >= 2 ? 0xFFFF0000u : 0u;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const float a = w[i] - __uint_as_float(__float_as_uint(w[i]) & m1);
+      r[i] = a - __uint_as_float(__float_as_uint(a) & m2);
+    }
+    put(pa[0], r);
+  } else {
+    float mid[N], lo[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      mid[i] = w[i] - top(w[i]);
+      lo[i] = mid[i] - top(mid[i]);
+    }
+    if constexpr (G == 8) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        r[i] = slot == 0 ? w[i] : mid[i];
+        lo[i] = slot == 0 ? lo[i] : 0.f;
+      }
+      put(pa[0], r);
+      put(pa[1], lo);
+    } else {
+      put(pa[0], w);
+      put(pa[1], mid);
+      put(pa[2], lo);
+    }
+  }
 }
 
 // One wave's online softmax over its groups of the block's U rows: row c0 + e of the
@@ -196,27 +212,21 @@ template <int SRC, bool LIST, int G, int D, int CP, class S>
 struct Rows {
   static constexpr int NT = row_tiles(SRC), kRows = 16 * NT, KB = D / 32, NP = row_parts(SRC);
   static constexpr int kSpan = S::kSpan, RB = row_bytes(SRC, D), LB = kSpan * elem_bits(SRC) / 8;   // bytes of a row, of a span
-  static constexpr bool kNib = is_kv4(SRC), kCodes = is_codes(SRC) && !kNib, kBase = SRC == RBQ_I4;
+  static constexpr bool kCodes = is_codes(SRC);
   // One group's registers are reused for the next: its K rows are requested as soon
   // as the logits are done, its V rows as soon as the values are. (fp32 rows, four
   // times the registers: each half is requested when its turn comes.)
   static constexpr bool kAhead = SRC != RBQ_F32;
   using Regs = RowRegs<SRC, D>;
   S& sh;
-  const __amdgpu_buffer_rsrc_t Kr, Vr, Pr;   // (Pr: the words of 4-bit rows)
+  const __amdgpu_buffer_rsrc_t Kr, Vr;
   const int c0, U, bshift, in_block, wave, x, j, ngroups;   // in_block: place of row c0 in its token block
   Regs cur;
   uint32_t mk;                // bit 4 t + i: row 4j + i of tile t is valid and taken by head x
   f32x2 sc[LIST ? NT : 1][4];   // its scales {ks, vs} (listed 8-bit rows)
-  // words of 4-bit rows: fp4, of row x (its K exponents); of row 4j + x % 4 (V's, int4 K's too)
-  uint32_t kw[kNib ? NT : 1];
-  u32x2 pw[kNib ? NT : 1];
 
   __device__ __forceinline__ Rows(S& s, __amdgpu_buffer_rsrc_t kr, __amdgpu_buffer_rsrc_t vr, int first, int rows, int shift)
-      : Rows(s, kr, vr, kr, first, rows, shift) {}
-  __device__ __forceinline__ Rows(S& s, __amdgpu_buffer_rsrc_t kr, __amdgpu_buffer_rsrc_t vr, __amdgpu_buffer_rsrc_t pr,
-                                  int first, int rows, int shift)
-      : sh(s), Kr(kr), Vr(vr), Pr(pr), c0(first), U(rows), bshift(shift), in_block(first & ((1 << shift) - 1)),
+      : sh(s), Kr(kr), Vr(vr), c0(first), U(rows), bshift(shift), in_block(first & ((1 << shift) - 1)),
         wave(threadIdx.x / kWave), x(lane_id() & 15), j(lane_id() >> 4), ngroups((rows + kRows - 1) / kRows) {}
 
   __device__ __forceinline__ int row_of(int grp, int e) const { return c0 + (e < U ? e : grp * kRows); }
@@ -230,7 +240,6 @@ struct Rows {
       const int off = skip ? kSkipOffset : row * RB + LB * j;
 #pragma unroll
       for (int i = 0; i < D / (4 * kSpan); ++i) load_words<LB / 4, CP>(&cur.k[t][LB / 4 * i], Kr, off + 4 * LB * i);
-      if constexpr (SRC == RBQ_FP4) load_words<1, CP>(&kw[t], Pr, skip ? kSkipOffset : row * 8);
     }
   }
   __device__ __forceinline__ void load_v(int grp, bool skip) {
@@ -248,23 +257,14 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           row[i] = row_of(grp, e0 + i);
-          mk |= uint32_t(e0 + i < U && x < G) << (4 * t + i);
+          mk |= uint32_t(e0 + i < U && (S::kSlotted || x < G)) << (4 * t + i);
         }
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        // (4 bits at D = 64: the word of dimensions 8 (x / 2) .. +8)
-        const int off = skip ? kSkipOffset : row[i] * RB + (kNib && D == 64 ? 4 * (x / 2) : D * elem_bits(SRC) / 128 * x);
+        const int off = skip ? kSkipOffset : row[i] * RB + D * elem_bits(SRC) / 128 * x;
         load_words<Regs::kVw, CP>(cur.v[t][i], Vr, off);
         if constexpr (LIST && kCodes) sc[t][i] = sh.scale[(in_block + row[i] - c0) >> bshift];
-      }
-      if constexpr (kNib) {
-        int own;
-        if constexpr (LIST) own = sh.lst[e0 + (x & 3)];
-        else own = row_of(grp, e0 + (x & 3));
-        const int off = skip ? kSkipOffset : own * 8;
-        if constexpr (kBase) load_words<2, CP>(reinterpret_cast<uint32_t*>(&pw[t]), Pr, off);
-        else load_words<1, CP>(reinterpret_cast<uint32_t*>(&pw[t]) + 1, Pr, off + 4);
       }
     }
   }
@@ -277,8 +277,6 @@ struct Rows {
 
   __device__ __forceinline__ void run(float& m, float& lsum, float& base, f32x4 (&acc)[D / 16]) {
     constexpr int kQOps = S::kQOps;
-    float qsum = 0.f;
-    if constexpr (kBase) qsum = sh.qsum[min(x, G - 1)];
     int grp = wave;
     while (grp < ngroups) {
       const int nxt = grp + kDWaves;
@@ -297,12 +295,6 @@ struct Rows {
           ts[t] = sh.scale[(in_block + (e < U ? e : 0)) >> bshift];
         }
       }
-      // 4-bit rows: K's scale of row x; scales and bases of rows 4j + i
-      float kscale[NT], ks[NT][4], kb0[NT][4], vs[NT][4], vb0[NT][4];
-      if constexpr (SRC == RBQ_FP4) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) kscale[t] = __uint_as_float((kw[t] >> (8 * j) & 255u) << 23);
-      }
       f32x4 s[NT];
 #pragma unroll
       for (int t = 0; t < NT; ++t) s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -314,7 +306,7 @@ struct Rows {
           __builtin_amdgcn_sched_barrier(0);
           bf16x8 a[NT];
 #pragma unroll
-          for (int t = 0; t < NT; ++t) a[t] = k_operand<SRC>(cur.k[t], kb, p, kscale[t]);
+          for (int t = 0; t < NT; ++t) a[t] = k_operand<SRC>(cur.k[t], kb, p);
 #pragma unroll
           for (int op = 0; op < kQOps; ++op) {
             const bf16x8 b = __builtin_bit_cast(bf16x8, qp[(kb * kQOps + op) * kWave]);
@@ -325,20 +317,6 @@ struct Rows {
       }
       if constexpr (kAhead) load_k(last ? grp : nxt, last);
       else load_v(grp, false);
-      if constexpr (kNib) {
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if constexpr (kBase) {   // the codes come as 16 + c
-            const float k1 = __uint_as_float(pw[t].x << 16), v1 = __uint_as_float(pw[t].y << 16);
-            spread4(k1, ks[t]);
-            spread4(fmaf(-16.f, k1, __uint_as_float(pw[t].x & 0xFFFF0000u)), kb0[t]);
-            spread4(v1, vs[t]);
-            spread4(fmaf(-16.f, v1, __uint_as_float(pw[t].y & 0xFFFF0000u)), vb0[t]);
-          } else {
-            spread4(__uint_as_float((pw[t].y >> (8 * (x / 4)) & 255u) << 23), vs[t]);
-          }
-        }
-      }
       // columns h + G and h + 2G hold the mid and lo parts of head h's logits (through
       // opaque copies: hipcc 7.2 reads one element's register for all four otherwise)
       float lg[NT][4];
@@ -348,7 +326,10 @@ struct Rows {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float sv = s[t][i];
-          if constexpr (S::kPackedQ) {
+          if constexpr (S::kSlotted) {
+            asm volatile("" : "+v"(sv));
+            sv = slots_sum<G>(sv);
+          } else if constexpr (S::kPackedQ) {
             asm volatile("" : "+v"(sv));
             const int v = __builtin_bit_cast(int, sv);
             const float mid = __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, v, 0x100 + G, 0xF, 0xF, false));
@@ -356,8 +337,7 @@ struct Rows {
             sv = (sv + mid) + lo;
           }
           if constexpr (kCodes) sv *= LIST ? sc[LIST ? t : 0][i].x : ts[t].x;
-          else if constexpr (kBase) sv = fmaf(qsum, kb0[t][i], sv * ks[t][i]);
-          else if constexpr (!kNib) sv = fmaf(sv, 0.f, sv);   // (an infinite key's, whatever the signs of the query's parts: NaN)
+          else sv = fmaf(sv, 0.f, sv);   // (an infinite key's, whatever the signs of the query's parts: NaN)
           lg[t][i] = ((mk >> (4 * t + i)) & 1u) ? sv : -INFINITY;
           tmax = fmaxf(tmax, lg[t][i]);
         }
@@ -367,23 +347,18 @@ struct Rows {
       const float mn = fmaxf(m, tmax);
       const float mref = mn == -INFINITY ? 0.f : mn;   // (no row yet: every exponential below is that of -inf)
       const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mref);
-      float w[NT * 4], sum = 0.f, bsum = 0.f;
+      float w[NT * 4], sum = 0.f;
 #pragma unroll
       for (int t = 0; t < NT; ++t) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p = __builtin_amdgcn_exp2f(lg[t][i] - mref);
           sum += p;
-          if constexpr (kBase) {
-            bsum = fmaf(p, vb0[t][i], bsum);
-            w[4 * t + i] = p * vs[t][i];
-          } else {
-            w[4 * t + i] = kCodes ? p * (LIST ? sc[LIST ? t : 0][i].y : ts[t].y) : p;
-          }
+          w[4 * t + i] = kCodes ? p * (LIST ? sc[LIST ? t : 0][i].y : ts[t].y) : p;
         }
       }
       lsum = fmaf(lsum, corr, sum);
-      if constexpr (S::kBase) base = fmaf(base, corr, bsum);
+      if constexpr (S::kBase) base *= corr;   // (of the 4-bit rows before)
       const bool moved = mn != m;
       m = mn;
       if (__ballot(moved)) {
@@ -399,7 +374,12 @@ struct Rows {
       // the weighted probabilities in three parts: A operands (row = head x; k = rows 4j .. 4j+3
       // of both tiles, or, of one tile, the same rows in two parts)
       bf16x8 pa[3];
-      if constexpr (NT == 2) {
+      if constexpr (S::kSlotted) {   // (the window: one tile, an operand's other four rows are zeros)
+        uint32_t ps[S::kQOps][2];
+        slot_parts<G, 4>(w, ps);
+#pragma unroll
+        for (int t = 0; t < S::kQOps; ++t) pa[t] = __builtin_bit_cast(bf16x8, u32x4{ps[t][0], ps[t][1], 0u, 0u});
+      } else if constexpr (NT == 2) {
         f32x8 wv;
 #pragma unroll
         for (int i = 0; i < 8; ++i) wv[i] = w[i];
@@ -417,28 +397,292 @@ struct Rows {
         pa[0] = __builtin_shufflevector(p3[0], p3[1], 0, 1, 2, 3, 4, 5, 6, 7);
         pa[1] = __builtin_shufflevector(p3[2], zero, 0, 1, 2, 3, 4, 5, 6, 7);
       }
-      if constexpr (kNib && D == 64) {   // the lane's four columns to the low end of each half, or of the word
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) cur.v[t][i][0] >>= (kBase ? 8 : 16) * (x & 1);
-      }
 #pragma unroll
       for (int c = 0; c < D / 16; ++c) {
         if (c % 2 == 0) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
-          const u32x2 v0 = v_column<SRC>(cur.v[0], c, p, vs[0]);
-          const u32x2 v1 = NT == 2 ? v_column<SRC>(cur.v[NT - 1], c, p, vs[NT - 1]) : v0;
+          const u32x2 v0 = v_column<SRC>(cur.v[0], c, p);
+          const u32x2 v1 = NT == 2 ? v_column<SRC>(cur.v[NT - 1], c, p) : v0;
           const bf16x8 bv = __builtin_bit_cast(bf16x8, u32x4{v0.x, v0.y, v1.x, v1.y});
 #pragma unroll
-          for (int t = 0; t < (NT == 2 ? 3 : 2); ++t)
+          for (int t = 0; t < (S::kSlotted ? S::kQOps : NT == 2 ? 3 : 2); ++t)
             acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[t], bv, acc[c], 0, 0, 0);
         }
       }
       if constexpr (kAhead) load_v(last ? grp : nxt, last);
       grp = nxt;
     }
+  }
+};
+
+// Eight 4-bit codes as eight bf16, in the order that the bytes of a word have after pick8
+// (int4) or lie in (fp4): e2m1 codes times a power of two, exact as far as bf16 reaches; whole
+// numbers 0 to 15 as they are: as bytes they are e4m3 codes of themselves times 2^-9 (that
+// format's subnormals and its first octave are one linear range).
+template <int FMT, bool HI>
+__device__ __forceinline__ uint32_t whole_bf16(uint32_t bytes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.f, HI));
+}
+constexpr uint32_t kNibbles = 0x0F0F0F0Fu;
+
+// One wave's online softmax over its groups of 32 4-bit rows (as Rows): row c0 + e, or lst[e].
+// Its columns and rows are slotted: every lane has the logits of head x % G, and the second
+// product takes the three parts of up to 4 heads' probabilities as rows of one operand (8
+// products for 128 dimensions where parts of their own would take 24).
+template <int FMT, bool LIST, int G, int D, int CP, class S>
+struct NibRows {
+  static constexpr int kGroup = 32, KB = D / 32, kOps = S::kQOps;
+  static constexpr bool kBase = FMT == RBQ_I4;
+  S& sh;
+  const __amdgpu_buffer_rsrc_t rec, words;   // from the buffers' first row (LIST), or from row c0
+  const int U, wave, x, j, ngroups;
+  int koff, voff, poff, woff;   // of the next group's: K's quarter rows, V's columns, words (fp4: of K's rows)
+  uint32_t k[2][KB], v[2][4];   // row x of each tile, D / 4 dimensions from D j / 4 on; columns of rows 4j + i
+  uint32_t kw[2];               // fp4: K's word of row x
+  u32x2 pw[2];                  // words of row 4j + x % 4 (fp4: V's)
+  u32x2 hm[LIST ? 2 : 1];       // the heads that take rows 4j + i
+
+  // (D = 64: a lane's four columns are half of the word of dimensions 8 (x / 2) .. +8)
+  static __device__ __forceinline__ int column_bytes(int x) { return D == 64 ? 4 * (x / 2) : 4 * x; }
+  __device__ __forceinline__ NibRows(S& s, __amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t w, int rows)
+      : sh(s), rec(r), words(w), U(rows), wave(threadIdx.x / kWave), x(lane_id() & 15), j(lane_id() >> 4),
+        ngroups((rows + kGroup - 1) / kGroup) {
+    const int first = wave * kGroup;
+    koff = (first + x) * D + D / 8 * j;
+    voff = (first + 4 * j) * D + D / 2 + column_bytes(x);
+    poff = (first + 4 * j + (x & 3)) * 8;
+    woff = (first + x) * 8;
+  }
+  __device__ __forceinline__ void load_k(int grp) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      int off, wo;
+      if constexpr (LIST) {
+        const int row = grp < ngroups ? sh.lst[grp * kGroup + 16 * t + x] : kSkipOffset / D;
+        off = row * D + D / 8 * j;
+        wo = row * 8;
+      } else {
+        off = (grp < ngroups ? koff : kSkipOffset) + 16 * t * D;
+        wo = (grp < ngroups ? woff : kSkipOffset) + 16 * t * 8;
+      }
+      load_words<KB, CP>(k[t], rec, off);
+      if constexpr (!kBase) load_words<1, CP>(&kw[t], words, wo);
+    }
+    koff += kDWaves * kGroup * D;
+    woff += kDWaves * kGroup * 8;
+  }
+  __device__ __forceinline__ void load_v(int grp) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      int po;
+      if constexpr (LIST) {
+        const bool live = grp < ngroups;
+        const int e0 = (live ? grp : 0) * kGroup + 16 * t + 4 * j;
+        const i32x4 row = *reinterpret_cast<const i32x4*>(sh.lst + e0);
+        hm[t] = *reinterpret_cast<const u32x2*>(sh.hmask + e0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          load_words<1, CP>(&v[t][i], rec, live ? row[i] * D + D / 2 + column_bytes(x) : kSkipOffset);
+        po = live ? sh.lst[e0 + (x & 3)] * 8 : kSkipOffset;
+      } else {
+        const int vo = grp < ngroups ? voff : kSkipOffset;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_words<1, CP>(&v[t][i], rec, vo + (16 * t + i) * D);
+        po = (grp < ngroups ? poff : kSkipOffset) + 16 * t * 8;
+      }
+      if constexpr (kBase) load_words<2, CP>(reinterpret_cast<uint32_t*>(&pw[t]), words, po);
+      else load_words<1, CP>(reinterpret_cast<uint32_t*>(&pw[t]) + 1, words, po + 4);
+    }
+    voff += kDWaves * kGroup * D;
+    poff += kDWaves * kGroup * 8;
+  }
+  __device__ __forceinline__ void begin() {
+    if (wave < ngroups) {
+      load_k(wave);
+      load_v(wave);
+    }
+  }
+  // K's row of tile t, dimensions kb, as an operand
+  __device__ __forceinline__ bf16x8 key(int t, int kb, float scale) const {
+    const uint32_t w = k[t][kb];
+    if constexpr (kBase) {
+      const uint32_t even = w & kNibbles, odd = w >> 4 & kNibbles;   // dimensions 0 4 1 5, 2 6 3 7
+      const uint32_t a = __builtin_amdgcn_perm(odd, even, 0x06040200u), b = __builtin_amdgcn_perm(odd, even, 0x07050301u);
+      return __builtin_bit_cast(bf16x8, u32x4{whole_bf16<FMT, false>(a), whole_bf16<FMT, true>(a), whole_bf16<FMT, false>(b),
+                                              whole_bf16<FMT, true>(b)});
+    } else {
+      return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))});
+    }
+  }
+  // Columns c .. c + 3 (c = 0 or 4) of rows 4j + i of tile t: to[m] the pairs {rows 0, 1}, {rows 2, 3} of column c + m
+  __device__ __forceinline__ void columns(int t, int c, const float (&scale)[4], u32x2 (&to)[4]) const {
+#pragma unroll
+    for (int p = 0; p < 2; ++p) {   // the pair of rows
+      const uint32_t a = v[t][2 * p], b = v[t][2 * p + 1];
+      if constexpr (kBase) {
+        // columns c .. c + 3 are nibbles c / 2, c / 2 + 4, c / 2 + 1, c / 2 + 5: of byte c / 4 and of the one two on
+        const uint32_t y = __builtin_amdgcn_perm(b, a, c == 0 ? 0x06020400u : 0x07030501u);
+        const uint32_t lo = y & kNibbles, hi = y >> 4 & kNibbles;
+        to[0][p] = whole_bf16<FMT, false>(lo);
+        to[1][p] = whole_bf16<FMT, true>(lo);
+        to[2][p] = whole_bf16<FMT, false>(hi);
+        to[3][p] = whole_bf16<FMT, true>(hi);
+      } else {
+        uint32_t q[2][2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+          const uint32_t w = r ? b : a;
+          const float s = scale[2 * p + r];
+          if (c == 0) {
+            q[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
+            q[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+          } else {
+            q[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
+            q[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+          }
+        }
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          to[m][p] = __builtin_amdgcn_perm(q[1][m / 2], q[0][m / 2], m % 2 ? 0x07060302u : 0x05040100u);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void run(float& m, float& lsum, float& base, f32x4 (&acc)[D / 16]) {
+    float qsum = 0.f;
+    if constexpr (kBase) qsum = sh.qsum[x % G];
+    for (int grp = wave; grp < ngroups; grp += kDWaves) {
+      // (an opaque offset: the query operands are re-read from LDS every group)
+      int qoff = lane_id();
+      asm volatile("" : "+v"(qoff));
+      const u32x4* qp = &sh.qB[0][0][0] + qoff;
+      f32x4 s[2];
+      float kscale[2];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        kscale[t] = kBase ? 0.f : __uint_as_float((kw[t] >> (8 * j) & 255u) << 23);
+      }
+#pragma unroll
+      for (int kb = 0; kb < KB; ++kb) {
+        __builtin_amdgcn_sched_barrier(0);   // (kept in this order: moved up, every group's operands would be held at once)
+        bf16x8 a[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) a[t] = key(t, kb, kscale[t]);
+#pragma unroll
+        for (int op = 0; op < kOps; ++op) {
+          const bf16x8 b = __builtin_bit_cast(bf16x8, qp[(kb * kOps + op) * kWave]);
+#pragma unroll
+          for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b, s[t], 0, 0, 0);
+        }
+      }
+      load_k(grp + kDWaves);
+      float lg[2][4], vs[2][4], top = -INFINITY;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const float k1 = __uint_as_float(pw[t].x << 16), k0 = __uint_as_float(pw[t].x & 0xFFFF0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float sv = s[t][i];
+          // (through opaque copies: hipcc 7.2 reads one element's register for all four otherwise)
+          asm volatile("" : "+v"(sv));
+          sv = slots_sum<G>(sv);
+          if constexpr (kBase) sv = fmaf(quad_lane(k0, i), qsum, sv * quad_lane(k1, i));
+          lg[t][i] = sv;
+        }
+      }
+      if constexpr (LIST) {
+        const int h = x % G;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            lg[t][i] = int32_t((i < 2 ? hm[t].x : hm[t].y) << (i % 2 ? 15 - h : 31 - h)) < 0 ? lg[t][i] : -INFINITY;
+      } else if (grp * kGroup + kGroup > U) {
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) lg[t][i] = grp * kGroup + 16 * t + 4 * j + i < U ? lg[t][i] : -INFINITY;
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = fmaxf(top, lg[t][i]);
+      top = fmaxf(top, __shfl_xor(top, 16, kWave));
+      top = fmaxf(top, __shfl_xor(top, 32, kWave));
+      const float mn = fmaxf(m, top);
+      const float mref = mn == -INFINITY ? 0.f : mn;   // (no row yet: every exponential below is that of -inf)
+      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mref);
+      float w[8], sum = 0.f, bsum = 0.f;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const float v1 = kBase ? __uint_as_float(pw[t].y << 16) : __uint_as_float((pw[t].y >> (8 * (x / 4)) & 255u) << 23);
+        const float v0 = __uint_as_float(pw[t].y & 0xFFFF0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(lg[t][i] - mref);
+          sum += p;
+          if constexpr (kBase) {
+            bsum = fmaf(quad_lane(v0, i), p, bsum);
+            w[4 * t + i] = quad_lane(v1, i) * p;
+          } else {
+            vs[t][i] = quad_lane(v1, i);
+            w[4 * t + i] = p;
+          }
+        }
+      }
+      lsum = fmaf(lsum, corr, sum);
+      if constexpr (kBase) base = fmaf(base, corr, bsum);
+      const bool moved = mn != m;
+      m = mn;
+      if (__ballot(moved)) {
+        float cr[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) cr[i] = __shfl(corr, 4 * j + i, kWave);
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[c][i] *= cr[i];
+        }
+      }
+      uint32_t pa[kOps][4];
+      slot_parts<G, 8>(w, pa);
+      if constexpr (D == 64) {   // the lane's four columns to the low end of the word (int4: of its halves)
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) v[t][i] >>= (kBase ? 8 : 16) * (x & 1);
+      }
+#pragma unroll
+      for (int c = 0; c < D / 16; c += 4) {
+        u32x2 b[2][4];
+        __builtin_amdgcn_sched_barrier(0);
+        columns(0, c, vs[0], b[0]);
+        columns(1, c, vs[1], b[1]);
+#pragma unroll
+        for (int n = 0; n < 4; ++n) {
+          const bf16x8 bv = __builtin_bit_cast(bf16x8, u32x4{b[0][n].x, b[0][n].y, b[1][n].x, b[1][n].y});
+#pragma unroll
+          for (int op = 0; op < kOps; ++op)
+            acc[c + n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, u32x4{pa[op][0], pa[op][1], pa[op][2], pa[op][3]}), bv, acc[c + n], 0, 0, 0);
+        }
+      }
+      load_v(grp + kDWaves);
+    }
+  }
+
+  // v of lane i of this lane's four (4 (x / 4) .. +4)
+  static __device__ __forceinline__ float quad_lane(float v, int i) {
+    const int u = __builtin_bit_cast(int, v);
+    return __builtin_bit_cast(float, i == 0   ? __builtin_amdgcn_mov_dpp(u, 0x00, 0xF, 0xF, true)
+                                     : i == 1 ? __builtin_amdgcn_mov_dpp(u, 0x55, 0xF, 0xF, true)
+                                     : i == 2 ? __builtin_amdgcn_mov_dpp(u, 0xAA, 0xF, 0xF, true)
+                                              : __builtin_amdgcn_mov_dpp(u, 0xFF, 0xF, 0xF, true));
   }
 };
 
@@ -594,9 +838,9 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
   constexpr int kLocEl = elem_bits(LOC) / 8;
   const int64_t locb = int64_t(bh) * loc_ld * (D * kLocEl);
   const char* Kb = window ? K_loc + locb : K8 + int64_t(bh) * cap * D;
-  const char* Vb = window ? V_loc + locb : kNib ? Kb + D / 2 : V8 + int64_t(bh) * cap * D;
+  const char* Vb = window ? V_loc + locb : V8 + int64_t(bh) * cap * D;
   const uint32_t region = uint32_t(lim) * uint32_t(window ? D * kLocEl : D);   // < 2^31
-  const __amdgpu_buffer_rsrc_t Kr = make_rsrc(Kb, region), Vr = make_rsrc(Vb, kNib && !window ? region - D / 2 : region);
+  const __amdgpu_buffer_rsrc_t Kr = make_rsrc(Kb, region), Vr = make_rsrc(Vb, region);
   const __amdgpu_buffer_rsrc_t Pr = kNib ? make_rsrc(k_scale + int64_t(bh) * cap * 2, uint32_t(lim) * 8u) : Kr;
   float m = -INFINITY, lsum = 0.f, base = 0.f;
   f32x4 acc[D / 16];
@@ -618,13 +862,18 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
     if (scales) sh.scale[threadIdx.x] = own_scale;
     if (!stages) return;
     const f32x8 qv = __builtin_shufflevector(qa, qb, 0, 1, 2, 3, 4, 5, 6, 7) * scale_log2e;
-    bf16x8 parts[kQParts];
+    bf16x8 parts[S::kSlotted ? S::kQOps * S::kSlots : kQParts];
     split3(qv, parts);
     constexpr int kSub = S::kSpan / 8;   // pieces of 8 dimensions in a span
     const int kb = kSub * (qch / (4 * kSub)) + qch % kSub, jj = qch % (4 * kSub) / kSub;
 #pragma unroll
-    for (int t = 0; t < kQParts; ++t)
-      sh.qB[kb][S::kPackedQ ? 0 : t][16 * jj + (S::kPackedQ ? t * G + qh : qh)] = __builtin_bit_cast(u32x4, parts[t]);
+    for (int t = 0; t < (S::kSlotted ? S::kQOps * S::kSlots : kQParts); ++t) {
+      if constexpr (S::kSlotted)
+        sh.qB[kb][t / S::kSlots][16 * jj + t % S::kSlots * G + qh] =
+            t < kQParts ? __builtin_bit_cast(u32x4, parts[t]) : u32x4{0u, 0u, 0u, 0u};
+      else
+        sh.qB[kb][S::kPackedQ ? 0 : t][16 * jj + (S::kPackedQ ? t * G + qh : qh)] = __builtin_bit_cast(u32x4, parts[t]);
+    }
     if constexpr (S::kBase) {   // over the head's 8 or 16 threads
       float t = ((qv[0] + qv[1]) + (qv[2] + qv[3])) + ((qv[4] + qv[5]) + (qv[6] + qv[7]));
       t += RBQ_DPP(t, 0xB1);
@@ -648,9 +897,15 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
     const int U = build_union_list<G, kDThreads, true, kPad8, true>(sel_idx, sel_mask, mask_words, row0, n, c0, c1, 0, 0, sh.bm,
                                                               sh.lst, sh.hmask, sh.rng_lo, sh.rng_hi, mword, hcount);
     auto attend = [&](auto cp) {
-      Rows<FMT, true, G, D, decltype(cp)::value, S> rows(sh, Kr, Vr, Pr, c0, U, bshift);
-      rows.begin();
-      rows.run(m, lsum, base, acc);
+      if constexpr (kNib) {
+        NibRows<FMT, true, G, D, decltype(cp)::value, S> rows(sh, Kr, Pr, U);
+        rows.begin();
+        rows.run(m, lsum, base, acc);
+      } else {
+        Rows<FMT, true, G, D, decltype(cp)::value, S> rows(sh, Kr, Vr, c0, U, bshift);
+        rows.begin();
+        rows.run(m, lsum, base, acc);
+      }
     };
     if (G <= 4 && int64_t(U) * kStreamDenDen >= int64_t(c1 - c0) * kStreamDenNum) attend(std::integral_constant<int, kStream>{});
     else attend(std::integral_constant<int, 0>{});
@@ -662,8 +917,16 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
       rows.run(m, lsum, base, acc);
       infinite_values<LOC, D>(V_loc + locb, f0, f1, acc);
     }
+  } else if constexpr (kNib) {
+    const uint32_t own = uint32_t(lim - c0);   // (rows behind the split's own are masked)
+    NibRows<FMT, false, G, D, kStream, S> rows(sh, make_rsrc(Kb + int64_t(c0) * D, own * D),
+                                               make_rsrc(k_scale + (int64_t(bh) * cap + c0) * 2, own * 8u), c1 - c0);
+    rows.begin();
+    stage();
+    __syncthreads();
+    rows.run(m, lsum, base, acc);
   } else {
-    Rows<FMT, false, G, D, kStream, S> rows(sh, Kr, Vr, Pr, c0, c1 - c0, bshift);
+    Rows<FMT, false, G, D, kStream, S> rows(sh, Kr, Vr, c0, c1 - c0, bshift);
     rows.begin();
     stage();
     __syncthreads();
@@ -682,10 +945,20 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
     sh.sm[wave][x] = lsum == lsum ? m : lsum;   // (a NaN among the logits goes through the joins as the maximum)
     sh.sl[wave][x] = lsum;
   }
+  if constexpr (S::kSlotted && (G == 4 || G == 8)) {   // the parts' rows onto those of lanes j = 0 (and 1)
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v = G == 4 && j == 3 ? 0.f : acc[c][i];
+        if constexpr (G == 4) v += __shfl_xor(v, 16, kWave);
+        acc[c][i] = v + __shfl_xor(v, 32, kWave);
+      }
+  }
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int h = 4 * j + i;
-    if (h < G) {
+    if (h < S::kSums * G) {
 #pragma unroll
       for (int c = 0; c < D / 16; c += 4)
         *reinterpret_cast<f32x4*>(&sh.sacc[wave][h][(D / 16) * x + c]) =
@@ -705,6 +978,8 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
       if (sh.sm[v][g] != -INFINITY) {
         const float sc = __builtin_amdgcn_exp2f(sh.sm[v][g] - M);
         f32x4 a = *reinterpret_cast<const f32x4*>(&sh.sacc[v][g][4 * d4]);
+#pragma unroll
+        for (int p = 1; p < S::kSums; ++p) a += *reinterpret_cast<const f32x4*>(&sh.sacc[v][p * G + g][4 * d4]);
         if constexpr (S::kBase) a += sh.sbase[v][g];
         r = f32x4{fmaf(a.x, sc, r.x), fmaf(a.y, sc, r.y), fmaf(a.z, sc, r.z), fmaf(a.w, sc, r.w)};
         l = fmaf(sh.sl[v][g], sc, l);
