@@ -581,7 +581,9 @@ struct NibRows {
         }
       }
       load_k(grp + kDWaves);
+      // logits less the running maximum
       float lg[2][4], vs[2][4], top = -INFINITY;
+      const float mref = m == -INFINITY ? 0.f : m;   // (no row yet: every exponential below is that of -inf)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         const float k1 = __uint_as_float(pw[t].x << 16), k0 = __uint_as_float(pw[t].x & 0xFFFF0000u);
@@ -591,8 +593,8 @@ struct NibRows {
           // (through opaque copies: hipcc 7.2 reads one element's register for all four otherwise)
           asm volatile("" : "+v"(sv));
           sv = slots_sum<G>(sv);
-          if constexpr (kBase) sv = fmaf(quad_lane(k0, i), qsum, sv * quad_lane(k1, i));
-          lg[t][i] = sv;
+          if constexpr (kBase) lg[t][i] = fmaf(quad_lane(k1, i), sv, fmaf(quad_lane(k0, i), qsum, -mref));
+          else lg[t][i] = sv - mref;
         }
       }
       if constexpr (LIST) {
@@ -612,34 +614,19 @@ struct NibRows {
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) top = fmaxf(top, lg[t][i]);
-      top = fmaxf(top, __shfl_xor(top, 16, kWave));
-      top = fmaxf(top, __shfl_xor(top, 32, kWave));
-      const float mn = fmaxf(m, top);
-      const float mref = mn == -INFINITY ? 0.f : mn;   // (no row yet: every exponential below is that of -inf)
-      const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mref);
-      float w[8], sum = 0.f, bsum = 0.f;
+      // The maximum moves in few groups; only there the lanes of a head agree on it.
+      if (__ballot(m == -INFINITY ? top > -INFINITY : top > 0.f)) {
+        top = fmaxf(top, __shfl_xor(top, 16, kWave));
+        top = fmaxf(top, __shfl_xor(top, 32, kWave));
+        const float up = m == -INFINITY ? (top == -INFINITY ? 0.f : top) : fmaxf(top, 0.f);
+        const float corr = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(-up);
+        m = m == -INFINITY ? top : m + up;
+        lsum *= corr;
+        if constexpr (kBase) base *= corr;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const float v1 = kBase ? __uint_as_float(pw[t].y << 16) : __uint_as_float((pw[t].y >> (8 * (x / 4)) & 255u) << 23);
-        const float v0 = __uint_as_float(pw[t].y & 0xFFFF0000u);
+        for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float p = __builtin_amdgcn_exp2f(lg[t][i] - mref);
-          sum += p;
-          if constexpr (kBase) {
-            bsum = fmaf(quad_lane(v0, i), p, bsum);
-            w[4 * t + i] = quad_lane(v1, i) * p;
-          } else {
-            vs[t][i] = quad_lane(v1, i);
-            w[4 * t + i] = p;
-          }
-        }
-      }
-      lsum = fmaf(lsum, corr, sum);
-      if constexpr (kBase) base = fmaf(base, corr, bsum);
-      const bool moved = mn != m;
-      m = mn;
-      if (__ballot(moved)) {
+          for (int i = 0; i < 4; ++i) lg[t][i] -= up;
         float cr[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) cr[i] = __shfl(corr, 4 * j + i, kWave);
@@ -647,6 +634,25 @@ struct NibRows {
         for (int c = 0; c < D / 16; ++c) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[c][i] *= cr[i];
+        }
+      }
+      float w[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        float v1 = kBase ? __uint_as_float(pw[t].y << 16) : __uint_as_float((pw[t].y >> (8 * (x / 4)) & 255u) << 23);
+        asm volatile("" : "+v"(v1));   // (spread here, where the products can take the lanes along)
+        const float v0 = __uint_as_float(pw[t].y & 0xFFFF0000u);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f(lg[t][i]);
+          lsum += p;
+          if constexpr (kBase) {
+            base = fmaf(quad_lane(v0, i), p, base);
+            w[4 * t + i] = quad_lane(v1, i) * p;
+          } else {
+            vs[t][i] = quad_lane(v1, i);
+            w[4 * t + i] = p;
+          }
         }
       }
       uint32_t pa[kOps][4];
@@ -919,7 +925,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
     }
   } else if constexpr (kNib) {
     const uint32_t own = uint32_t(lim - c0);   // (rows behind the split's own are masked)
-    NibRows<FMT, false, G, D, kStream, S> rows(sh, make_rsrc(Kb + int64_t(c0) * D, own * D),
+    NibRows<FMT, false, G, D, 0, S> rows(sh, make_rsrc(Kb + int64_t(c0) * D, own * D),
                                                make_rsrc(k_scale + (int64_t(bh) * cap + c0) * 2, own * 8u), c1 - c0);
     rows.begin();
     stage();
