@@ -8,6 +8,7 @@
 #include <type_traits>
 
 #include "decode_dev.h"
+#include "kv4_dev.h"
 
 namespace rbq {
 namespace {
@@ -416,14 +417,6 @@ struct Rows {
   }
 };
 
-// Eight 4-bit codes as eight bf16, in the order that the bytes of a word have after pick8
-// (int4) or lie in (fp4): e2m1 codes times a power of two, exact as far as bf16 reaches; whole
-// numbers 0 to 15 as they are: as bytes they are e4m3 codes of themselves times 2^-9 (that
-// format's subnormals and its first octave are one linear range).
-template <int FMT, bool HI>
-__device__ __forceinline__ uint32_t whole_bf16(uint32_t bytes) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 512.f, HI));
-}
 constexpr uint32_t kNibbles = 0x0F0F0F0Fu;
 
 // One wave's online softmax over its groups of 32 4-bit rows (as Rows): row c0 + e, or lst[e].
@@ -505,18 +498,8 @@ struct NibRows {
   }
   // K's row of tile t, dimensions kb, as an operand
   __device__ __forceinline__ bf16x8 key(int t, int kb, float scale) const {
-    const uint32_t w = k[t][kb];
-    if constexpr (kBase) {
-      const uint32_t even = w & kNibbles, odd = w >> 4 & kNibbles;   // dimensions 0 4 1 5, 2 6 3 7
-      const uint32_t a = __builtin_amdgcn_perm(odd, even, 0x06040200u), b = __builtin_amdgcn_perm(odd, even, 0x07050301u);
-      return __builtin_bit_cast(bf16x8, u32x4{whole_bf16<FMT, false>(a), whole_bf16<FMT, true>(a), whole_bf16<FMT, false>(b),
-                                              whole_bf16<FMT, true>(b)});
-    } else {
-      return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
-                                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
-                                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
-                                              __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))});
-    }
+    if constexpr (kBase) return __builtin_bit_cast(bf16x8, word_whole(k[t][kb]));
+    else return __builtin_bit_cast(bf16x8, word_bf16<FMT>(k[t][kb], f32x2{scale, 0.f}));
   }
   // Columns c .. c + 3 (c = 0 or 4) of rows 4j + i of tile t: to[m] the pairs {rows 0, 1}, {rows 2, 3} of column c + m
   __device__ __forceinline__ void columns(int t, int c, const float (&scale)[4], u32x2 (&to)[4]) const {
@@ -527,10 +510,10 @@ struct NibRows {
         // columns c .. c + 3 are nibbles c / 2, c / 2 + 4, c / 2 + 1, c / 2 + 5: of byte c / 4 and of the one two on
         const uint32_t y = __builtin_amdgcn_perm(b, a, c == 0 ? 0x06020400u : 0x07030501u);
         const uint32_t lo = y & kNibbles, hi = y >> 4 & kNibbles;
-        to[0][p] = whole_bf16<FMT, false>(lo);
-        to[1][p] = whole_bf16<FMT, true>(lo);
-        to[2][p] = whole_bf16<FMT, false>(hi);
-        to[3][p] = whole_bf16<FMT, true>(hi);
+        to[0][p] = bytes_bf16<false>(lo);
+        to[1][p] = bytes_bf16<true>(lo);
+        to[2][p] = bytes_bf16<false>(hi);
+        to[3][p] = bytes_bf16<true>(hi);
       } else {
         uint32_t q[2][2];
 #pragma unroll
@@ -538,11 +521,11 @@ struct NibRows {
           const uint32_t w = r ? b : a;
           const float s = scale[2 * p + r];
           if (c == 0) {
-            q[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 0));
-            q[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 1));
+            q[r][0] = fp4_pair<0>(w, s);
+            q[r][1] = fp4_pair<1>(w, s);
           } else {
-            q[r][0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 2));
-            q[r][1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, s, 3));
+            q[r][0] = fp4_pair<2>(w, s);
+            q[r][1] = fp4_pair<3>(w, s);
           }
         }
 #pragma unroll

@@ -31,15 +31,30 @@ __device__ __forceinline__ float code_value(uint32_t c, f32x2 sc) {
   }
 }
 
+// Two whole numbers of 0 to 15 (bytes 2 HI, 2 HI + 1 of w) as a pair of bf16: as bytes they are e4m3
+// codes of themselves times 2^-9 (that format's subnormals and its first octave are one linear range)
+template <bool HI>
+__device__ __forceinline__ uint32_t bytes_bf16(uint32_t w) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 512.f, HI));
+}
+// int4's 8 codes of a word as bf16, in their order
+__device__ __forceinline__ u32x4 word_whole(uint32_t w) {
+  const uint32_t even = w & 0x0F0F0F0Fu, odd = w >> 4 & 0x0F0F0F0Fu;   // dimensions 0 4 1 5, 2 6 3 7
+  const uint32_t a = __builtin_amdgcn_perm(odd, even, 0x06040200u), b = __builtin_amdgcn_perm(odd, even, 0x07050301u);
+  return u32x4{bytes_bf16<false>(a), bytes_bf16<true>(a), bytes_bf16<false>(b), bytes_bf16<true>(b)};
+}
+// fp4's two codes of byte B of w, scaled, as a pair of bf16
+template <int B>
+__device__ __forceinline__ uint32_t fp4_pair(uint32_t w, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, B));
+}
+
 // The 8 values of a word of codes as bf16, in their order
 template <int FMT>
 __device__ __forceinline__ u32x4 word_bf16(uint32_t w, f32x2 sc) {
   u32x4 r;
   if constexpr (FMT == RBQ_FP4) {
-    r[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 0));
-    r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 1));
-    r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 2));
-    r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, sc.x, 3));
+    r = u32x4{fp4_pair<0>(w, sc.x), fp4_pair<1>(w, sc.x), fp4_pair<2>(w, sc.x), fp4_pair<3>(w, sc.x)};
   } else {
     typedef float f32x2v __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));

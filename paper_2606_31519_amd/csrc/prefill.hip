@@ -245,6 +245,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   constexpr int BM = 32 * kPWaves, C = D / 8, KB = D / 16, DT = D / 32, RB = D * 2;   // chunks, k-blocks, dim tiles, bytes of a row
   __shared__ __attribute__((aligned(1024))) char ldsK[2][kPKeys * RB], ldsV[2][kPKeys * RB];
   __shared__ int odd;   // values were replaced (below)
+  // int4: the keys' codes go into LDS as whole numbers, their steps and bases meet the logits (a
+  // key rounded to bf16 would move them by up to 2^-8)
+  constexpr bool kBase = FMT == RBQ_I4;
+  __shared__ __attribute__((aligned(16))) float kpar[2][2][kBase ? kPKeys : 4];
   const int G = Hq / Hkv;
   const int hk = blockIdx.x % Hkv;
   const TileId t = find_tile<FMT>(int(blockIdx.x) / Hkv, tiles, splits, kchunk, batch, G, BM, total_q, max_k, kv_rows, kv_seq == 0,
@@ -270,6 +274,14 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     const uint16_t* p = q + int64_t(t.q0 + token) * q_ld + head * D + 8 * h;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) qf[kb] = *reinterpret_cast<const bf16x8*>(p + 16 * kb);
+  }
+  float qsum = 0.f;
+  if constexpr (kBase) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) qsum += float(qf[kb][i]);
+    qsum += __shfl_xor(qsum, 32, kWave);
   }
 
   const int64_t kvoff = (kv_seq == 0 ? t.k0 * kv_ld : int64_t(t.b) * kv_seq) + int64_t(hk) * kv_head;
@@ -316,10 +328,15 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   auto deliver = [&](const Quarter& r, char* lds, int k0, bool v) {
     if (FMT == 0 || k0 >= nbp) return;
     const f32x2 sc = row_scale<FMT>(r.word, pq);
+    if (kBase && !v && pq == 0) {
+      float* to = kpar[lds == ldsK[1]][0] + prow;
+      to[0] = sc.x;
+      to[kPKeys] = sc.y;
+    }
 #pragma unroll
     for (int i = 0; i < kQuarter; ++i)
       *reinterpret_cast<u32x4*>(lds + prow * RB + ((pq * kQuarter + i) ^ (v ? v_swizzle<D>(prow) : k_swizzle<D>(prow))) * 16) =
-          word_bf16<FMT>(r.w[i], sc);
+          kBase && !v ? word_whole(r.w[i]) : word_bf16<FMT>(r.w[i], sc);
   };
   // read addresses: K rows (lane: key x, chunk 2 kb + h), V columns by the transposing
   // read (16 lanes: 4 keys x 16 dimensions; lane i gives key i / 4, dimensions 4 (i % 4) .. +4)
@@ -334,13 +351,24 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][0][r] = 0.f;
 
-  auto logits = [&](f32x16& d, const char* tile) {   // of the 32 keys whose rows start at `tile`
+  // of 32 keys of a tile from k0 on, half t (the keys `tile` + 32 t ..)
+  auto logits = [&](f32x16& d, const char* at, int t, int k0) {
+    const char* tile = at + t * 32 * RB;
 #pragma unroll
     for (int r = 0; r < 16; ++r) d[r] = 0.f;
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       const bf16x8 a = *reinterpret_cast<const bf16x8*>(tile + (kbase ^ (kb * 32)));
       d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qf[kb], d, 0, 0, 0);
+    }
+    if (kBase && k0 < nbp) {
+      const float* par = kpar[at == ldsK[1]][0] + 32 * t + 4 * h;
+#pragma unroll
+      for (int a = 0; a < 4; ++a) {
+        const f32x4 s = *reinterpret_cast<const f32x4*>(par + 8 * a), m = *reinterpret_cast<const f32x4*>(par + kPKeys + 8 * a);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[4 * a + i] = fmaf(s[i], d[4 * a + i], m[i] * qsum);
+      }
     }
   };
   // the softmax of s (64 keys from k0) and its product with V, and the logits nx of the 64 keys after
@@ -383,7 +411,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      logits(nx[t], next_k + t * 32 * RB);
+      logits(nx[t], next_k, t, k0 + kPKeys);
 #pragma unroll
       for (int g = 0; g < 2; ++g) {
         f32x8 e;
@@ -454,8 +482,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     if (threadIdx.x == 0) odd = 0;
     wait_lds();
     __syncthreads();
-    logits(sa[0], ldsK[0]);
-    logits(sa[1], &ldsK[0][32 * RB]);
+    logits(sa[0], ldsK[0], 0, kbeg);
+    logits(sa[1], ldsK[0], 1, kbeg);
   }
   const int wstop = min(wend, kstop);
   auto publish = [&](int k0, int buf) {   // tile i of V and i + 1 of K have arrived; the ones after are requested
@@ -502,6 +530,12 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     store_row<D, RBQ_BF16>(o, 0, m, sum, int64_t(t.q0 + token) * Hq + head, h, out, lse, part, t.split, splits,
                            batch <= kWave ? (kend + kchunk - 1) / kchunk + (kend == 0) : splits);
 }
+
+}  // namespace
+}  // namespace rbq
+#include "prefill_few.h"
+namespace rbq {
+namespace {
 
 // fp32 rows: the same on v_mfma_f32_32x32x2_f32, products and probabilities in fp32.
 // Lane half h of the logits product takes dimensions h D / 2 .. +D / 2 (the order of the
@@ -751,7 +785,8 @@ __global__ __launch_bounds__(kPThreads) void prefill_combine_kernel(const float*
 rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const PrefillArgs& a,
                           hipStream_t stream) {
   if (a.total_q == 0) return RBQ_OK;
-  const PrefillPlan pl = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype);
+  const PrefillPlan pl =
+      prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype, a.cache != nullptr);
   const float c = float(double(a.sm_scale) * 1.4426950408889634);
   Cached c4{};
   if (a.cache != nullptr)
@@ -765,6 +800,11 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
                                          static_cast<const T*>(a.V), a.kv_ld, a.kv_head, a.kv_seq, a.kv_rows, a.cu_q,   \
                                          a.cu_k, batch, a.total_q, a.max_k, a.causal, c, static_cast<T*>(a.out), a.lse, \
                                          part, heads_q, heads_kv, pl.tiles, pl.splits, pl.kchunk, c4)
+#define RBQ_PREFILL_FEW(D, FMT)                                                                                          \
+  prefill_few_kernel<D, FMT><<<grid, kPThreads, 0, stream>>>(                                                            \
+      static_cast<const uint16_t*>(a.q), a.q_ld, static_cast<const uint16_t*>(a.K), static_cast<const uint16_t*>(a.V),   \
+      a.kv_ld, a.kv_head, a.cu_q, batch, a.total_q, a.causal, c, static_cast<uint16_t*>(a.out), a.lse, part, heads_q,      \
+      heads_kv, pl.splits, pl.kchunk, c4)
 #define RBQ_PREFILL_OF(KERNEL, D, T)                                     \
   do {                                                                   \
     if (a.cache == nullptr) RBQ_PREFILL((KERNEL<D, 0>), T);              \
@@ -778,7 +818,18 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
   else if (part)                                                                                                   \
     prefill_combine_kernel<D, DT, 8><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, \
                                                                       a.out, a.lse)
-  if (a.dtype == RBQ_F32) {
+  const bool few = pl.rows < 128, i4 = a.cache != nullptr && a.cache->dtype == RBQ_I4;
+  if (few) {
+    if (head_dim == 64) {
+      if (i4) RBQ_PREFILL_FEW(64, RBQ_I4);
+      else RBQ_PREFILL_FEW(64, RBQ_FP4);
+      RBQ_PREFILL_JOIN(64, RBQ_BF16);
+    } else {
+      if (i4) RBQ_PREFILL_FEW(128, RBQ_I4);
+      else RBQ_PREFILL_FEW(128, RBQ_FP4);
+      RBQ_PREFILL_JOIN(128, RBQ_BF16);
+    }
+  } else if (a.dtype == RBQ_F32) {
     if (head_dim == 64) {
       RBQ_PREFILL_OF(prefill_f32_kernel, 64, float);
       RBQ_PREFILL_JOIN(64, RBQ_F32);
@@ -795,6 +846,7 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
   }
 #undef RBQ_PREFILL_JOIN
 #undef RBQ_PREFILL_OF
+#undef RBQ_PREFILL_FEW
 #undef RBQ_PREFILL
   return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
 }

@@ -104,9 +104,9 @@ struct PrefillPlan {
   int32_t splits, kchunk;
 };
 PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
-                         int32_t total_q, int32_t dtype);
+                         int32_t total_q, int32_t dtype, bool kv4 = false);
 size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
-                               int32_t total_q);
+                               int32_t total_q, bool kv4 = false);
 
 // ---------------------------------------------------------------- workspace layouts
 // Top-p: a row of scores of at most kSelRowMax keys is selected by one block; a

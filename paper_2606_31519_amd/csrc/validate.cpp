@@ -338,10 +338,28 @@ double prefill_cost(int64_t blocks, int32_t batch, int64_t rows, int32_t head_di
 }
 }  // namespace
 
+// Rows (token, head of the group) a sequence up to which chunks over a 4-bit cache take the
+// kernel of few rows, two blocks per compute unit: 32 / 8 heads, 8 x 7 tokens over up to 8000 rows
+// 22.4 us (in tiles of 128 rows 37.1), 8 tokens over 30000 24.5 (36.0), 128 tokens over 30000 95.5
+// (119.6); 256 tokens 172.6 (157.8), 512 over 8000 129.3 (119.1).
+constexpr int64_t kFewRows = 512;
+
 PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k, int32_t total_q,
-                         int32_t dtype) {
+                         int32_t dtype, bool kv4) {
   const int64_t rows = int64_t(total_q) * (heads_q / heads_kv);
   PrefillPlan p;
+  if (kv4 && dtype == RBQ_BF16 && rows <= kFewRows * std::min<int64_t>(batch, total_q)) {
+    p.rows = 32;
+    const int64_t ends = std::min<int64_t>(batch, total_q);
+    p.tiles = int32_t(rows / p.rows + ends);
+    // (sequences end in a tile half full, and have, of several, half the longest one's keys)
+    const double blocks = double(std::max<int64_t>(rows / p.rows + ends / 2, ends)) * heads_kv * (0.5 + 1.0 / (batch + 1.0));
+    const int64_t want = std::min<int64_t>(std::max<int64_t>(int64_t(2 * kCus / blocks), 1), 64);   // (the joining kernel's most)
+    const int64_t kchunk = std::max<int64_t>(((int64_t(max_k) + want - 1) / want + 63) / 64 * 64, 128);
+    p.kchunk = int32_t(std::min<int64_t>(kchunk, (int64_t(1) << 31) - 64));
+    p.splits = std::max<int32_t>(int32_t((int64_t(max_k) + p.kchunk - 1) / p.kchunk), 1);
+    return p;
+  }
   p.rows = 128;
   // every sequence with tokens may end in a tile of its own
   const int64_t ends = std::min<int64_t>(batch, total_q);
@@ -366,12 +384,12 @@ PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
 }
 
 size_t prefill_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k,
-                               int32_t total_q) {
+                               int32_t total_q, bool kv4) {
   if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || max_k < 0 || total_q <= 0) return 0;
   if (heads_q % heads_kv != 0) return 0;
   size_t need = 0;
   for (int32_t dtype : {RBQ_F32, RBQ_BF16}) {
-    const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, head_dim, max_k, total_q, dtype);
+    const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, head_dim, max_k, total_q, dtype, kv4);
     if (p.splits > 1) need = std::max(need, size_t(total_q) * heads_q * p.splits * (size_t(head_dim) + 2) * sizeof(float));
   }
   return align_up(need, 256);
@@ -398,13 +416,15 @@ rbq_status check_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int32
   if (a.total_q == 0) return RBQ_OK;
   // the rows of a sequence (tokens times heads of a group) and the grid are 32-bit numbers
   const int64_t rows = int64_t(a.total_q) * (heads_q / heads_kv);
-  if (rows >= kMaxRows - 256 || (rows / 128 + std::min<int64_t>(batch, a.total_q)) * heads_kv >= (int64_t(1) << 24))
+  const int64_t tile = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype, a.cache != nullptr).rows;
+  if (rows >= kMaxRows - 256 || (rows / tile + std::min<int64_t>(batch, a.total_q)) * heads_kv >= (int64_t(1) << 24))
     return RBQ_EUNSUPPORTED;
   if (bad_ptr(a.q) || bad_ptr(a.out) || bad_ptr(a.cu_q) || bad_ptr(a.cu_k)) return RBQ_EINVAL;
   if (a.kv_rows > 0 && a.max_k > 0 && (bad_ptr(a.K) || bad_ptr(a.V))) return RBQ_EINVAL;
-  const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype);
+  const bool kv4 = a.cache != nullptr;
+  const PrefillPlan p = prefill_plan(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, a.dtype, kv4);
   if (p.splits > 1 &&
-      (bad_ptr(a.ws) || a.ws_bytes < prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q)))
+      (bad_ptr(a.ws) || a.ws_bytes < prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, a.max_k, a.total_q, kv4)))
     return RBQ_EINVAL;
   return RBQ_OK;
 }
@@ -462,7 +482,7 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
     case RBQ_OP_PREFILL_KV4: {
       const int64_t keys = rbq::prefill_kv4_keys(n, w);
       return keys < rbq::kMaxRows - 64
-                 ? rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, int32_t(keys), w) : 0;
+                 ? rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, int32_t(keys), w, true) : 0;
     }
     case RBQ_OP_DECODE_STEP:
     case RBQ_OP_DECODE_STEP_KV8:
