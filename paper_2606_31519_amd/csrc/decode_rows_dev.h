@@ -535,10 +535,20 @@ struct NibRows {
     }
   }
 
-  __device__ __forceinline__ void run(float& m, float& lsum, float& base, f32x4 (&acc)[D / 16]) {
+  __device__ __forceinline__ void run(float& m, float& lsum, float& base, f32x4 (&acc)[D / 16], bool turns = false) {
     float qsum = 0.f;
     if constexpr (kBase) qsum = sh.qsum[x % G];
     for (int grp = wave; grp < ngroups; grp += kDWaves) {
+      // In one round of blocks the waves of a SIMD start together and the oldest is served first: the
+      // youngest ends alone, 38 us after the start where the oldest took 23. So those that are
+      // behind go first. (Where blocks follow each other the order of age is the better one.)
+      if (!LIST && turns) {
+        const int done = __builtin_amdgcn_readfirstlane(4 * grp);
+        if (done >= 3 * ngroups) __builtin_amdgcn_s_setprio(0);
+        else if (done >= 2 * ngroups) __builtin_amdgcn_s_setprio(1);
+        else if (done >= ngroups) __builtin_amdgcn_s_setprio(2);
+        else __builtin_amdgcn_s_setprio(3);
+      }
       // (an opaque offset: the query operands are re-read from LDS every group)
       int qoff = lane_id();
       asm volatile("" : "+v"(qoff));
@@ -913,7 +923,7 @@ __global__ __launch_bounds__(kDThreads, G == 16 ? 2 : 4) void decode_rows_kernel
     rows.begin();
     stage();
     __syncthreads();
-    rows.run(m, lsum, base, acc);
+    rows.run(m, lsum, base, acc, !ragged);
   } else {
     Rows<FMT, false, G, D, kStream, S> rows(sh, Kr, Vr, c0, c1 - c0, bshift);
     rows.begin();

@@ -194,6 +194,11 @@ constexpr int kKv8DenseChunk = 2048;   // positions per dense split (at most)
 // which the host does not know: then no split takes window rows along)
 DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
                                bool own_windows);
+// The splits over a 4-bit cache: the same but for uniform dense calls, which take one round of
+// blocks whatever the rows (no scales of a split lie in LDS): 500K rows of 8 KV heads 107.5 us, in
+// rounds of 2048 rows a block 125.8; 8 x 32000 61.2 and 65.8.
+DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
+                               bool own_windows);
 // The states of any form of the calls, or of the fused step's (uniform and sparse), with any window up to w: the
 // number of splits may fall as the window grows, the size does not.
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,

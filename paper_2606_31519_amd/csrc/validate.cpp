@@ -220,6 +220,18 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
   return s;
 }
 
+DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
+                               bool own_windows) {
+  DecodeSplits s = decode_kv8_splits(batch, heads_kv, n, w, sparse, ragged, own_windows);
+  const int64_t groups = int64_t(batch) * heads_kv;
+  if (sparse || ragged || groups * n < kKv8Resident * kDecodeMinChunk) return s;
+  const int64_t splits = std::max<int64_t>(kKv8Resident / groups - s.win_splits, 1);
+  const int64_t chunk = ((int64_t(n) + splits - 1) / splits + 63) / 64 * 64;
+  s.chunk = int32_t(std::max<int64_t>(chunk, kDecodeMinChunk));
+  s.idx_splits = int32_t((int64_t(n) + s.chunk - 1) / s.chunk);
+  return s;
+}
+
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                                   int32_t w, bool step) {
   if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || n < 0 || w < 0) return 0;

@@ -638,18 +638,20 @@ def rbq_prefill_attention(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V, kv_
 # ---- the 4-bit cache: kv4 [B][Hkv][cap][D] torch.uint8 (records), par [B][Hkv][cap][2] torch.int32 (words), fmt RBQ_FP4
 # or RBQ_I4 (KV4_FORMATS by name); seq_*: as above.
 
-def _check_kv4(name, groups, head_dim, cap, kv4, par):
-    """The types of the cache's buffers."""
-    for arg, t, dt in (("kv4", kv4, torch.uint8), ("par", par, torch.int32)):
-        if t.dtype is not dt:
-            raise ValueError(f"{name}: {arg} is {t.dtype}, {dt} is taken")
-    return groups * cap * head_dim, groups * cap * 2
+_U8, _I32 = torch.uint8, torch.int32
+
+
+def _kv4_types(name, kv4, par):
+    """Refuse the call: the cache's buffers are of other types."""
+    raise ValueError(f"{name}: kv4 is {kv4.dtype}, par {par.dtype}; {_U8} and {_I32} are taken")
 
 
 def _check_kv4_rows(name, batch, heads_kv, head_dim, K, V, ld, rows, cap, kv4, par, seq_off, seq_rows):
     """Types of the cache and of the rows, once every buffer is large enough."""
     groups, dt = batch * heads_kv, _KV_CODES.get(K.dtype)
-    count, words = _check_kv4(name, groups, head_dim, cap, kv4, par)
+    count, words = groups * cap * head_dim, groups * cap * 2
+    if kv4.dtype is not _U8 or par.dtype is not _I32:
+        _kv4_types(name, kv4, par)
     if dt is None or K.dtype is not V.dtype:
         _pair_code(name, _KV_CODES, "K", K, "V", V)
     need = ((groups - 1) * ld + rows) * head_dim if rows > 0 else 0
@@ -685,7 +687,9 @@ def _check_decode_kv4(name, batch, heads_q, heads_kv, head_dim, q, kv4, par, cap
                       seq_w):
     """Types of the cache and of the window, once every buffer is large enough."""
     loc, groups, rows, need = RBQ_BF16, batch * heads_kv, batch * heads_q, 0
-    count, words = _check_kv4(name, groups, head_dim, cap, kv4, par)
+    count, words = groups * cap * head_dim, groups * cap * 2
+    if kv4.dtype is not _U8 or par.dtype is not _I32:
+        _kv4_types(name, kv4, par)
     if K_loc is not None and V_loc is not None:
         loc = _KV_CODES.get(K_loc.dtype)
         if loc is None or K_loc.dtype is not V_loc.dtype:
@@ -756,7 +760,9 @@ def rbq_prefill_attention_kv4(batch, heads_q, heads_kv, head_dim, q, q_ld, K, V,
     dt = _pair_code(name, _KV_CODES, "K", K, "V", V)
     if q.dtype != K.dtype or out.dtype != K.dtype:
         raise ValueError(f"{name}: q, K, V and out are {q.dtype}, {K.dtype}, {V.dtype}, {out.dtype}")
-    count, words = _check_kv4(name, batch * heads_kv, head_dim, cap, kv4, par)
+    count, words = batch * heads_kv * cap * head_dim, batch * heads_kv * cap * 2
+    if kv4.dtype is not _U8 or par.dtype is not _I32:
+        _kv4_types(name, kv4, par)
     rows = total_q * heads_q
     need_q = (total_q - 1) * q_ld + heads_q * head_dim if total_q > 0 else 0
     need = (total_q - 1) * kv_ld + (heads_kv - 1) * kv_head + head_dim if total_q > 0 else 0
