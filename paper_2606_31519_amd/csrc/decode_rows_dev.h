@@ -436,6 +436,9 @@ struct NibRows {
   u32x2 pw[2];                  // words of row 4j + x % 4 (fp4: V's)
   u32x2 hm[LIST ? 2 : 1];       // the heads that take rows 4j + i
 
+  // where the loads of a group behind the last go: past the buffers' ends (or, of a buffer of almost
+  // 2^31 bytes, onto rows that are not used), a group's rows before an int's end
+  static constexpr int kNone = kSkipOffset - kGroup * D;
   // (D = 64: a lane's four columns are half of the word of dimensions 8 (x / 2) .. +8)
   static __device__ __forceinline__ int column_bytes(int x) { return D == 64 ? 4 * (x / 2) : 4 * x; }
   __device__ __forceinline__ NibRows(S& s, __amdgpu_buffer_rsrc_t r, __amdgpu_buffer_rsrc_t w, int rows)
@@ -452,12 +455,12 @@ struct NibRows {
     for (int t = 0; t < 2; ++t) {
       int off, wo;
       if constexpr (LIST) {
-        const int row = grp < ngroups ? sh.lst[grp * kGroup + 16 * t + x] : kSkipOffset / D;
+        const int row = grp < ngroups ? sh.lst[grp * kGroup + 16 * t + x] : kNone / D;
         off = row * D + D / 8 * j;
         wo = row * 8;
       } else {
-        off = (grp < ngroups ? koff : kSkipOffset) + 16 * t * D;
-        wo = (grp < ngroups ? woff : kSkipOffset) + 16 * t * 8;
+        off = (grp < ngroups ? koff : kNone) + 16 * t * D;
+        wo = (grp < ngroups ? woff : kNone) + 16 * t * 8;
       }
       load_words<KB, CP>(k[t], rec, off);
       if constexpr (!kBase) load_words<1, CP>(&kw[t], words, wo);
@@ -476,13 +479,13 @@ struct NibRows {
         hm[t] = *reinterpret_cast<const u32x2*>(sh.hmask + e0);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          load_words<1, CP>(&v[t][i], rec, live ? row[i] * D + D / 2 + column_bytes(x) : kSkipOffset);
-        po = live ? sh.lst[e0 + (x & 3)] * 8 : kSkipOffset;
+          load_words<1, CP>(&v[t][i], rec, live ? row[i] * D + D / 2 + column_bytes(x) : kNone);
+        po = live ? sh.lst[e0 + (x & 3)] * 8 : kNone;
       } else {
-        const int vo = grp < ngroups ? voff : kSkipOffset;
+        const int vo = grp < ngroups ? voff : kNone;
 #pragma unroll
         for (int i = 0; i < 4; ++i) load_words<1, CP>(&v[t][i], rec, vo + (16 * t + i) * D);
-        po = (grp < ngroups ? poff : kSkipOffset) + 16 * t * 8;
+        po = (grp < ngroups ? poff : kNone) + 16 * t * 8;
       }
       if constexpr (kBase) load_words<2, CP>(reinterpret_cast<uint32_t*>(&pw[t]), words, po);
       else load_words<1, CP>(reinterpret_cast<uint32_t*>(&pw[t]) + 1, words, po + 4);

@@ -108,12 +108,12 @@ def exact_values(codes: np.ndarray, word: np.ndarray, fmt: str) -> np.ndarray:
 
 
 def bulk(codes: np.ndarray, word: np.ndarray, fmt: str) -> np.ndarray:
-    """What the sums of a product over these rows hold at most in place of each value: int4's codes meet the products as
-    16 + c and the base as m - 16 s, which cancel."""
+    """What the sums of a product over these rows hold at most in place of each value: int4's codes meet the products
+    apart from their base, and the two cancel."""
     if fmt == "fp4":
         return np.abs(row_values(codes, word, fmt))
     s, m = parts(word)
-    return ((16.0 + codes) * s[..., None]) + np.abs(m - 16.0 * s)[..., None]
+    return codes * s[..., None] + np.abs(m)[..., None]
 
 
 def attention_tolerance(q, K, V, Kb, Vb, tau):

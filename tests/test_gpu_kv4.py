@@ -261,3 +261,168 @@ def test_a_selection_of_everything_is_the_dense_call(R, fmt):
         out, lse, ws = inp.buffers(R)
         inp.call(R, kind, out, lse, ws)
         inp.check(kind, out.cpu().numpy(), lse.cpu().numpy())
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+def test_append_and_attend_in_a_graph_and_on_two_streams(R, fmt):
+    """A token appended and attended to, captured once and replayed with new rows and queries (the program's own work
+    between the replays), against the same calls made eagerly; and the same on a stream of its own beside another call."""
+    B, Hq, Hkv, D, cap, n = 2, 8, 2, 64, 256, 100
+    g = torch.Generator(device="cuda").manual_seed(5)
+    rnd = lambda *s: torch.randn(*s, device="cuda", generator=g)  # noqa: E731
+    K, V = rnd(B, Hkv, n, D), rnd(B, Hkv, n, D)
+    fc = R.KV4_FORMATS[fmt]
+
+    def fresh():
+        kv, par = (torch.zeros(B, Hkv, cap, D, dtype=torch.uint8, device="cuda"),
+                   torch.zeros(B, Hkv, cap, 2, dtype=torch.int32, device="cuda"))
+        R.rbq_quantize_kv4(B, Hkv, D, K, V, n, n, 0, cap, fc, kv, par)
+        return kv, par, torch.zeros(B, Hq, D, device="cuda"), torch.zeros(B, Hq, device="cuda"), \
+            R.workspace(R.RBQ_OP_DECODE_KV4, B, Hq, Hkv, D, cap, 0)
+
+    off = torch.full((B,), n, dtype=torch.int32, device="cuda")
+    k1, v1, q = rnd(B, Hkv, 1, D), rnd(B, Hkv, 1, D), rnd(B, Hq, D)
+
+    def token(st, stream=None):
+        kv, par, out, lse, ws = st
+        R.rbq_quantize_kv4(B, Hkv, D, k1, v1, 1, 1, cap - 1, cap, fc, kv, par, off, None, stream=stream)
+        R.rbq_dense_decode_kv4(B, Hq, Hkv, D, q, kv, par, fc, cap, cap, None, None, 0, 0, 0.125, out, lse, ws, cnt, None,
+                               stream=stream)
+
+    cnt = off + 1
+    ref, cap_st = fresh(), fresh()
+    token(fresh())
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        token(cap_st)
+    for i in range(5):
+        k1.copy_(rnd(B, Hkv, 1, D) * 2.0 ** i)
+        v1.copy_(rnd(B, Hkv, 1, D))
+        q.copy_(rnd(B, Hq, D))
+        off.fill_(n + i)
+        cnt.fill_(n + i + 1)
+        graph.replay()
+        token(ref)
+        torch.cuda.synchronize()
+        for a, b in zip(ref[:4], cap_st[:4]):
+            assert torch.equal(a, b)
+    side = torch.cuda.Stream()
+    a, b = fresh(), fresh()
+    torch.cuda.synchronize()
+    token(a, stream=side)
+    token(b)
+    torch.cuda.synchronize()
+    assert all(torch.equal(s, t) for s, t in zip(a[:4], b[:4]))
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("sparse", [False, True])
+@pytest.mark.parametrize("Hq,Hkv,D,ldt", [(8, 2, 128, "bf16"), (16, 1, 64, "f32"), (2, 2, 128, "f32"), (16, 2, 64, "bf16"),
+                                          (16, 1, 128, "bf16"), (4, 2, 64, "bf16"), (16, 2, 128, "f32")])
+def test_short_contexts(R, Hq, Hkv, D, ldt, sparse, fmt):
+    """Every group size, lengths from none to a few groups of rows, with and without a window; runs are bitwise alike."""
+    for n, w in ((0, 0), (1, 0), (0, 1), (31, 3), (32, 0), (33, 1), (129, 17), (257, 0)):
+        case = (1, Hq, Hkv, D, max(n, 1), [n], [w], 0.4, ldt)
+        print("short", case, sparse, fmt, flush=True)
+        inp = Reads(case, fmt)
+        kind = "sparse" if sparse else "dense"
+        res = []
+        for _ in range(2):
+            out, lse, ws = inp.buffers(R)
+            inp.call(R, kind, out, lse, ws)
+            torch.cuda.synchronize()
+            res.append((out.cpu().numpy(), lse.cpu().numpy()))
+        assert np.array_equal(res[0][0], res[1][0]) and np.array_equal(res[0][1], res[1][1])
+        inp.check(kind, *res[0])
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("B,Hq,Hkv,D,n,w,ldt", [
+    (2, 8, 2, 128, 700, 40, "bf16"),
+    (2, 16, 2, 64, 700, 300, "f32"),
+    (1, 16, 1, 128, 0, 17, "f32"),
+    (2, 2, 2, 128, 100, 1, "bf16"),
+    (1, 4, 2, 64, 60, 20, "f32"),
+    (8, 32, 8, 64, 15700, 300, "bf16"),      # sparse: windows taken along by the last splits
+    (8, 8, 8, 128, 15700, 200, "f32"),
+])
+def test_infinities_in_the_window(R, B, Hq, Hkv, D, n, w, ldt, fmt):
+    """An infinity in a value of the window is the result in its dimension (one of each sign, or a NaN: NaN), and every
+    other dimension, and every other KV head, keeps its bits; one in a key or a query gives its heads NaN."""
+    print("inf", B, Hq, Hkv, D, n, w, ldt, fmt, flush=True)
+    G, tau, cap = Hq // Hkv, 0.05, n + 1
+    rng = np.random.default_rng(D + w)
+    (ck, wk), (cv, wv) = (ku.random_cache(rng, (B, Hkv, cap), D, fmt) for _ in range(2))
+    kv, par, fc = dev(ku.records(ck, cv, fmt)), words(np.stack([wk, wv], axis=-1)), R.KV4_FORMATS[fmt]
+    q = dev(rng.standard_normal((B, Hq, D)).astype(np.float32))
+    K, V = (dev(rng.standard_normal((B, Hkv, w, D)), DT[ldt]) for _ in range(2))
+    sel = torch.arange(max(n, 1), dtype=torch.int32, device="cuda").expand(B, Hq, max(n, 1)).contiguous()
+    cnt = torch.full((B, Hq), n // 3, dtype=torch.int32, device="cuda")
+    seq_w = torch.full((B,), w, dtype=torch.int32, device="cuda")
+
+    def run():
+        res = []
+        for sparse in (False, True):
+            for ragged in (False, True):
+                out, lse = torch.empty(B, Hq, D, device="cuda"), torch.empty(B, Hq, device="cuda")
+                ws = R.workspace(R.RBQ_OP_DECODE_KV4, B, Hq, Hkv, D, n, w)
+                head, loc = (B, Hq, Hkv, D, q, kv, par, fc, cap, n), (K, V, w, w, tau, out, lse, ws)
+                seqs = (None, seq_w) if ragged else (None, None)
+                if sparse:
+                    R.rbq_sparse_decode_kv4(*head, sel, cnt, *loc, *seqs)
+                else:
+                    R.rbq_dense_decode_kv4(*head, *loc, *seqs)
+                torch.cuda.synchronize()
+                res.append((out, lse))
+        return res
+
+    same = lambda a, b: bool(((a == b) | (torch.isnan(a) & torch.isnan(b))).all())  # noqa: E731
+    inf, nan = float("inf"), float("nan")
+    clean = run()
+    b, hk = B - 1, Hkv - 1
+    heads = slice(hk * G, (hk + 1) * G)
+    V[b, hk, w // 2, 5], V[b, hk, w - 1, D - 1], V[b, hk, 0, 6] = inf, -inf, nan
+    marks = {5: inf, D - 1: -inf, 6: nan}
+    if w > 1:
+        V[b, hk, 0, 7], V[b, hk, w - 1, 7] = inf, -inf
+        marks[7] = nan
+    if ldt == "f32":
+        V[b, hk, w // 3, 8] = -3.4e38        # beyond bf16's range: counts as an infinity
+        marks[8] = -inf
+    got = run()
+    for (out, lse), (o, l) in zip(got, clean):
+        want = o.clone()
+        for d, v in marks.items():
+            want[b, heads, d] = v
+        assert same(out, want) and torch.equal(lse, l)
+    K[b, hk, w // 2, 3] = -inf
+    q[0, 0, 1] = inf
+    for (out, lse), (o, l) in zip(run(), got):
+        want, wl = o.clone(), l.clone()
+        for t in (want, wl):
+            t[b, heads], t[0, 0] = nan, nan
+        assert same(out, want) and same(lse, wl)
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+def test_a_rising_maximum_and_rows_of_no_weight(R, fmt):
+    """Logits that grow along the rows by hundreds, so that every group moves the maximum, and fall again; and rows whose
+    step is zero or whose values are far from zero."""
+    B, Hq, Hkv, D, n = 1, 4, 1, 128, 1500
+    inp = Reads((B, Hq, Hkv, D, n, [n], [0], 0.5, "bf16"), fmt)
+    rng = np.random.default_rng(2)
+    q = np.abs(rng.standard_normal((B, Hq, D))).astype(np.float32)
+    x = rng.standard_normal((2, n, D)) + np.sin(np.arange(n) / 200.0)[None, :, None] * np.array([4.0, 30.0])[:, None, None]
+    x[1, 7] = 0.25                         # one value: a step of zero
+    x[0, 9] = 0.0
+    for i, k in enumerate("KV"):
+        enc = [ku.encode_row(torch.from_numpy(r).bfloat16().double().numpy(), fmt) for r in x[i]]
+        inp.code[k] = (np.stack([e[0] for e in enc])[None, None], np.array([e[1] for e in enc], np.uint32)[None, None])
+    inp.kv = dev(ku.records(inp.code["K"][0], inp.code["V"][0], fmt))
+    inp.par = words(np.stack([inp.code["K"][1], inp.code["V"][1]], axis=-1))
+    inp.q, inp.dq, inp.tau = q, dev(q), 0.3
+    for kind in ("dense", "sparse"):
+        out, lse, ws = inp.buffers(R)
+        inp.call(R, kind, out, lse, ws)
+        inp.check(kind, out.cpu().numpy(), lse.cpu().numpy())
