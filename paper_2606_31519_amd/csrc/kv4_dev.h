@@ -37,10 +37,26 @@ template <bool HI>
 __device__ __forceinline__ uint32_t bytes_bf16(uint32_t w) {
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 512.f, HI));
 }
-// int4's 8 codes of a word as bf16, in their order
+// The same less 7.5, so that sums over them do not grow beside their bases: 2 c - 15 by sign and magnitude
+__device__ __forceinline__ uint32_t centred_bytes(uint32_t c) {   // four numbers of 0 to 15, as e4m3 of (2 c - 15) 2^-9
+  const uint32_t low = ~c & 0x08080808u;                       // below 8: negative
+  const uint32_t m = (c & 0x07070707u) ^ (low - (low >> 3));   // 7 - c there, c - 8 otherwise
+  return m << 1 | 0x01010101u | low << 4;
+}
+template <bool HI>
+__device__ __forceinline__ uint32_t centred_bf16(uint32_t bytes) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(bytes, 256.f, HI));
+}
+// int4's 8 codes of a word as bf16, in their order (CENTRED: less 7.5)
+template <bool CENTRED = false>
 __device__ __forceinline__ u32x4 word_whole(uint32_t w) {
-  const uint32_t even = w & 0x0F0F0F0Fu, odd = w >> 4 & 0x0F0F0F0Fu;   // dimensions 0 4 1 5, 2 6 3 7
+  uint32_t even = w & 0x0F0F0F0Fu, odd = w >> 4 & 0x0F0F0F0Fu;   // dimensions 0 4 1 5, 2 6 3 7
+  if constexpr (CENTRED) {
+    even = centred_bytes(even);
+    odd = centred_bytes(odd);
+  }
   const uint32_t a = __builtin_amdgcn_perm(odd, even, 0x06040200u), b = __builtin_amdgcn_perm(odd, even, 0x07050301u);
+  if constexpr (CENTRED) return u32x4{centred_bf16<false>(a), centred_bf16<true>(a), centred_bf16<false>(b), centred_bf16<true>(b)};
   return u32x4{bytes_bf16<false>(a), bytes_bf16<true>(a), bytes_bf16<false>(b), bytes_bf16<true>(b)};
 }
 // fp4's two codes of byte B of w, scaled, as a pair of bf16

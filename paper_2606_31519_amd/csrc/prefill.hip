@@ -800,11 +800,17 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
                                          static_cast<const T*>(a.V), a.kv_ld, a.kv_head, a.kv_seq, a.kv_rows, a.cu_q,   \
                                          a.cu_k, batch, a.total_q, a.max_k, a.causal, c, static_cast<T*>(a.out), a.lse, \
                                          part, heads_q, heads_kv, pl.tiles, pl.splits, pl.kchunk, c4)
-#define RBQ_PREFILL_FEW(D, FMT)                                                                                          \
-  prefill_few_kernel<D, FMT><<<grid, kPThreads, 0, stream>>>(                                                            \
-      static_cast<const uint16_t*>(a.q), a.q_ld, static_cast<const uint16_t*>(a.K), static_cast<const uint16_t*>(a.V),   \
-      a.kv_ld, a.kv_head, a.cu_q, batch, a.total_q, a.causal, c, static_cast<uint16_t*>(a.out), a.lse, part, heads_q,      \
-      heads_kv, pl.splits, pl.kchunk, c4)
+#define RBQ_PREFILL_FEW_OF(D, FMT, DT, T)                                                                                \
+  prefill_few_kernel<D, FMT, DT><<<grid, kPThreads, 0, stream>>>(                                                        \
+      static_cast<const T*>(a.q), a.q_ld, static_cast<const T*>(a.K), static_cast<const T*>(a.V), a.kv_ld, a.kv_head,    \
+      a.cu_q, batch, a.total_q, a.causal, c, static_cast<T*>(a.out), a.lse, part, heads_q, heads_kv, pl.splits,          \
+      pl.kchunk, c4)
+#define RBQ_PREFILL_FEW(D, DT, T)                     \
+  do {                                                \
+    if (i4) RBQ_PREFILL_FEW_OF(D, RBQ_I4, DT, T);     \
+    else RBQ_PREFILL_FEW_OF(D, RBQ_FP4, DT, T);       \
+    RBQ_PREFILL_JOIN(D, DT);                          \
+  } while (0)
 #define RBQ_PREFILL_OF(KERNEL, D, T)                                     \
   do {                                                                   \
     if (a.cache == nullptr) RBQ_PREFILL((KERNEL<D, 0>), T);              \
@@ -819,16 +825,12 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
     prefill_combine_kernel<D, DT, 8><<<cgrid, kPThreads, 0, stream>>>(part, pl.splits, rows, heads_q, a.cu_q, batch, \
                                                                       a.out, a.lse)
   const bool few = pl.rows < 128, i4 = a.cache != nullptr && a.cache->dtype == RBQ_I4;
-  if (few) {
-    if (head_dim == 64) {
-      if (i4) RBQ_PREFILL_FEW(64, RBQ_I4);
-      else RBQ_PREFILL_FEW(64, RBQ_FP4);
-      RBQ_PREFILL_JOIN(64, RBQ_BF16);
-    } else {
-      if (i4) RBQ_PREFILL_FEW(128, RBQ_I4);
-      else RBQ_PREFILL_FEW(128, RBQ_FP4);
-      RBQ_PREFILL_JOIN(128, RBQ_BF16);
-    }
+  if (few && a.dtype == RBQ_F32) {
+    if (head_dim == 64) RBQ_PREFILL_FEW(64, RBQ_F32, float);
+    else RBQ_PREFILL_FEW(128, RBQ_F32, float);
+  } else if (few) {
+    if (head_dim == 64) RBQ_PREFILL_FEW(64, RBQ_BF16, uint16_t);
+    else RBQ_PREFILL_FEW(128, RBQ_BF16, uint16_t);
   } else if (a.dtype == RBQ_F32) {
     if (head_dim == 64) {
       RBQ_PREFILL_OF(prefill_f32_kernel, 64, float);
@@ -847,6 +849,7 @@ rbq_status launch_prefill(int32_t batch, int32_t heads_q, int32_t heads_kv, int3
 #undef RBQ_PREFILL_JOIN
 #undef RBQ_PREFILL_OF
 #undef RBQ_PREFILL_FEW
+#undef RBQ_PREFILL_FEW_OF
 #undef RBQ_PREFILL
   return hipGetLastError() == hipSuccess ? RBQ_OK : RBQ_EDEVICE;
 }

@@ -5,6 +5,36 @@
 namespace rbq {
 namespace {
 
+template <int DTYPE>
+struct Elem {
+  typedef uint16_t T;
+};
+template <>
+struct Elem<RBQ_F32> {
+  typedef float T;
+};
+__device__ __forceinline__ float element(const uint16_t* p) { return __uint_as_float(uint32_t(*p) << 16); }
+__device__ __forceinline__ float element(const float* p) { return *p; }
+__device__ __forceinline__ f32x8 load8(const float* p) {
+  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+}
+// N bf16 parts of eight values, each the top 8 bits of what the ones before leave (24 bits in three,
+// the largest floats among them)
+template <int N>
+__device__ __forceinline__ void top_parts(f32x8 v, u32x4* to) {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      to[n][i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
+    if (n + 1 < N) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= __uint_as_float(__float_as_uint(v[i]) & 0xFFFF0000u);
+    }
+  }
+}
+
 // Block id of a KV head: sequence after sequence, tile after tile, the splits that the sequence's
 // keys call for; the grid's rest has none (b < 0).
 template <int FMT>
@@ -51,18 +81,25 @@ __device__ __forceinline__ TileId find_few(int id, int kchunk, int batch, int G,
 //   O^T = V^T P^T  A = 32 x (D / 32) dimensions: lane (x, h) holds dimensions (D / 32) x .. of the 16
 //                  keys whose probabilities it has; int4: weights w = bf16(p s) on the codes, and
 //                  w (m / s) beside them, so that both see the same rounding
+// fp32: int4's rows as c - 7.5 and m + 7.5 s (the sums of c itself, 7.5 times the steps', would
+// round away what they leave: rel. error 1.6e-6 where this has less than half); queries and weights in three bf16 parts, 24 bits (4-bit codes and values are exact in bf16), the
+// chunk's own rows too: three products for one are a fifth of what the fp32 matrix instructions take.
 // (In prefill_kernel, 128 rows and tiles through LDS, 8 x 7 tokens of 32 / 8 heads over up to
 // 8000 rows took 33 us.)
-template <int D, int FMT>
+template <int D, int FMT, int DTYPE>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
-    const uint16_t* __restrict__ q, int64_t q_ld, const uint16_t* __restrict__ K, const uint16_t* __restrict__ V,
+    const typename Elem<DTYPE>::T* __restrict__ q, int64_t q_ld, const typename Elem<DTYPE>::T* __restrict__ K,
+    const typename Elem<DTYPE>::T* __restrict__ V,
     int64_t kv_ld, int64_t kv_head, const int32_t* __restrict__ cu_q, int batch, int total_q, int causal,
-    float scale_log2e, uint16_t* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv,
+    float scale_log2e, typename Elem<DTYPE>::T* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv,
     int splits, int kchunk, Cached c4) {
   constexpr int KB = D / 16, DT = D / 32, kGroup = 32, KW = D / 16;   // k-blocks, dimensions of a lane, words of K
-  constexpr bool kBase = FMT == RBQ_I4;
+  constexpr bool kBase = FMT == RBQ_I4, kF32 = DTYPE == RBQ_F32;
+  constexpr int NP = kF32 ? 3 : 1;   // bf16 parts of a query, a probability, a row of the chunk's own
+  using T = typename Elem<DTYPE>::T;
+  __shared__ u32x4 qparts[kF32 ? NP : 1][kF32 ? KB : 1][kF32 ? kWave : 1];   // fp32: the queries' operands
   struct Wave {
-    __attribute__((aligned(16))) float word[4][kGroup];   // fp4: V's scales of four groups; int4: K's s, m, V's s, m / s
+    __attribute__((aligned(16))) float word[4][kGroup];   // fp4: V's scales of four groups; int4: K's s, m, V's s and m / s (fp32: m + 7.5 s of both)
   };
   __shared__ Wave per_wave[kPWaves];
   __shared__ __attribute__((aligned(16))) f32x4 held[2][4 * DT][kWave];   // outputs of two waves
@@ -80,26 +117,42 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
   const int kend = visible((min(row0 + kGroup, rows) - 1) / G), kbeg = t.split * kchunk, kstop = min(kend, kbeg + kchunk);
   const int all = visible(row0 / G);                                 // keys that every row sees
   const int qrow = min(row0 + x, rows - 1), token = qrow / G, head = hk * G + (qrow - token * G), lim = visible(token);
-  bf16x8 qf[KB];
-  {
-    const uint16_t* p = q + int64_t(t.q0 + token) * q_ld + head * D + (D / 2) * h;
-#pragma unroll
-    for (int kb = 0; kb < KB; ++kb) qf[kb] = *reinterpret_cast<const bf16x8*>(p + 8 * kb);
-  }
+  bf16x8 qf[kF32 ? 1 : KB];
   float qsum = 0.f;
-  if constexpr (kBase) {
+  {
+    const T* p = q + int64_t(t.q0 + token) * q_ld + head * D + (D / 2) * h;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
+    for (int kb = 0; kb < KB; ++kb) {
+      if constexpr (kF32) {
+        const f32x8 v = load8(p + 8 * kb);
+        if constexpr (kBase) qsum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        if (kb % kPWaves == wave) {
+          u32x4 part[NP];
+          top_parts<NP>(v, part);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) qsum += float(qf[kb][i]);
-    qsum += __shfl_xor(qsum, 32, kWave);
+          for (int n = 0; n < NP; ++n) qparts[n][kb][lane] = part[n];
+        }
+      } else {
+        qf[kb] = *reinterpret_cast<const bf16x8*>(p + 8 * kb);
+        if constexpr (kBase) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) qsum += float(qf[kb][i]);
+        }
+      }
+    }
+    if constexpr (kBase) qsum += __shfl_xor(qsum, 32, kWave);
   }
+  // part n of the queries' dimensions 8 kb .. of the lane's
+  auto query = [&](int n, int kb) {
+    if constexpr (kF32) return __builtin_bit_cast(bf16x8, qparts[n][kb][lane]);
+    else return qf[kb];
+  };
   if (threadIdx.x == 0) odd = 0;
   __syncthreads();
   const int64_t first = (int64_t(t.b) * Hkv + hk) * c4.cap;
   const __amdgpu_buffer_rsrc_t rec = make_rsrc(c4.KV4 + first * D, uint32_t(cached) * D);   // < 2^31
   const __amdgpu_buffer_rsrc_t words = make_rsrc(c4.par + 2 * first, uint32_t(cached) * 8u);
-  const uint16_t *Kb = K + t.k0 * kv_ld + int64_t(hk) * kv_head, *Vb = V + t.k0 * kv_ld + int64_t(hk) * kv_head;
+  const T *Kb = K + t.k0 * kv_ld + int64_t(hk) * kv_head, *Vb = V + t.k0 * kv_ld + int64_t(hk) * kv_head;
   float(*word)[kGroup] = per_wave[wave].word;
 
   // a group of 4-bit keys on its way; places behind the last row lie past the buffers' ends: zeros
@@ -159,11 +212,16 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
       l += s[r];
     }
   };
-  auto weights = [&](const f32x16& p, int g) {   // of keys 16 g .. +16, as an operand (rounded, as in prefill_kernel)
+  // weights of keys 16 g .. +16 as operands (bf16: rounded, as in prefill_kernel)
+  auto weights = [&](const f32x16& p, int g, u32x4 (&to)[NP]) {
     f32x8 e;
 #pragma unroll
     for (int r = 0; r < 8; ++r) e[r] = p[8 * g + r];
-    return __builtin_convertvector(e, bf16x8);
+    if constexpr (kF32) top_parts<NP>(e, to);
+    else to[0] = __builtin_bit_cast(u32x4, __builtin_convertvector(e, bf16x8));
+  };
+  auto product = [](u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
   };
 
   const int c4groups = max(min(kstop, cached) - kbeg + kGroup - 1, 0) / kGroup;   // of 4-bit keys
@@ -175,38 +233,51 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
   // the chunk's own keys, few of them, by the waves that have fewer of the others
   const int own0 = max(kbeg, nbp);   // (a multiple of the groups' 32)
   for (int k0 = own0 + (wave - c4groups & 3) * kGroup; k0 < kstop; k0 += kPWaves * kGroup) {
-    const uint16_t* kp = Kb + int64_t(min(k0 - nbp + x, t.nq - 1)) * kv_ld + (D / 2) * h;
+    const T* kp = Kb + int64_t(min(k0 - nbp + x, t.nq - 1)) * kv_ld + (D / 2) * h;
     f32x16 s;
 #pragma unroll
     for (int r = 0; r < 16; ++r) s[r] = 0.f;
 #pragma unroll
-    for (int kb = 0; kb < KB; ++kb)
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kp + 8 * kb), qf[kb], s, 0, 0, 0);
+    for (int kb = 0; kb < KB; ++kb) {
+      if constexpr (kF32) {
+        u32x4 a[NP];
+        top_parts<NP>(load8(kp + 8 * kb), a);
+#pragma unroll
+        for (int i = 0; i < NP; ++i)   // (the products of 2^-24 and less are left out)
+#pragma unroll
+          for (int n = 0; i + n < NP; ++n) s = product(a[i], __builtin_bit_cast(u32x4, query(n, kb)), s);
+      } else {
+        s = product(*reinterpret_cast<const u32x4*>(kp + 8 * kb), __builtin_bit_cast(u32x4, query(0, kb)), s);
+      }
+    }
     softmax(s, k0);
     bool inf = false;
-#pragma unroll
+#pragma unroll 1
     for (int g = 0; g < 2; ++g) {
-      const bf16x8 p = weights(s, g);
-      uint32_t w[8][DT / 2];
+      u32x4 p[NP];
+      weights(s, g, p);
+      float v[8][DT];
 #pragma unroll
       for (int r = 0; r < 8; ++r) {
-        const uint16_t* vp = Vb + int64_t(min(k0 - nbp + key_of(8 * g + r), t.nq - 1)) * kv_ld + DT * x;
+        const T* vp = Vb + int64_t(min(k0 - nbp + key_of(8 * g + r), t.nq - 1)) * kv_ld + DT * x;
 #pragma unroll
-        for (int i = 0; i < DT / 2; ++i) {
-          uint32_t v = reinterpret_cast<const uint32_t*>(vp)[i];
+        for (int d = 0; d < DT; ++d) {
+          v[r][d] = element(vp + d);
           // (infinities and NaN: replaced here, added where they are seen, at the end)
-          if ((v & 0x7F80u) == 0x7F80u) v &= 0xFFFF0000u, inf = true;
-          if ((v & 0x7F800000u) == 0x7F800000u) v &= 0xFFFFu, inf = true;
-          w[r][i] = v;
+          if (!(fabsf(v[r][d]) < INFINITY)) v[r][d] = 0.f, inf = true;
         }
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d) {
-        u32x4 a;
+        f32x8 col;
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          a[r] = __builtin_amdgcn_perm(w[2 * r + 1][d / 2], w[2 * r][d / 2], d % 2 ? 0x07060302u : 0x05040100u);
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), p, o[d], 0, 0, 0);
+        for (int r = 0; r < 8; ++r) col[r] = v[r][d];
+        u32x4 a[NP];
+        top_parts<NP>(col, a);   // (bf16: itself)
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+          for (int n = 0; i + n < NP; ++n) o[d] = product(a[i], p[n], o[d]);
       }
     }
     if (inf) odd = 1;
@@ -220,9 +291,9 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
       const float ks = __uint_as_float(pw.x << 16), km = __uint_as_float(pw.x & 0xFFFF0000u);
       float vs = __uint_as_float(pw.y << 16);
       const float vm = __uint_as_float(pw.y & 0xFFFF0000u);
-      vs = vs == 0.f ? 1.f : vs;   // (a row of one value: its codes are 0)
+      if (!kF32) vs = vs == 0.f ? 1.f : vs;   // (a row of one value: its codes are 0)
       word[2 * h][x] = h ? vs : ks;
-      word[2 * h + 1][x] = h ? vm / vs : km;
+      word[2 * h + 1][x] = h ? (kF32 ? fmaf(7.5f, vs, vm) : vm / vs) : kF32 ? fmaf(7.5f, ks, km) : km;
     } else {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
@@ -237,9 +308,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) {
       u32x4 a;
-      if constexpr (kBase) a = word_whole(kw[kb]);
+      if constexpr (kBase) a = word_whole<kF32>(kw[kb]);
       else a = word_bf16<FMT>(kw[kb], f32x2{kscale[kb / (KB / 2)], 0.f});
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), qf[kb], s, 0, 0, 0);
+#pragma unroll
+      for (int n = 0; n < NP; ++n) s = product(a, __builtin_bit_cast(u32x4, query(n, kb)), s);
     }
     load_k(next);
     if constexpr (kBase) {
@@ -259,18 +331,27 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
 #pragma unroll
       for (int i = 0; i < 4; ++i) vscale[4 * a + i] = v[i];
     }
+    u32x4 p[2][NP];
     if constexpr (kBase) {
+      f32x16 w;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) s[r] *= vscale[r];
-    }
-    bf16x8 p[2] = {weights(s, 0), weights(s, 1)};
-    if constexpr (kBase) {
+      for (int r = 0; r < 16; ++r) w[r] = s[r] * vscale[r];
+      weights(w, 0, p[0]);
+      weights(w, 1, p[1]);
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
-        const f32x4 ratio = *reinterpret_cast<const f32x4*>(&word[3][8 * a + 4 * h]);
+        const f32x4 m4 = *reinterpret_cast<const f32x4*>(&word[3][8 * a + 4 * h]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) base = fmaf(float(p[a / 2][4 * (a % 2) + i]), ratio[i], base);
+        for (int i = 0; i < 4; ++i) {
+          const int r = 4 * (a % 2) + i;
+          float weight = s[4 * a + i];
+          if constexpr (!kF32) weight = r % 2 ? bf16_hi(p[a / 2][0][r / 2]) : bf16_lo(p[a / 2][0][r / 2]);
+          base = fmaf(weight, m4[i], base);
+        }
       }
+    } else {
+      weights(s, 0, p[0]);
+      weights(s, 1, p[1]);
     }
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -283,13 +364,23 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
       for (int r = 0; r < 4; ++r) {   // pairs of keys
         const uint32_t w0 = vw[8 * g + 2 * r], w1 = vw[8 * g + 2 * r + 1];
         if constexpr (kBase) {
-          const uint32_t y = __builtin_amdgcn_perm(w1, w0, 0x06020400u), lo = y & 0x0F0F0F0Fu;
-          a[0][r] = bytes_bf16<false>(lo);
-          a[1][r] = bytes_bf16<true>(lo);
-          if constexpr (DT == 4) {
-            const uint32_t hi = y >> 4 & 0x0F0F0F0Fu;
-            a[2][r] = bytes_bf16<false>(hi);
-            a[3][r] = bytes_bf16<true>(hi);
+          const uint32_t y = __builtin_amdgcn_perm(w1, w0, 0x06020400u), lo = y & 0x0F0F0F0Fu, hi = y >> 4 & 0x0F0F0F0Fu;
+          if constexpr (kF32) {
+            const uint32_t cl = centred_bytes(lo);
+            a[0][r] = centred_bf16<false>(cl);
+            a[1][r] = centred_bf16<true>(cl);
+            if constexpr (DT == 4) {
+              const uint32_t ch = centred_bytes(hi);
+              a[2][r] = centred_bf16<false>(ch);
+              a[3][r] = centred_bf16<true>(ch);
+            }
+          } else {
+            a[0][r] = bytes_bf16<false>(lo);
+            a[1][r] = bytes_bf16<true>(lo);
+            if constexpr (DT == 4) {
+              a[2][r] = bytes_bf16<false>(hi);
+              a[3][r] = bytes_bf16<true>(hi);
+            }
           }
         } else {
           const float s0 = vscale[8 * g + 2 * r], s1 = vscale[8 * g + 2 * r + 1];
@@ -304,8 +395,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
       }
 #pragma unroll
       for (int d = 0; d < DT; ++d)
-        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{a[d][0], a[d][1], a[d][2], a[d][3]}),
-                                                       p[g], o[d], 0, 0, 0);
+#pragma unroll
+        for (int n = 0; n < NP; ++n) o[d] = product(u32x4{a[d][0], a[d][1], a[d][2], a[d][3]}, p[g][n], o[d]);
     }
     load_v(next);
   }
@@ -362,10 +453,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
     for (int key = own0; key < min(lim, kstop); ++key) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {   // dimensions DT (8 (r / 4) + 4 h + r % 4) .. +DT
-        const uint16_t* vp = Vb + int64_t(key - nbp) * kv_ld + DT * (8 * (r / 4) + 4 * h + r % 4);
+        const T* vp = Vb + int64_t(key - nbp) * kv_ld + DT * (8 * (r / 4) + 4 * h + r % 4);
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-          const float v = __uint_as_float(uint32_t(vp[d]) << 16);
+          const float v = element(vp + d);
           o[d][r] += fabsf(v) < INFINITY ? 0.f : v;
         }
       }
@@ -386,6 +477,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
     if (part) {
 #pragma unroll
       for (int d = 0; d < DT; d += 2) *reinterpret_cast<f32x2*>(pr + 2 + at + d) = f32x2{v[d], v[d + 1]};
+    } else if constexpr (kF32) {
+      *reinterpret_cast<vec*>(out + row * D + at) = v;
     } else {
       *reinterpret_cast<hvec*>(out + row * D + at) = __builtin_convertvector(v, hvec);
     }

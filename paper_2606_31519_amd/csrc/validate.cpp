@@ -350,17 +350,26 @@ double prefill_cost(int64_t blocks, int32_t batch, int64_t rows, int32_t head_di
 }
 }  // namespace
 
+namespace {
 // Rows (token, head of the group) a sequence up to which chunks over a 4-bit cache take the
 // kernel of few rows, two blocks per compute unit: 32 / 8 heads, 8 x 7 tokens over up to 8000 rows
 // 22.4 us (in tiles of 128 rows 37.1), 8 tokens over 30000 24.5 (36.0), 128 tokens over 30000 95.5
-// (119.6); 256 tokens 172.6 (157.8), 512 over 8000 129.3 (119.1).
-constexpr int64_t kFewRows = 512;
+// (119.6); 256 tokens 172.6 (157.8), 512 over 8000 129.3 (119.1). fp32 takes it, whatever the rows,
+// unless more keys are the chunk's own than are cached: 1000 tokens of 32 / 8 heads over 8000 470 us
+// (1455), 1000 of 4 / 1 over none 33.0 (34.9), 2500 over none 146 (112).
+constexpr int64_t kFewRows = 512, kFewOwn = 1024;
+bool few_rows(int64_t rows, int32_t batch, int32_t max_k, int32_t total_q, int32_t dtype) {
+  const int64_t ends = std::min<int64_t>(batch, total_q);
+  if (dtype == RBQ_F32) return total_q <= ends * std::max<int64_t>(max_k - total_q, kFewOwn);
+  return rows <= kFewRows * ends;
+}
+}  // namespace
 
 PrefillPlan prefill_plan(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t max_k, int32_t total_q,
                          int32_t dtype, bool kv4) {
   const int64_t rows = int64_t(total_q) * (heads_q / heads_kv);
   PrefillPlan p;
-  if (kv4 && dtype == RBQ_BF16 && rows <= kFewRows * std::min<int64_t>(batch, total_q)) {
+  if (kv4 && few_rows(rows, batch, max_k, total_q, dtype)) {
     p.rows = 32;
     const int64_t ends = std::min<int64_t>(batch, total_q);
     p.tiles = int32_t(rows / p.rows + ends);

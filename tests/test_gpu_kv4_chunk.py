@@ -123,6 +123,9 @@ CASES = [
     ("f32", 6, 2, 128, [20, 5], [90, 3], False, True),
     ("f32", 2, 1, 64, [31], [64], False, False),
     ("f32", 4, 1, 128, [3], [3001], False, True),
+    ("f32", 12, 1, 64, [150, 3], [300, 70], False, True),
+    ("f32", 2, 1, 128, [1200], [70], False, True),                              # mostly keys of its own
+    ("f32", 1, 1, 64, [1100], [100], True, False),
 ]
 
 
