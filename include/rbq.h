@@ -620,9 +620,9 @@ rbq_status rbq_decode_step_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv,
  *   seq_n  NULL (n rows each), or [B] int32 (device): n_b, clamped to [0, n]
  *   ws:    at least rbq_workspace_bytes(RBQ_OP_PREFILL_KV4, B, Hq, Hkv, D, n, total_q) bytes,
  *          0 (then NULL is allowed) unless few rows attend to long keys.
- * With RBQ_BF16 the cached values (RBQ_I4) and the probabilities are rounded to bf16 before
- * they meet the products. Everything else as in rbq_prefill_attention. RBQ_EINVAL also where
- * n * D >= 2^31.
+ * With RBQ_BF16 the probabilities and, with RBQ_I4, the cached values (or their weights, the
+ * probabilities times the steps) are rounded to bf16 before they meet the products; cached keys
+ * never are. Everything else as in rbq_prefill_attention. RBQ_EINVAL also where n * D >= 2^31.
  */
 rbq_status rbq_prefill_attention_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
                                      const void* q, int64_t q_ld, const void* K, const void* V, int32_t dtype,

@@ -541,6 +541,13 @@ struct NibRows {
   __device__ __forceinline__ void run(float& m, float& lsum, float& base, f32x4 (&acc)[D / 16], bool turns = false) {
     float qsum = 0.f;
     if constexpr (kBase) qsum = sh.qsum[x % G];
+    // int4's codes as c - 7.5 and its bases as m + 7.5 s: sums of c itself, which m then cancels, would
+    // carry twice the rounding (1.2e-6 of the outputs' norm where this has 6e-7). -7.5 is a product of
+    // its own, once per sum of 32, which the matrix cores have the time for (as bytes of c - 7.5, or taken
+    // off the finished sums, it is the vector units'): 128K rows 35.0 -> 36.3 us.
+    constexpr float kCentre = 7.5f;
+    constexpr uint32_t kMinus = 0xC0F0C0F0u;   // twice -7.5
+    const bf16x8 centre = __builtin_bit_cast(bf16x8, u32x4{kMinus, kMinus, kMinus, kMinus});
     for (int grp = wave; grp < ngroups; grp += kDWaves) {
       // In one round of blocks the waves of a SIMD start together and the oldest is served first: the
       // youngest ends alone, 38 us after the start where the oldest took 23. So those that are
@@ -572,6 +579,10 @@ struct NibRows {
 #pragma unroll
         for (int op = 0; op < kOps; ++op) {
           const bf16x8 b = __builtin_bit_cast(bf16x8, qp[(kb * kOps + op) * kWave]);
+          if constexpr (kBase) {
+#pragma unroll
+            for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(centre, b, s[t], 0, 0, 0);
+          }
 #pragma unroll
           for (int t = 0; t < 2; ++t) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[t], b, s[t], 0, 0, 0);
         }
@@ -582,7 +593,7 @@ struct NibRows {
       const float mref = m == -INFINITY ? 0.f : m;   // (no row yet: every exponential below is that of -inf)
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const float k1 = __uint_as_float(pw[t].x << 16), k0 = __uint_as_float(pw[t].x & 0xFFFF0000u);
+        const float k1 = __uint_as_float(pw[t].x << 16), k0 = fmaf(kCentre, k1, __uint_as_float(pw[t].x & 0xFFFF0000u));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float sv = s[t][i];
@@ -637,7 +648,7 @@ struct NibRows {
       for (int t = 0; t < 2; ++t) {
         float v1 = kBase ? __uint_as_float(pw[t].y << 16) : __uint_as_float((pw[t].y >> (8 * (x / 4)) & 255u) << 23);
         asm volatile("" : "+v"(v1));   // (spread here, where the products can take the lanes along)
-        const float v0 = __uint_as_float(pw[t].y & 0xFFFF0000u);
+        const float v0 = fmaf(kCentre, v1, __uint_as_float(pw[t].y & 0xFFFF0000u));
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const float p = __builtin_amdgcn_exp2f(lg[t][i]);
@@ -663,6 +674,14 @@ struct NibRows {
       for (int c = 0; c < D / 16; c += 4) {
         u32x2 b[2][4];
         __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kBase) {
+#pragma unroll
+          for (int n = 0; n < 4; ++n)
+#pragma unroll
+            for (int op = 0; op < kOps; ++op)
+              acc[c + n] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  __builtin_bit_cast(bf16x8, u32x4{pa[op][0], pa[op][1], pa[op][2], pa[op][3]}), centre, acc[c + n], 0, 0, 0);
+        }
         columns(0, c, vs[0], b[0]);
         columns(1, c, vs[1], b[1]);
 #pragma unroll

@@ -81,25 +81,28 @@ __device__ __forceinline__ TileId find_few(int id, int kchunk, int batch, int G,
 //   O^T = V^T P^T  A = 32 x (D / 32) dimensions: lane (x, h) holds dimensions (D / 32) x .. of the 16
 //                  keys whose probabilities it has; int4: weights w = bf16(p s) on the codes, and
 //                  w (m / s) beside them, so that both see the same rounding
-// fp32: int4's rows as c - 7.5 and m + 7.5 s (the sums of c itself, 7.5 times the steps', would
-// round away what they leave: rel. error 1.6e-6 where this has less than half); queries and weights in three bf16 parts, 24 bits (4-bit codes and values are exact in bf16), the
-// chunk's own rows too: three products for one are a fifth of what the fp32 matrix instructions take.
+// fp32: queries and weights in three bf16 parts, 24 bits (4-bit codes and values are exact in
+// bf16), the chunk's own rows too: three products for one are a fifth of what the fp32 matrix
+// instructions take (2 x 31-500 tokens of 8 / 2 heads of 64 over up to 6000 rows: 37.8 us, 67.1
+// with them). int4's rows as c - 7.5 and m + 7.5 s: sums of c itself, which m then cancels, cost
+// twice the rounding (rel. error of the outputs 1.6e-6, so 7.8e-7).
 // (In prefill_kernel, 128 rows and tiles through LDS, 8 x 7 tokens of 32 / 8 heads over up to
 // 8000 rows took 33 us.)
 template <int D, int FMT, int DTYPE>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
     const typename Elem<DTYPE>::T* __restrict__ q, int64_t q_ld, const typename Elem<DTYPE>::T* __restrict__ K,
-    const typename Elem<DTYPE>::T* __restrict__ V,
-    int64_t kv_ld, int64_t kv_head, const int32_t* __restrict__ cu_q, int batch, int total_q, int causal,
-    float scale_log2e, typename Elem<DTYPE>::T* __restrict__ out, float* __restrict__ lse, float* __restrict__ part, int Hq, int Hkv,
-    int splits, int kchunk, Cached c4) {
+    const typename Elem<DTYPE>::T* __restrict__ V, int64_t kv_ld, int64_t kv_head, const int32_t* __restrict__ cu_q,
+    int batch, int total_q, int causal,
+    float scale_log2e, typename Elem<DTYPE>::T* __restrict__ out, float* __restrict__ lse, float* __restrict__ part,
+    int Hq, int Hkv, int splits, int kchunk, Cached c4) {
   constexpr int KB = D / 16, DT = D / 32, kGroup = 32, KW = D / 16;   // k-blocks, dimensions of a lane, words of K
   constexpr bool kBase = FMT == RBQ_I4, kF32 = DTYPE == RBQ_F32;
   constexpr int NP = kF32 ? 3 : 1;   // bf16 parts of a query, a probability, a row of the chunk's own
   using T = typename Elem<DTYPE>::T;
   __shared__ u32x4 qparts[kF32 ? NP : 1][kF32 ? KB : 1][kF32 ? kWave : 1];   // fp32: the queries' operands
   struct Wave {
-    __attribute__((aligned(16))) float word[4][kGroup];   // fp4: V's scales of four groups; int4: K's s, m, V's s and m / s (fp32: m + 7.5 s of both)
+    // fp4: V's scales of four groups; int4: K's s and m, V's s and m / s (fp32: m + 7.5 s of both)
+    __attribute__((aligned(16))) float word[4][kGroup];
   };
   __shared__ Wave per_wave[kPWaves];
   __shared__ __attribute__((aligned(16))) f32x4 held[2][4 * DT][kWave];   // outputs of two waves
@@ -232,7 +235,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
   }
   // the chunk's own keys, few of them, by the waves that have fewer of the others
   const int own0 = max(kbeg, nbp);   // (a multiple of the groups' 32)
-  for (int k0 = own0 + (wave - c4groups & 3) * kGroup; k0 < kstop; k0 += kPWaves * kGroup) {
+  for (int k0 = own0 + ((wave - c4groups) & 3) * kGroup; k0 < kstop; k0 += kPWaves * kGroup) {
     const T* kp = Kb + int64_t(min(k0 - nbp + x, t.nq - 1)) * kv_ld + (D / 2) * h;
     f32x16 s;
 #pragma unroll
@@ -252,7 +255,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
     }
     softmax(s, k0);
     bool inf = false;
-#pragma unroll 1
+#pragma unroll
     for (int g = 0; g < 2; ++g) {
       u32x4 p[NP];
       weights(s, g, p);
