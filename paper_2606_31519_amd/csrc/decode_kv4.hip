@@ -15,8 +15,8 @@
 // instead of 19.2). A lane of the logits product takes a quarter of a row, one load of 16
 // bytes at D = 128 and one exponent; the words of four rows are loaded by the four lanes of a
 // quad and spread from there.
-// Bound by memory while rows stream (5.5 TB/s, both formats), by latency around that: of the
-// 36.6 us of 128K rows x 8 heads (143 MB) the rows take 26, starting a block 0.9, joining its
+// Bound by memory while rows stream (5.3 TB/s), by latency around that: of the
+// 37.1 us of 128K rows x 8 heads (143 MB) the rows take 27, starting a block 0.9, joining its
 // waves 1.7, the second kernel with its launch 4.6; of the 33.8 us with a fifth of them listed
 // (88 MB with the lists) the rows take 19, reading a list 4.7. Four waves a SIMD: five spill,
 // and three that load further ahead are slower.
