@@ -10,9 +10,12 @@
 //         step of a code
 //
 // Bound by the bytes of the rows and the records: K and V of 130816 tokens x 8 heads x 128 in
-// bf16, 678 MB either way, written in 125 us (5.4 TB/s) and read back in 104 (6.5; stores that
-// the caches keep 121, one row a thread 110). (Two rows a thread write the same in 122, but 16 x
-// 256 rows in 8.3 us instead of 7.8.)
+// bf16, 678 MB either way, written in 114 us (5.9 TB/s) and read back in 102 (6.6; stores that
+// the caches keep 121, one row a thread 110). Writing has its arithmetic beside the bytes: with a
+// look at each value for infinities and NaN (now for a wave's at once, and the values' own way
+// only where there is one) 16 values took 210 (fp4) to 400 (int4) vector instructions, and the
+// rows above 125 us, 16 x 256 of int4 7.5 instead of 5.6. (Two rows a thread were no faster then,
+// and 16 x 256 rows slower by 0.5.)
 #include <type_traits>
 
 #include "kv4_dev.h"
@@ -24,8 +27,13 @@ constexpr int kThreads4 = 256;
 constexpr float kLeast = 1.17549435e-38f;   // 2^-126, the least scale and step
 constexpr float kMost = 8.50705917e37f;     // 2^126: int4 takes finite values beyond as this
 constexpr float kRound = 12582912.f;        // 1.5 * 2^23: adding it rounds to a whole number, kept in the low bits
+constexpr uint32_t kRoundBits = 0x4B400000u;   // its bits
 constexpr int kTake = 16;                   // values of a row and tensor that a thread takes
 constexpr int kRowsR = 2;                   // rows that a thread reads back
+
+typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 
 // The rows of one call: sequence b's rows [off, off + cnt) of the cache.
 struct Span {
@@ -53,9 +61,102 @@ __device__ __forceinline__ float bf16_down(float x) {   // |x| <= 2^126
   return __uint_as_float((int32_t(u) < 0 ? u + 0xFFFFu : u) & 0xFFFF0000u);
 }
 
-// 16 values of fp4: their codes, and their group's exponent byte
-template <int LANES>
-__device__ __forceinline__ u32x2 encode_fp4(const float* x, uint32_t& byte) {
+// A thread's 16 values as they were loaded.
+template <int DT>
+struct Taken {
+  static constexpr int kWords = DT == RBQ_BF16 ? kTake / 2 : kTake;
+  uint32_t w[kWords];
+  __device__ __forceinline__ void values(float* x) const {
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) {
+      if constexpr (DT == RBQ_BF16) {
+        x[2 * i] = bf16_lo(w[i]);
+        x[2 * i + 1] = bf16_hi(w[i]);
+      } else {
+        x[i] = __uint_as_float(w[i]);
+      }
+    }
+  }
+  // the bits of the largest magnitude (their order is the magnitudes', NaN's above infinity's)
+  __device__ __forceinline__ uint32_t amax() const {
+    if constexpr (DT == RBQ_BF16) {
+      u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7FFF7FFFu);
+#pragma unroll
+      for (int i = 1; i < kWords; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7FFF7FFFu));
+      return uint32_t(max(m.x, m.y)) << 16;
+    } else {
+      uint32_t m = 0u;
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) m = max(m, w[i] & 0x7FFFFFFFu);
+      return m;
+    }
+  }
+  // the smallest and the largest, NaN below or above all (as whole numbers, whose order the values'
+  // is once negative ones' lower bits are turned)
+  __device__ __forceinline__ f32x2 extremes() const {
+    if constexpr (DT == RBQ_BF16) {
+      auto turn = [](i16x2 v) { return v ^ ((v >> 15) & i16x2{0x7FFF, 0x7FFF}); };
+      i16x2 lo = turn(__builtin_bit_cast(i16x2, w[0])), hi = lo;
+#pragma unroll
+      for (int i = 1; i < kWords; ++i) {
+        const i16x2 v = turn(__builtin_bit_cast(i16x2, w[i]));
+        lo = __builtin_elementwise_min(lo, v);
+        hi = __builtin_elementwise_max(hi, v);
+      }
+      const uint32_t r = __builtin_bit_cast(uint32_t, turn(i16x2{min(lo.x, lo.y), max(hi.x, hi.y)}));
+      return f32x2{bf16_lo(r), bf16_hi(r)};
+    } else {
+      auto turn = [](int32_t v) { return v ^ ((v >> 31) & 0x7FFFFFFF); };
+      int32_t lo = turn(int32_t(w[0])), hi = lo;
+#pragma unroll
+      for (int i = 1; i < kWords; ++i) {
+        lo = min(lo, turn(int32_t(w[i])));
+        hi = max(hi, turn(int32_t(w[i])));
+      }
+      return f32x2{__uint_as_float(uint32_t(turn(lo))), __uint_as_float(uint32_t(turn(hi)))};
+    }
+  }
+};
+
+// e of a group whose largest magnitude is amax = m 2^x, m in [1, 2): 7 = 1.75 * 2^2, so x - 2,
+// one more above m = 1.75
+__device__ __forceinline__ int fp4_exponent(uint32_t amax) {
+  const int e = int(amax >> 23) - 127 - 2 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+  return min(max(e, -126), 125);
+}
+
+// 16 values of fp4: their codes, and their group's exponent byte. Where a whole wave's are finite
+// the conversion takes them as they are, scale and bounds with it.
+template <int LANES, int DT>
+__device__ __forceinline__ u32x2 encode_fp4(const Taken<DT>& raw, uint32_t& byte) {
+  uint32_t top = raw.amax();
+  if (__ballot(top >= 0x7F800000u) == 0ull) {
+    if constexpr (LANES >= 2) top = max(top, RBQ_DPP_U32(top, 0xB1));
+    const int ec = fp4_exponent(top);
+    byte = top == 0u ? 0u : uint32_t(ec + 127);
+    const float scale = __uint_as_float(uint32_t(ec + 127) << 23);
+    u32x2 w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      auto pair = [&](uint32_t v, int p, auto place) {
+        if constexpr (DT == RBQ_BF16) {
+          return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(v, __builtin_bit_cast(bf16x2_t, raw.w[4 * h + p]), scale,
+                                                           decltype(place)::value);
+        } else {
+          return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(v, __uint_as_float(raw.w[8 * h + 2 * p]),
+                                                          __uint_as_float(raw.w[8 * h + 2 * p + 1]), scale, decltype(place)::value);
+        }
+      };
+      uint32_t v = pair(0u, 0, std::integral_constant<int, 0>{});
+      v = pair(v, 1, std::integral_constant<int, 1>{});
+      v = pair(v, 2, std::integral_constant<int, 2>{});
+      v = pair(v, 3, std::integral_constant<int, 3>{});
+      w[h] = top == 0u ? 0u : v;
+    }
+    return w;
+  }
+  float x[kTake];
+  raw.values(x);
   uint32_t amax = 0u;
 #pragma unroll
   for (int i = 0; i < kTake; ++i) {
@@ -63,9 +164,7 @@ __device__ __forceinline__ u32x2 encode_fp4(const float* x, uint32_t& byte) {
     amax = max(amax, u < 0x7F800000u ? u : 0u);   // (the order of magnitudes is the order of the bits)
   }
   if constexpr (LANES >= 2) amax = max(amax, RBQ_DPP_U32(amax, 0xB1));
-  // amax = m 2^x with m in [1, 2); 7 = 1.75 * 2^2, so e = x - 2, one more above m = 1.75
-  const int e = int(amax >> 23) - 127 - 2 + ((amax & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-  const int ec = min(max(e, -126), 125);
+  const int ec = fp4_exponent(amax);
   byte = amax == 0u ? 0u : uint32_t(ec + 127);
   const float r = __uint_as_float(uint32_t(127 - ec) << 23);
   u32x2 w;
@@ -91,10 +190,45 @@ __device__ __forceinline__ u32x2 encode_fp4(const float* x, uint32_t& byte) {
   return w;
 }
 
-// 16 values of int4: their codes, and their row's word
-template <int LANES>
-__device__ __forceinline__ u32x2 encode_i4(const float* x, uint32_t& word) {
-  float lo = INFINITY, hi = -INFINITY;
+// A row's base, step and the step's reciprocal from its extremes
+struct Line {
+  float m, s, r;
+};
+__device__ __forceinline__ Line line_of(float lo, float hi) {
+  Line a;
+  a.m = bf16_down(lo);
+  const float d = hi - a.m;
+  a.s = d > 0.f ? bf16_up(fmaxf(d / 15.f, kLeast)) : 0.f;
+  a.r = a.s > 0.f ? 1.f / a.s : 0.f;
+  return a;
+}
+
+// 16 values of int4: their codes, and their row's word. Where a whole wave's are within 2^126 no
+// code is beyond 0 .. 15: x lies between m and hi, and s is no less than d / 15.
+template <int LANES, int DT>
+__device__ __forceinline__ u32x2 encode_i4(const Taken<DT>& raw, uint32_t& word) {
+  float x[kTake];
+  raw.values(x);
+  const f32x2 ends = raw.extremes();
+  float lo = ends.x, hi = ends.y;
+  auto least = [](float a, float b) { return fminf(a, b); };
+  auto most = [](float a, float b) { return fmaxf(a, b); };
+  u32x2 w;
+  if (__ballot(!(lo >= -kMost && hi <= kMost)) == 0ull) {
+    const Line a = line_of(lanes_reduce<LANES>(lo, least), lanes_reduce<LANES>(hi, most));
+    word = __float_as_uint(a.s) >> 16 | __float_as_uint(a.m);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      uint32_t v = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)   // (what the numbers have beside their low bits is taken off the word)
+        v += (__float_as_uint(fmaf(x[8 * h + i] - a.m, a.r, kRound)) << nibble_shift<RBQ_I4>(i)) -
+             (kRoundBits << nibble_shift<RBQ_I4>(i));
+      w[h] = v;
+    }
+    return w;
+  }
+  lo = INFINITY, hi = -INFINITY;
 #pragma unroll
   for (int i = 0; i < kTake; ++i) {
     const bool f = is_finite(x[i]);
@@ -102,21 +236,18 @@ __device__ __forceinline__ u32x2 encode_i4(const float* x, uint32_t& word) {
     lo = f ? fminf(lo, v) : lo;
     hi = f ? fmaxf(hi, v) : hi;
   }
-  lo = lanes_reduce<LANES>(lo, [](float a, float b) { return fminf(a, b); });
-  hi = lanes_reduce<LANES>(hi, [](float a, float b) { return fmaxf(a, b); });
+  lo = lanes_reduce<LANES>(lo, least);
+  hi = lanes_reduce<LANES>(hi, most);
   if (lo > hi) lo = hi = 0.f;   // no finite value
-  const float m = bf16_down(lo), d = hi - m;
-  const float s = d > 0.f ? bf16_up(fmaxf(d / 15.f, kLeast)) : 0.f;
-  const float r = s > 0.f ? 1.f / s : 0.f;
-  word = __float_as_uint(s) >> 16 | __float_as_uint(m);
-  u32x2 w;
+  const Line a = line_of(lo, hi);
+  word = __float_as_uint(a.s) >> 16 | __float_as_uint(a.m);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     uint32_t v = 0u;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float y = x[8 * h + i] == x[8 * h + i] ? x[8 * h + i] : 0.f;
-      const float t = fmaf(y - m, r, kRound);   // one rounding, to a whole number
+      const float t = fmaf(y - a.m, a.r, kRound);   // one rounding, to a whole number
       const uint32_t c = __float_as_uint(t == t ? fminf(fmaxf(t, kRound), kRound + 15.f) : kRound) & 15u;
       v |= c << nibble_shift<RBQ_I4>(i);
     }
@@ -140,19 +271,12 @@ __global__ __launch_bounds__(kThreads4) void quantize_kv4_kernel(
   const bool isv = l >= kLanes;
   if (row >= sp.cnt) return;   // (all lanes of a row alike)
   const u32x4* src = reinterpret_cast<const u32x4*>((isv ? V : K) + ((int64_t(bh) * ld + row) * D + piece * kTake) * kEl);
-  float x[kTake];
+  Taken<DT> x;
 #pragma unroll
   for (int i = 0; i < kTake * kEl / 16; ++i) {
     const u32x4 v = __builtin_nontemporal_load(src + i);
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if constexpr (DT == RBQ_BF16) {
-        x[8 * i + 2 * k] = bf16_lo(v[k]);
-        x[8 * i + 2 * k + 1] = bf16_hi(v[k]);
-      } else {
-        x[4 * i + k] = __uint_as_float(v[k]);
-      }
-    }
+    for (int k = 0; k < 4; ++k) x.w[4 * i + k] = v[k];
   }
   const int64_t at = int64_t(bh) * cap + sp.off + row;
   uint32_t word;

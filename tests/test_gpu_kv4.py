@@ -95,6 +95,48 @@ def test_rows_written_are_those_of_the_definition(R, case, dt, fmt):
 @pytest.mark.parametrize("fmt", ku.FORMATS)
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("D", [64, 128])
+def test_finite_rows_of_every_size(R, D, dt, fmt):
+    """Without an infinity or NaN near them (which take another way through the kernel): rows of any finite bits below a
+    bound, for bounds from the least subnormal to the largest value; bounds, ties and values of one size, rows of each alone."""
+    rng = np.random.default_rng(17)
+    top = (1 << 15) if dt == "bf16" else (1 << 31)
+    limit = 0x7F80 if dt == "bf16" else 0x7F800000                        # infinity's bits
+    bounds = np.concatenate([np.geomspace(2, limit, 600).astype(np.int64), limit * np.arange(1, 256) // 255,
+                             np.arange(1, 256) * (limit // 255) + (limit // 255) * 3 // 4])
+    bounds = np.clip(np.repeat(bounds, 2), 2, limit)
+    mag = rng.integers(0, bounds[:, None], (len(bounds), D))
+    # half of the rows close to their bound in size, so that the codes spread
+    near = np.maximum(bounds[:, None] - (rng.integers(0, 5, mag.shape) << (7 if dt == "bf16" else 23)) - rng.integers(1, 99, mag.shape), 0)
+    mag = np.where(rng.random((len(bounds), 1)) < 0.5, mag, near)
+    sign = np.where(rng.random((len(bounds), 1)) < 0.8, rng.integers(0, 2, mag.shape), rng.integers(0, 2, (len(bounds), 1)))
+    bits = mag + sign * top
+    x = (torch.from_numpy(bits.astype(np.uint16).view(np.int16)).view(torch.bfloat16) if dt == "bf16" else
+         torch.from_numpy(bits.astype(np.uint32).view(np.float32)))
+    same = [np.zeros(D), np.full(D, 0.1), np.full(D, -0.1), np.full(D, 2.0 ** 126), np.full(D, -2.0 ** 126), np.full(D, 1e-40),
+            np.resize([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.0, -0.25, -0.75, -1.25, -2.5, -5.0], D),
+            np.resize(np.arange(16) / 2.0, D), np.resize([1e6, 1e6 + 0.0625, 1e6 + 4], D), np.resize([-7.0, 0.0], D),
+            np.resize([-2.0 ** 126, 2.0 ** 126, 1.0], D), np.resize([7 * 2.0 ** -126, 2.0 ** -127], D)]
+    x = torch.cat([x, torch.from_numpy(np.repeat(np.stack(same), 8, axis=0)).to(DT[dt])])
+    assert torch.all(torch.isfinite(x.float()))
+    n = len(x)
+    kv, par = torch.zeros(1, 1, n, D, dtype=torch.uint8, device="cuda"), torch.zeros(1, 1, n, 2, dtype=torch.int32, device="cuda")
+    d = x.cuda().view(1, 1, n, D)
+    R.rbq_quantize_kv4(1, 1, D, d, -d, n, n, 0, n, R.KV4_FORMATS[fmt], kv, par)
+    got, p = kv.cpu().numpy()[0, 0], par.cpu().numpy().view(np.uint32)[0, 0]
+    for k, v in ((0, x), (1, -x)):
+        codes, word = encoded(v.double().numpy(), fmt)
+        # (a base of zero may have either sign)
+        zero = lambda a: np.where((a >> 16) == 0x8000, a & 0xFFFF, a) if fmt == "int4" else a  # noqa: E731
+        assert np.array_equal(zero(p[:, k]), zero(word)), np.flatnonzero(zero(p[:, k]) != zero(word))[:5]
+        c = ku.unpack(got[:, k * D // 2:(k + 1) * D // 2], fmt)
+        if fmt == "fp4":
+            c, codes = (np.where(a == 8, 0, a) for a in (c, codes))
+        assert np.array_equal(c, codes), np.argwhere(c != codes)[:5]
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
 def test_extreme_values(R, D, dt, fmt):
     """Rows of zeros, of one value, of subnormals, at the type's largest and lowest value, at the format's borders and
     ties, with infinities and NaN beside ordinary values, and of nothing else; read back in both types."""
