@@ -1,6 +1,8 @@
 // Reading the rows of the 4-bit cache: what the kernels that turn them into values share.
 #pragma once
 
+#include <type_traits>
+
 #include "rbq_device.h"
 #include "rbq_internal.h"
 
@@ -75,14 +77,13 @@ __device__ __forceinline__ u32x4 word_bf16(uint32_t w, f32x2 sc) {
     typedef float f32x2v __attribute__((ext_vector_type(2)));
     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
     const uint32_t even = w & 0x0F0F0F0Fu, odd = w >> 4 & 0x0F0F0F0Fu;   // nibbles 0 2 4 6 (dimensions 0 4 1 5), 1 3 5 7 (2 6 3 7)
-    auto value = [&](uint32_t v, int byte) { return fmaf(float(uint8_t(v >> (8 * byte))), sc.x, sc.y); };
-    auto pair = [&](float a, float b) {
-      return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{a, b}), bf16x2));
+    // (as bytes they are e4m3's codes of themselves times 2^-9)
+    auto pair = [&](uint32_t v, auto high) {
+      const f32x2v c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(v, 512.f, decltype(high)::value);
+      return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2v{fmaf(c.x, sc.x, sc.y), fmaf(c.y, sc.x, sc.y)}), bf16x2));
     };
-    r[0] = pair(value(even, 0), value(even, 2));
-    r[1] = pair(value(odd, 0), value(odd, 2));
-    r[2] = pair(value(even, 1), value(even, 3));
-    r[3] = pair(value(odd, 1), value(odd, 3));
+    const uint32_t a = __builtin_amdgcn_perm(odd, even, 0x06040200u), b = __builtin_amdgcn_perm(odd, even, 0x07050301u);
+    r = u32x4{pair(a, std::false_type{}), pair(a, std::true_type{}), pair(b, std::false_type{}), pair(b, std::true_type{})};
   }
   return r;
 }
