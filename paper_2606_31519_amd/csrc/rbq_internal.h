@@ -203,6 +203,8 @@ DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
 // number of splits may fall as the window grows, the size does not.
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                                   int32_t w, bool step = false);
+size_t decode_kv4_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
+                                  int32_t w, bool step = false);   // the same over a 4-bit cache
 size_t decode_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                               int32_t w);
 

@@ -232,6 +232,12 @@ DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
   return s;
 }
 
+namespace {
+size_t decode_states_bytes(int32_t batch, int32_t heads_q, int32_t head_dim, int64_t splits) {
+  return size_t(batch) * heads_q * splits * (size_t(head_dim) + 2) * sizeof(float);
+}
+}  // namespace
+
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                                   int32_t w, bool step) {
   if (batch <= 0 || heads_q <= 0 || heads_kv <= 0 || head_dim <= 0 || n < 0 || w < 0) return 0;
@@ -243,7 +249,18 @@ size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_
     total = std::max<int64_t>({total, ragged, decode_kv8_splits(batch, heads_kv, n, w, false, false, false).total()});
     if (groups * n >= kKv8Resident * kDecodeMinChunk) total = std::max(total, kv8_round_blocks(groups * ragged) / groups);
   }
-  return align_up(size_t(batch) * heads_q * total * (head_dim + 2) * sizeof(float), 256);
+  return align_up(decode_states_bytes(batch, heads_q, head_dim, total), 256);
+}
+
+size_t decode_kv4_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
+                                  int32_t w, bool step) {
+  // sparse and ragged calls have the 8-bit cache's splits, dense ones at most a round's with any window, or those of the window
+  const size_t as_kv8 = decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w, step);
+  if (as_kv8 == 0 || step) return as_kv8;
+  const int64_t groups = int64_t(batch) * heads_kv;
+  int64_t dense = decode_kv4_splits(batch, heads_kv, n, w, false, false, false).total();
+  if (groups * n >= kKv8Resident * kDecodeMinChunk) dense = std::max(dense, kKv8Resident / groups);
+  return std::max(as_kv8, align_up(decode_states_bytes(batch, heads_q, head_dim, dense), 256));
 }
 
 namespace {
@@ -293,7 +310,7 @@ rbq_status check_decode_kv8(int32_t batch, int32_t heads_q, int32_t heads_kv, in
   if (int64_t(n) * head_dim >= (int64_t(1) << 31)) return RBQ_EINVAL;
   // (what this form of the call needs: rbq_workspace_bytes gives the largest of the forms')
   const int64_t splits = decode_kv8_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr).total();
-  if (bad_ptr(ws) || ws_bytes < size_t(batch) * heads_q * splits * (size_t(head_dim) + 2) * sizeof(float)) return RBQ_EINVAL;
+  if (bad_ptr(ws) || ws_bytes < decode_states_bytes(batch, heads_q, head_dim, splits)) return RBQ_EINVAL;
   // a ragged batch's blocks are numbered along one dimension of the grid
   if ((seq_n || seq_w) && int64_t(batch) * heads_kv * splits >= (int64_t(1) << 24)) return RBQ_EUNSUPPORTED;
   return RBQ_OK;
@@ -324,13 +341,17 @@ rbq_status check_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, in
                             const Kv4Cache& c, int32_t n, bool sparse, const int32_t* sel_idx,
                             const int32_t* sel_count, const Kv8Window& win, float sm_scale, const float* out,
                             const void* ws, size_t ws_bytes, const int32_t* seq_n, const int32_t* seq_w) {
-  const rbq_status s = check_kv4_form(c.dtype);
+  rbq_status s = check_kv4_form(c.dtype);
   if (s != RBQ_OK) return s;
-  // the same call over another cache: a row's record takes the bytes that K's row takes there, and the splits are its
+  // the same call over another cache: a row's record takes the bytes that K's row takes there
   const float* par = reinterpret_cast<const float*>(c.par);
   const Kv8Cache as{c.KV4, c.KV4, par, par, RBQ_E4M3, kMinKv8Block, c.cap};
-  return check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, as, n, sparse, sel_idx, sel_count, win, sm_scale, out,
-                          ws, ws_bytes, seq_n, seq_w);
+  s = check_decode_kv8(batch, heads_q, heads_kv, head_dim, q, as, n, sparse, sel_idx, sel_count, win, sm_scale, out, ws,
+                       ws_bytes, seq_n, seq_w);
+  if (s != RBQ_OK) return s;
+  // (the splits of dense calls are its own)
+  const DecodeSplits sp = decode_kv4_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr);
+  return ws_bytes < decode_states_bytes(batch, heads_q, head_dim, sp.total()) ? RBQ_EINVAL : RBQ_OK;
 }
 
 namespace {
@@ -496,8 +517,9 @@ size_t rbq_workspace_bytes(int32_t op, int32_t batch, int32_t heads_q, int32_t h
     case RBQ_OP_DENSE_DECODE:
       return rbq::decode_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_DECODE_KV8:
-    case RBQ_OP_DECODE_KV4:
       return rbq::decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
+    case RBQ_OP_DECODE_KV4:
+      return rbq::decode_kv4_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_PREFILL:
       return rbq::prefill_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w);
     case RBQ_OP_PREFILL_KV4: {
