@@ -30,7 +30,8 @@ rbq_status launch_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, i
                              hipStream_t stream, const unsigned long long* sel_mask, int32_t mask_words,
                              const int32_t* seq_n, const int32_t* seq_w) {
   const int G = heads_q / heads_kv;
-  const DecodeSplits sp = decode_kv4_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr);
+  const DecodeSplits sp =
+      decode_kv4_splits(batch, heads_q, heads_kv, head_dim, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr);
   Call a = make_call(batch, heads_q, heads_kv, head_dim, q, n, sel_idx, sel_count, win, sm_scale, ws, sparse, stream,
                      sel_mask, mask_words, seq_n, seq_w, sp);
   a.K = static_cast<const char*>(cache.KV4);

@@ -194,11 +194,18 @@ constexpr int kKv8DenseChunk = 2048;   // positions per dense split (at most)
 // which the host does not know: then no split takes window rows along)
 DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
                                bool own_windows);
-// The splits over a 4-bit cache: the same but for uniform dense calls, which take one round of
-// blocks whatever the rows (no scales of a split lie in LDS): 500K rows of 8 KV heads 107.5 us, in
-// rounds of 2048 rows a block 125.8; 8 x 32000 61.2 and 65.8.
-DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
-                               bool own_windows);
+// The splits over a 4-bit cache: the same but for uniform dense calls, which take one round of blocks (no scales of a
+// split lie in LDS) where the places that the window's leave, by whole splits of every group, are 0.85 of the GPU's or
+// more. us, so and in the 8-bit cache's rounds, 8 KV heads of 128 (share of the places in brackets): 500K rows 107.5 and
+// 125.8; 8 x 32000 with a window of 256 (0.94) 60.3 and 64.3, of 1024 (0.75) 70.9 and 68.5, of 4096 (0.06) 270 and 94;
+// 16 x 8000 with 256 (0.88) 36.5 and 37.1, 20 x 8000 (0.78) 46.7 and 47.6, 24 x 8000 (0.75) 55.7 and 52.8, 43 x 8000
+// (0.34) 133 and 94; 64 x 8000 without one (1) 111 and 124, 65 x 8000 (0.51) 142 and 123.
+// (ragged: with lengths of their own the sequences' splits are the 8-bit cache's)
+DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n, int32_t w,
+                               bool sparse, bool ragged, bool own_windows);
+// Blocks of the dense kernel that run at once, and are planned for: 4 a compute unit at D = 128, 3 in groups of 16 (46 KB of
+// LDS each; 128K rows of 128 / 8 heads 48.7 us in 768 blocks, 54.9 in 1024); at D = 64, where 5 do, 4 too.
+int64_t kv4_places(int32_t heads_q, int32_t heads_kv, int32_t head_dim);
 // The states of any form of the calls, or of the fused step's (uniform and sparse), with any window up to w: the
 // number of splits may fall as the window grows, the size does not.
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,

@@ -220,12 +220,17 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
   return s;
 }
 
-DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_kv, int32_t n, int32_t w, bool sparse, bool ragged,
-                               bool own_windows) {
+int64_t kv4_places(int32_t heads_q, int32_t heads_kv, int32_t head_dim) {
+  return head_dim == kHeadDim && heads_q / heads_kv == 16 ? 3 * kCus : kKv8Resident;
+}
+
+DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n, int32_t w,
+                               bool sparse, bool ragged, bool own_windows) {
   DecodeSplits s = decode_kv8_splits(batch, heads_kv, n, w, sparse, ragged, own_windows);
   const int64_t groups = int64_t(batch) * heads_kv;
   if (sparse || ragged || groups * n < kKv8Resident * kDecodeMinChunk) return s;
-  const int64_t splits = std::max<int64_t>(kKv8Resident / groups - s.win_splits, 1);
+  const int64_t places = kv4_places(heads_q, heads_kv, head_dim), splits = places / groups - s.win_splits;
+  if (20 * splits * groups < 17 * places) return s;
   const int64_t chunk = ((int64_t(n) + splits - 1) / splits + 63) / 64 * 64;
   s.chunk = int32_t(std::max<int64_t>(chunk, kDecodeMinChunk));
   s.idx_splits = int32_t((int64_t(n) + s.chunk - 1) / s.chunk);
@@ -254,12 +259,12 @@ size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_
 
 size_t decode_kv4_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,
                                   int32_t w, bool step) {
-  // sparse and ragged calls have the 8-bit cache's splits, dense ones at most a round's with any window, or those of the window
+  // the 8-bit cache's splits, or, of a dense call with any window, at most a round of blocks
   const size_t as_kv8 = decode_kv8_workspace_bytes(batch, heads_q, heads_kv, head_dim, n, w, step);
   if (as_kv8 == 0 || step) return as_kv8;
   const int64_t groups = int64_t(batch) * heads_kv;
-  int64_t dense = decode_kv4_splits(batch, heads_kv, n, w, false, false, false).total();
-  if (groups * n >= kKv8Resident * kDecodeMinChunk) dense = std::max(dense, kKv8Resident / groups);
+  int64_t dense = decode_kv4_splits(batch, heads_q, heads_kv, head_dim, n, w, false, false, false).total();
+  if (groups * n >= kKv8Resident * kDecodeMinChunk) dense = std::max(dense, kv4_places(heads_q, heads_kv, head_dim) / groups);
   return std::max(as_kv8, align_up(decode_states_bytes(batch, heads_q, head_dim, dense), 256));
 }
 
@@ -350,7 +355,8 @@ rbq_status check_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, in
                        ws_bytes, seq_n, seq_w);
   if (s != RBQ_OK) return s;
   // (the splits of dense calls are its own)
-  const DecodeSplits sp = decode_kv4_splits(batch, heads_kv, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr);
+  const DecodeSplits sp =
+      decode_kv4_splits(batch, heads_q, heads_kv, head_dim, n, win.w, sparse, seq_n != nullptr, seq_w != nullptr);
   return ws_bytes < decode_states_bytes(batch, heads_q, head_dim, sp.total()) ? RBQ_EINVAL : RBQ_OK;
 }
 

@@ -22,7 +22,7 @@ int main() {
   int B, Hq, Hkv, D, n, w, form;
   while (std::scanf("%d %d %d %d %d %d %d", &B, &Hq, &Hkv, &D, &n, &w, &form) == 7) {
     const bool sparse = form & 1, rows = form & 2, windows = form & 4;
-    const DecodeSplits a = decode_kv4_splits(B, Hkv, n, w, sparse, rows, windows);
+    const DecodeSplits a = decode_kv4_splits(B, Hq, Hkv, D, n, w, sparse, rows, windows);
     const DecodeSplits b = decode_kv8_splits(B, Hkv, n, w, sparse, rows, windows);
     const size_t bytes = size_t(B) * Hq * std::max(a.total(), b.total()) * (D + 2) * sizeof(float);
     const Kv4Cache c{p, static_cast<const uint32_t*>(p), RBQ_FP4, n};

@@ -62,3 +62,19 @@ def test_the_workspace_size_covers_every_plan_and_every_shorter_window(plans):
         assert states <= R.rbq_workspace_bytes(R.RBQ_OP_DECODE_KV4, *s), (s, w, form, r)
         if form == 1:    # the fused step's
             assert states <= R.rbq_workspace_bytes(R.RBQ_OP_DECODE_STEP_KV4, *s), (s, w, r)
+
+
+def test_dense_plans_leave_no_part_of_the_gpu_empty(plans):
+    """A uniform dense call's blocks of cached rows are no longer than 1 / 0.85 of what the blocks that run at once (4 a
+    compute unit, 3 in groups of 16 at D = 128) would take if they shared them evenly, up to the 64 rows that they are
+    rounded to, or they are the 8-bit plan's."""
+    cases = shapes()
+    short = 0
+    for c, r in zip(cases, plans([(*c, 0) for c in cases])):
+        B, Hq, Hkv, D, n, w = c
+        places = 256 * (3 if D == 128 and Hq // Hkv == 16 else 4)
+        even = n * B * Hkv / (0.85 * places)
+        assert r[0] <= 64 * np.ceil(even / 64) or (r[:3] == r[3:6]).all(), (c, r)
+        short += n > 0 and (r[:3] != r[3:6]).any()
+        assert n == 0 or (r[1] - 1) * r[0] < n <= r[1] * r[0], (c, r)       # every row is in a split, none of them empty
+    assert short > 20     # (plans of their own are among them)
