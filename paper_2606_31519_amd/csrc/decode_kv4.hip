@@ -37,6 +37,7 @@ rbq_status launch_decode_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, i
   a.K = static_cast<const char*>(cache.KV4);
   a.k_scale = reinterpret_cast<const float*>(cache.par);
   a.cap = cache.cap;
+  a.turns = !sparse && !a.ragged && kv4_one_round(batch, heads_q, heads_kv, head_dim, sp);
   const bool f32 = win.dtype == RBQ_F32 && win.w > 0, i4 = cache.dtype == RBQ_I4;
   rbq_status st;
 #define RBQ_KV4(D)                                                                                          \

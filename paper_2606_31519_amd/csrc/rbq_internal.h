@@ -199,13 +199,17 @@ DecodeSplits decode_kv8_splits(int32_t batch, int32_t heads_kv, int32_t n, int32
 // more. us, so and in the 8-bit cache's rounds, 8 KV heads of 128 (share of the places in brackets): 500K rows 107.5 and
 // 125.8; 8 x 32000 with a window of 256 (0.94) 60.3 and 64.3, of 1024 (0.75) 70.9 and 68.5, of 4096 (0.06) 270 and 94;
 // 16 x 8000 with 256 (0.88) 36.5 and 37.1, 20 x 8000 (0.78) 46.7 and 47.6, 24 x 8000 (0.75) 55.7 and 52.8, 43 x 8000
-// (0.34) 133 and 94; 64 x 8000 without one (1) 111 and 124, 65 x 8000 (0.51) 142 and 123.
+// (0.34) 133 and 94; without one 64 x 8000 (1) 111 and 124, 43 x 8000 (0.67) 83 and 85, 65 x 8000 (0.51) 142 and 123.
 // (ragged: with lengths of their own the sequences' splits are the 8-bit cache's)
 DecodeSplits decode_kv4_splits(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n, int32_t w,
                                bool sparse, bool ragged, bool own_windows);
 // Blocks of the dense kernel that run at once, and are planned for: 4 a compute unit at D = 128, 3 in groups of 16 (46 KB of
 // LDS each; 128K rows of 128 / 8 heads 48.7 us in 768 blocks, 54.9 in 1024); at D = 64, where 5 do, 4 too.
 int64_t kv4_places(int32_t heads_q, int32_t heads_kv, int32_t head_dim);
+// Whether a dense call's blocks all run at once
+inline bool kv4_one_round(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, const DecodeSplits& s) {
+  return int64_t(batch) * heads_kv * s.total() <= kv4_places(heads_q, heads_kv, head_dim);
+}
 // The states of any form of the calls, or of the fused step's (uniform and sparse), with any window up to w: the
 // number of splits may fall as the window grows, the size does not.
 size_t decode_kv8_workspace_bytes(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim, int32_t n,

@@ -5,6 +5,7 @@
 //   chunk idx_splits win_splits   of the same call over an 8-bit cache
 //   the check of its arguments with a workspace of exactly the states of the larger of the two, and of
 //   one byte less
+//   whether its blocks are taken for one round
 // Built by tests/test_kv4_plans.py with g++ from csrc/validate.cpp and this file; no HIP runtime, no GPU.
 #include <algorithm>
 #include <cstdint>
@@ -31,8 +32,8 @@ int main() {
       return int(check_decode_kv4(B, Hq, Hkv, D, f, c, n, sparse, i, i, win, 0.1f, f, p, have, rows ? i : nullptr,
                                   windows ? i : nullptr));
     };
-    std::printf("%d %d %d %d %d %d %d %d\n", a.chunk, a.idx_splits, a.win_splits, b.chunk, b.idx_splits, b.win_splits,
-                check(bytes), check(bytes - 1));
+    std::printf("%d %d %d %d %d %d %d %d %d\n", a.chunk, a.idx_splits, a.win_splits, b.chunk, b.idx_splits, b.win_splits,
+                check(bytes), check(bytes - 1), int(kv4_one_round(B, Hq, Hkv, D, a)));
   }
   return 0;
 }

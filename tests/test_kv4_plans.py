@@ -78,3 +78,15 @@ def test_dense_plans_leave_no_part_of_the_gpu_empty(plans):
         short += n > 0 and (r[:3] != r[3:6]).any()
         assert n == 0 or (r[1] - 1) * r[0] < n <= r[1] * r[0], (c, r)       # every row is in a split, none of them empty
     assert short > 20     # (plans of their own are among them)
+
+
+def test_one_round_is_as_many_blocks_as_run_at_once(plans):
+    """Waves take turns (a priority that belongs to blocks which start together) in such calls only, those of the window
+    counted: not in groups of 16 at D = 128 beyond 768 blocks, nor beyond 1024."""
+    cases = shapes()
+    rounds = {True: 0, False: 0}
+    for c, r in zip(cases, plans([(*c, 0) for c in cases])):
+        places = 256 * (3 if c[3] == 128 and c[1] // c[2] == 16 else 4)
+        assert bool(r[8]) == (c[0] * c[2] * (r[1] + r[2]) <= places), (c, r)
+        rounds[bool(r[8])] += 1
+    assert min(rounds.values()) > 20
