@@ -253,6 +253,29 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
         s = product(*reinterpret_cast<const u32x4*>(kp + 8 * kb), __builtin_bit_cast(u32x4, query(0, kb)), s);
       }
     }
+    if constexpr (kF32) {
+      // An infinity has no parts (those after the first are NaN): logits that came out infinite or NaN are
+      // formed again, from the values themselves.
+      float odd_logit = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) odd_logit = fmaf(s[r], 0.f, odd_logit);
+      if (__ballot(odd_logit != odd_logit)) {
+        const T* qp = q + int64_t(t.q0 + token) * q_ld + head * D;
+#pragma unroll 1
+        for (int r = 0; r < 16; ++r) {   // (one at a time: registers are short)
+          const T* k = Kb + int64_t(min(k0 - nbp + key_of(r), t.nq - 1)) * kv_ld;
+          float v = 0.f;
+#pragma unroll 2
+          for (int d = 0; d < D; d += 8) {
+            const f32x8 a = load8(k + d), b = load8(qp + d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v = fmaf(a[e], b[e], v);
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = i == r && !(fabsf(s[i]) < INFINITY) ? v : s[i];
+        }
+      }
+    }
     softmax(s, k0);
     bool inf = false;
 #pragma unroll
