@@ -624,7 +624,7 @@ rbq_status rbq_decode_step_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv,
  * probabilities times the steps) are rounded to bf16 before they meet the products; cached keys
  * never are. Everything else as in rbq_prefill_attention, so that a key of the chunk with an
  * infinity has the weight of its logit: 0 where that is -infinity, NaN in its head where it is
- * +infinity or NaN. RBQ_EINVAL also where n * D >= 2^31.
+ * +infinity or NaN; a query with an infinity is NaN. RBQ_EINVAL also where n * D >= 2^31.
  */
 rbq_status rbq_prefill_attention_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv, int32_t head_dim,
                                      const void* q, int64_t q_ld, const void* K, const void* V, int32_t dtype,

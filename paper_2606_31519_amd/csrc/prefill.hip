@@ -275,6 +275,13 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb) qf[kb] = *reinterpret_cast<const bf16x8*>(p + 16 * kb);
   }
+  float odd_q = 0.f;   // NaN where the lane's half of the query has an infinity or NaN
+  if constexpr (FMT != 0) {
+#pragma unroll
+    for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) odd_q = fmaf(float(qf[kb][i]), 0.f, odd_q);
+  }
   float qsum = 0.f;
   if constexpr (kBase) {
 #pragma unroll
@@ -345,7 +352,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
   const int vbase = (4 * h + (i16 >> 2)) * RB + (((2 * g16 + ((i16 & 3) >> 1)) ^ v_swizzle<D>(i16 >> 2)) * 16) + (i16 & 1) * 8;
 
   f32x16 o[DT][1];
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = odd_q;   // (such a query is NaN, also where all its logits are -infinity)
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -574,6 +581,13 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) qf[i] = *reinterpret_cast<const f32x4*>(p + 4 * i) * scale_log2e;
   }
+  float odd_q = 0.f;   // (as in the bf16 kernel)
+  if constexpr (FMT != 0) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) odd_q = fmaf(qf[i][e], 0.f, odd_q);
+  }
   const int64_t kvoff = (kv_seq == 0 ? t.k0 * kv_ld : int64_t(t.b) * kv_seq) + int64_t(hk) * kv_head;
   f32x4 kreg[kPieces], vreg[kPieces];
   const int nbp = FMT != 0 ? (t.nb + kPKeys - 1) / kPKeys * kPKeys : 0;   // first of the chunk's own keys
@@ -606,7 +620,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
   for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o[d][0][r] = 0.f;
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = odd_q;
   // (infinities and NaN of V as in the bf16 kernel)
   const int bmin = visible(row0 / G);
   const int kodd = bmin > kbeg ? kbeg + (bmin - kbeg) / kFKeys * kFKeys : kbeg;

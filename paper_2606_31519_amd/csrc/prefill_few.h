@@ -121,7 +121,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
   const int all = visible(row0 / G);                                 // keys that every row sees
   const int qrow = min(row0 + x, rows - 1), token = qrow / G, head = hk * G + (qrow - token * G), lim = visible(token);
   bf16x8 qf[kF32 ? 1 : KB];
-  float qsum = 0.f;
+  float qsum = 0.f, odd_q = 0.f;   // odd_q (bf16): NaN where the lane's half of the query has an infinity or NaN
   {
     const T* p = q + int64_t(t.q0 + token) * q_ld + head * D + (D / 2) * h;
 #pragma unroll
@@ -137,6 +137,8 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
         }
       } else {
         qf[kb] = *reinterpret_cast<const bf16x8*>(p + 8 * kb);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) odd_q = fmaf(float(qf[kb][i]), 0.f, odd_q);
         if constexpr (kBase) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) qsum += float(qf[kb][i]);
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
   };
 
   f32x16 o[DT];
-  float m = -INFINITY, l = 0.f, base = 0.f;
+  float m = -INFINITY, l = odd_q, base = 0.f;   // (such a query is NaN, also where all its logits are -infinity)
 #pragma unroll
   for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -269,7 +271,10 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
           for (int d = 0; d < D; d += 8) {
             const f32x8 a = load8(k + d), b = load8(qp + d);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v = fmaf(a[e], b[e], v);
+            for (int e = 0; e < 8; ++e) {
+              v = fmaf(a[e], b[e], v);
+              l = fmaf(b[e], 0.f, l);   // (as with odd_q)
+            }
           }
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = i == r && !(fabsf(s[i]) < INFINITY) ? v : s[i];

@@ -1,7 +1,7 @@
-"""Infinities among a chunk's own keys (rbq_prefill_attention_kv4): a key with one has the
-logits that IEEE arithmetic gives it, so that a logit of -infinity is a weight of 0 and one
-of +infinity, or the product of an infinity with 0, is NaN in its head. Alike in the
-kernels of few rows and of tiles, for either type."""
+"""Infinities among a chunk's own keys and queries (rbq_prefill_attention_kv4): a key with
+one has the logits that IEEE arithmetic gives it, so that a logit of -infinity is a weight
+of 0 and one of +infinity, or the product of an infinity with 0, is NaN in its head; a
+query with one is NaN. Alike in the kernels of few rows and of tiles, for either type."""
 import numpy as np
 import pytest
 import torch
@@ -60,3 +60,20 @@ def test_an_infinite_key_has_the_logits_of_its_sign(R, case, fmt):  # noqa: F811
                 if dt == "bf16":      # half a step of each probability, cached value and output
                     ot = ot + 2.0 ** -8 * ((2 if fmt == "int4" else 1) * (p @ np.abs(val[1][keys])) / p.sum() + np.abs(want))
                 assert np.all(np.abs(out[t, h] - want) <= ot) and abs(lse[t, h] - wl) <= lt, (t, h, q[col])
+
+
+@pytest.mark.parametrize("fmt", ku.FORMATS)
+@pytest.mark.parametrize("case", CASES, ids=IDS)
+def test_an_infinite_query_is_nan_whatever_its_logits(R, case, fmt):  # noqa: F811
+    """Also where the only key that it sees has a logit of -infinity."""
+    dt, D, qs, ns = case
+    print("query", case, fmt, flush=True)
+    for rows in (ns, [0] * len(ns)):
+        inp = Inputs(43, fmt, dt, 4, 2, D, qs, rows, cap=max(ns) + 3)
+        inp.K[0, 0, 3] = -1.0
+        clean = [t.clone() for t in inp.run(R, True)]
+        inp.q[0, 1, 3] = float("inf")
+        out, lse = inp.run(R, True)
+        assert out[0, 1].isnan().all() and lse[0, 1].isnan()
+        out[0, 1], lse[0, 1] = clean[0][0, 1], clean[1][0, 1]
+        assert torch.equal(out, clean[0]) and torch.equal(lse, clean[1])
