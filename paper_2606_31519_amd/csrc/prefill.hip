@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_kernel(
     for (int kb = 0; kb < KB; ++kb) qf[kb] = *reinterpret_cast<const bf16x8*>(p + 16 * kb);
   }
   float odd_q = 0.f;   // NaN where the lane's half of the query has an infinity or NaN
-  if constexpr (FMT != 0) {
+  if (FMT != 0 || lim > 0) {   // (a token that sees no key is 0)
 #pragma unroll
     for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -582,7 +582,7 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_f32_kernel(
     for (int i = 0; i < D / 8; ++i) qf[i] = *reinterpret_cast<const f32x4*>(p + 4 * i) * scale_log2e;
   }
   float odd_q = 0.f;   // (as in the bf16 kernel)
-  if constexpr (FMT != 0) {
+  if (FMT != 0 || lim > 0) {
 #pragma unroll
     for (int i = 0; i < D / 8; ++i)
 #pragma unroll
