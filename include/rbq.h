@@ -613,7 +613,8 @@ rbq_status rbq_decode_step_kv4(int32_t batch, int32_t heads_q, int32_t heads_kv,
  * are in the 4-bit cache: token i of sequence b attends over its cached rows [0, n_b) and the
  * rows of its own chunk in full precision, those of tokens j <= i (causal) or all of them. So a
  * session's next turn, or drafted tokens that are to be checked, need no full-precision
- * copy of the cache.
+ * copy of the cache. Rows that are not in the cache yet, such as those of a local window, go
+ * before the new tokens' among the chunk's own, with queries of any kind whose outputs are not used.
  *   q, q_ld, cu_q, total_q, dtype, out, lse, sm_scale: as in rbq_prefill_attention
  *   K, V   the chunks' rows, packed like q: KV head h of token t at K + t * kv_ld + h * kv_head (kv_ld >= D)
  *   KV4, par, kv4_dtype, cap: the cache; n: the most rows that a sequence has there (n <= cap);

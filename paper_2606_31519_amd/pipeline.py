@@ -302,7 +302,8 @@ class PromptAttention:
 class ChunkAttention:
     """The attention of chunks of prompts whose earlier rows are in a Kv4Cache (rbq_prefill_attention_kv4): q_lens tokens
     and n_lens cached rows per sequence of the cache; the lengths' device arrays and the workspace are kept for every
-    call (calls that overlap in time, on several streams, need plans of their own)."""
+    call (calls that overlap in time, on several streams, need plans of their own). Rows that are not in the cache yet,
+    as a session's window, go before the new tokens' among q, K and V (DecodeSession.turn does so)."""
 
     def __init__(self, Hq, cache, q_lens, n_lens, causal=True):
         if len(q_lens) != cache.B or len(n_lens) != cache.B or min(min(q_lens), min(n_lens)) < 0:
@@ -359,7 +360,8 @@ class DecodeSession:
     scale), the window in K's type in buffers of its own; K and V [B][Hkv][at least
     n_prefill][D] are then read here only, and every step is one rbq_decode_step_kv8.
 
-    kv4 ("fp4" or "int4"): the same in 4 bits, every step one rbq_decode_step_kv4."""
+    kv4 ("fp4" or "int4"): the same in 4 bits, every step one rbq_decode_step_kv4. turn() takes a further turn's tokens at
+    once."""
 
     def __init__(self, B, Hq, Hkv, D, cap, n_prefill, window, K, V, P, c_q=None, device="cuda", compact=False, kv8=None,
                  kv8_block=64, kv4=None):
@@ -457,3 +459,42 @@ class DecodeSession:
             self.n += self.w
             self.w = 0
         return flush
+
+    def turn(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor) -> torch.Tensor:
+        """A further turn of T tokens a sequence, over a 4-bit cache: their attention, causal, over every row that the
+        session holds, the window's among them, and then their rows entered as append() and step() enter them, whole
+        windows into the cache and the index, up to `window` rows kept in the window. q [B][T][Hq][D], k and v
+        [B][T][Hkv][D] in the window's type; returns [B][T][Hq][D]. On the current stream."""
+        st, c = self.state, self.kv4
+        if c is None:
+            raise ValueError("a turn attends over a 4-bit cache: the session needs kv4")
+        T = q.shape[1]
+        if tuple(q.shape) != (st.B, T, st.Hq, st.D) or tuple(k.shape) != (st.B, T, st.Hkv, st.D) or v.shape != k.shape:
+            raise ValueError(f"q, k and v are {tuple(q.shape)}, {tuple(k.shape)} and {tuple(v.shape)}")
+        if not q.dtype == k.dtype == v.dtype == self.K_win.dtype:
+            raise ValueError(f"q, k and v are {q.dtype}, {k.dtype} and {v.dtype}, the window {self.K_win.dtype}")
+        rows = self.w + T
+        if self.n + rows > st.cap:
+            raise RuntimeError(f"{self.n + rows} rows exceed the cache's {st.cap}")
+        if T == 0:
+            return torch.empty_like(q)
+        # The window's rows are the first of the chunk's own; their queries are zeros, and what those give is not used.
+        own = [torch.cat([win[:, :, :self.w], x.transpose(1, 2)], dim=2).contiguous()
+               for win, x in ((self.K_win, k), (self.V_win, v))]
+        K, V = (x.transpose(1, 2).reshape(st.B * rows, st.Hkv, st.D) for x in own)
+        q = torch.cat([q.new_zeros(st.B, self.w, st.Hq, st.D), q], dim=1).reshape(st.B * rows, st.Hq, st.D)
+        out = ChunkAttention(st.Hq, c, [rows] * st.B, [self.n] * st.B)(q, K, V)
+        out = out.view(st.B, rows, st.Hq, st.D)[:, self.w:]
+        flush = (rows - 1) // self.window * self.window
+        if flush > 0:
+            if st.compact:
+                rbq.rbq_encode_keys_f16(st.B, st.Hkv, st.D, own[0], rows, flush, self.n, st.cap, st.P, st.c_k, st.codes,
+                                        st.kfac16, 0, None)
+            else:
+                rbq.rbq_encode_keys(st.B, st.Hkv, st.D, own[0], rows, flush, self.n, st.cap, st.P, st.c_q, st.c_k, st.codes,
+                                    st.kfac, 0, None, None)
+            c.append(*own, rows, flush, self.n)
+        for win, x in ((self.K_win, own[0]), (self.V_win, own[1])):
+            win[:, :, :rows - flush].copy_(x[:, :, flush:])
+        self.n, self.w = self.n + flush, rows - flush
+        return out
