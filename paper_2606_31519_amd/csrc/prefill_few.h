@@ -83,11 +83,13 @@ __device__ __forceinline__ TileId find_few(int id, int kchunk, int batch, int G,
 //                  w (m / s) beside them, so that both see the same rounding
 // fp32: queries and weights in three bf16 parts, 24 bits (4-bit codes and values are exact in
 // bf16), the chunk's own rows too: three products for one are a fifth of what the fp32 matrix
-// instructions take (2 x 31-500 tokens of 8 / 2 heads of 64 over up to 6000 rows: 37.8 us, 67.1
-// with them). int4's rows as c - 7.5 and m + 7.5 s: sums of c itself, which m then cancels, cost
+// instructions take (2 x 31-500 tokens of 8 / 2 heads of 64 over up to 6000 rows, int4: 38.8 us,
+// 72.1 with them in prefill_f32_kernel). int4's rows as c - 7.5 and m + 7.5 s: sums of c itself, which m then cancels, cost
 // twice the rounding (rel. error of the outputs 1.6e-6, so 7.8e-7).
 // (In prefill_kernel, 128 rows and tiles through LDS, 8 x 7 tokens of 32 / 8 heads over up to
-// 8000 rows took 33 us.)
+// 8000 rows take 36.2 us in int4 and 30.3 in fp4, here 22.2 and 20.1.)
+// At D = 128 fp32 has all 256 registers and 96 (fp4) or 108 bytes (int4) of scratch a lane: 2 x 31-500 tokens of
+// 8 / 2 heads over up to 6000 rows, int4, 70 us (in prefill_f32_kernel 130).
 template <int D, int FMT, int DTYPE>
 __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
     const typename Elem<DTYPE>::T* __restrict__ q, int64_t q_ld, const typename Elem<DTYPE>::T* __restrict__ K,
@@ -230,7 +232,9 @@ __global__ __launch_bounds__(kPThreads, 2) void prefill_few_kernel(
   };
 
   const int c4groups = max(min(kstop, cached) - kbeg + kGroup - 1, 0) / kGroup;   // of 4-bit keys
-  constexpr int kNoRow = 0x7FFE0000 / D;   // past every buffer's end (below 2^31 bytes of records), and so is its word
+  // where the loads of a group behind the last go: past the buffers' ends (or, of a buffer of almost 2^31 bytes, onto
+  // rows that are not used), a group's rows before an int's end
+  constexpr int kNoRow = 0x7FFE0000 / D;
   if (wave < c4groups) {
     load_k(kbeg + wave * kGroup);
     load_v(kbeg + wave * kGroup);

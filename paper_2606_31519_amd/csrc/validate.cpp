@@ -379,11 +379,13 @@ double prefill_cost(int64_t blocks, int32_t batch, int64_t rows, int32_t head_di
 
 namespace {
 // Rows (token, head of the group) a sequence up to which chunks over a 4-bit cache take the
-// kernel of few rows, two blocks per compute unit: 32 / 8 heads, 8 x 7 tokens over up to 8000 rows
-// 22.4 us (in tiles of 128 rows 37.1), 8 tokens over 30000 24.5 (36.0), 128 tokens over 30000 95.5
-// (119.6); 256 tokens 172.6 (157.8), 512 over 8000 129.3 (119.1). fp32 takes it, whatever the rows,
-// unless more keys are the chunk's own than are cached: 1000 tokens of 32 / 8 heads over 8000 470 us
-// (1455), 1000 of 4 / 1 over none 33.0 (34.9), 2500 over none 146 (112).
+// kernel of few rows, two blocks per compute unit (us, in brackets in tiles of 128 rows): 32 / 8 heads of 128, fp4,
+// 8 x 7 tokens over up to 8000 rows 20.1 (30.3), 8 tokens over 30000 22.8 (30.0), 128 tokens 92.6 (120), 256 tokens
+// 168 (157), 512 over 8000 99.8 (98.6), 2001 over 30011 1243 (1054). (A batch goes by its mean: a long chunk beside many
+// single tokens takes that, 2000 tokens and 63 single ones over 1000 to 30000 rows each 1019 us, apart 664 and 286.)
+// fp32 takes it, whatever the rows, unless more keys are the chunk's own than are cached: 1000 tokens of 32 / 8 heads
+// over 8000 rows 409 us (1508), 1000 of 4 / 1 over none 35.4 (35.2), 2500 180 (112); at D = 64, where it is the faster
+// one there too (16.9 and 24.0, 55.5 and 59.2), no rule of its own is made.
 constexpr int64_t kFewRows = 512, kFewOwn = 1024;
 bool few_rows(int64_t rows, int32_t batch, int32_t max_k, int32_t total_q, int32_t dtype) {
   const int64_t ends = std::min<int64_t>(batch, total_q);
