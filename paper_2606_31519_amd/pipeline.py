@@ -319,20 +319,25 @@ class ChunkAttention:
         self.ws = rbq.workspace(rbq.RBQ_OP_PREFILL_KV4, cache.B, Hq, cache.Hkv, cache.D, self.n, self.total_q, device)
         self.sm_scale = 1.0 / math.sqrt(cache.D)
 
+    def _strides(self, t):
+        """Of K or V, from a row and a head to the next (a dimension of one entry has no stride that means anything)."""
+        c = self.cache
+        return t.stride(0) if self.total_q > 1 else c.Hkv * c.D, t.stride(1) if c.Hkv > 1 else c.D
+
     def __call__(self, q, K, V, out=None, lse=None, stream=None):
         """q [total_q][Hq][D]; K, V [total_q][Hkv][D], the chunks' own rows; any strides whose last dimension (of q: two)
         is contiguous. Returns out [total_q][Hq][D] in q's type."""
         c, T = self.cache, self.total_q
         if tuple(q.shape[1:]) != (self.Hq, c.D) or q.shape[0] < T:
             raise ValueError(f"q is {tuple(q.shape)}, the plan needs ({T}, {self.Hq}, {c.D})")
-        if K.shape != V.shape or tuple(K.shape[1:]) != (c.Hkv, c.D) or K.shape[0] < T or K.stride() != V.stride():
+        if (K.shape != V.shape or tuple(K.shape[1:]) != (c.Hkv, c.D) or K.shape[0] < T
+                or self._strides(K) != self._strides(V)):
             raise ValueError(f"K and V are {tuple(K.shape)} and {tuple(V.shape)}, the plan needs ({T}, {c.Hkv}, {c.D}) and "
                              "equal strides")
-        if q.stride(2) != 1 or (self.Hq > 1 and q.stride(1) != c.D) or K.stride(2) != 1:
+        if q.stride(2) != 1 or (self.Hq > 1 and q.stride(1) != c.D) or K.stride(2) != 1 or V.stride(2) != 1:
             raise ValueError("the head dimension (and the heads of q) must be contiguous")
-        # (a dimension of one entry has no stride that means anything)
         q_ld = q.stride(0) if T > 1 else self.Hq * c.D
-        kv_ld, kv_head = K.stride(0) if T > 1 else c.Hkv * c.D, K.stride(1) if c.Hkv > 1 else c.D
+        kv_ld, kv_head = self._strides(K)
         out = torch.empty(T, self.Hq, c.D, dtype=q.dtype, device=q.device) if out is None else out
         if not out.is_contiguous() or (lse is not None and not lse.is_contiguous()):
             raise ValueError("out and lse must be contiguous")
