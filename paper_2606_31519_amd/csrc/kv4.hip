@@ -10,7 +10,7 @@
 //         step of a code
 //
 // Bound by the bytes of the rows and the records: K and V of 130816 tokens x 8 heads x 128 in
-// bf16, 678 MB either way, written in 114 us (5.9 TB/s) and read back in 102 (6.6; stores that
+// bf16, 678 MB either way, written in 115 us (5.9 TB/s) and read back in 104 (6.5; stores that
 // the caches keep 121, one row a thread 110). Writing has its arithmetic beside the bytes: with a
 // look at each value for infinities and NaN (now for a wave's at once, and the values' own way
 // only where there is one) 16 values took 210 (fp4) to 400 (int4) vector instructions, and the
